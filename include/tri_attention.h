@@ -325,6 +325,110 @@ tri_status tri_calib_finalize(const void *state, int32_t n_heads, int32_t pair_l
                               float *q_mean_norm, float *mrl, void *stream);
 
 /*
+ * ---- The decode step around the round: append, attend ----
+ *
+ * One layer of a cache as the calls below take it.  `view` is the same description the round uses (any of its formats
+ * and layouts); rows [0, length) of a unit are cached, where the length is view->seq_lens[s], or
+ * unit_lens[(layer * S + s) * n_kv_heads + h] when unit_lens is given: after tri_compress_budgets the heads of a
+ * sequence hold different numbers of rows, and its kept_cnt array is such an array.  A length below 0 counts as 0, one
+ * above n_max as n_max.  S is the number of sequences of the view.
+ */
+typedef struct {
+    const tri_cache_view *view;
+    int32_t layer;             /* 0 <= layer < n_layers                                                            */
+    const int32_t *unit_lens;  /* device [n_layers][S][n_kv_heads] or NULL: view->seq_lens                          */
+    const float *k_scale;      /* device [n_layers][n_kv_heads] fp32 or NULL = 1; k_kind 3 only: a cached byte      */
+    const float *v_scale;      /* stands for its e4m3 value times the scale of its head (finite, > 0)               */
+} tri_layer_cache;
+
+/*
+ * New rows of one layer, as its projections leave them: up to T tokens per sequence.
+ *   k, v   device [S][T][H][128], q device [S][T][H*G][128] or NULL; rows start on 16-byte boundaries, components are
+ *          contiguous, strides are in elements.  v must be given exactly when the cache has values.
+ */
+typedef struct {
+    const void *k, *v, *q;
+    int32_t kind;              /* 0: k, v, q are bf16, 1: fp32                                                      */
+    int32_t T;                 /* >= 1                                                                              */
+    int64_t k_stride_seq, k_stride_tok, k_stride_head;
+    int64_t v_stride_seq, v_stride_tok, v_stride_head;
+    int64_t q_stride_seq, q_stride_tok, q_stride_head;
+    void *q_out;               /* device bf16 [S][T][H*G][128], with q: the rotated queries; may be q itself (same
+                                  strides, kind 0)                                                                 */
+    int64_t qo_stride_seq, qo_stride_tok, qo_stride_head;
+    const int32_t *n_new;      /* device [S] or NULL: sequence s brings n_new[s] tokens (0..T), NULL: T             */
+    const int64_t *pos;        /* device [S] or NULL: original position of each sequence's first new token; NULL: the
+                                  slot it goes to (an uncompressed cache; not with unit_lens).  Positions lie in
+                                  [0, 2^31)                                                                         */
+} tri_append_rows;
+
+/*
+ * Appends rows to a cache.  Token t < n_new[s] of sequence s goes to slot length + t of each of its heads; with
+ * p = pos[s] + t
+ *   keys     k_kind 0, 3: band f of the key is rotated by the angle p * omega_f (Section 2.1; the band layout is the
+ *            context's pair_layout), in fp32 with the angle reduced in fp64, and rounded once to bf16 or e4m3;
+ *            k_kind 1, 2: stored as they are (fp32, bf16), these caches hold pre-RoPE vectors
+ *   values   rounded to the cache's format
+ *   e4m3     round(x / scale) to nearest even, beyond +-448 to +-448, NaN to NaN
+ *   positions of the view, if any, receive p
+ *   queries  rotated likewise into q_out
+ * Nothing else of the cache or of q_out is written, rows of padding tokens (t >= n_new[s]) are not read.
+ *   new_lens  device [S], or [U] with unit_lens (this layer's entries), or NULL: receives length + n_new, at most
+ *             n_max.  It may be the array the lengths come from; the layers of a step share the lengths, so hand it
+ *             over with the step's last layer only.
+ *   device_status  device int32[1] or NULL; set to TRI_ERR_DEVICE_CHECK if a row had no slot below n_max, a page id
+ *             outside [0, n_pages) or a position outside [0, 2^31) -- such rows are skipped -- or if n_new[s] was
+ *             outside [0, T] (the nearest bound counts)
+ * The rows must not overlap the cache, and two sequences must not append into one page.
+ */
+tri_status tri_append(tri_ctx *ctx, const tri_layer_cache *dst, int32_t S, const tri_append_rows *rows,
+                      int32_t *new_lens, int32_t *device_status, void *stream);
+
+/* Queries and outputs of an attention call: one query token per sequence, rotated like the cached keys. */
+typedef struct {
+    const void *q;             /* device bf16 [S][H*G][128], 16-byte rows                                          */
+    int64_t q_stride_seq, q_stride_head;
+    void *out;                 /* device bf16 [S][H*G][128], 16-byte rows; must not overlap q                      */
+    int64_t out_stride_seq, out_stride_head;
+    float *lse;                /* device fp32 [S][H*G] or NULL: log sum_n exp(logit_n), -infinity without rows      */
+    float scale;               /* logit_n = scale * (q . k_n); finite                                              */
+} tri_attend_io;
+
+/* Bytes of device workspace the calls below need for S sequences and P prefixes (0: tri_attend); 0 for bad arguments. */
+size_t tri_attend_workspace_bytes(const tri_ctx *ctx, int32_t S, int32_t P);
+
+/*
+ * Attention of one decode step over one layer of the cache, compressed or not:
+ *   out[s, h*G + g] = sum_n softmax_n(scale * q[s, h*G + g] . k_n) v_n     over the cached rows n of unit (s, h).
+ * A unit without rows gives zeros.  Key formats 0 and 3; the pre-RoPE formats hold unrotated keys and are refused
+ * (TRI_ERR_UNSUPPORTED), as is a cache without values (TRI_ERR_INVALID_ARG).  Rows at or behind the length are never
+ * used, whatever they hold.  Logits, softmax statistics and sums are fp32; the weights of the sum over values enter
+ * the tensor cores as a 16-bit value plus the 16-bit rest of it.  Sums are formed in a fixed order: equal inputs give
+ * equal bits.  Any length up to 2^31 - 1; ragged batches are cut into equal shares over the GPU.
+ *   ws  device workspace of tri_attend_workspace_bytes(ctx, S, 0) bytes, 256-byte aligned; nothing in it has to be
+ *       set, nothing is kept in it from call to call.  Calls that may overlap on the GPU need a workspace each.
+ *   device_status  device int32[1] or NULL; TRI_ERR_DEVICE_CHECK if a kernel met a page id outside [0, n_pages): such
+ *       rows count as absent.
+ */
+tri_status tri_attend(tri_ctx *ctx, const tri_layer_cache *src, int32_t S, const tri_attend_io *io,
+                      int32_t *device_status, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * The same for sequences that continue shared prefixes (several samples of one prompt): sequence s of group p attends
+ * over the rows of prefix p and over its own rows, in one softmax, and the rows of a prefix are read for all sequences
+ * of its group together.
+ *   prefix       a cache view of P sequences, the prefixes; its format may differ from that of src
+ *   group_start  device int32 [P + 1], ascending within [0, S]: prefix p belongs to the sequences group_start[p] <= s
+ *                < group_start[p + 1]; the others have no prefix.  Entries outside [0, S] count as the nearest bound;
+ *                if they descend, TRI_ERR_DEVICE_CHECK is set in device_status and the outputs are unspecified.
+ *   ws           tri_attend_workspace_bytes(ctx, S, P) bytes
+ * Queries must be rotated to positions behind the prefix, as the model would have them.
+ */
+tri_status tri_attend_shared(tri_ctx *ctx, const tri_layer_cache *prefix, int32_t P, const int32_t *group_start,
+                             const tri_layer_cache *src, int32_t S, const tri_attend_io *io,
+                             int32_t *device_status, void *ws, size_t ws_bytes, void *stream);
+
+/*
  * Self-test of the bounded waits the scoring kernels use for their copy-engine and tensor-core barriers (the paper has no
  * counterpart): one warp waits on a barrier that nothing ever completes, once with the spinning wait of the mma.sync
  * kernel and once with the sleeping wait of the tcgen05 kernel; each gives up after a short poll limit.  *device_status

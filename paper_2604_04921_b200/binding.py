@@ -21,13 +21,15 @@ LIB_PATH = _PKG / "lib" / "libtriattn.so"
 SOURCES = [_PKG / "csrc" / "tri_api.cu"]
 HEADERS = [_ROOT / "include" / "tri_attention.h", _PKG / "csrc" / "tri_common.cuh", _PKG / "csrc" / "tri_score.cuh",
            _PKG / "csrc" / "tri_score_pre.cuh", _PKG / "csrc" / "tri_score_tma.cuh", _PKG / "csrc" / "tri_score_umma.cuh", _PKG / "csrc" / "tri_calib.cuh", _PKG / "csrc" / "tri_calib_tma.cuh",
-           _PKG / "csrc" / "tri_select.cuh", _PKG / "csrc" / "tri_compact.cuh"]
+           _PKG / "csrc" / "tri_select.cuh", _PKG / "csrc" / "tri_compact.cuh",
+           _PKG / "csrc" / "tri_append.cuh", _PKG / "csrc" / "tri_attend.cuh"]
 
 EXPORTS = ["tri_create", "tri_destroy", "tri_workspace_bytes", "tri_score", "tri_select", "tri_compact",
            "tri_compress", "tri_select_budgets", "tri_compress_budgets", "tri_compress_windowed", "tri_compress_host", "tri_score_static", "tri_score_static_bytes", "tri_compress_launches", "tri_set_pipeline", "tri_set_score_kernel", "tri_last_cuda_error",
            "tri_profile_begin", "tri_profile_read", "tri_profile_end",
            "tri_calib_state_bytes", "tri_calib_workspace_bytes", "tri_calib_reset", "tri_calib_accumulate",
-           "tri_calib_finalize", "tri_selftest_bounded_wait"]
+           "tri_calib_finalize", "tri_selftest_bounded_wait",
+           "tri_append", "tri_attend_workspace_bytes", "tri_attend", "tri_attend_shared"]
 
 STATUS = {0: "TRI_OK", 1: "TRI_ERR_INVALID_ARG", 2: "TRI_ERR_UNSUPPORTED", 3: "TRI_ERR_WORKSPACE",
           4: "TRI_ERR_CUDA", 5: "TRI_ERR_DEVICE_CHECK", 6: "TRI_ERR_TIMEOUT"}
@@ -71,6 +73,28 @@ class _CacheView(ctypes.Structure):
                 ("max_pages_per_seq", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32),
                 ("stride_page", ctypes.c_int64), ("stride_slot", ctypes.c_int64), ("seq_lens", ctypes.c_void_p),
                 ("positions", ctypes.c_void_p), ("n_max", ctypes.c_int32)]
+
+
+class _LayerCache(ctypes.Structure):
+    _fields_ = [("view", ctypes.POINTER(_CacheView)), ("layer", ctypes.c_int32), ("unit_lens", ctypes.c_void_p),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class _AppendRows(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q", ctypes.c_void_p), ("kind", ctypes.c_int32),
+                ("T", ctypes.c_int32),
+                ("k_stride_seq", ctypes.c_int64), ("k_stride_tok", ctypes.c_int64), ("k_stride_head", ctypes.c_int64),
+                ("v_stride_seq", ctypes.c_int64), ("v_stride_tok", ctypes.c_int64), ("v_stride_head", ctypes.c_int64),
+                ("q_stride_seq", ctypes.c_int64), ("q_stride_tok", ctypes.c_int64), ("q_stride_head", ctypes.c_int64),
+                ("q_out", ctypes.c_void_p),
+                ("qo_stride_seq", ctypes.c_int64), ("qo_stride_tok", ctypes.c_int64), ("qo_stride_head", ctypes.c_int64),
+                ("n_new", ctypes.c_void_p), ("pos", ctypes.c_void_p)]
+
+
+class _AttendIo(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("q_stride_seq", ctypes.c_int64), ("q_stride_head", ctypes.c_int64),
+                ("out", ctypes.c_void_p), ("out_stride_seq", ctypes.c_int64), ("out_stride_head", ctypes.c_int64),
+                ("lse", ctypes.c_void_p), ("scale", ctypes.c_float)]
 
 
 _lib = None
@@ -137,6 +161,15 @@ def lib():
     L.tri_calib_finalize.restype = ctypes.c_int
     L.tri_selftest_bounded_wait.argtypes = [P, P]
     L.tri_selftest_bounded_wait.restype = ctypes.c_int
+    LP = ctypes.POINTER(_LayerCache)
+    L.tri_append.argtypes = [P, LP, i32, ctypes.POINTER(_AppendRows), P, P, P]
+    L.tri_append.restype = ctypes.c_int
+    L.tri_attend_workspace_bytes.argtypes = [P, i32, i32]
+    L.tri_attend_workspace_bytes.restype = sz
+    L.tri_attend.argtypes = [P, LP, i32, ctypes.POINTER(_AttendIo), P, P, sz, P]
+    L.tri_attend.restype = ctypes.c_int
+    L.tri_attend_shared.argtypes = [P, LP, i32, P, LP, i32, ctypes.POINTER(_AttendIo), P, P, sz, P]
+    L.tri_attend_shared.restype = ctypes.c_int
     L.tri_last_cuda_error.argtypes = []
     L.tri_last_cuda_error.restype = ctypes.c_char_p
     _lib = L
@@ -153,8 +186,20 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
+def _addr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
 def _stream():
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
+def _stream_of(device: torch.device):
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _check_status_tensor(t: Optional[torch.Tensor], device: torch.device):
+    assert t is None or (t.dtype == torch.int32 and t.numel() >= 1 and t.device == device)
 
 
 @dataclasses.dataclass
@@ -205,6 +250,39 @@ class CacheView:
             assert self.positions.shape[-1] == cv.n_max
             cv.positions = self.positions.data_ptr()
         return cv
+
+
+class LayerCache:
+    """One layer of a cache as append() and attend() take it.
+
+    view       the cache (CacheView); seq_lens needed unless unit_lens is given
+    unit_lens  [L, S, H] int32, a length per head: what compress(..., unit_budgets=...) leaves in kept_cnt
+    k_scale, v_scale  [L, H] fp32, 8-bit caches only: a byte stands for its value times the scale of its head
+    The description is laid out once, here; the tensors behind it (lengths, tables, rows) are read anew by every call.
+    """
+
+    def __init__(self, view: CacheView, layer: int, unit_lens: Optional[torch.Tensor] = None,
+                 k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None):
+        self.view, self.layer, self.unit_lens, self.k_scale, self.v_scale = view, layer, unit_lens, k_scale, v_scale
+        self._cv = view.c_view()
+        self.device = view.k.device
+        L, H = view.k.shape[0], view.k.shape[2]
+        assert 0 <= layer < L
+        self.n_layers, self.n_kv_heads = L, H
+        S = view.k.shape[1] if view.page_table is None else view.page_table.shape[0]
+        self.n_seqs = S
+        for t in (view.v, view.seq_lens, view.positions, view.page_table, unit_lens, k_scale, v_scale):
+            assert t is None or t.device == self.device, "all parts of a cache live on one device"
+        if unit_lens is not None:
+            assert unit_lens.dtype == torch.int32 and unit_lens.is_contiguous() and unit_lens.numel() == L * S * H
+        else:
+            assert view.seq_lens is not None and view.seq_lens.numel() == S
+        if view.positions is not None:
+            assert view.positions.numel() == L * S * H * self._cv.n_max
+        for sc in (k_scale, v_scale):
+            assert sc is None or (sc.dtype == torch.float32 and sc.is_contiguous() and sc.numel() == L * H)
+        self._c = _LayerCache(ctypes.pointer(self._cv), layer, _addr(unit_lens), _addr(k_scale), _addr(v_scale))
+        self._ref = ctypes.byref(self._c)
 
 
 class TriContext:
@@ -352,6 +430,92 @@ class TriContext:
                                        _ptr(cur_pos_dev), budget, ctypes.byref(c), ctypes.byref(d),
                                        _ptr(kept_cnt_host), _ptr(kept_cnt_dev), _ptr(ws), ws.numel(), _stream()),
                "tri_compress_host")
+
+    # -- the decode step around the round ----------------------------------------------------
+    def append(self, dst: LayerCache, k: torch.Tensor, v: Optional[torch.Tensor], pos: Optional[torch.Tensor],
+               q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+               n_new: Optional[torch.Tensor] = None, new_lens: Optional[torch.Tensor] = None,
+               device_status: Optional[torch.Tensor] = None):
+        """Append T tokens per sequence to one layer: k, v [S, T, H, 128] (bf16 or fp32, any strides with 16-byte rows),
+        pre-RoPE; keys are rotated to positions pos[s] + t on the way (kept as they are in a pre-RoPE cache) and, if
+        given, q [S, T, H * G, 128] into q_out (bf16).  n_new [S] int32: tokens each sequence brings, default T.
+        new_lens receives the lengths after the append and may be the array they come from (last layer of a step)."""
+        S, T, H, D = k.shape
+        Hq = H * self.group_size
+        dev = dst.device
+        assert S == dst.n_seqs and H == self.n_kv_heads == dst.n_kv_heads and dst.n_layers == self.n_layers and D == 128
+        assert k.dtype in (torch.bfloat16, torch.float32) and k.device == dev and k.stride(3) == 1
+        r = _AppendRows()
+        r.k, r.kind, r.T = k.data_ptr(), 0 if k.dtype == torch.bfloat16 else 1, T
+        r.k_stride_seq, r.k_stride_tok, r.k_stride_head, _ = k.stride()
+        assert (v is not None) == (dst.view.v is not None), "values go with a cache that holds values"
+        if v is not None:
+            assert v.shape == k.shape and v.dtype == k.dtype and v.device == dev and v.stride(3) == 1
+            r.v = v.data_ptr()
+            r.v_stride_seq, r.v_stride_tok, r.v_stride_head, _ = v.stride()
+        assert (q is None) == (q_out is None)
+        if q is not None:
+            assert q.shape == q_out.shape == (S, T, Hq, 128) and q.dtype == k.dtype and q_out.dtype == torch.bfloat16
+            assert q.device == dev and q_out.device == dev and q.stride(3) == 1 and q_out.stride(3) == 1
+            r.q, r.q_out = q.data_ptr(), q_out.data_ptr()
+            r.q_stride_seq, r.q_stride_tok, r.q_stride_head, _ = q.stride()
+            r.qo_stride_seq, r.qo_stride_tok, r.qo_stride_head, _ = q_out.stride()
+        if n_new is not None:
+            assert n_new.dtype == torch.int32 and n_new.numel() == S and n_new.is_contiguous() and n_new.device == dev
+            r.n_new = n_new.data_ptr()
+        if pos is not None:
+            assert pos.dtype == torch.int64 and pos.numel() == S and pos.is_contiguous() and pos.device == dev
+            r.pos = pos.data_ptr()
+        if new_lens is not None:
+            assert new_lens.dtype == torch.int32 and new_lens.is_contiguous() and new_lens.device == dev
+            assert new_lens.numel() == (S if dst.unit_lens is None else self.units(S))
+        _check_status_tensor(device_status, dev)
+        _check(lib().tri_append(self._h, dst._ref, S, ctypes.byref(r), _addr(new_lens), _addr(device_status),
+                                _stream_of(dev)), "tri_append")
+
+    def attend_workspace_bytes(self, S: int, n_prefixes: int = 0) -> int:
+        return int(lib().tri_attend_workspace_bytes(self._h, S, n_prefixes))
+
+    def attend_workspace(self, S: int, n_prefixes: int = 0, device="cuda") -> torch.Tensor:
+        return torch.empty(self.attend_workspace_bytes(S, n_prefixes), dtype=torch.uint8, device=device)
+
+    def _attend_io(self, src: LayerCache, q: torch.Tensor, out: torch.Tensor, ws: torch.Tensor, scale: Optional[float],
+                   lse: Optional[torch.Tensor], device_status: Optional[torch.Tensor]) -> _AttendIo:
+        shape, dev = q.shape, src.device
+        assert src.n_kv_heads == self.n_kv_heads and src.n_layers == self.n_layers
+        assert shape == (src.n_seqs, self.n_kv_heads * self.group_size, 128) and out.shape == shape
+        assert q.dtype == torch.bfloat16 and out.dtype == torch.bfloat16 and q.device == dev and out.device == dev
+        assert ws.device == dev and ws.is_contiguous()
+        sq, so = q.stride(), out.stride()
+        assert sq[2] == 1 and so[2] == 1
+        if lse is not None:
+            assert lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == shape[:2] and lse.device == dev
+        _check_status_tensor(device_status, dev)
+        return _AttendIo(q.data_ptr(), sq[0], sq[1], out.data_ptr(), so[0], so[1], _addr(lse),
+                         128.0 ** -0.5 if scale is None else scale)
+
+    def attend(self, src: LayerCache, q: torch.Tensor, out: torch.Tensor, ws: torch.Tensor, scale: Optional[float] = None,
+               lse: Optional[torch.Tensor] = None, device_status: Optional[torch.Tensor] = None):
+        """Attention of one query token per sequence over one layer of the cache: q, out [S, H * G, 128] bf16 (q rotated
+        like the cached keys), lse [S, H * G] fp32 or None, scale 1/sqrt(128) by default, ws from attend_workspace(S)."""
+        io = self._attend_io(src, q, out, ws, scale, lse, device_status)
+        _check(lib().tri_attend(self._h, src._ref, src.n_seqs, ctypes.byref(io), _addr(device_status), ws.data_ptr(),
+                                ws.numel() * ws.element_size(), _stream_of(src.device)), "tri_attend")
+
+    def attend_shared(self, prefix: LayerCache, group_start: torch.Tensor, src: LayerCache, q: torch.Tensor,
+                      out: torch.Tensor, ws: torch.Tensor, scale: Optional[float] = None,
+                      lse: Optional[torch.Tensor] = None, device_status: Optional[torch.Tensor] = None):
+        """attend() for sequences that continue shared prefixes: `prefix` is a cache of P sequences, sequences
+        group_start[p] <= s < group_start[p + 1] ([P + 1] int32, ascending) attend over prefix p and their own rows.
+        ws from attend_workspace(S, P)."""
+        io = self._attend_io(src, q, out, ws, scale, lse, device_status)
+        P = prefix.n_seqs
+        assert prefix.n_kv_heads == self.n_kv_heads and prefix.n_layers == self.n_layers and prefix.device == src.device
+        assert group_start.dtype == torch.int32 and group_start.shape == (P + 1,) and group_start.is_contiguous()
+        assert group_start.device == src.device
+        _check(lib().tri_attend_shared(self._h, prefix._ref, P, group_start.data_ptr(), src._ref, src.n_seqs,
+                                       ctypes.byref(io), _addr(device_status), ws.data_ptr(),
+                                       ws.numel() * ws.element_size(), _stream_of(src.device)), "tri_attend_shared")
 
     KERNELS = ("fold_phasors", "score", "normalize", "select", "compact")
 

@@ -10,6 +10,8 @@
 
 #include <nvtx3/nvToolsExt.h>
 
+#include "tri_append.cuh"
+#include "tri_attend.cuh"
 #include "tri_calib.cuh"
 #include "tri_calib_tma.cuh"
 #include "tri_compact.cuh"
@@ -35,6 +37,8 @@ struct tri_ctx {
     double2 *dbar_d;     // [64]  (1/|D|) sum_delta e^{i omega_f delta}
     float *qc_d;         // [L][H*G][128]
     float *mw_d;         // [L][H*G][64]   weight of |k_f| in the norm term
+    double2 *turn_d;     // [64]  omega_f / 2 pi as hi + lo (tri_append)
+    int n_sm;            // multiprocessors of the device
     float2 *rot_lo_d, *rot_hi_d;   // phasor tables of the bf16 pre-RoPE path (see k_score_bf16_pre)
     // tri_profile_begin .. tri_profile_end: an event pair around every launch of tri_compress
     bool profiling;
@@ -114,7 +118,7 @@ extern "C" tri_status tri_create(const tri_model_desc *desc, const float *q_cent
     if (!c) return TRI_ERR_INVALID_ARG;
     c->desc = *desc;
     c->desc.offsets = nullptr;
-    c->omega_d = nullptr; c->dbar_d = nullptr; c->qc_d = nullptr; c->mw_d = nullptr; c->rot_lo_d = nullptr; c->rot_hi_d = nullptr;
+    c->omega_d = nullptr; c->dbar_d = nullptr; c->qc_d = nullptr; c->mw_d = nullptr; c->turn_d = nullptr; c->rot_lo_d = nullptr; c->rot_hi_d = nullptr;
     c->profiling = false;
     c->prof_used = 0;
     c->have_back = false;
@@ -138,6 +142,13 @@ extern "C" tri_status tri_create(const tri_model_desc *desc, const float *q_cent
             im += std::sin(a);
         }
         dbar[f] = make_double2(re / desc->n_offsets, im / desc->n_offsets);
+    }
+    // omega_f in turns per position, split into two doubles: positions run to 2^31 and the fraction of a turn is what counts
+    double2 turn[kBands];
+    for (int f = 0; f < kBands; ++f) {
+        const long double w = expl(-(2.0L * f / kHeadDim) * logl((long double)desc->rope_theta)) / 6.283185307179586476925286766559L;
+        turn[f].x = (double)w;
+        turn[f].y = (double)(w - (long double)turn[f].x);
     }
     const size_t nq = (size_t)desc->n_layers * desc->n_kv_heads * desc->group_size;
     std::vector<float> mw(nq * kBands);
@@ -165,7 +176,10 @@ extern "C" tri_status tri_create(const tri_model_desc *desc, const float *q_cent
     tri_status st = TRI_OK;
     do {
         if ((e = prepare_device()) != cudaSuccess) break;
+        if ((e = cudaDeviceGetAttribute(&c->n_sm, cudaDevAttrMultiProcessorCount, c->device)) != cudaSuccess) break;
         if ((e = cudaMalloc(&c->omega_d, sizeof omega)) != cudaSuccess) break;
+        if ((e = cudaMalloc(&c->turn_d, sizeof turn)) != cudaSuccess) break;
+        if ((e = cudaMemcpy(c->turn_d, turn, sizeof turn, cudaMemcpyHostToDevice)) != cudaSuccess) break;
         if ((e = cudaMalloc(&c->dbar_d, sizeof dbar)) != cudaSuccess) break;
         if ((e = cudaMalloc(&c->qc_d, nq * kHeadDim * sizeof(float))) != cudaSuccess) break;
         if ((e = cudaMalloc(&c->mw_d, nq * kBands * sizeof(float))) != cudaSuccess) break;
@@ -229,6 +243,7 @@ extern "C" tri_status tri_destroy(tri_ctx *c)
         cudaStreamDestroy(c->back);
     }
     cudaFree(c->omega_d);
+    cudaFree(c->turn_d);
     cudaFree(c->dbar_d);
     cudaFree(c->qc_d);
     cudaFree(c->mw_d);
@@ -407,6 +422,12 @@ cudaError_t allow_umma_smem()
     return cudaFuncSetAttribute(k_score_umma<NCOL, LAYOUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, umma_smem_bytes(NCOL));
 }
 
+template <bool KEY8, int RT>
+cudaError_t allow_attend_smem()
+{
+    return cudaFuncSetAttribute(k_attend<KEY8, RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttRingBytes);
+}
+
 cudaError_t prepare_device()
 {
     cudaError_t e;
@@ -419,7 +440,11 @@ cudaError_t prepare_device()
     if ((e = allow_umma_smem<16, 0>()) != cudaSuccess) return e;
     if ((e = allow_umma_smem<32, 0>()) != cudaSuccess) return e;
     if ((e = allow_umma_smem<16, 1>()) != cudaSuccess) return e;
-    return allow_umma_smem<32, 1>();
+    if ((e = allow_umma_smem<32, 1>()) != cudaSuccess) return e;
+    if ((e = allow_attend_smem<false, 8>()) != cudaSuccess) return e;
+    if ((e = allow_attend_smem<false, 16>()) != cudaSuccess) return e;
+    if ((e = allow_attend_smem<true, 8>()) != cudaSuccess) return e;
+    return allow_attend_smem<true, 16>();
 }
 
 // Every entry point that launches kernels runs on the device the context was created on.
@@ -1102,6 +1127,237 @@ extern "C" tri_status tri_score_static(tri_ctx *c, const tri_cache_view *src, in
     if ((r = score_scratch_address(dev, &ws)) != TRI_OK) return r;
     if ((r = run_fold(c, S, cur_pos, (char *)ws, pl, (cudaStream_t)stream, src->k_kind == 0)) != TRI_OK) return r;
     return run_score(c, src, S, cur_pos, scores, raw, (char *)ws, pl, nullptr, (cudaStream_t)stream, Units{0, pl.U});
+}
+
+// ----------------------------------------------------------------------------------------------
+// the decode step around the round: append, attend
+// ----------------------------------------------------------------------------------------------
+namespace {
+
+tri_status check_layer_cache(const tri_ctx *c, const tri_layer_cache *lc, int32_t S)
+{
+    if (!c || !lc || !lc->view || S <= 0) return TRI_ERR_INVALID_ARG;
+    tri_status r;
+    if ((r = check_view(lc->view, lc->unit_lens == nullptr)) != TRI_OK) return r;
+    if ((r = check_common(c, S, lc->view->n_max, 1)) != TRI_OK) return r;
+    if (lc->layer < 0 || lc->layer >= c->desc.n_layers) return TRI_ERR_INVALID_ARG;
+    if ((lc->k_scale || lc->v_scale) && lc->view->k_kind != 3) return TRI_ERR_INVALID_ARG;
+    return TRI_OK;
+}
+
+// Rows of `es`-byte elements that start on 16-byte boundaries.
+bool rows16_ok(const void *p, int64_t a, int64_t b, int64_t c, int es)
+{
+    return p && !((uintptr_t)p & 15) && (a * es) % 16 == 0 && (b * es) % 16 == 0 && (c * es) % 16 == 0;
+}
+
+template <int KIND, int KK, bool SPLIT>
+void launch_append(unsigned blocks, int tt, cudaStream_t st, const AppendParams &p)
+{
+    if (tt == 1) k_append<KIND, KK, SPLIT, 1><<<blocks, kAppendThreads, 0, st>>>(p);
+    else k_append<KIND, KK, SPLIT, kAppendTokens><<<blocks, kAppendThreads, 0, st>>>(p);
+}
+
+template <int KIND, int KK>
+void launch_append(bool split, unsigned blocks, int tt, cudaStream_t st, const AppendParams &p)
+{
+    if (split) launch_append<KIND, KK, true>(blocks, tt, st, p);
+    else launch_append<KIND, KK, false>(blocks, tt, st, p);
+}
+
+template <int KIND>
+void launch_append(int kk, bool split, unsigned blocks, int tt, cudaStream_t st, const AppendParams &p)
+{
+    if (kk == 0) launch_append<KIND, 0>(split, blocks, tt, st, p);
+    else if (kk == 1) launch_append<KIND, 1>(split, blocks, tt, st, p);
+    else if (kk == 2) launch_append<KIND, 2>(split, blocks, tt, st, p);
+    else launch_append<KIND, 3>(split, blocks, tt, st, p);
+}
+
+}  // namespace
+
+extern "C" tri_status tri_append(tri_ctx *c, const tri_layer_cache *dst, int32_t S, const tri_append_rows *rows,
+                                 int32_t *new_lens, int32_t *device_status, void *stream)
+{
+    tri_status r;
+    if ((r = check_layer_cache(c, dst, S)) != TRI_OK) return r;
+    if (!rows || rows->T <= 0 || rows->kind < 0 || rows->kind > 1) return TRI_ERR_INVALID_ARG;
+    const int es = rows->kind == 0 ? 2 : 4;
+    if (!rows16_ok(rows->k, rows->k_stride_seq, rows->k_stride_tok, rows->k_stride_head, es)) return TRI_ERR_INVALID_ARG;
+    if ((rows->v != nullptr) != (dst->view->v != nullptr)) return TRI_ERR_INVALID_ARG;
+    if (rows->v && !rows16_ok(rows->v, rows->v_stride_seq, rows->v_stride_tok, rows->v_stride_head, es)) return TRI_ERR_INVALID_ARG;
+    if ((rows->q != nullptr) != (rows->q_out != nullptr)) return TRI_ERR_INVALID_ARG;
+    if (rows->q) {
+        if (!rows16_ok(rows->q, rows->q_stride_seq, rows->q_stride_tok, rows->q_stride_head, es)) return TRI_ERR_INVALID_ARG;
+        if (!rows16_ok(rows->q_out, rows->qo_stride_seq, rows->qo_stride_tok, rows->qo_stride_head, 2)) return TRI_ERR_INVALID_ARG;
+        if (rows->q == rows->q_out && (rows->kind != 0 || rows->q_stride_seq != rows->qo_stride_seq ||
+                                       rows->q_stride_tok != rows->qo_stride_tok || rows->q_stride_head != rows->qo_stride_head))
+            return TRI_ERR_INVALID_ARG;
+    }
+    if (!rows->pos && dst->unit_lens) return TRI_ERR_INVALID_ARG;
+    if ((r = check_device(c)) != TRI_OK) return r;
+
+    const int32_t H = c->desc.n_kv_heads;
+    AppendParams p;
+    p.dst = to_view(dst->view);
+    p.layer = dst->layer; p.S = S; p.H = H; p.G = c->desc.group_size; p.T = rows->T;
+    p.unit_lens = dst->unit_lens ? dst->unit_lens + (int64_t)dst->layer * S * H : nullptr;
+    p.k_scale = dst->k_scale ? dst->k_scale + (int64_t)dst->layer * H : nullptr;
+    p.v_scale = dst->v_scale ? dst->v_scale + (int64_t)dst->layer * H : nullptr;
+    p.k = (const char *)rows->k; p.v = (const char *)rows->v; p.q = (const char *)rows->q; p.q_out = (char *)rows->q_out;
+    p.ks_seq = rows->k_stride_seq; p.ks_tok = rows->k_stride_tok; p.ks_head = rows->k_stride_head;
+    p.vs_seq = rows->v_stride_seq; p.vs_tok = rows->v_stride_tok; p.vs_head = rows->v_stride_head;
+    p.qs_seq = rows->q_stride_seq; p.qs_tok = rows->q_stride_tok; p.qs_head = rows->q_stride_head;
+    p.qo_seq = rows->qo_stride_seq; p.qo_tok = rows->qo_stride_tok; p.qo_head = rows->qo_stride_head;
+    p.n_new = rows->n_new; p.pos = rows->pos; p.turn = c->turn_d; p.device_status = device_status;
+    const int tt = rows->T == 1 ? 1 : kAppendTokens;
+    p.ntiles = (int32_t)(((int64_t)rows->T + tt - 1) / tt);
+    if ((int64_t)p.ntiles * S > 0x7fffffff) return TRI_ERR_UNSUPPORTED;
+    int32_t *lens_out = new_lens ? new_lens + (dst->unit_lens ? (int64_t)dst->layer * S * H : 0) : nullptr;
+    p.new_lens = p.ntiles == 1 ? lens_out : nullptr;
+    const unsigned blocks = (unsigned)(p.ntiles * S);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (rows->kind == 0) launch_append<0>(dst->view->k_kind, c->desc.pair_layout == 1, blocks, tt, st, p);
+    else launch_append<1>(dst->view->k_kind, c->desc.pair_layout == 1, blocks, tt, st, p);
+    if ((r = check_launch("k_append")) != TRI_OK) return r;
+    if (lens_out && p.ntiles > 1) {
+        p.new_lens = lens_out;
+        const int64_t n = (int64_t)S * (dst->unit_lens ? H : 1);
+        k_append_lens<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(p);
+        return check_launch("k_append_lens");
+    }
+    return TRI_OK;
+}
+
+namespace {
+
+// Workspace of an attention call.
+struct AttendPlan {
+    int32_t blocks;                                    // grid of the streaming passes
+    int32_t own_rows, pre_rows, spt;                   // query rows per slot; sequences per tile of a prefix's query rows
+    size_t own_rec, own_slots, own_whole, pre_rec, pre_slots, pre_whole, total;
+};
+
+AttendPlan make_attend_plan(const tri_ctx *c, int32_t S, int32_t P)
+{
+    AttendPlan a;
+    const int32_t H = c->desc.n_kv_heads, G = c->desc.group_size;
+    a.blocks = c->n_sm * kAttBlocksPerSM;
+    a.own_rows = G <= 8 ? 8 : 16;
+    a.pre_rows = 16;
+    a.spt = a.pre_rows / G;
+    const size_t row = kAttRowPitch * sizeof(float), whole = align256((size_t)S * H * G * row);
+    size_t o = 0;
+    a.own_rec = o;   o += align256((size_t)S * H * sizeof(int2));
+    a.own_slots = o; o += align256((size_t)a.blocks * 2 * a.own_rows * row);
+    a.own_whole = o; o += P > 0 ? whole : 0;
+    a.pre_rec = o;   o += P > 0 ? align256(((size_t)P + S / a.spt + 2) * H * sizeof(int2)) : 0;
+    a.pre_slots = o; o += P > 0 ? align256((size_t)a.blocks * 2 * a.pre_rows * row) : 0;
+    a.pre_whole = o; o += P > 0 ? whole : 0;
+    a.total = o;
+    return a;
+}
+
+template <bool KEY8>
+void launch_attend(int rows, unsigned blocks, cudaStream_t st, const AttendParams &p)
+{
+    if (rows == 8) k_attend<KEY8, 8><<<blocks, kAttThreads, kAttRingBytes, st>>>(p);
+    else k_attend<KEY8, 16><<<blocks, kAttThreads, kAttRingBytes, st>>>(p);
+}
+
+tri_status check_attend_cache(const tri_ctx *c, const tri_layer_cache *lc, int32_t n)
+{
+    tri_status r = check_layer_cache(c, lc, n);
+    if (r != TRI_OK) return r;
+    if (lc->view->k_kind != 0 && lc->view->k_kind != 3) return TRI_ERR_UNSUPPORTED;
+    return lc->view->v ? TRI_OK : TRI_ERR_INVALID_ARG;
+}
+
+// The part of AttendParams that depends on the cache and the call only.
+AttendParams attend_params(const tri_ctx *c, const tri_layer_cache *lc, int32_t n, int32_t S, const tri_attend_io *io,
+                           int32_t *device_status)
+{
+    const int32_t H = c->desc.n_kv_heads;
+    AttendParams p;
+    p.src = to_view(lc->view);
+    p.layer = lc->layer; p.nseq = n; p.H = H; p.G = c->desc.group_size; p.spt = 0; p.S = S;
+    p.unit_lens = lc->unit_lens ? lc->unit_lens + (int64_t)lc->layer * n * H : nullptr;
+    p.k_scale = lc->k_scale ? lc->k_scale + (int64_t)lc->layer * H : nullptr;
+    p.v_scale = lc->v_scale ? lc->v_scale + (int64_t)lc->layer * H : nullptr;
+    p.group_start = nullptr;
+    p.q = (const char *)io->q; p.q_seq = io->q_stride_seq; p.q_head = io->q_stride_head;
+    p.out = (char *)io->out; p.out_seq = io->out_stride_seq; p.out_head = io->out_stride_head; p.lse = io->lse;
+    p.scale = io->scale * 1.44269504f;
+    p.device_status = device_status;
+    return p;
+}
+
+tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, const int32_t *group_start,
+                      const tri_layer_cache *src, int32_t S, const tri_attend_io *io, int32_t *device_status,
+                      void *ws, size_t ws_bytes, cudaStream_t st)
+{
+    tri_status r;
+    if (!io || !ws || ((uintptr_t)ws & 255)) return TRI_ERR_INVALID_ARG;
+    if (!rows16_ok(io->q, io->q_stride_seq, io->q_stride_head, 0, 2) || !rows16_ok(io->out, io->out_stride_seq, io->out_stride_head, 0, 2) ||
+        !std::isfinite(io->scale))
+        return TRI_ERR_INVALID_ARG;
+    if ((r = check_device(c)) != TRI_OK) return r;
+    const AttendPlan pl = make_attend_plan(c, S, P);
+    if (ws_bytes < pl.total) return TRI_ERR_WORKSPACE;
+    char *w = (char *)ws;
+    const int32_t H = c->desc.n_kv_heads, G = c->desc.group_size;
+
+    MergeParams mp;
+    mp.pre.rec = nullptr; mp.pre.slots = mp.pre.whole = nullptr; mp.pre.rows = 0; mp.pre.spt = 0;
+    if (P > 0) {
+        AttendParams p = attend_params(c, prefix, P, S, io, device_status);
+        p.spt = pl.spt; p.group_start = group_start; p.finish = 0;
+        p.rec = (int2 *)(w + pl.pre_rec); p.slots = (float *)(w + pl.pre_slots); p.whole = (float *)(w + pl.pre_whole);
+        if (prefix->view->k_kind == 3) launch_attend<true>(pl.pre_rows, (unsigned)pl.blocks, st, p);
+        else launch_attend<false>(pl.pre_rows, (unsigned)pl.blocks, st, p);
+        if ((r = check_launch("k_attend (prefix)")) != TRI_OK) return r;
+        mp.pre.rec = p.rec; mp.pre.slots = p.slots; mp.pre.whole = p.whole; mp.pre.rows = pl.pre_rows; mp.pre.spt = pl.spt;
+    }
+    AttendParams p = attend_params(c, src, S, S, io, device_status);
+    p.finish = P > 0 ? 0 : 1;
+    p.rec = (int2 *)(w + pl.own_rec); p.slots = (float *)(w + pl.own_slots);
+    p.whole = P > 0 ? (float *)(w + pl.own_whole) : nullptr;
+    if (src->view->k_kind == 3) launch_attend<true>(pl.own_rows, (unsigned)pl.blocks, st, p);
+    else launch_attend<false>(pl.own_rows, (unsigned)pl.blocks, st, p);
+    if ((r = check_launch("k_attend")) != TRI_OK) return r;
+
+    mp.own.rec = p.rec; mp.own.slots = p.slots; mp.own.whole = p.whole; mp.own.rows = pl.own_rows; mp.own.spt = 0;
+    mp.S = S; mp.P = P; mp.H = H; mp.G = G; mp.group_start = group_start;
+    mp.out = p.out; mp.out_seq = p.out_seq; mp.out_head = p.out_head; mp.lse = io->lse; mp.device_status = device_status;
+    k_attend_merge<<<(unsigned)(S * H), kMergeThreads, 0, st>>>(mp);
+    return check_launch("k_attend_merge");
+}
+
+}  // namespace
+
+extern "C" size_t tri_attend_workspace_bytes(const tri_ctx *c, int32_t S, int32_t P)
+{
+    if (!c || S <= 0 || P < 0) return 0;
+    return make_attend_plan(c, S, P).total;
+}
+
+extern "C" tri_status tri_attend(tri_ctx *c, const tri_layer_cache *src, int32_t S, const tri_attend_io *io,
+                                 int32_t *device_status, void *ws, size_t ws_bytes, void *stream)
+{
+    const tri_status r = check_attend_cache(c, src, S);
+    if (r != TRI_OK) return r;
+    return run_attend(c, nullptr, 0, nullptr, src, S, io, device_status, ws, ws_bytes, (cudaStream_t)stream);
+}
+
+extern "C" tri_status tri_attend_shared(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, const int32_t *group_start,
+                                        const tri_layer_cache *src, int32_t S, const tri_attend_io *io,
+                                        int32_t *device_status, void *ws, size_t ws_bytes, void *stream)
+{
+    tri_status r;
+    if ((r = check_attend_cache(c, src, S)) != TRI_OK) return r;
+    if ((r = check_attend_cache(c, prefix, P)) != TRI_OK) return r;
+    if (!group_start) return TRI_ERR_INVALID_ARG;
+    return run_attend(c, prefix, P, group_start, src, S, io, device_status, ws, ws_bytes, (cudaStream_t)stream);
 }
 
 // ----------------------------------------------------------------------------------------------

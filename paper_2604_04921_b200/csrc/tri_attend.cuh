@@ -1,0 +1,585 @@
+// Attention of one decode step over the cache, and over shared prefixes.
+//
+// Mathematics.  With logits x_n = scale * q . k_n a set N of rows is summarised by
+//       m = a bound near max x_n (base-2 exponents),  l = sum 2^(x_n - m),  o = sum 2^(x_n - m) v_n,
+// and two summaries merge by bringing both to the larger m and adding.  out = o / l, so the rows of a unit may be cut
+// anywhere: over the warps of a block, over blocks, over a prefix and a sequence's own rows.
+//
+// What bounds it.  2 x 128 cached values are read for 4 * 128 * G flops: the kernel is bound by HBM.  Every cached row is
+// read once, with 16-byte asynchronous copies into a ring of shared-memory stages that each warp keeps for itself (no
+// block-wide barrier in the loop), 16 rows a stage.
+//
+// Work split.  All units of a call (sequence x KV head [x tile of query rows]) are laid end to end as tiles of 64 rows,
+// and each block of a grid that fills the GPU takes an equal share of that line, which begins and ends anywhere inside a
+// unit.  A unit that lies in one block is finished there; the parts of the others go to the workspace, one slot for a
+// block's first unit and one for its last, and k_attend_merge joins them in a fixed order.  The lengths are on the
+// device only, so every block finds its share by a sum over them.
+#pragma once
+#include "tri_score_tma.cuh"
+
+namespace tri {
+
+constexpr int kAttWarps = 4, kAttThreads = 32 * kAttWarps;
+constexpr int kAttSub = 16;                               // rows of a warp's stage
+constexpr int kAttTile = kAttWarps * kAttSub;             // rows of a block's step
+constexpr int kAttBlocksPerSM = 2;
+constexpr int kAttRowPitch = kHeadDim + 4;                // floats per row of a part: 128 sums, m, l, two unused
+constexpr float kAttLazy = 8.0f;                          // the bound m is raised when a logit passes it by this much
+
+// Stages of a warp's ring: 3 x 8 KB (bf16) or 6 x 4 KB (e4m3), so that 2 blocks per SM keep 128 KB or more in flight.
+template <bool KEY8> constexpr int kAttStages = KEY8 ? 6 : 3;
+constexpr int kAttRingBytes = kAttWarps * 3 * (kAttSub * kHeadDim * 2 * 2);     // 98304
+
+struct AttendParams {
+    View src;
+    int32_t layer, nseq, H, G;                            // nseq: sequences (or prefixes) of src
+    int32_t spt;                                          // prefixes: sequences per tile of query rows; own rows: 0
+    int32_t S;                                            // sequences of the call
+    const int32_t *unit_lens;                             // [nseq][H] of this layer or NULL
+    const float *k_scale, *v_scale;                       // [H] of this layer or NULL
+    const int32_t *group_start;                           // [nseq + 1], prefixes only
+    const char *q;
+    int64_t q_seq, q_head;
+    char *out;
+    int64_t out_seq, out_head;
+    float *lse;
+    float scale;                                          // times log2 e
+    int32_t finish;                                       // units that lie in one block are written to out
+    float *slots;                                         // [blocks][2][rows][kAttRowPitch] parts of cut units
+    float *whole;                                         // [S][H][G][kAttRowPitch] summaries of uncut units (finish == 0)
+    int2 *rec;                                            // per unit: first block and number of parts
+    int32_t *device_status;
+};
+
+__device__ __forceinline__ int att_len(const AttendParams &p, int seq, int h)
+{
+    const int n = p.unit_lens ? __ldg(p.unit_lens + (int64_t)seq * p.H + h) : __ldg(p.src.seq_lens + seq);
+    return min(max(n, 0), p.src.n_max);
+}
+// Sequences [first, first + count) of a group.
+__device__ __forceinline__ int2 att_group(const int32_t *start, int S, int g)
+{
+    const int a = min(max(__ldg(start + g), 0), S), b = min(max(__ldg(start + g + 1), 0), S);
+    return make_int2(a, max(b - a, 0));
+}
+__device__ __forceinline__ int att_row_tiles(const AttendParams &p, int seq)
+{
+    if (p.spt == 0) return 1;
+    return (att_group(p.group_start, p.S, seq).y + p.spt - 1) / p.spt;
+}
+// Index of tile `rt` of group g in units before the head is added: the tiles of ascending groups never collide, and no
+// index reaches P + S / spt + 1 whatever group_start holds.
+__device__ __forceinline__ int att_tile_index(int g, int first, int spt, int rt) { return g + first / spt + rt; }
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint32_t bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void ldmatrix_x4_t(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];\n"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+__device__ __forceinline__ void mma_bf16_16816_acc(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                                   uint32_t b0, uint32_t b1)
+{
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+template <bool F16>
+__device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    if (F16) mma_f16_16816(d, a0, a1, a2, a3, b0, b1);
+    else mma_bf16_16816_acc(d, a0, a1, a2, a3, b0, b1);
+}
+// (lower, upper) as a 16-bit pair, and what the rounding left over as a second pair.
+template <bool F16>
+__device__ __forceinline__ void split16(float lower, float upper, uint32_t &hi, uint32_t &lo)
+{
+    if (F16) {
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;\n" : "=r"(hi) : "f"(upper), "f"(lower));
+        const float rl = lower - f16_value(hi & 0xffffu), ru = upper - f16_value(hi >> 16);
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;\n" : "=r"(lo) : "f"(ru), "f"(rl));
+    } else {
+        hi = cvt_bf16x2(upper, lower);
+        lo = cvt_bf16x2(upper - bf16_hi(hi), lower - bf16_lo(hi));
+    }
+}
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// The share of one block: where it begins on the line of tiles and which unit lies there.
+struct AttShare {
+    int64_t total, t0, t1;        // tiles of the call; this block's [t0, t1)
+    int64_t start;                // first tile of the unit (all of its row tiles) below
+    int32_t blocks, unit;         // blocks that get tiles; seq * H + h, nseq * H if there is none
+};
+
+// Units are entries seq * H + h; where the heads of a sequence have equal lengths the sums run over sequences only.
+__device__ __forceinline__ AttShare att_share(const AttendParams &p, int tile_rows)
+{
+    __shared__ long long part_s[kAttWarps];
+    __shared__ long long found_start;
+    __shared__ int found;
+    const int tid = threadIdx.x, nth = blockDim.x, lane = tid & 31, warp = tid >> 5;
+    const bool by_head = p.unit_lens != nullptr;
+    const int n = by_head ? p.nseq * p.H : p.nseq;
+    const int per = (n + nth - 1) / nth;
+    const int a = min(tid * per, n), b = min(a + per, n);
+    auto cost = [&](int x) -> long long {
+        const int seq = by_head ? x / p.H : x, h = by_head ? x - seq * p.H : 0;
+        const long long kt = ((long long)att_len(p, seq, h) + tile_rows - 1) / tile_rows;
+        return kt == 0 ? 0 : kt * att_row_tiles(p, seq) * (by_head ? 1 : p.H);
+    };
+    long long sum = 0;
+    for (int x = a; x < b; ++x) sum += cost(x);
+    long long incl = sum;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const long long o = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += o;
+    }
+    if (lane == 31) part_s[warp] = incl;
+    if (tid == 0) found = n;
+    __syncthreads();
+    long long before = 0, total = 0;
+    for (int w = 0; w < nth / 32; ++w) {
+        if (w < warp) before += part_s[w];
+        total += part_s[w];
+    }
+    AttShare r;
+    r.total = total;
+    r.blocks = total < (long long)gridDim.x ? (total > 0 ? (int)total : 1) : (int)gridDim.x;
+    const int blk = (int)blockIdx.x;
+    r.t0 = blk < r.blocks ? blk * total / r.blocks : total;
+    r.t1 = blk < r.blocks ? (blk + 1) * total / r.blocks : total;
+    // the first entry that ends behind t0 or starts at it: units without tiles belong to the block that reaches them
+    long long at = before + incl - sum;
+    for (int x = a; x < b; ++x) {
+        const long long c = cost(x);
+        if (at >= r.t0 || at + c > r.t0) { atomicMin(&found, x); break; }
+        at += c;
+    }
+    __syncthreads();
+    const int x = found;
+    if (x >= a && x < b) found_start = at;
+    __syncthreads();
+    if (x >= n) { r.unit = p.nseq * p.H; r.start = total; return r; }
+    r.start = found_start;
+    r.unit = by_head ? x : x * p.H;
+    if (!by_head && r.start < r.t0) {
+        const long long c = cost(x) / p.H;
+        const int skip = (int)((r.t0 - r.start) / c);
+        r.unit += skip;
+        r.start += skip * c;
+    }
+    return r;
+}
+
+// Which block holds tile t of the line.
+__device__ __forceinline__ int att_block_of(const AttShare &r, int64_t t) { return (int)(((t + 1) * r.blocks - 1) / r.total); }
+
+// KEY8: e4m3 rows, widened exactly to f16 (the queries are brought to f16 by a power of two per row).
+// RT = 8: at most 8 query rows; the rest of the rounded weights rides in the upper 8 rows of the 16-row MMA, for free.
+// RT = 16: up to 16 query rows; that rest takes a second MMA.
+template <bool KEY8, int RT>
+__global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const AttendParams p)
+{
+    constexpr int ST = kAttStages<KEY8>;
+    constexpr int kRowBytes = KEY8 ? 128 : 256, kHalf = kAttSub * kRowBytes, kStage = 2 * kHalf;      // K | V
+    constexpr int kChunks = kRowBytes / 16, kCopies = kAttSub * kChunks / 32;
+    constexpr int NR = RT / 8;                            // query rows per thread
+    extern __shared__ __align__(128) uint8_t dyn[];
+    __shared__ float stat[kAttWarps][RT][2];
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
+    const uint32_t ring = smem_u32(dyn) + warp * (ST * kStage);
+    const AttShare sh = att_share(p, kAttTile);
+    const bool last_block = (int)blockIdx.x == sh.blocks - 1;
+    if ((int)blockIdx.x >= sh.blocks) return;
+
+    int64_t start = sh.start;
+    for (int unit = sh.unit; unit < p.nseq * p.H; ++unit) {
+        if (start >= sh.t1 && !(last_block && start == sh.total)) break;
+        const int seq = unit / p.H, h = unit - seq * p.H;
+        const int len = att_len(p, seq, h), kt = (int)(((int64_t)len + kAttTile - 1) / kAttTile), rts = att_row_tiles(p, seq);
+        const int2 grp = p.spt ? att_group(p.group_start, p.S, seq) : make_int2(seq, 1);
+        for (int rt = 0; rt < rts; ++rt) {
+            const int64_t js = start + (int64_t)rt * kt, je = js + kt;       // this unit's tiles on the line
+            if (je <= sh.t0 && !(kt == 0 && js >= sh.t0)) continue;
+            if (js >= sh.t1 && !(last_block && js == sh.total)) break;
+            const int first_seq = grp.x + rt * p.spt;                        // first sequence of the tile's query rows
+            const int nrows = p.spt ? min(p.spt, grp.y - rt * p.spt) * p.G : p.G;
+            const int rec = p.spt ? att_tile_index(seq, grp.x, p.spt, rt) * p.H + h : unit;
+            const int ka = js < sh.t0 ? (int)(sh.t0 - js) : 0, kb = je > sh.t1 ? (int)(sh.t1 - js) : kt;
+            const bool begins = js >= sh.t0, complete = begins && kb == kt;
+            if (begins && tid == 0) {
+                const int first = blockIdx.x, lastb = kt ? att_block_of(sh, je - 1) : first;
+                p.rec[rec] = make_int2(first, kt == 0 ? 0 : lastb - first + 1);
+            }
+            if (kt == 0 && !p.finish) continue;
+
+            // ---------------- query rows as the A operand ----------------
+            uint32_t qa[8][4];
+            float mul[NR];                                                   // logit in base-2 units per accumulator unit
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int r = g8 + 8 * i;
+                const bool have = r < nrows && (RT == 16 || i == 0);
+                const char *qr = nullptr;
+                if (have) {
+                    const int sq = p.spt ? first_seq + r / p.G : seq, gg = p.spt ? r % p.G : r;
+                    qr = p.q + ((int64_t)sq * p.q_seq + (int64_t)(h * p.G + gg) * p.q_head) * 2;
+                }
+                float amax = 0.f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    // slots 2 t4, 2 t4 + 1 and 2 t4 + 8, + 9 of step k: dims 16 k + slot, for 8-bit keys dims 16 k + 4 t4 + 0..3
+                    const int d0 = 16 * k + (KEY8 ? 4 * t4 : 2 * t4), d1 = KEY8 ? d0 + 2 : d0 + 8;
+                    qa[k][i] = have ? *reinterpret_cast<const uint32_t *>(qr + 2 * d0) : 0u;
+                    qa[k][i + 2] = have ? *reinterpret_cast<const uint32_t *>(qr + 2 * d1) : 0u;
+                    if (KEY8) {
+                        amax = fmaxf(amax, fmaxf(fmaxf(fabsf(bf16_lo(qa[k][i])), fabsf(bf16_hi(qa[k][i]))),
+                                                 fmaxf(fabsf(bf16_lo(qa[k][i + 2])), fabsf(bf16_hi(qa[k][i + 2])))));
+                    }
+                }
+                float back = 1.f;
+                if (KEY8) {
+                    // f16 holds 11 bits down to 2^-14: with the row's largest entry brought to [1, 2) a bf16 entry is exact
+                    // unless it is 2^14 times smaller than that one
+                    amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+                    amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+                    int e = (int)((__float_as_uint(amax) >> 23) & 255u) - 127;
+                    e = min(max(e, -126), 126);
+                    if (amax == 0.f) e = 0;
+                    const float by = __uint_as_float((uint32_t)(127 - e) << 23);
+                    back = __uint_as_float((uint32_t)(127 + e) << 23);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const uint32_t w = qa[k][i + 2 * j];
+                            qa[k][i + 2 * j] = f16_bits(bf16_lo(w) * by) | (f16_bits(bf16_hi(w) * by) << 16);
+                        }
+                }
+                if (i < NR) mul[i % NR] = p.scale * (p.k_scale ? __ldg(p.k_scale + h) : 1.f) * back;
+            }
+
+            // ---------------- stream the rows ----------------
+            float o[16][4], m[NR], l[NR];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) { o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f; }
+#pragma unroll
+            for (int i = 0; i < NR; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
+            const int nit = kb - ka;
+            // subtile `it` of this warp: rows row(it) .. row(it) + 15
+            auto row_of = [&](int it) { return (int64_t)(ka + it) * kAttTile + warp * kAttSub; };
+            auto page_of = [&](int it) -> int {
+                const int64_t r = row_of(it);
+                if (!p.src.paged || it >= nit || r >= len) return 0;
+                const int pg = p.src.page_shift >= 0 ? (int)r >> p.src.page_shift : (int)r / p.src.page_size;
+                return __ldg(p.src.page_table + (int64_t)seq * p.src.max_pages_per_seq + pg);
+            };
+            uint32_t bad = 0;                                                // bit i: the rows of stage i are absent
+            int page_next = page_of(0);
+            auto issue = [&](int it) {
+                const int64_t r = row_of(it);
+                const int stage = it % ST;
+                if (it < nit && r < len) {
+                    int64_t base = (int64_t)p.layer * p.src.stride_layer + (int64_t)h * p.src.stride_head, step;
+                    bool ok = true;
+                    if (p.src.paged) {
+                        ok = p.src.n_pages <= 0 || (page_next >= 0 && page_next < p.src.n_pages);
+                        const int off = (int)r - (p.src.page_shift >= 0 ? ((int)r >> p.src.page_shift) << p.src.page_shift
+                                                                         : (int)r / p.src.page_size * p.src.page_size);
+                        step = p.src.stride_slot;
+                        base += (ok ? (int64_t)page_next * p.src.stride_page : 0) + (int64_t)off * step;
+                    } else {
+                        step = p.src.stride_tok;
+                        base += (int64_t)seq * p.src.stride_seq + r * step;
+                    }
+                    bad = (bad & ~(1u << stage)) | (ok ? 0u : 1u << stage);
+                    if (!ok && lane == 0 && p.device_status) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
+                    const int have = ok ? (int)(len - r < kAttSub ? len - r : kAttSub) : 0;
+                    const uint32_t dst = ring + stage * kStage;
+                    constexpr int es = KEY8 ? 1 : 2;
+                    const int c = lane % kChunks, r0 = lane / kChunks;
+#pragma unroll
+                    for (int i = 0; i < kCopies; ++i) {
+                        // rows behind the length (or absent ones) arrive as zeros and are not read
+                        const int row = i * (32 / kChunks) + r0;
+                        const uint32_t bytes = row < have ? 16u : 0u;
+                        const int64_t off = (base + (int64_t)(row < have ? row : 0) * step) * es + 16 * c;
+                        const uint32_t to = dst + row * kRowBytes + (((c & 8) | ((c ^ row) & 7)) << 4);
+                        const int64_t from = have ? off : 16 * c;
+                        cp_async16(to, p.src.k + from, bytes);
+                        cp_async16(to + kHalf, p.src.v + from, bytes);
+                    }
+                }
+                page_next = page_of(it + 1);
+                cp_commit();
+            };
+            if (nit > 0) {
+#pragma unroll
+                for (int i = 0; i < ST - 1; ++i) issue(i);
+            }
+            for (int it = 0; it < nit; ++it) {
+                cp_wait<ST - 2>();
+                __syncwarp();
+                const int64_t r0 = row_of(it);
+                const int stage = it % ST;
+                if (r0 < len && !((bad >> stage) & 1u)) {
+                    const int have = len - r0 < kAttSub ? (int)(len - r0) : kAttSub;
+                    const uint32_t kb_s = ring + stage * kStage, vb_s = kb_s + kHalf;
+                    float sc[2][4];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) sc[j][0] = sc[j][1] = sc[j][2] = sc[j][3] = 0.f;
+                    if (KEY8) {
+#pragma unroll
+                        for (int k = 0; k < 8; k += 2) {
+                            uint32_t f[4];
+                            const int row = (lane & 7) + (lane & 8), ch = k + (lane >> 4);
+                            ldmatrix_x4(f, kb_s + row * 128 + (((ch ^ row) & 7) << 4));
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                uint32_t b0, b1;
+                                e4m3x4_to_f16x2(f[j], b0, b1);
+                                const int kk = k + (j >> 1);
+                                mma16<true>(sc[j & 1], qa[kk][0], qa[kk][1], qa[kk][2], qa[kk][3], b0, b1);
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            uint32_t f[4];
+                            const int row = (lane & 7) + ((lane & 16) >> 1), ch = 2 * k + ((lane >> 3) & 1);
+                            ldmatrix_x4(f, kb_s + row * 256 + (((ch & 8) | ((ch ^ row) & 7)) << 4));
+                            mma16<false>(sc[0], qa[k][0], qa[k][1], qa[k][2], qa[k][3], f[0], f[1]);
+                            mma16<false>(sc[1], qa[k][0], qa[k][1], qa[k][2], qa[k][3], f[2], f[3]);
+                        }
+                    }
+                    // logits, running bound, weights; thread holds keys 8 j + 2 t4 + x of row g8 (+ 8)
+                    float w[NR][4];
+#pragma unroll
+                    for (int i = 0; i < NR; ++i) {
+                        float mx = -INFINITY;
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const int key = 8 * (x >> 1) + 2 * t4 + (x & 1);
+                            w[i][x] = key < have ? sc[x >> 1][2 * i + (x & 1)] * mul[i] : -INFINITY;
+                            mx = fmaxf(mx, w[i][x]);
+                        }
+                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+                        const bool raise = mx > m[i] + kAttLazy || (m[i] == -INFINITY && mx > m[i]);
+                        if (__any_sync(0xffffffffu, raise)) {
+                            const float by = raise ? ex2(m[i] - mx) : 1.f;   // 0 where there was no bound yet
+                            if (raise) m[i] = mx;
+                            l[i] *= by;
+#pragma unroll
+                            for (int n = 0; n < 16; ++n) {
+                                o[n][2 * i] *= by; o[n][2 * i + 1] *= by;
+                                if (RT == 8) { o[n][2] *= by; o[n][3] *= by; }
+                            }
+                        }
+                        const float ref = m[i] == -INFINITY ? 0.f : m[i];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            w[i][x] = ex2(w[i][x] - ref);
+                            l[i] += w[i][x];
+                        }
+                    }
+                    uint32_t ph[NR][2], pl[NR][2];
+#pragma unroll
+                    for (int i = 0; i < NR; ++i) {
+                        split16<KEY8>(w[i][0], w[i][1], ph[i][0], pl[i][0]);
+                        split16<KEY8>(w[i][2], w[i][3], ph[i][1], pl[i][1]);
+                    }
+                    auto pv = [&](float (&acc)[4], uint32_t b0, uint32_t b1) {
+                        if (RT == 8) {
+                            mma16<KEY8>(acc, ph[0][0], pl[0][0], ph[0][1], pl[0][1], b0, b1);
+                        } else {
+                            mma16<KEY8>(acc, ph[0][0], ph[NR - 1][0], ph[0][1], ph[NR - 1][1], b0, b1);
+                            mma16<KEY8>(acc, pl[0][0], pl[NR - 1][0], pl[0][1], pl[NR - 1][1], b0, b1);
+                        }
+                    };
+                    if (KEY8) {
+#pragma unroll
+                        for (int ch = 0; ch < 8; ch += 2) {
+                            uint32_t f[4];
+                            const int row = (lane & 7) + (lane & 8), cc = ch + (lane >> 4);
+                            ldmatrix_x4_t(f, vb_s + row * 128 + (((cc ^ row) & 7) << 4));
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                // bytes of a word: key 2 t4 dims (2 g8, 2 g8 + 1), key 2 t4 + 1 the same dims
+                                uint32_t e0, d0, e1, d1;
+                                e4m3x4_to_f16x2(__byte_perm(f[2 * j], 0, 0x3120), e0, d0);
+                                e4m3x4_to_f16x2(__byte_perm(f[2 * j + 1], 0, 0x3120), e1, d1);
+                                pv(o[2 * (ch + j)], e0, e1);
+                                pv(o[2 * (ch + j) + 1], d0, d1);
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int n = 0; n < 16; n += 2) {
+                            uint32_t f[4];
+                            const int row = (lane & 7) + (lane & 8), cc = n + (lane >> 4);
+                            ldmatrix_x4_t(f, vb_s + row * 256 + (((cc & 8) | ((cc ^ row) & 7)) << 4));
+                            pv(o[n], f[0], f[1]);
+                            pv(o[n + 1], f[2], f[3]);
+                        }
+                    }
+                }
+                __syncwarp();
+                issue(it + ST - 1);
+            }
+            cp_wait<0>();
+
+            // ---------------- join the warps ----------------
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+                l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+                l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+                if (t4 == 0) { stat[warp][g8 + 8 * i][0] = m[i]; stat[warp][g8 + 8 * i][1] = l[i]; }
+            }
+            __syncthreads();
+            float *red = reinterpret_cast<float *>(dyn);                     // [warps][RT][132]: the ring has been read
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+                const int r = g8 + 8 * i;
+                float mm = stat[0][r][0];
+#pragma unroll
+                for (int w2 = 1; w2 < kAttWarps; ++w2) mm = fmaxf(mm, stat[w2][r][0]);
+                const float by = m[i] == -INFINITY ? 0.f : ex2(m[i] - mm);
+                float *to = red + (warp * RT + r) * kAttRowPitch;
+#pragma unroll
+                for (int n = 0; n < 16; ++n) {
+                    const int d0 = KEY8 ? 16 * (n >> 1) + 4 * t4 + (n & 1) : 8 * n + 2 * t4, d1 = d0 + (KEY8 ? 2 : 1);
+                    to[d0] = (o[n][2 * i] + (RT == 8 ? o[n][2] : 0.f)) * by;
+                    to[d1] = (o[n][2 * i + 1] + (RT == 8 ? o[n][3] : 0.f)) * by;
+                }
+            }
+            __syncthreads();
+            const float vs = p.v_scale ? __ldg(p.v_scale + h) : 1.f;
+            float *slot = p.slots + ((int64_t)blockIdx.x * 2 + (begins ? 1 : 0)) * (RT * kAttRowPitch);
+            for (int r = warp; r < nrows; r += kAttWarps) {
+                float mm = stat[0][r][0], ll = 0.f;
+#pragma unroll
+                for (int w2 = 1; w2 < kAttWarps; ++w2) mm = fmaxf(mm, stat[w2][r][0]);
+                float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int w2 = 0; w2 < kAttWarps; ++w2) {
+                    const float4 x = *reinterpret_cast<const float4 *>(red + (w2 * RT + r) * kAttRowPitch + 4 * lane);
+                    a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
+                    ll += stat[w2][r][0] == -INFINITY ? 0.f : stat[w2][r][1] * ex2(stat[w2][r][0] - mm);
+                }
+                const int sq = p.spt ? first_seq + r / p.G : seq, hq = h * p.G + (p.spt ? r % p.G : r);
+                if (complete && p.finish) {
+                    const float inv = ll == 0.f ? 0.f : vs / ll;
+                    uint2 y = make_uint2(cvt_bf16x2(a.y * inv, a.x * inv), cvt_bf16x2(a.w * inv, a.z * inv));
+                    *reinterpret_cast<uint2 *>(p.out + ((int64_t)sq * p.out_seq + (int64_t)hq * p.out_head) * 2 + 8 * lane) = y;
+                    if (p.lse && lane == 0) p.lse[(int64_t)sq * p.H * p.G + hq] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.69314718f;
+                } else {
+                    float *to = complete ? p.whole + ((int64_t)sq * p.H * p.G + hq) * kAttRowPitch : slot + r * kAttRowPitch;
+                    *reinterpret_cast<float4 *>(to + 4 * lane) = make_float4(a.x * vs, a.y * vs, a.z * vs, a.w * vs);
+                    if (lane == 0) *reinterpret_cast<float2 *>(to + kHeadDim) = make_float2(mm, ll);
+                }
+            }
+            __syncthreads();                                                 // the ring may be refilled
+        }
+        start += (int64_t)kt * rts;
+    }
+}
+
+// ----------------------------------------------------------------------------------------------
+// Joins the parts of every (sequence, KV head): those of its own rows and those of its prefix.
+// ----------------------------------------------------------------------------------------------
+struct AttendPass {                // where a pass left its parts
+    const int2 *rec;
+    const float *slots, *whole;
+    int32_t rows;                  // query rows per slot
+    int32_t spt;                   // prefixes: sequences per tile
+};
+
+struct MergeParams {
+    AttendPass own, pre;           // pre.rec == NULL: no prefixes
+    int32_t S, P, H, G;
+    const int32_t *group_start;
+    char *out;
+    int64_t out_seq, out_head;
+    float *lse;
+    int32_t *device_status;
+};
+
+constexpr int kMergeThreads = 128;
+
+__global__ void __launch_bounds__(kMergeThreads) k_attend_merge(const MergeParams p)
+{
+    const int s = blockIdx.x / p.H, h = blockIdx.x - s * p.H, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int2 own = __ldg(p.own.rec + blockIdx.x);
+    if (!p.pre.rec && own.y < 2) return;           // finished by its block
+    int2 pre = make_int2(0, 0);
+    int row0 = 0;
+    if (p.pre.rec) {
+        // the group of this sequence: the last one that starts at or before it
+        int lo = 0, hi = p.P;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (__ldg(p.group_start + mid) <= s) lo = mid; else hi = mid;
+        }
+        const int2 g = att_group(p.group_start, p.S, lo);
+        if (s >= g.x && s < g.x + g.y) {
+            const int rt = (s - g.x) / p.pre.spt;
+            pre = __ldg(p.pre.rec + (int64_t)att_tile_index(lo, g.x, p.pre.spt, rt) * p.H + h);
+            row0 = (s - g.x - rt * p.pre.spt) * p.G;
+        }
+        if (blockIdx.x == 0 && p.device_status)
+            for (int i = threadIdx.x; i < p.P; i += kMergeThreads)
+                if (__ldg(p.group_start + i) > __ldg(p.group_start + i + 1)) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
+    }
+    const int parts = own.y + pre.y;
+    for (int g = warp; g < p.G; g += kMergeThreads / 32) {
+        const int64_t hq = (int64_t)h * p.G + g;
+        // part i: the own rows' parts in ascending order, then the prefix's
+        auto at = [&](int i) -> const float * {
+            const bool is_own = i < own.y;
+            const AttendPass &a = is_own ? p.own : p.pre;
+            const int2 rc = is_own ? own : pre;
+            const int k = is_own ? i : i - own.y;
+            if (rc.y == 1) return a.whole + ((int64_t)s * p.H * p.G + hq) * kAttRowPitch;
+            return a.slots + (((int64_t)(rc.x + k) * 2 + (k == 0 ? 1 : 0)) * a.rows + (is_own ? 0 : row0) + g) * kAttRowPitch;
+        };
+        float mm = -INFINITY;
+        for (int i = lane; i < parts; i += 32) mm = fmaxf(mm, __ldg(at(i) + kHeadDim));
+#pragma unroll
+        for (int d = 16; d; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, d));
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+        float ll = 0.f;
+#pragma unroll 4
+        for (int i = 0; i < parts; ++i) {
+            const float *src = at(i);
+            const float2 ml = *reinterpret_cast<const float2 *>(src + kHeadDim);
+            const float4 x = *reinterpret_cast<const float4 *>(src + 4 * lane);
+            const float by = ml.x == -INFINITY ? 0.f : ex2(ml.x - mm);
+            ll += ml.y * by;
+            a.x += x.x * by; a.y += x.y * by; a.z += x.z * by; a.w += x.w * by;
+        }
+        const float inv = ll == 0.f ? 0.f : 1.f / ll;
+        *reinterpret_cast<uint2 *>(p.out + ((int64_t)s * p.out_seq + hq * p.out_head) * 2 + 8 * lane) =
+            make_uint2(cvt_bf16x2(a.y * inv, a.x * inv), cvt_bf16x2(a.w * inv, a.z * inv));
+        if (p.lse && lane == 0) p.lse[(int64_t)s * p.H * p.G + hq] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.69314718f;
+    }
+}
+
+}  // namespace tri

@@ -1,0 +1,79 @@
+"""Host-only checks of the decode step's entry points: structure layouts, null arguments, the binding's own checks, and the
+64-bit forms the GPU tests compare with."""
+import ctypes
+import math
+import os
+import subprocess
+
+import pytest
+import torch
+
+from paper_2604_04921_b200 import binding as tb
+from step_reference import Cache, attention, pair_magnitude, rope
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def test_struct_layouts_match_the_header(tmp_path):
+    mirrors = {"tri_layer_cache": tb._LayerCache, "tri_append_rows": tb._AppendRows, "tri_attend_io": tb._AttendIo}
+    src = ['#include <stdio.h>', '#include <stddef.h>', '#include "tri_attention.h"', 'int main(void){']
+    for st, cls in mirrors.items():
+        src.append(f'printf("{st} %zu\\n", sizeof({st}));')
+        src += [f'printf("{st}.{f} %zu\\n", offsetof({st}, {f}));' for f, _ in cls._fields_]
+    (tmp_path / "l.c").write_text("\n".join(src + ['return 0;}']))
+    subprocess.run(["gcc", "-I", os.path.join(ROOT, "include"), "-o", str(tmp_path / "l"), str(tmp_path / "l.c")], check=True)
+    out = dict(x.split() for x in subprocess.run([str(tmp_path / "l")], check=True, capture_output=True, text=True).stdout.splitlines())
+    for st, cls in mirrors.items():
+        assert int(out[st]) == ctypes.sizeof(cls)
+        for f, _ in cls._fields_:
+            assert int(out[f"{st}.{f}"]) == getattr(cls, f).offset, (st, f)
+
+
+def test_null_arguments_are_rejected():
+    tb.build()
+    lib = tb.lib()
+    assert lib.tri_append(None, None, 1, None, None, None, None) == 1
+    assert lib.tri_attend(None, None, 1, None, None, None, 0, None) == 1
+    assert lib.tri_attend_shared(None, None, 1, None, None, 1, None, None, None, 0, None) == 1
+    assert lib.tri_attend_workspace_bytes(None, 1, 1) == 0
+
+
+def test_layer_cache_checks_its_parts():
+    c = Cache(2, 3, 2, 16, page=16, device="cpu")
+    lens = torch.zeros(3, dtype=torch.int32)
+    view = c.view(tb, seq_lens=lens)
+    lc = tb.LayerCache(view, 1)
+    assert (lc.n_layers, lc.n_seqs, lc.n_kv_heads) == (2, 3, 2)
+    assert lc._c.view.contents.page_size == 16 and lc._c.layer == 1 and lc._c.unit_lens is None
+    tb.LayerCache(c.view(tb), 0, unit_lens=torch.zeros(2, 3, 2, dtype=torch.int32))
+    for bad in (lambda: tb.LayerCache(view, 2), lambda: tb.LayerCache(c.view(tb), 0),
+                lambda: tb.LayerCache(view, 0, unit_lens=torch.zeros(2, 3, dtype=torch.int32)),
+                lambda: tb.LayerCache(view, 0, unit_lens=torch.zeros(2, 3, 2, dtype=torch.int64)),
+                lambda: tb.LayerCache(view, 0, k_scale=torch.zeros(2, 2, dtype=torch.float64)),
+                lambda: tb.LayerCache(view, 0, k_scale=torch.zeros(3)),
+                lambda: tb.LayerCache(c.view(tb, seq_lens=lens, positions=torch.zeros(1, 3, 2, 16, dtype=torch.int32)), 0)):
+        with pytest.raises(AssertionError):
+            bad()
+
+
+@pytest.mark.parametrize("half_split", [False, True])
+def test_reference_rotation(half_split):
+    """Keeps magnitudes, composes, and leaves position 0 alone."""
+    x = torch.randn(128, dtype=torch.float64, generator=torch.Generator().manual_seed(0))
+    assert torch.equal(rope(x, 0, 1e6, half_split), x)
+    y = rope(x, 1234, 1e6, half_split)
+    assert torch.allclose(pair_magnitude(x, half_split), pair_magnitude(y, half_split), atol=1e-12)
+    assert torch.allclose(rope(y, 766, 1e6, half_split), rope(x, 2000, 1e6, half_split), atol=1e-9)
+
+
+def test_reference_attention_merges_over_cuts():
+    """The identity every split of the kernels rests on: parts joined by their lse give the whole."""
+    g = torch.Generator().manual_seed(1)
+    q, k, v = torch.randn(128, generator=g).double(), torch.randn(50, 128, generator=g).double(), torch.randn(50, 128, generator=g).double()
+    whole, lse, _ = attention(q, k, v, 0.1)
+    a, la, _ = attention(q, k[:17], v[:17], 0.1)
+    b, lb, _ = attention(q, k[17:], v[17:], 0.1)
+    m = max(la, lb)
+    wa, wb = math.exp(la - m), math.exp(lb - m)
+    assert torch.allclose((wa * a + wb * b) / (wa + wb), whole, atol=1e-12)
+    assert abs(m + math.log(wa + wb) - lse) < 1e-12
