@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import dataclasses
 import os
+import struct
 import subprocess
 from pathlib import Path
 from typing import Optional, Sequence
@@ -97,6 +98,11 @@ class _AttendIo(ctypes.Structure):
                 ("lse", ctypes.c_void_p), ("scale", ctypes.c_float)]
 
 
+# The same two structures in one packing step: these calls are made per layer and token, where every microsecond of the
+# host counts (setting 20 fields one by one takes 2 us, packing them 0.5 us).
+_pack_append = struct.Struct("@PPPiiqqqqqqqqqPqqqPP").pack
+_pack_attend = struct.Struct("@PqqPqqPfi").pack
+
 _lib = None
 
 
@@ -161,14 +167,13 @@ def lib():
     L.tri_calib_finalize.restype = ctypes.c_int
     L.tri_selftest_bounded_wait.argtypes = [P, P]
     L.tri_selftest_bounded_wait.restype = ctypes.c_int
-    LP = ctypes.POINTER(_LayerCache)
-    L.tri_append.argtypes = [P, LP, i32, ctypes.POINTER(_AppendRows), P, P, P]
+    L.tri_append.argtypes = [P, P, i32, P, P, P, P]          # structures as addresses or packed bytes
     L.tri_append.restype = ctypes.c_int
     L.tri_attend_workspace_bytes.argtypes = [P, i32, i32]
     L.tri_attend_workspace_bytes.restype = sz
-    L.tri_attend.argtypes = [P, LP, i32, ctypes.POINTER(_AttendIo), P, P, sz, P]
+    L.tri_attend.argtypes = [P, P, i32, P, P, P, sz, P]
     L.tri_attend.restype = ctypes.c_int
-    L.tri_attend_shared.argtypes = [P, LP, i32, P, LP, i32, ctypes.POINTER(_AttendIo), P, P, sz, P]
+    L.tri_attend_shared.argtypes = [P, P, i32, P, P, i32, P, P, P, sz, P]
     L.tri_attend_shared.restype = ctypes.c_int
     L.tri_last_cuda_error.argtypes = []
     L.tri_last_cuda_error.restype = ctypes.c_char_p
@@ -194,12 +199,19 @@ def _stream():
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
-def _stream_of(device: torch.device):
-    return torch.cuda.current_stream(device).cuda_stream
+def _stream_on(device: int) -> int:
+    """The current stream of a device, as an address (current_stream() makes an object of it, 1 us)."""
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
-def _check_status_tensor(t: Optional[torch.Tensor], device: torch.device):
-    assert t is None or (t.dtype == torch.int32 and t.numel() >= 1 and t.device == device)
+def _status_addr(t: Optional[torch.Tensor], device: int) -> int:
+    if t is None:
+        return 0
+    assert t.dtype is torch.int32 and t.numel() >= 1 and t.get_device() == device
+    return t.data_ptr()
+
+
+_SCALE = 128.0 ** -0.5
 
 
 @dataclasses.dataclass
@@ -282,7 +294,8 @@ class LayerCache:
         for sc in (k_scale, v_scale):
             assert sc is None or (sc.dtype == torch.float32 and sc.is_contiguous() and sc.numel() == L * H)
         self._c = _LayerCache(ctypes.pointer(self._cv), layer, _addr(unit_lens), _addr(k_scale), _addr(v_scale))
-        self._ref = ctypes.byref(self._c)
+        self._ref = ctypes.addressof(self._c)
+        self._dev = view.k.get_device()
 
 
 class TriContext:
@@ -432,6 +445,9 @@ class TriContext:
                "tri_compress_host")
 
     # -- the decode step around the round ----------------------------------------------------
+    def _check_cache(self, c: LayerCache):
+        assert c.n_kv_heads == self.n_kv_heads and c.n_layers == self.n_layers, "the cache is of another model"
+
     def append(self, dst: LayerCache, k: torch.Tensor, v: Optional[torch.Tensor], pos: Optional[torch.Tensor],
                q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
                n_new: Optional[torch.Tensor] = None, new_lens: Optional[torch.Tensor] = None,
@@ -440,38 +456,43 @@ class TriContext:
         pre-RoPE; keys are rotated to positions pos[s] + t on the way (kept as they are in a pre-RoPE cache) and, if
         given, q [S, T, H * G, 128] into q_out (bf16).  n_new [S] int32: tokens each sequence brings, default T.
         new_lens receives the lengths after the append and may be the array they come from (last layer of a step)."""
-        S, T, H, D = k.shape
-        Hq = H * self.group_size
-        dev = dst.device
-        assert S == dst.n_seqs and H == self.n_kv_heads == dst.n_kv_heads and dst.n_layers == self.n_layers and D == 128
-        assert k.dtype in (torch.bfloat16, torch.float32) and k.device == dev and k.stride(3) == 1
-        r = _AppendRows()
-        r.k, r.kind, r.T = k.data_ptr(), 0 if k.dtype == torch.bfloat16 else 1, T
-        r.k_stride_seq, r.k_stride_tok, r.k_stride_head, _ = k.stride()
-        assert (v is not None) == (dst.view.v is not None), "values go with a cache that holds values"
+        self._check_cache(dst)
+        dev, S, shape, dt = dst._dev, dst.n_seqs, k.shape, k.dtype
+        T = shape[1]
+        assert shape == (S, T, self.n_kv_heads, 128) and k.get_device() == dev
+        assert dt is torch.bfloat16 or dt is torch.float32
+        ks, kt, kh, one = k.stride()
+        assert one == 1 and (v is not None) == (dst.view.v is not None), "values go with a cache that holds values"
+        vp = vs = vt = vh = 0
         if v is not None:
-            assert v.shape == k.shape and v.dtype == k.dtype and v.device == dev and v.stride(3) == 1
-            r.v = v.data_ptr()
-            r.v_stride_seq, r.v_stride_tok, r.v_stride_head, _ = v.stride()
+            vs, vt, vh, one = v.stride()
+            assert v.shape == shape and v.dtype is dt and v.get_device() == dev and one == 1
+            vp = v.data_ptr()
+        qp = qs = qt = qh = op = os_ = ot = oh = 0
         assert (q is None) == (q_out is None)
         if q is not None:
-            assert q.shape == q_out.shape == (S, T, Hq, 128) and q.dtype == k.dtype and q_out.dtype == torch.bfloat16
-            assert q.device == dev and q_out.device == dev and q.stride(3) == 1 and q_out.stride(3) == 1
-            r.q, r.q_out = q.data_ptr(), q_out.data_ptr()
-            r.q_stride_seq, r.q_stride_tok, r.q_stride_head, _ = q.stride()
-            r.qo_stride_seq, r.qo_stride_tok, r.qo_stride_head, _ = q_out.stride()
+            assert q.shape == q_out.shape == (S, T, self.n_kv_heads * self.group_size, 128)
+            assert q.dtype is dt and q_out.dtype is torch.bfloat16 and q.get_device() == dev and q_out.get_device() == dev
+            qs, qt, qh, one = q.stride()
+            os_, ot, oh, one_out = q_out.stride()
+            assert one == 1 and one_out == 1
+            qp, op = q.data_ptr(), q_out.data_ptr()
+        np_ = pp = lp = 0
         if n_new is not None:
-            assert n_new.dtype == torch.int32 and n_new.numel() == S and n_new.is_contiguous() and n_new.device == dev
-            r.n_new = n_new.data_ptr()
+            assert n_new.dtype is torch.int32 and n_new.numel() == S and n_new.is_contiguous() and n_new.get_device() == dev
+            np_ = n_new.data_ptr()
         if pos is not None:
-            assert pos.dtype == torch.int64 and pos.numel() == S and pos.is_contiguous() and pos.device == dev
-            r.pos = pos.data_ptr()
+            assert pos.dtype is torch.int64 and pos.numel() == S and pos.is_contiguous() and pos.get_device() == dev
+            pp = pos.data_ptr()
         if new_lens is not None:
-            assert new_lens.dtype == torch.int32 and new_lens.is_contiguous() and new_lens.device == dev
+            assert new_lens.dtype is torch.int32 and new_lens.is_contiguous() and new_lens.get_device() == dev
             assert new_lens.numel() == (S if dst.unit_lens is None else self.units(S))
-        _check_status_tensor(device_status, dev)
-        _check(lib().tri_append(self._h, dst._ref, S, ctypes.byref(r), _addr(new_lens), _addr(device_status),
-                                _stream_of(dev)), "tri_append")
+            lp = new_lens.data_ptr()
+        rows = _pack_append(k.data_ptr(), vp, qp, 0 if dt is torch.bfloat16 else 1, T, ks, kt, kh, vs, vt, vh, qs, qt, qh,
+                            op, os_, ot, oh, np_, pp)
+        code = lib().tri_append(self._h, dst._ref, S, rows, lp, _status_addr(device_status, dev), _stream_on(dev))
+        if code:
+            _check(code, "tri_append")
 
     def attend_workspace_bytes(self, S: int, n_prefixes: int = 0) -> int:
         return int(lib().tri_attend_workspace_bytes(self._h, S, n_prefixes))
@@ -480,27 +501,30 @@ class TriContext:
         return torch.empty(self.attend_workspace_bytes(S, n_prefixes), dtype=torch.uint8, device=device)
 
     def _attend_io(self, src: LayerCache, q: torch.Tensor, out: torch.Tensor, ws: torch.Tensor, scale: Optional[float],
-                   lse: Optional[torch.Tensor], device_status: Optional[torch.Tensor]) -> _AttendIo:
-        shape, dev = q.shape, src.device
-        assert src.n_kv_heads == self.n_kv_heads and src.n_layers == self.n_layers
-        assert shape == (src.n_seqs, self.n_kv_heads * self.group_size, 128) and out.shape == shape
-        assert q.dtype == torch.bfloat16 and out.dtype == torch.bfloat16 and q.device == dev and out.device == dev
-        assert ws.device == dev and ws.is_contiguous()
-        sq, so = q.stride(), out.stride()
-        assert sq[2] == 1 and so[2] == 1
+                   lse: Optional[torch.Tensor]) -> bytes:
+        self._check_cache(src)
+        dev, shape = src._dev, (src.n_seqs, self.n_kv_heads * self.group_size, 128)
+        assert q.shape == shape and out.shape == shape and q.dtype is torch.bfloat16 and out.dtype is torch.bfloat16
+        assert q.get_device() == dev and out.get_device() == dev and ws.get_device() == dev
+        assert ws.dtype is torch.uint8 and ws.is_contiguous()
+        qs, qh, one = q.stride()
+        os_, oh, one_out = out.stride()
+        assert one == 1 and one_out == 1
+        lp = 0
         if lse is not None:
-            assert lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == shape[:2] and lse.device == dev
-        _check_status_tensor(device_status, dev)
-        return _AttendIo(q.data_ptr(), sq[0], sq[1], out.data_ptr(), so[0], so[1], _addr(lse),
-                         128.0 ** -0.5 if scale is None else scale)
+            assert lse.dtype is torch.float32 and lse.is_contiguous() and lse.shape == shape[:2] and lse.get_device() == dev
+            lp = lse.data_ptr()
+        return _pack_attend(q.data_ptr(), qs, qh, out.data_ptr(), os_, oh, lp, _SCALE if scale is None else scale, 0)
 
     def attend(self, src: LayerCache, q: torch.Tensor, out: torch.Tensor, ws: torch.Tensor, scale: Optional[float] = None,
                lse: Optional[torch.Tensor] = None, device_status: Optional[torch.Tensor] = None):
         """Attention of one query token per sequence over one layer of the cache: q, out [S, H * G, 128] bf16 (q rotated
         like the cached keys), lse [S, H * G] fp32 or None, scale 1/sqrt(128) by default, ws from attend_workspace(S)."""
-        io = self._attend_io(src, q, out, ws, scale, lse, device_status)
-        _check(lib().tri_attend(self._h, src._ref, src.n_seqs, ctypes.byref(io), _addr(device_status), ws.data_ptr(),
-                                ws.numel() * ws.element_size(), _stream_of(src.device)), "tri_attend")
+        io, dev = self._attend_io(src, q, out, ws, scale, lse), src._dev
+        code = lib().tri_attend(self._h, src._ref, src.n_seqs, io, _status_addr(device_status, dev), ws.data_ptr(),
+                                ws.numel(), _stream_on(dev))
+        if code:
+            _check(code, "tri_attend")
 
     def attend_shared(self, prefix: LayerCache, group_start: torch.Tensor, src: LayerCache, q: torch.Tensor,
                       out: torch.Tensor, ws: torch.Tensor, scale: Optional[float] = None,
@@ -508,14 +532,14 @@ class TriContext:
         """attend() for sequences that continue shared prefixes: `prefix` is a cache of P sequences, sequences
         group_start[p] <= s < group_start[p + 1] ([P + 1] int32, ascending) attend over prefix p and their own rows.
         ws from attend_workspace(S, P)."""
-        io = self._attend_io(src, q, out, ws, scale, lse, device_status)
-        P = prefix.n_seqs
-        assert prefix.n_kv_heads == self.n_kv_heads and prefix.n_layers == self.n_layers and prefix.device == src.device
-        assert group_start.dtype == torch.int32 and group_start.shape == (P + 1,) and group_start.is_contiguous()
-        assert group_start.device == src.device
-        _check(lib().tri_attend_shared(self._h, prefix._ref, P, group_start.data_ptr(), src._ref, src.n_seqs,
-                                       ctypes.byref(io), _addr(device_status), ws.data_ptr(),
-                                       ws.numel() * ws.element_size(), _stream_of(src.device)), "tri_attend_shared")
+        io, dev, P = self._attend_io(src, q, out, ws, scale, lse), src._dev, prefix.n_seqs
+        self._check_cache(prefix)
+        assert prefix._dev == dev and group_start.get_device() == dev
+        assert group_start.dtype is torch.int32 and group_start.shape == (P + 1,) and group_start.is_contiguous()
+        code = lib().tri_attend_shared(self._h, prefix._ref, P, group_start.data_ptr(), src._ref, src.n_seqs, io,
+                                       _status_addr(device_status, dev), ws.data_ptr(), ws.numel(), _stream_on(dev))
+        if code:
+            _check(code, "tri_attend_shared")
 
     KERNELS = ("fold_phasors", "score", "normalize", "select", "compact")
 

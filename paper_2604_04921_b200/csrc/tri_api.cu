@@ -1329,8 +1329,14 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
     mp.own.rec = p.rec; mp.own.slots = p.slots; mp.own.whole = p.whole; mp.own.rows = pl.own_rows; mp.own.spt = 0;
     mp.S = S; mp.P = P; mp.H = H; mp.G = G; mp.group_start = group_start;
     mp.out = p.out; mp.out_seq = p.out_seq; mp.out_head = p.out_head; mp.lse = io->lse; mp.device_status = device_status;
-    k_attend_merge<<<(unsigned)(S * H), kMergeThreads, 0, st>>>(mp);
-    return check_launch("k_attend_merge");
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(S * H)); cfg.blockDim = dim3(kMergeThreads); cfg.stream = st;
+    cfg.attrs = &attr; cfg.numAttrs = 1;
+    TRI_CUDA(cudaLaunchKernelEx(&cfg, k_attend_merge, mp));
+    return TRI_OK;
 }
 
 }  // namespace

@@ -71,6 +71,9 @@ __device__ __forceinline__ int att_row_tiles(const AttendParams &p, int seq)
 // index reaches P + S / spt + 1 whatever group_start holds.
 __device__ __forceinline__ int att_tile_index(int g, int first, int spt, int rt) { return g + first / spt + rt; }
 
+__device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
+__device__ __forceinline__ void grid_dependents_launch() { asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory"); }
+
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint32_t bytes)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -205,6 +208,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
     const uint32_t ring = smem_u32(dyn) + warp * (ST * kStage);
+    grid_dependents_launch();                             // the joining kernel may be set up under this one
     const AttShare sh = att_share(p, kAttTile);
     const bool last_block = (int)blockIdx.x == sh.blocks - 1;
     if ((int)blockIdx.x >= sh.blocks) return;
@@ -522,13 +526,17 @@ struct MergeParams {
     int32_t *device_status;
 };
 
-constexpr int kMergeThreads = 128;
+// A block joins the G rows of one (sequence, KV head): 16 / G warps per row take its parts in turn, each lane four sums.
+// The kernel is launched while the pass before it still runs (programmatic dependent launch) and waits for it here.
+constexpr int kMergeWarps = 16, kMergeThreads = 32 * kMergeWarps;
 
 __global__ void __launch_bounds__(kMergeThreads) k_attend_merge(const MergeParams p)
 {
+    __shared__ float4 red[kMergeWarps][32];
     const int s = blockIdx.x / p.H, h = blockIdx.x - s * p.H, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int2 own = __ldg(p.own.rec + blockIdx.x);
-    if (!p.pre.rec && own.y < 2) return;           // finished by its block
+    grid_dependency_wait();
+    const int2 own = p.own.rec[blockIdx.x];
+    if (!p.pre.rec && own.y < 2) return;                                     // finished by its block
     int2 pre = make_int2(0, 0);
     int row0 = 0;
     if (p.pre.rec) {
@@ -541,7 +549,7 @@ __global__ void __launch_bounds__(kMergeThreads) k_attend_merge(const MergeParam
         const int2 g = att_group(p.group_start, p.S, lo);
         if (s >= g.x && s < g.x + g.y) {
             const int rt = (s - g.x) / p.pre.spt;
-            pre = __ldg(p.pre.rec + (int64_t)att_tile_index(lo, g.x, p.pre.spt, rt) * p.H + h);
+            pre = p.pre.rec[(int64_t)att_tile_index(lo, g.x, p.pre.spt, rt) * p.H + h];
             row0 = (s - g.x - rt * p.pre.spt) * p.G;
         }
         if (blockIdx.x == 0 && p.device_status)
@@ -549,37 +557,57 @@ __global__ void __launch_bounds__(kMergeThreads) k_attend_merge(const MergeParam
                 if (__ldg(p.group_start + i) > __ldg(p.group_start + i + 1)) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
     }
     const int parts = own.y + pre.y;
-    for (int g = warp; g < p.G; g += kMergeThreads / 32) {
-        const int64_t hq = (int64_t)h * p.G + g;
-        // part i: the own rows' parts in ascending order, then the prefix's
-        auto at = [&](int i) -> const float * {
-            const bool is_own = i < own.y;
-            const AttendPass &a = is_own ? p.own : p.pre;
-            const int2 rc = is_own ? own : pre;
-            const int k = is_own ? i : i - own.y;
-            if (rc.y == 1) return a.whole + ((int64_t)s * p.H * p.G + hq) * kAttRowPitch;
-            return a.slots + (((int64_t)(rc.x + k) * 2 + (k == 0 ? 1 : 0)) * a.rows + (is_own ? 0 : row0) + g) * kAttRowPitch;
-        };
-        float mm = -INFINITY;
-        for (int i = lane; i < parts; i += 32) mm = fmaxf(mm, __ldg(at(i) + kHeadDim));
+    const int wpr = kMergeWarps / p.G, g = warp / wpr, sub = warp - g * wpr;
+    const bool active = g < p.G;
+    const int64_t hq = (int64_t)h * p.G + g;
+    // part i: the own rows' parts in ascending order, then the prefix's
+    auto at = [&](int i) -> const float * {
+        const bool is_own = i < own.y;
+        const AttendPass &a = is_own ? p.own : p.pre;
+        const int2 rc = is_own ? own : pre;
+        const int k = is_own ? i : i - own.y;
+        if (rc.y == 1) return a.whole + ((int64_t)s * p.H * p.G + hq) * kAttRowPitch;
+        return a.slots + (((int64_t)(rc.x + k) * 2 + (k == 0 ? 1 : 0)) * a.rows + (is_own ? 0 : row0) + g) * kAttRowPitch;
+    };
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    float mm = -INFINITY, ll = 0.f;
+    if (active) {
+        for (int b = 0; b < parts; b += 32) {
+            // summaries of up to 32 parts, one per lane, then their sums; a larger bound met on the way rescales what is there
+            const float *mine = b + lane < parts ? at(b + lane) : nullptr;
+            const float2 ml = mine ? *reinterpret_cast<const float2 *>(mine + kHeadDim) : make_float2(-INFINITY, 0.f);
+            float top = fmaxf(mm, ml.x);
 #pragma unroll
-        for (int d = 16; d; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, d));
-        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-        float ll = 0.f;
-#pragma unroll 4
-        for (int i = 0; i < parts; ++i) {
-            const float *src = at(i);
-            const float2 ml = *reinterpret_cast<const float2 *>(src + kHeadDim);
-            const float4 x = *reinterpret_cast<const float4 *>(src + 4 * lane);
+            for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            const float old = mm == -INFINITY ? 0.f : ex2(mm - top);
+            mm = top;
             const float by = ml.x == -INFINITY ? 0.f : ex2(ml.x - mm);
-            ll += ml.y * by;
-            a.x += x.x * by; a.y += x.y * by; a.z += x.z * by; a.w += x.w * by;
+            float l = ml.y * by;
+#pragma unroll
+            for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+            ll = ll * old + l;
+            a.x *= old; a.y *= old; a.z *= old; a.w *= old;
+            const int n = min(32, parts - b);
+#pragma unroll 4
+            for (int j = sub; j < n; j += wpr) {
+                const float *src = reinterpret_cast<const float *>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), j));
+                const float w = __shfl_sync(0xffffffffu, by, j);
+                const float4 x = *reinterpret_cast<const float4 *>(src + 4 * lane);
+                a.x += x.x * w; a.y += x.y * w; a.z += x.z * w; a.w += x.w * w;
+            }
         }
-        const float inv = ll == 0.f ? 0.f : 1.f / ll;
-        *reinterpret_cast<uint2 *>(p.out + ((int64_t)s * p.out_seq + hq * p.out_head) * 2 + 8 * lane) =
-            make_uint2(cvt_bf16x2(a.y * inv, a.x * inv), cvt_bf16x2(a.w * inv, a.z * inv));
-        if (p.lse && lane == 0) p.lse[(int64_t)s * p.H * p.G + hq] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.69314718f;
+        red[warp][lane] = a;
     }
+    __syncthreads();
+    if (!active || sub != 0) return;
+    for (int w = 1; w < wpr; ++w) {
+        const float4 x = red[warp + w][lane];
+        a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
+    }
+    const float inv = ll == 0.f ? 0.f : 1.f / ll;
+    *reinterpret_cast<uint2 *>(p.out + ((int64_t)s * p.out_seq + hq * p.out_head) * 2 + 8 * lane) =
+        make_uint2(cvt_bf16x2(a.y * inv, a.x * inv), cvt_bf16x2(a.w * inv, a.z * inv));
+    if (p.lse && lane == 0) p.lse[(int64_t)s * p.H * p.G + hq] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.69314718f;
 }
 
 }  // namespace tri
