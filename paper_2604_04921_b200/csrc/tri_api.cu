@@ -12,6 +12,7 @@
 
 #include "tri_append.cuh"
 #include "tri_attend.cuh"
+#include "tri_attend_umma.cuh"
 #include "tri_calib.cuh"
 #include "tri_calib_tma.cuh"
 #include "tri_compact.cuh"
@@ -373,7 +374,9 @@ tri_status encode_fn(EncodeTiledFn *out)
     return TRI_OK;
 }
 
-tri_status encode_key_map(const tri_ctx *c, const tri_cache_view *v, int32_t S, int32_t n_layers, CUtensorMap *out)
+// (rows: the keys of the view, or its values when given)
+tri_status encode_key_map(const tri_ctx *c, const tri_cache_view *v, int32_t S, int32_t n_layers, CUtensorMap *out,
+                          void *rows = nullptr)
 {
     EncodeTiledFn fn;
     tri_status fs = encode_fn(&fn);
@@ -398,7 +401,7 @@ tri_status encode_key_map(const tri_ctx *c, const tri_cache_view *v, int32_t S, 
     strides[1] = bytes(v->stride_head);
     strides[3] = bytes(v->stride_layer);
     cuuint32_t box[5] = {(cuuint32_t)(key8 ? kHeadDim : kHeadDim / 2), kTileKeys, 1, 1, 1}, estr[5] = {1, 1, 1, 1, 1};
-    CUresult r = fn(out, key8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, v->k, dims, strides, box, estr,
+    CUresult r = fn(out, key8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, rows ? rows : v->k, dims, strides, box, estr,
                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) {
@@ -444,7 +447,8 @@ cudaError_t prepare_device()
     if ((e = allow_attend_smem<false, 8>()) != cudaSuccess) return e;
     if ((e = allow_attend_smem<false, 16>()) != cudaSuccess) return e;
     if ((e = allow_attend_smem<true, 8>()) != cudaSuccess) return e;
-    return allow_attend_smem<true, 16>();
+    if ((e = allow_attend_smem<true, 16>()) != cudaSuccess) return e;
+    return cudaFuncSetAttribute(k_attend_prefix, cudaFuncAttributeMaxDynamicSharedMemorySize, kPDynSmem);
 }
 
 // Every entry point that launches kernels runs on the device the context was created on.
@@ -1234,7 +1238,7 @@ namespace {
 // Workspace of an attention call.
 struct AttendPlan {
     int32_t blocks;                                    // grid of the streaming passes
-    int32_t own_rows, pre_rows, spt;                   // query rows per slot; sequences per tile of a prefix's query rows
+    int32_t own_rows;                                  // query rows per slot of the own rows' pass
     size_t own_rec, own_slots, own_whole, pre_rec, pre_slots, pre_whole, total;
 };
 
@@ -1244,15 +1248,15 @@ AttendPlan make_attend_plan(const tri_ctx *c, int32_t S, int32_t P)
     const int32_t H = c->desc.n_kv_heads, G = c->desc.group_size;
     a.blocks = c->n_sm * kAttBlocksPerSM;
     a.own_rows = G <= 8 ? 8 : 16;
-    a.pre_rows = 16;
-    a.spt = a.pre_rows / G;
     const size_t row = kAttRowPitch * sizeof(float), whole = align256((size_t)S * H * G * row);
     size_t o = 0;
     a.own_rec = o;   o += align256((size_t)S * H * sizeof(int2));
     a.own_slots = o; o += align256((size_t)a.blocks * 2 * a.own_rows * row);
     a.own_whole = o; o += P > 0 ? whole : 0;
-    a.pre_rec = o;   o += P > 0 ? align256(((size_t)P + S / a.spt + 2) * H * sizeof(int2)) : 0;
-    a.pre_slots = o; o += P > 0 ? align256((size_t)a.blocks * 2 * a.pre_rows * row) : 0;
+    // either pass over prefixes fits: tiles of 16 query rows on all blocks, or of 128 on one block per multiprocessor
+    a.pre_rec = o;   o += P > 0 ? align256(((size_t)P + S / (16 / G) + 2) * H * sizeof(int2)) : 0;
+    a.pre_slots = o; o += P > 0 ? align256((size_t)c->n_sm * 2 * kPTile * row) : 0;
+    static_assert(kPTile >= 16 * kAttBlocksPerSM, "slots of the 128-row pass cover those of the 16-row pass");
     a.pre_whole = o; o += P > 0 ? whole : 0;
     a.total = o;
     return a;
@@ -1271,6 +1275,16 @@ tri_status check_attend_cache(const tri_ctx *c, const tri_layer_cache *lc, int32
     if (r != TRI_OK) return r;
     if (lc->view->k_kind != 0 && lc->view->k_kind != 3) return TRI_ERR_UNSUPPORTED;
     return lc->view->v ? TRI_OK : TRI_ERR_INVALID_ARG;
+}
+
+// Whether the rows of a prefix can be addressed by the TMA unit: bf16, every stride that is used positive (a broadcast
+// head has stride 0) and below the unit's 2^40 bytes.
+bool prefix_umma_ok(const tri_ctx *c, const tri_cache_view *v, int32_t P)
+{
+    if (v->k_kind != 0) return false;
+    auto ok = [](int64_t n, int64_t stride) { return n <= 1 || (stride > 0 && stride < ((int64_t)1 << 38)); };
+    if (!ok(c->desc.n_kv_heads, v->stride_head) || !ok(c->desc.n_layers, v->stride_layer)) return false;
+    return v->paged ? ok(2, v->stride_page) && ok(2, v->stride_slot) : ok(P, v->stride_seq) && ok(2, v->stride_tok);
 }
 
 // The part of AttendParams that depends on the cache and the call only.
@@ -1311,12 +1325,22 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
     mp.pre.rec = nullptr; mp.pre.slots = mp.pre.whole = nullptr; mp.pre.rows = 0; mp.pre.spt = 0;
     if (P > 0) {
         AttendParams p = attend_params(c, prefix, P, S, io, device_status);
-        p.spt = pl.spt; p.group_start = group_start; p.finish = 0;
+        const bool umma = prefix_umma_ok(c, prefix->view, P);
+        const int rows = umma ? kPTile : 16;
+        p.spt = rows / G; p.group_start = group_start; p.finish = 0;
         p.rec = (int2 *)(w + pl.pre_rec); p.slots = (float *)(w + pl.pre_slots); p.whole = (float *)(w + pl.pre_whole);
-        if (prefix->view->k_kind == 3) launch_attend<true>(pl.pre_rows, (unsigned)pl.blocks, st, p);
-        else launch_attend<false>(pl.pre_rows, (unsigned)pl.blocks, st, p);
+        if (umma) {
+            CUtensorMap km, vm;
+            if ((r = encode_key_map(c, prefix->view, P, c->desc.n_layers, &km)) != TRI_OK) return r;
+            if ((r = encode_key_map(c, prefix->view, P, c->desc.n_layers, &vm, prefix->view->v)) != TRI_OK) return r;
+            k_attend_prefix<<<(unsigned)c->n_sm, kPThreads, kPDynSmem, st>>>(km, vm, p);
+        } else if (prefix->view->k_kind == 3) {
+            launch_attend<true>(rows, (unsigned)pl.blocks, st, p);
+        } else {
+            launch_attend<false>(rows, (unsigned)pl.blocks, st, p);
+        }
         if ((r = check_launch("k_attend (prefix)")) != TRI_OK) return r;
-        mp.pre.rec = p.rec; mp.pre.slots = p.slots; mp.pre.whole = p.whole; mp.pre.rows = pl.pre_rows; mp.pre.spt = pl.spt;
+        mp.pre.rec = p.rec; mp.pre.slots = p.slots; mp.pre.whole = p.whole; mp.pre.rows = rows; mp.pre.spt = p.spt;
     }
     AttendParams p = attend_params(c, src, S, S, io, device_status);
     p.finish = P > 0 ? 0 : 1;

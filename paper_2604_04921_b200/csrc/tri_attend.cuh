@@ -132,7 +132,7 @@ struct AttShare {
 // Units are entries seq * H + h; where the heads of a sequence have equal lengths the sums run over sequences only.
 __device__ __forceinline__ AttShare att_share(const AttendParams &p, int tile_rows)
 {
-    __shared__ long long part_s[kAttWarps];
+    __shared__ long long part_s[32];
     __shared__ long long found_start;
     __shared__ int found;
     const int tid = threadIdx.x, nth = blockDim.x, lane = tid & 31, warp = tid >> 5;
@@ -193,6 +193,47 @@ __device__ __forceinline__ AttShare att_share(const AttendParams &p, int tile_ro
 // Which block holds tile t of the line.
 __device__ __forceinline__ int att_block_of(const AttShare &r, int64_t t) { return (int)(((t + 1) * r.blocks - 1) / r.total); }
 
+// Where a block stands on the line, and what it finds there: rows ka .. kb (in tiles) of one unit and tile of query rows.
+struct AttCursor { int unit, rt; int64_t start; };
+struct AttJob {
+    int seq, h, len, kt, ka, kb;      // tiles [ka, kb) of the unit's kt
+    int first_seq, nrows;             // query rows: G of each sequence from first_seq on (prefixes), or of seq
+    int rec;                          // index of the unit's record
+    int2 record;                      // first block and number of parts
+    bool begins, complete;            // the unit's first tile / all of its tiles lie in this block
+};
+__device__ __forceinline__ bool att_next(const AttendParams &p, const AttShare &sh, int tile_rows, AttCursor &c, AttJob &j)
+{
+    const bool last = (int)blockIdx.x == sh.blocks - 1;
+    while (c.unit < p.nseq * p.H) {
+        if (c.start >= sh.t1 && !(last && c.start == sh.total)) return false;
+        j.seq = c.unit / p.H; j.h = c.unit - j.seq * p.H;
+        j.len = att_len(p, j.seq, j.h);
+        j.kt = (int)(((int64_t)j.len + tile_rows - 1) / tile_rows);
+        const int2 grp = p.spt ? att_group(p.group_start, p.S, j.seq) : make_int2(j.seq, 1);
+        const int rts = p.spt ? (grp.y + p.spt - 1) / p.spt : 1, rt = c.rt++;
+        if (rt >= rts) {
+            c.start += (int64_t)j.kt * rts;
+            ++c.unit;
+            c.rt = 0;
+            continue;
+        }
+        const int64_t js = c.start + (int64_t)rt * j.kt, je = js + j.kt;
+        if (je <= sh.t0 && !(j.kt == 0 && js >= sh.t0)) continue;
+        if (js >= sh.t1 && !(last && js == sh.total)) return false;
+        j.first_seq = grp.x + rt * p.spt;
+        j.nrows = p.spt ? min(p.spt, grp.y - rt * p.spt) * p.G : p.G;
+        j.rec = p.spt ? att_tile_index(j.seq, grp.x, p.spt, rt) * p.H + j.h : c.unit;
+        j.ka = js < sh.t0 ? (int)(sh.t0 - js) : 0;
+        j.kb = je > sh.t1 ? (int)(sh.t1 - js) : j.kt;
+        j.begins = js >= sh.t0;
+        j.complete = j.begins && j.kb == j.kt;
+        j.record = make_int2((int)blockIdx.x, j.kt == 0 ? 0 : att_block_of(sh, je - 1) - (int)blockIdx.x + 1);
+        return true;
+    }
+    return false;
+}
+
 // KEY8: e4m3 rows, widened exactly to f16 (the queries are brought to f16 by a power of two per row).
 // RT = 8: at most 8 query rows; the rest of the rounded weights rides in the upper 8 rows of the 16-row MMA, for free.
 // RT = 16: up to 16 query rows; that rest takes a second MMA.
@@ -210,299 +251,282 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
     const uint32_t ring = smem_u32(dyn) + warp * (ST * kStage);
     grid_dependents_launch();                             // the joining kernel may be set up under this one
     const AttShare sh = att_share(p, kAttTile);
-    const bool last_block = (int)blockIdx.x == sh.blocks - 1;
     if ((int)blockIdx.x >= sh.blocks) return;
 
-    int64_t start = sh.start;
-    for (int unit = sh.unit; unit < p.nseq * p.H; ++unit) {
-        if (start >= sh.t1 && !(last_block && start == sh.total)) break;
-        const int seq = unit / p.H, h = unit - seq * p.H;
-        const int len = att_len(p, seq, h), kt = (int)(((int64_t)len + kAttTile - 1) / kAttTile), rts = att_row_tiles(p, seq);
-        const int2 grp = p.spt ? att_group(p.group_start, p.S, seq) : make_int2(seq, 1);
-        for (int rt = 0; rt < rts; ++rt) {
-            const int64_t js = start + (int64_t)rt * kt, je = js + kt;       // this unit's tiles on the line
-            if (je <= sh.t0 && !(kt == 0 && js >= sh.t0)) continue;
-            if (js >= sh.t1 && !(last_block && js == sh.total)) break;
-            const int first_seq = grp.x + rt * p.spt;                        // first sequence of the tile's query rows
-            const int nrows = p.spt ? min(p.spt, grp.y - rt * p.spt) * p.G : p.G;
-            const int rec = p.spt ? att_tile_index(seq, grp.x, p.spt, rt) * p.H + h : unit;
-            const int ka = js < sh.t0 ? (int)(sh.t0 - js) : 0, kb = je > sh.t1 ? (int)(sh.t1 - js) : kt;
-            const bool begins = js >= sh.t0, complete = begins && kb == kt;
-            if (begins && tid == 0) {
-                const int first = blockIdx.x, lastb = kt ? att_block_of(sh, je - 1) : first;
-                p.rec[rec] = make_int2(first, kt == 0 ? 0 : lastb - first + 1);
-            }
-            if (kt == 0 && !p.finish) continue;
+    AttCursor cur = {sh.unit, 0, sh.start};
+    AttJob j;
+    while (att_next(p, sh, kAttTile, cur, j)) {
+        const int seq = j.seq, h = j.h, len = j.len, ka = j.ka, kb = j.kb, nrows = j.nrows, first_seq = j.first_seq;
+        if (j.begins && tid == 0) p.rec[j.rec] = j.record;
+        if (j.kt == 0 && !p.finish) continue;
 
-            // ---------------- query rows as the A operand ----------------
-            uint32_t qa[8][4];
-            float mul[NR];                                                   // logit in base-2 units per accumulator unit
+        // ---------------- query rows as the A operand ----------------
+        uint32_t qa[8][4];
+        float mul[NR];                                                   // logit in base-2 units per accumulator unit
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int r = g8 + 8 * i;
-                const bool have = r < nrows && (RT == 16 || i == 0);
-                const char *qr = nullptr;
-                if (have) {
-                    const int sq = p.spt ? first_seq + r / p.G : seq, gg = p.spt ? r % p.G : r;
-                    qr = p.q + ((int64_t)sq * p.q_seq + (int64_t)(h * p.G + gg) * p.q_head) * 2;
+        for (int i = 0; i < 2; ++i) {
+            const int r = g8 + 8 * i;
+            const bool have = r < nrows && (RT == 16 || i == 0);
+            const char *qr = nullptr;
+            if (have) {
+                const int sq = p.spt ? first_seq + r / p.G : seq, gg = p.spt ? r % p.G : r;
+                qr = p.q + ((int64_t)sq * p.q_seq + (int64_t)(h * p.G + gg) * p.q_head) * 2;
+            }
+            float amax = 0.f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                // slots 2 t4, 2 t4 + 1 and 2 t4 + 8, + 9 of step k: dims 16 k + slot, for 8-bit keys dims 16 k + 4 t4 + 0..3
+                const int d0 = 16 * k + (KEY8 ? 4 * t4 : 2 * t4), d1 = KEY8 ? d0 + 2 : d0 + 8;
+                qa[k][i] = have ? *reinterpret_cast<const uint32_t *>(qr + 2 * d0) : 0u;
+                qa[k][i + 2] = have ? *reinterpret_cast<const uint32_t *>(qr + 2 * d1) : 0u;
+                if (KEY8) {
+                    amax = fmaxf(amax, fmaxf(fmaxf(fabsf(bf16_lo(qa[k][i])), fabsf(bf16_hi(qa[k][i]))),
+                                             fmaxf(fabsf(bf16_lo(qa[k][i + 2])), fabsf(bf16_hi(qa[k][i + 2])))));
                 }
-                float amax = 0.f;
+            }
+            float back = 1.f;
+            if (KEY8) {
+                // f16 holds 11 bits down to 2^-14: with the row's largest entry brought to [1, 2) a bf16 entry is exact
+                // unless it is 2^14 times smaller than that one
+                amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+                amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+                int e = (int)((__float_as_uint(amax) >> 23) & 255u) - 127;
+                e = min(max(e, -126), 126);
+                if (amax == 0.f) e = 0;
+                const float by = __uint_as_float((uint32_t)(127 - e) << 23);
+                back = __uint_as_float((uint32_t)(127 + e) << 23);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    // slots 2 t4, 2 t4 + 1 and 2 t4 + 8, + 9 of step k: dims 16 k + slot, for 8-bit keys dims 16 k + 4 t4 + 0..3
-                    const int d0 = 16 * k + (KEY8 ? 4 * t4 : 2 * t4), d1 = KEY8 ? d0 + 2 : d0 + 8;
-                    qa[k][i] = have ? *reinterpret_cast<const uint32_t *>(qr + 2 * d0) : 0u;
-                    qa[k][i + 2] = have ? *reinterpret_cast<const uint32_t *>(qr + 2 * d1) : 0u;
-                    if (KEY8) {
-                        amax = fmaxf(amax, fmaxf(fmaxf(fabsf(bf16_lo(qa[k][i])), fabsf(bf16_hi(qa[k][i]))),
-                                                 fmaxf(fabsf(bf16_lo(qa[k][i + 2])), fabsf(bf16_hi(qa[k][i + 2])))));
+                for (int k = 0; k < 8; ++k)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const uint32_t w = qa[k][i + 2 * j];
+                        qa[k][i + 2 * j] = f16_bits(bf16_lo(w) * by) | (f16_bits(bf16_hi(w) * by) << 16);
+                    }
+            }
+            if (i < NR) mul[i % NR] = p.scale * (p.k_scale ? __ldg(p.k_scale + h) : 1.f) * back;
+        }
+
+        // ---------------- stream the rows ----------------
+        float o[16][4], m[NR], l[NR];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) { o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f; }
+#pragma unroll
+        for (int i = 0; i < NR; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
+        const int nit = kb - ka;
+        // subtile `it` of this warp: rows row(it) .. row(it) + 15
+        auto row_of = [&](int it) { return (int64_t)(ka + it) * kAttTile + warp * kAttSub; };
+        auto page_of = [&](int it) -> int {
+            const int64_t r = row_of(it);
+            if (!p.src.paged || it >= nit || r >= len) return 0;
+            const int pg = p.src.page_shift >= 0 ? (int)r >> p.src.page_shift : (int)r / p.src.page_size;
+            return __ldg(p.src.page_table + (int64_t)seq * p.src.max_pages_per_seq + pg);
+        };
+        uint32_t bad = 0;                                                // bit i: the rows of stage i are absent
+        int page_next = page_of(0);
+        auto issue = [&](int it) {
+            const int64_t r = row_of(it);
+            const int stage = it % ST;
+            if (it < nit && r < len) {
+                int64_t base = (int64_t)p.layer * p.src.stride_layer + (int64_t)h * p.src.stride_head, step;
+                bool ok = true;
+                if (p.src.paged) {
+                    ok = p.src.n_pages <= 0 || (page_next >= 0 && page_next < p.src.n_pages);
+                    const int off = (int)r - (p.src.page_shift >= 0 ? ((int)r >> p.src.page_shift) << p.src.page_shift
+                                                                     : (int)r / p.src.page_size * p.src.page_size);
+                    step = p.src.stride_slot;
+                    base += (ok ? (int64_t)page_next * p.src.stride_page : 0) + (int64_t)off * step;
+                } else {
+                    step = p.src.stride_tok;
+                    base += (int64_t)seq * p.src.stride_seq + r * step;
+                }
+                bad = (bad & ~(1u << stage)) | (ok ? 0u : 1u << stage);
+                if (!ok && lane == 0 && p.device_status) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
+                const int have = ok ? (int)(len - r < kAttSub ? len - r : kAttSub) : 0;
+                const uint32_t dst = ring + stage * kStage;
+                constexpr int es = KEY8 ? 1 : 2;
+                const int c = lane % kChunks, r0 = lane / kChunks;
+#pragma unroll
+                for (int i = 0; i < kCopies; ++i) {
+                    // rows behind the length (or absent ones) arrive as zeros and are not read
+                    const int row = i * (32 / kChunks) + r0;
+                    const uint32_t bytes = row < have ? 16u : 0u;
+                    const int64_t off = (base + (int64_t)(row < have ? row : 0) * step) * es + 16 * c;
+                    const uint32_t to = dst + row * kRowBytes + (((c & 8) | ((c ^ row) & 7)) << 4);
+                    const int64_t from = have ? off : 16 * c;
+                    cp_async16(to, p.src.k + from, bytes);
+                    cp_async16(to + kHalf, p.src.v + from, bytes);
+                }
+            }
+            page_next = page_of(it + 1);
+            cp_commit();
+        };
+        if (nit > 0) {
+#pragma unroll
+            for (int i = 0; i < ST - 1; ++i) issue(i);
+        }
+        for (int it = 0; it < nit; ++it) {
+            cp_wait<ST - 2>();
+            __syncwarp();
+            const int64_t r0 = row_of(it);
+            const int stage = it % ST;
+            if (r0 < len && !((bad >> stage) & 1u)) {
+                const int have = len - r0 < kAttSub ? (int)(len - r0) : kAttSub;
+                const uint32_t kb_s = ring + stage * kStage, vb_s = kb_s + kHalf;
+                float sc[2][4];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) sc[j][0] = sc[j][1] = sc[j][2] = sc[j][3] = 0.f;
+                if (KEY8) {
+#pragma unroll
+                    for (int k = 0; k < 8; k += 2) {
+                        uint32_t f[4];
+                        const int row = (lane & 7) + (lane & 8), ch = k + (lane >> 4);
+                        ldmatrix_x4(f, kb_s + row * 128 + (((ch ^ row) & 7) << 4));
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            uint32_t b0, b1;
+                            e4m3x4_to_f16x2(f[j], b0, b1);
+                            const int kk = k + (j >> 1);
+                            mma16<true>(sc[j & 1], qa[kk][0], qa[kk][1], qa[kk][2], qa[kk][3], b0, b1);
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        uint32_t f[4];
+                        const int row = (lane & 7) + ((lane & 16) >> 1), ch = 2 * k + ((lane >> 3) & 1);
+                        ldmatrix_x4(f, kb_s + row * 256 + (((ch & 8) | ((ch ^ row) & 7)) << 4));
+                        mma16<false>(sc[0], qa[k][0], qa[k][1], qa[k][2], qa[k][3], f[0], f[1]);
+                        mma16<false>(sc[1], qa[k][0], qa[k][1], qa[k][2], qa[k][3], f[2], f[3]);
                     }
                 }
-                float back = 1.f;
-                if (KEY8) {
-                    // f16 holds 11 bits down to 2^-14: with the row's largest entry brought to [1, 2) a bf16 entry is exact
-                    // unless it is 2^14 times smaller than that one
-                    amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-                    amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-                    int e = (int)((__float_as_uint(amax) >> 23) & 255u) - 127;
-                    e = min(max(e, -126), 126);
-                    if (amax == 0.f) e = 0;
-                    const float by = __uint_as_float((uint32_t)(127 - e) << 23);
-                    back = __uint_as_float((uint32_t)(127 + e) << 23);
+                // logits, running bound, weights; thread holds keys 8 j + 2 t4 + x of row g8 (+ 8)
+                float w[NR][4];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
+                for (int i = 0; i < NR; ++i) {
+                    float mx = -INFINITY;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const int key = 8 * (x >> 1) + 2 * t4 + (x & 1);
+                        w[i][x] = key < have ? sc[x >> 1][2 * i + (x & 1)] * mul[i] : -INFINITY;
+                        mx = fmaxf(mx, w[i][x]);
+                    }
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+                    const bool raise = mx > m[i] + kAttLazy || (m[i] == -INFINITY && mx > m[i]);
+                    if (__any_sync(0xffffffffu, raise)) {
+                        const float by = raise ? ex2(m[i] - mx) : 1.f;   // 0 where there was no bound yet
+                        if (raise) m[i] = mx;
+                        l[i] *= by;
+#pragma unroll
+                        for (int n = 0; n < 16; ++n) {
+                            o[n][2 * i] *= by; o[n][2 * i + 1] *= by;
+                            if (RT == 8) { o[n][2] *= by; o[n][3] *= by; }
+                        }
+                    }
+                    const float ref = m[i] == -INFINITY ? 0.f : m[i];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        w[i][x] = ex2(w[i][x] - ref);
+                        l[i] += w[i][x];
+                    }
+                }
+                uint32_t ph[NR][2], pl[NR][2];
+#pragma unroll
+                for (int i = 0; i < NR; ++i) {
+                    split16<KEY8>(w[i][0], w[i][1], ph[i][0], pl[i][0]);
+                    split16<KEY8>(w[i][2], w[i][3], ph[i][1], pl[i][1]);
+                }
+                auto pv = [&](float (&acc)[4], uint32_t b0, uint32_t b1) {
+                    if (RT == 8) {
+                        mma16<KEY8>(acc, ph[0][0], pl[0][0], ph[0][1], pl[0][1], b0, b1);
+                    } else {
+                        mma16<KEY8>(acc, ph[0][0], ph[NR - 1][0], ph[0][1], ph[NR - 1][1], b0, b1);
+                        mma16<KEY8>(acc, pl[0][0], pl[NR - 1][0], pl[0][1], pl[NR - 1][1], b0, b1);
+                    }
+                };
+                if (KEY8) {
+#pragma unroll
+                    for (int ch = 0; ch < 8; ch += 2) {
+                        uint32_t f[4];
+                        const int row = (lane & 7) + (lane & 8), cc = ch + (lane >> 4);
+                        ldmatrix_x4_t(f, vb_s + row * 128 + (((cc ^ row) & 7) << 4));
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
-                            const uint32_t w = qa[k][i + 2 * j];
-                            qa[k][i + 2 * j] = f16_bits(bf16_lo(w) * by) | (f16_bits(bf16_hi(w) * by) << 16);
-                        }
-                }
-                if (i < NR) mul[i % NR] = p.scale * (p.k_scale ? __ldg(p.k_scale + h) : 1.f) * back;
-            }
-
-            // ---------------- stream the rows ----------------
-            float o[16][4], m[NR], l[NR];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) { o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f; }
-#pragma unroll
-            for (int i = 0; i < NR; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
-            const int nit = kb - ka;
-            // subtile `it` of this warp: rows row(it) .. row(it) + 15
-            auto row_of = [&](int it) { return (int64_t)(ka + it) * kAttTile + warp * kAttSub; };
-            auto page_of = [&](int it) -> int {
-                const int64_t r = row_of(it);
-                if (!p.src.paged || it >= nit || r >= len) return 0;
-                const int pg = p.src.page_shift >= 0 ? (int)r >> p.src.page_shift : (int)r / p.src.page_size;
-                return __ldg(p.src.page_table + (int64_t)seq * p.src.max_pages_per_seq + pg);
-            };
-            uint32_t bad = 0;                                                // bit i: the rows of stage i are absent
-            int page_next = page_of(0);
-            auto issue = [&](int it) {
-                const int64_t r = row_of(it);
-                const int stage = it % ST;
-                if (it < nit && r < len) {
-                    int64_t base = (int64_t)p.layer * p.src.stride_layer + (int64_t)h * p.src.stride_head, step;
-                    bool ok = true;
-                    if (p.src.paged) {
-                        ok = p.src.n_pages <= 0 || (page_next >= 0 && page_next < p.src.n_pages);
-                        const int off = (int)r - (p.src.page_shift >= 0 ? ((int)r >> p.src.page_shift) << p.src.page_shift
-                                                                         : (int)r / p.src.page_size * p.src.page_size);
-                        step = p.src.stride_slot;
-                        base += (ok ? (int64_t)page_next * p.src.stride_page : 0) + (int64_t)off * step;
-                    } else {
-                        step = p.src.stride_tok;
-                        base += (int64_t)seq * p.src.stride_seq + r * step;
-                    }
-                    bad = (bad & ~(1u << stage)) | (ok ? 0u : 1u << stage);
-                    if (!ok && lane == 0 && p.device_status) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
-                    const int have = ok ? (int)(len - r < kAttSub ? len - r : kAttSub) : 0;
-                    const uint32_t dst = ring + stage * kStage;
-                    constexpr int es = KEY8 ? 1 : 2;
-                    const int c = lane % kChunks, r0 = lane / kChunks;
-#pragma unroll
-                    for (int i = 0; i < kCopies; ++i) {
-                        // rows behind the length (or absent ones) arrive as zeros and are not read
-                        const int row = i * (32 / kChunks) + r0;
-                        const uint32_t bytes = row < have ? 16u : 0u;
-                        const int64_t off = (base + (int64_t)(row < have ? row : 0) * step) * es + 16 * c;
-                        const uint32_t to = dst + row * kRowBytes + (((c & 8) | ((c ^ row) & 7)) << 4);
-                        const int64_t from = have ? off : 16 * c;
-                        cp_async16(to, p.src.k + from, bytes);
-                        cp_async16(to + kHalf, p.src.v + from, bytes);
-                    }
-                }
-                page_next = page_of(it + 1);
-                cp_commit();
-            };
-            if (nit > 0) {
-#pragma unroll
-                for (int i = 0; i < ST - 1; ++i) issue(i);
-            }
-            for (int it = 0; it < nit; ++it) {
-                cp_wait<ST - 2>();
-                __syncwarp();
-                const int64_t r0 = row_of(it);
-                const int stage = it % ST;
-                if (r0 < len && !((bad >> stage) & 1u)) {
-                    const int have = len - r0 < kAttSub ? (int)(len - r0) : kAttSub;
-                    const uint32_t kb_s = ring + stage * kStage, vb_s = kb_s + kHalf;
-                    float sc[2][4];
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) sc[j][0] = sc[j][1] = sc[j][2] = sc[j][3] = 0.f;
-                    if (KEY8) {
-#pragma unroll
-                        for (int k = 0; k < 8; k += 2) {
-                            uint32_t f[4];
-                            const int row = (lane & 7) + (lane & 8), ch = k + (lane >> 4);
-                            ldmatrix_x4(f, kb_s + row * 128 + (((ch ^ row) & 7) << 4));
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                uint32_t b0, b1;
-                                e4m3x4_to_f16x2(f[j], b0, b1);
-                                const int kk = k + (j >> 1);
-                                mma16<true>(sc[j & 1], qa[kk][0], qa[kk][1], qa[kk][2], qa[kk][3], b0, b1);
-                            }
-                        }
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            uint32_t f[4];
-                            const int row = (lane & 7) + ((lane & 16) >> 1), ch = 2 * k + ((lane >> 3) & 1);
-                            ldmatrix_x4(f, kb_s + row * 256 + (((ch & 8) | ((ch ^ row) & 7)) << 4));
-                            mma16<false>(sc[0], qa[k][0], qa[k][1], qa[k][2], qa[k][3], f[0], f[1]);
-                            mma16<false>(sc[1], qa[k][0], qa[k][1], qa[k][2], qa[k][3], f[2], f[3]);
+                            // bytes of a word: key 2 t4 dims (2 g8, 2 g8 + 1), key 2 t4 + 1 the same dims
+                            uint32_t e0, d0, e1, d1;
+                            e4m3x4_to_f16x2(__byte_perm(f[2 * j], 0, 0x3120), e0, d0);
+                            e4m3x4_to_f16x2(__byte_perm(f[2 * j + 1], 0, 0x3120), e1, d1);
+                            pv(o[2 * (ch + j)], e0, e1);
+                            pv(o[2 * (ch + j) + 1], d0, d1);
                         }
                     }
-                    // logits, running bound, weights; thread holds keys 8 j + 2 t4 + x of row g8 (+ 8)
-                    float w[NR][4];
-#pragma unroll
-                    for (int i = 0; i < NR; ++i) {
-                        float mx = -INFINITY;
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            const int key = 8 * (x >> 1) + 2 * t4 + (x & 1);
-                            w[i][x] = key < have ? sc[x >> 1][2 * i + (x & 1)] * mul[i] : -INFINITY;
-                            mx = fmaxf(mx, w[i][x]);
-                        }
-                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-                        const bool raise = mx > m[i] + kAttLazy || (m[i] == -INFINITY && mx > m[i]);
-                        if (__any_sync(0xffffffffu, raise)) {
-                            const float by = raise ? ex2(m[i] - mx) : 1.f;   // 0 where there was no bound yet
-                            if (raise) m[i] = mx;
-                            l[i] *= by;
-#pragma unroll
-                            for (int n = 0; n < 16; ++n) {
-                                o[n][2 * i] *= by; o[n][2 * i + 1] *= by;
-                                if (RT == 8) { o[n][2] *= by; o[n][3] *= by; }
-                            }
-                        }
-                        const float ref = m[i] == -INFINITY ? 0.f : m[i];
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            w[i][x] = ex2(w[i][x] - ref);
-                            l[i] += w[i][x];
-                        }
-                    }
-                    uint32_t ph[NR][2], pl[NR][2];
-#pragma unroll
-                    for (int i = 0; i < NR; ++i) {
-                        split16<KEY8>(w[i][0], w[i][1], ph[i][0], pl[i][0]);
-                        split16<KEY8>(w[i][2], w[i][3], ph[i][1], pl[i][1]);
-                    }
-                    auto pv = [&](float (&acc)[4], uint32_t b0, uint32_t b1) {
-                        if (RT == 8) {
-                            mma16<KEY8>(acc, ph[0][0], pl[0][0], ph[0][1], pl[0][1], b0, b1);
-                        } else {
-                            mma16<KEY8>(acc, ph[0][0], ph[NR - 1][0], ph[0][1], ph[NR - 1][1], b0, b1);
-                            mma16<KEY8>(acc, pl[0][0], pl[NR - 1][0], pl[0][1], pl[NR - 1][1], b0, b1);
-                        }
-                    };
-                    if (KEY8) {
-#pragma unroll
-                        for (int ch = 0; ch < 8; ch += 2) {
-                            uint32_t f[4];
-                            const int row = (lane & 7) + (lane & 8), cc = ch + (lane >> 4);
-                            ldmatrix_x4_t(f, vb_s + row * 128 + (((cc ^ row) & 7) << 4));
-#pragma unroll
-                            for (int j = 0; j < 2; ++j) {
-                                // bytes of a word: key 2 t4 dims (2 g8, 2 g8 + 1), key 2 t4 + 1 the same dims
-                                uint32_t e0, d0, e1, d1;
-                                e4m3x4_to_f16x2(__byte_perm(f[2 * j], 0, 0x3120), e0, d0);
-                                e4m3x4_to_f16x2(__byte_perm(f[2 * j + 1], 0, 0x3120), e1, d1);
-                                pv(o[2 * (ch + j)], e0, e1);
-                                pv(o[2 * (ch + j) + 1], d0, d1);
-                            }
-                        }
-                    } else {
-#pragma unroll
-                        for (int n = 0; n < 16; n += 2) {
-                            uint32_t f[4];
-                            const int row = (lane & 7) + (lane & 8), cc = n + (lane >> 4);
-                            ldmatrix_x4_t(f, vb_s + row * 256 + (((cc & 8) | ((cc ^ row) & 7)) << 4));
-                            pv(o[n], f[0], f[1]);
-                            pv(o[n + 1], f[2], f[3]);
-                        }
-                    }
-                }
-                __syncwarp();
-                issue(it + ST - 1);
-            }
-            cp_wait<0>();
-
-            // ---------------- join the warps ----------------
-#pragma unroll
-            for (int i = 0; i < NR; ++i) {
-                l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-                l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-                if (t4 == 0) { stat[warp][g8 + 8 * i][0] = m[i]; stat[warp][g8 + 8 * i][1] = l[i]; }
-            }
-            __syncthreads();
-            float *red = reinterpret_cast<float *>(dyn);                     // [warps][RT][132]: the ring has been read
-#pragma unroll
-            for (int i = 0; i < NR; ++i) {
-                const int r = g8 + 8 * i;
-                float mm = stat[0][r][0];
-#pragma unroll
-                for (int w2 = 1; w2 < kAttWarps; ++w2) mm = fmaxf(mm, stat[w2][r][0]);
-                const float by = m[i] == -INFINITY ? 0.f : ex2(m[i] - mm);
-                float *to = red + (warp * RT + r) * kAttRowPitch;
-#pragma unroll
-                for (int n = 0; n < 16; ++n) {
-                    const int d0 = KEY8 ? 16 * (n >> 1) + 4 * t4 + (n & 1) : 8 * n + 2 * t4, d1 = d0 + (KEY8 ? 2 : 1);
-                    to[d0] = (o[n][2 * i] + (RT == 8 ? o[n][2] : 0.f)) * by;
-                    to[d1] = (o[n][2 * i + 1] + (RT == 8 ? o[n][3] : 0.f)) * by;
-                }
-            }
-            __syncthreads();
-            const float vs = p.v_scale ? __ldg(p.v_scale + h) : 1.f;
-            float *slot = p.slots + ((int64_t)blockIdx.x * 2 + (begins ? 1 : 0)) * (RT * kAttRowPitch);
-            for (int r = warp; r < nrows; r += kAttWarps) {
-                float mm = stat[0][r][0], ll = 0.f;
-#pragma unroll
-                for (int w2 = 1; w2 < kAttWarps; ++w2) mm = fmaxf(mm, stat[w2][r][0]);
-                float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (int w2 = 0; w2 < kAttWarps; ++w2) {
-                    const float4 x = *reinterpret_cast<const float4 *>(red + (w2 * RT + r) * kAttRowPitch + 4 * lane);
-                    a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
-                    ll += stat[w2][r][0] == -INFINITY ? 0.f : stat[w2][r][1] * ex2(stat[w2][r][0] - mm);
-                }
-                const int sq = p.spt ? first_seq + r / p.G : seq, hq = h * p.G + (p.spt ? r % p.G : r);
-                if (complete && p.finish) {
-                    const float inv = ll == 0.f ? 0.f : vs / ll;
-                    uint2 y = make_uint2(cvt_bf16x2(a.y * inv, a.x * inv), cvt_bf16x2(a.w * inv, a.z * inv));
-                    *reinterpret_cast<uint2 *>(p.out + ((int64_t)sq * p.out_seq + (int64_t)hq * p.out_head) * 2 + 8 * lane) = y;
-                    if (p.lse && lane == 0) p.lse[(int64_t)sq * p.H * p.G + hq] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.69314718f;
                 } else {
-                    float *to = complete ? p.whole + ((int64_t)sq * p.H * p.G + hq) * kAttRowPitch : slot + r * kAttRowPitch;
-                    *reinterpret_cast<float4 *>(to + 4 * lane) = make_float4(a.x * vs, a.y * vs, a.z * vs, a.w * vs);
-                    if (lane == 0) *reinterpret_cast<float2 *>(to + kHeadDim) = make_float2(mm, ll);
+#pragma unroll
+                    for (int n = 0; n < 16; n += 2) {
+                        uint32_t f[4];
+                        const int row = (lane & 7) + (lane & 8), cc = n + (lane >> 4);
+                        ldmatrix_x4_t(f, vb_s + row * 256 + (((cc & 8) | ((cc ^ row) & 7)) << 4));
+                        pv(o[n], f[0], f[1]);
+                        pv(o[n + 1], f[2], f[3]);
+                    }
                 }
             }
-            __syncthreads();                                                 // the ring may be refilled
+            __syncwarp();
+            issue(it + ST - 1);
         }
-        start += (int64_t)kt * rts;
+        cp_wait<0>();
+
+        // ---------------- join the warps ----------------
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+            if (t4 == 0) { stat[warp][g8 + 8 * i][0] = m[i]; stat[warp][g8 + 8 * i][1] = l[i]; }
+        }
+        __syncthreads();
+        float *red = reinterpret_cast<float *>(dyn);                     // [warps][RT][132]: the ring has been read
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const int r = g8 + 8 * i;
+            float mm = stat[0][r][0];
+#pragma unroll
+            for (int w2 = 1; w2 < kAttWarps; ++w2) mm = fmaxf(mm, stat[w2][r][0]);
+            const float by = m[i] == -INFINITY ? 0.f : ex2(m[i] - mm);
+            float *to = red + (warp * RT + r) * kAttRowPitch;
+#pragma unroll
+            for (int n = 0; n < 16; ++n) {
+                const int d0 = KEY8 ? 16 * (n >> 1) + 4 * t4 + (n & 1) : 8 * n + 2 * t4, d1 = d0 + (KEY8 ? 2 : 1);
+                to[d0] = (o[n][2 * i] + (RT == 8 ? o[n][2] : 0.f)) * by;
+                to[d1] = (o[n][2 * i + 1] + (RT == 8 ? o[n][3] : 0.f)) * by;
+            }
+        }
+        __syncthreads();
+        const float vs = p.v_scale ? __ldg(p.v_scale + h) : 1.f;
+        float *slot = p.slots + ((int64_t)blockIdx.x * 2 + (j.begins ? 1 : 0)) * (RT * kAttRowPitch);
+        for (int r = warp; r < nrows; r += kAttWarps) {
+            float mm = stat[0][r][0], ll = 0.f;
+#pragma unroll
+            for (int w2 = 1; w2 < kAttWarps; ++w2) mm = fmaxf(mm, stat[w2][r][0]);
+            float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w2 = 0; w2 < kAttWarps; ++w2) {
+                const float4 x = *reinterpret_cast<const float4 *>(red + (w2 * RT + r) * kAttRowPitch + 4 * lane);
+                a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
+                ll += stat[w2][r][0] == -INFINITY ? 0.f : stat[w2][r][1] * ex2(stat[w2][r][0] - mm);
+            }
+            const int sq = p.spt ? first_seq + r / p.G : seq, hq = h * p.G + (p.spt ? r % p.G : r);
+            if (j.complete && p.finish) {
+                const float inv = ll == 0.f ? 0.f : vs / ll;
+                uint2 y = make_uint2(cvt_bf16x2(a.y * inv, a.x * inv), cvt_bf16x2(a.w * inv, a.z * inv));
+                *reinterpret_cast<uint2 *>(p.out + ((int64_t)sq * p.out_seq + (int64_t)hq * p.out_head) * 2 + 8 * lane) = y;
+                if (p.lse && lane == 0) p.lse[(int64_t)sq * p.H * p.G + hq] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.69314718f;
+            } else {
+                float *to = j.complete ? p.whole + ((int64_t)sq * p.H * p.G + hq) * kAttRowPitch : slot + r * kAttRowPitch;
+                *reinterpret_cast<float4 *>(to + 4 * lane) = make_float4(a.x * vs, a.y * vs, a.z * vs, a.w * vs);
+                if (lane == 0) *reinterpret_cast<float2 *>(to + kHeadDim) = make_float2(mm, ll);
+            }
+        }
+        __syncthreads();                                                 // the ring may be refilled
     }
 }
 
