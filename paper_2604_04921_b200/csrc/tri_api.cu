@@ -1237,7 +1237,7 @@ namespace {
 
 // Workspace of an attention call.
 struct AttendPlan {
-    int32_t blocks;                                    // grid of the streaming passes
+    int32_t blocks;                                    // grid of k_attend
     int32_t own_rows;                                  // query rows per slot of the own rows' pass
     size_t own_rec, own_slots, own_whole, pre_rec, pre_slots, pre_whole, total;
 };
@@ -1253,7 +1253,7 @@ AttendPlan make_attend_plan(const tri_ctx *c, int32_t S, int32_t P)
     a.own_rec = o;   o += align256((size_t)S * H * sizeof(int2));
     a.own_slots = o; o += align256((size_t)a.blocks * 2 * a.own_rows * row);
     a.own_whole = o; o += P > 0 ? whole : 0;
-    // either pass over prefixes fits: tiles of 16 query rows on all blocks, or of 128 on one block per multiprocessor
+    // either pass over prefixes fits: tiles of 16 query rows, or of 128 with one block per multiprocessor
     a.pre_rec = o;   o += P > 0 ? align256(((size_t)P + S / (16 / G) + 2) * H * sizeof(int2)) : 0;
     a.pre_slots = o; o += P > 0 ? align256((size_t)c->n_sm * 2 * kPTile * row) : 0;
     static_assert(kPTile >= 16 * kAttBlocksPerSM, "slots of the 128-row pass cover those of the 16-row pass");

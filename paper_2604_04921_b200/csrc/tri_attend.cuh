@@ -6,29 +6,29 @@
 // anywhere: over the warps of a block, over blocks, over a prefix and a sequence's own rows.
 //
 // What bounds it.  2 x 128 cached values are read for 4 * 128 * G flops: the kernel is bound by HBM.  Every cached row is
-// read once, with 16-byte asynchronous copies into a ring of shared-memory stages that each warp keeps for itself (no
-// block-wide barrier in the loop), 16 rows a stage.
+// read once, with 16-byte asynchronous copies into a ring of two 8 KB stages that each warp keeps for itself; the copies run
+// one step ahead, across the units of a block's share.  128 KB in flight per multiprocessor measured best: 192 KB cost 5 %.
 //
-// Work split.  All units of a call (sequence x KV head [x tile of query rows]) are laid end to end as tiles of 64 rows,
-// and each block of a grid that fills the GPU takes an equal share of that line, which begins and ends anywhere inside a
-// unit.  A unit that lies in one block is finished there; the parts of the others go to the workspace, one slot for a
-// block's first unit and one for its last, and k_attend_merge joins them in a fixed order.  The lengths are on the
-// device only, so every block finds its share by a sum over them.
+// Work split.  All units of a call (sequence x KV head [x tile of query rows]) are laid end to end on a line, each as many
+// steps long as it has tiles of rows plus a fixed number that stands for its own cost (queries, joining, output), and
+// every block takes an equal share of that line, which begins and ends anywhere inside a unit.  (Shares per warp instead
+// of per block measured 10 % slower on long units: 1,184 streams of 4 KB against 296 of 16 KB, and four times the parts.)
+// A unit that lies in one share is finished there; the parts of the others go to the workspace, one slot for a block's
+// first unit and one for its last, and k_attend_merge joins them in a fixed order.  The lengths are on the device only,
+// so every block finds its share by a sum over them.
 #pragma once
 #include "tri_score_tma.cuh"
 
 namespace tri {
 
-constexpr int kAttWarps = 4, kAttThreads = 32 * kAttWarps;
-constexpr int kAttSub = 16;                               // rows of a warp's stage
-constexpr int kAttTile = kAttWarps * kAttSub;             // rows of a block's step
-constexpr int kAttBlocksPerSM = 2;
-constexpr int kAttRowPitch = kHeadDim + 4;                // floats per row of a part: 128 sums, m, l, two unused
-constexpr float kAttLazy = 8.0f;                          // the bound m is raised when a logit passes it by this much
-
-// Stages of a warp's ring: 3 x 8 KB (bf16) or 6 x 4 KB (e4m3), so that 2 blocks per SM keep 128 KB or more in flight.
-template <bool KEY8> constexpr int kAttStages = KEY8 ? 6 : 3;
-constexpr int kAttRingBytes = kAttWarps * 3 * (kAttSub * kHeadDim * 2 * 2);     // 98304
+constexpr int kAttWarps = 4, kAttThreads = 32 * kAttWarps, kAttBlocksPerSM = 2;
+constexpr int kAttStages = 2, kAttStageBytes = 8192;             // K and V of 16 bf16 or 32 e4m3 rows (three stages: 5 % slower)
+constexpr int kAttRingBytes = kAttWarps * kAttStages * kAttStageBytes;
+template <bool KEY8> constexpr int kAttRows = KEY8 ? 32 : 16;    // rows of a warp's step; a tile is one step of all warps
+constexpr int kAttUnitCost = 2;                                  // a unit's own cost, in tiles
+constexpr int kAttMinShare = 1;                                  // tiles a share has at least (if there are that many)
+constexpr int kAttRowPitch = kHeadDim + 4;                       // floats per row of a part: 128 sums, m, l, two unused
+constexpr float kAttLazy = 8.0f;                                 // the bound m is raised when a logit passes it by this much
 
 struct AttendParams {
     View src;
@@ -47,7 +47,7 @@ struct AttendParams {
     int32_t finish;                                       // units that lie in one block are written to out
     float *slots;                                         // [blocks][2][rows][kAttRowPitch] parts of cut units
     float *whole;                                         // [S][H][G][kAttRowPitch] summaries of uncut units (finish == 0)
-    int2 *rec;                                            // per unit: first block and number of parts
+    int2 *rec;                                            // per unit: slot of its first part, number of parts
     int32_t *device_status;
 };
 
@@ -122,31 +122,49 @@ __device__ __forceinline__ float ex2(float x)
     return y;
 }
 
-// The share of one block: where it begins on the line of tiles and which unit lies there.
+// The share of one block: where it begins on the line and which unit lies there.
 struct AttShare {
-    int64_t total, t0, t1;        // tiles of the call; this block's [t0, t1)
-    int64_t start;                // first tile of the unit (all of its row tiles) below
-    int32_t blocks, unit;         // blocks that get tiles; seq * H + h, nseq * H if there is none
+    int64_t total, t0, t1;        // steps of the call; this worker's [t0, t1)
+    int64_t each;                 // steps per share; the first `longer` shares have one more
+    int32_t longer;
+    int64_t start;                // first step of the unit (all of its row tiles) below
+    int32_t shares, worker;       // blocks that get steps; this one
+    int32_t unit;                 // seq * H + h
+};
+// Where a block stands on the line, and what it finds there: tiles [ka, kb) of one unit and tile of query rows.
+struct AttCursor { int unit, rt; int64_t start; };
+struct AttJob {
+    int seq, h, len, kt, ka, kb;      // tiles [ka, kb) of the unit's kt
+    int first_seq, nrows;             // query rows: G of each sequence from first_seq on (prefixes), or of seq
+    int rec;                          // index of the unit's record
+    int64_t rows0;                    // step of the unit's first tile
+    bool begins, tail, complete;      // the unit's first step is here; its part goes to the last slot; all tiles are here
 };
 
-// Units are entries seq * H + h; where the heads of a sequence have equal lengths the sums run over sequences only.
-__device__ __forceinline__ AttShare att_share(const AttendParams &p, int tile_rows)
+// a / b for a >= 0, b > 0; the 64-bit division takes several hundred cycles, and steps rarely need it.
+__device__ __forceinline__ int64_t att_div(int64_t a, int64_t b)
 {
-    __shared__ long long part_s[32];
-    __shared__ long long found_start;
-    __shared__ int found;
+    return ((uint64_t)(a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
+// The share of this block.  Units are entries seq * H + h; where the heads of a sequence have equal lengths the sums run
+// over sequences only.
+__device__ __forceinline__ AttShare att_share(const AttendParams &p, int tile_rows, int unit_cost, int min_share)
+{
+    __shared__ long long part_s[32], start_s;
+    __shared__ int unit_s;
     const int tid = threadIdx.x, nth = blockDim.x, lane = tid & 31, warp = tid >> 5;
     const bool by_head = p.unit_lens != nullptr;
-    const int n = by_head ? p.nseq * p.H : p.nseq;
+    const int n = by_head ? p.nseq * p.H : p.nseq, heads = by_head ? 1 : p.H;
     const int per = (n + nth - 1) / nth;
     const int a = min(tid * per, n), b = min(a + per, n);
-    auto cost = [&](int x) -> long long {
+    auto cost = [&](int x) -> long long {                 // of one head
         const int seq = by_head ? x / p.H : x, h = by_head ? x - seq * p.H : 0;
         const long long kt = ((long long)att_len(p, seq, h) + tile_rows - 1) / tile_rows;
-        return kt == 0 ? 0 : kt * att_row_tiles(p, seq) * (by_head ? 1 : p.H);
+        return (kt + unit_cost) * att_row_tiles(p, seq);
     };
     long long sum = 0;
-    for (int x = a; x < b; ++x) sum += cost(x);
+    for (int x = a; x < b; ++x) sum += cost(x) * heads;
     long long incl = sum;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -154,7 +172,6 @@ __device__ __forceinline__ AttShare att_share(const AttendParams &p, int tile_ro
         if (lane >= d) incl += o;
     }
     if (lane == 31) part_s[warp] = incl;
-    if (tid == 0) found = n;
     __syncthreads();
     long long before = 0, total = 0;
     for (int w = 0; w < nth / 32; ++w) {
@@ -163,72 +180,77 @@ __device__ __forceinline__ AttShare att_share(const AttendParams &p, int tile_ro
     }
     AttShare r;
     r.total = total;
-    r.blocks = total < (long long)gridDim.x ? (total > 0 ? (int)total : 1) : (int)gridDim.x;
-    const int blk = (int)blockIdx.x;
-    r.t0 = blk < r.blocks ? blk * total / r.blocks : total;
-    r.t1 = blk < r.blocks ? (blk + 1) * total / r.blocks : total;
-    // the first entry that ends behind t0 or starts at it: units without tiles belong to the block that reaches them
-    long long at = before + incl - sum;
-    for (int x = a; x < b; ++x) {
-        const long long c = cost(x);
-        if (at >= r.t0 || at + c > r.t0) { atomicMin(&found, x); break; }
-        at += c;
+    const long long want = att_div(total, min_share), most = gridDim.x;
+    r.shares = (int)(want < 1 ? 1 : (want < most ? want : most));
+    r.each = att_div(total, r.shares);
+    r.longer = (int)(total - r.each * r.shares);
+    r.worker = (int)blockIdx.x;
+    const bool have = r.worker < r.shares && total > 0;
+    r.t0 = have ? r.worker * r.each + min(r.worker, r.longer) : total;
+    r.t1 = have ? r.t0 + r.each + (r.worker < r.longer ? 1 : 0) : total;
+    long long at = before + incl - sum;                   // this thread's entries: steps [at, at + sum)
+    if (r.t0 >= at && r.t0 < at + sum) {
+        for (int x = a; x < b; ++x) {
+            const long long c = cost(x);
+            if (r.t0 < at + c * heads) {
+                const int skip = (int)att_div(r.t0 - at, c);
+                unit_s = by_head ? x : x * p.H + skip;
+                start_s = at + skip * c;
+                break;
+            }
+            at += c * heads;
+        }
     }
     __syncthreads();
-    const int x = found;
-    if (x >= a && x < b) found_start = at;
-    __syncthreads();
-    if (x >= n) { r.unit = p.nseq * p.H; r.start = total; return r; }
-    r.start = found_start;
-    r.unit = by_head ? x : x * p.H;
-    if (!by_head && r.start < r.t0) {
-        const long long c = cost(x) / p.H;
-        const int skip = (int)((r.t0 - r.start) / c);
-        r.unit += skip;
-        r.start += skip * c;
-    }
+    r.unit = have ? unit_s : p.nseq * p.H;
+    r.start = have ? start_s : total;
     return r;
 }
 
-// Which block holds tile t of the line.
-__device__ __forceinline__ int att_block_of(const AttShare &r, int64_t t) { return (int)(((t + 1) * r.blocks - 1) / r.total); }
-
-// Where a block stands on the line, and what it finds there: rows ka .. kb (in tiles) of one unit and tile of query rows.
-struct AttCursor { int unit, rt; int64_t start; };
-struct AttJob {
-    int seq, h, len, kt, ka, kb;      // tiles [ka, kb) of the unit's kt
-    int first_seq, nrows;             // query rows: G of each sequence from first_seq on (prefixes), or of seq
-    int rec;                          // index of the unit's record
-    int2 record;                      // first block and number of parts
-    bool begins, complete;            // the unit's first tile / all of its tiles lie in this block
-};
-__device__ __forceinline__ bool att_next(const AttendParams &p, const AttShare &sh, int tile_rows, AttCursor &c, AttJob &j)
+// Which block holds step t of the line.
+__device__ __forceinline__ int att_worker_of(const AttShare &r, int64_t t)
 {
-    const bool last = (int)blockIdx.x == sh.blocks - 1;
-    while (c.unit < p.nseq * p.H) {
-        if (c.start >= sh.t1 && !(last && c.start == sh.total)) return false;
+    const int64_t split = r.longer * (r.each + 1);
+    return t < split ? (int)att_div(t, r.each + 1) : r.longer + (int)att_div(t - split, r.each);
+}
+
+// The record of a unit, made by the block that holds its first step: slot of its first part, number of parts.
+__device__ __forceinline__ int2 att_record(const AttShare &sh, const AttJob &j)
+{
+    if (j.kt == 0) return make_int2(0, 0);
+    const int first = att_worker_of(sh, j.rows0);
+    return make_int2(2 * first + (first == sh.worker ? 1 : 0), att_worker_of(sh, j.rows0 + j.kt - 1) - first + 1);
+}
+
+// The next unit of a share; false at its end.  Units without rows come too, and units of which the share holds only the
+// steps that stand for their own cost (kb <= ka).
+__device__ __forceinline__ bool att_next(const AttendParams &p, const AttShare &sh, int tile_rows, int unit_cost, AttCursor &c, AttJob &j)
+{
+    while (c.unit < p.nseq * p.H && c.start < sh.t1) {
         j.seq = c.unit / p.H; j.h = c.unit - j.seq * p.H;
         j.len = att_len(p, j.seq, j.h);
         j.kt = (int)(((int64_t)j.len + tile_rows - 1) / tile_rows);
         const int2 grp = p.spt ? att_group(p.group_start, p.S, j.seq) : make_int2(j.seq, 1);
         const int rts = p.spt ? (grp.y + p.spt - 1) / p.spt : 1, rt = c.rt++;
+        const int64_t c1 = (int64_t)j.kt + unit_cost;
         if (rt >= rts) {
-            c.start += (int64_t)j.kt * rts;
+            c.start += c1 * rts;
             ++c.unit;
             c.rt = 0;
             continue;
         }
-        const int64_t js = c.start + (int64_t)rt * j.kt, je = js + j.kt;
-        if (je <= sh.t0 && !(j.kt == 0 && js >= sh.t0)) continue;
-        if (js >= sh.t1 && !(last && js == sh.total)) return false;
+        const int64_t js = c.start + rt * c1, rows0 = js + unit_cost, je = js + c1;      // the unit's steps; its first tile
+        if (je <= sh.t0) continue;
+        if (js >= sh.t1) return false;
         j.first_seq = grp.x + rt * p.spt;
         j.nrows = p.spt ? min(p.spt, grp.y - rt * p.spt) * p.G : p.G;
         j.rec = p.spt ? att_tile_index(j.seq, grp.x, p.spt, rt) * p.H + j.h : c.unit;
-        j.ka = js < sh.t0 ? (int)(sh.t0 - js) : 0;
-        j.kb = je > sh.t1 ? (int)(sh.t1 - js) : j.kt;
+        j.ka = sh.t0 > rows0 ? (int)(sh.t0 - rows0) : 0;
+        j.kb = je > sh.t1 ? (sh.t1 > rows0 ? (int)(sh.t1 - rows0) : 0) : j.kt;
         j.begins = js >= sh.t0;
-        j.complete = j.begins && j.kb == j.kt;
-        j.record = make_int2((int)blockIdx.x, j.kt == 0 ? 0 : att_block_of(sh, je - 1) - (int)blockIdx.x + 1);
+        j.tail = js >= sh.t0;
+        j.complete = j.ka == 0 && j.kb == j.kt;
+        j.rows0 = rows0;
         return true;
     }
     return false;
@@ -240,294 +262,355 @@ __device__ __forceinline__ bool att_next(const AttendParams &p, const AttShare &
 template <bool KEY8, int RT>
 __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const AttendParams p)
 {
-    constexpr int ST = kAttStages<KEY8>;
-    constexpr int kRowBytes = KEY8 ? 128 : 256, kHalf = kAttSub * kRowBytes, kStage = 2 * kHalf;      // K | V
-    constexpr int kChunks = kRowBytes / 16, kCopies = kAttSub * kChunks / 32;
+    constexpr int ST = kAttStages, ROWS = kAttRows<KEY8>, NK = ROWS / 16, TILE = kAttWarps * ROWS;
+    constexpr int kRowBytes = KEY8 ? 128 : 256, kHalf = ROWS * kRowBytes;                             // K | V
+    constexpr int kChunks = kRowBytes / 16, kCopies = ROWS * kChunks / 32;
     constexpr int NR = RT / 8;                            // query rows per thread
     extern __shared__ __align__(128) uint8_t dyn[];
-    __shared__ float stat[kAttWarps][RT][2];
+    __shared__ float2 stat[kAttWarps][RT];
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
-    const uint32_t ring = smem_u32(dyn) + warp * (ST * kStage);
+    const uint32_t ring = smem_u32(dyn) + warp * (ST * kAttStageBytes);
     grid_dependents_launch();                             // the joining kernel may be set up under this one
-    const AttShare sh = att_share(p, kAttTile);
-    if ((int)blockIdx.x >= sh.blocks) return;
+    const AttShare sh = att_share(p, TILE, kAttUnitCost, kAttMinShare);
+    if (sh.worker >= sh.shares) return;
 
-    AttCursor cur = {sh.unit, 0, sh.start};
-    AttJob j;
-    while (att_next(p, sh, kAttTile, cur, j)) {
-        const int seq = j.seq, h = j.h, len = j.len, ka = j.ka, kb = j.kb, nrows = j.nrows, first_seq = j.first_seq;
-        if (j.begins && tid == 0) p.rec[j.rec] = j.record;
-        if (j.kt == 0 && !p.finish) continue;
-
-        // ---------------- query rows as the A operand ----------------
-        uint32_t qa[8][4];
-        float mul[NR];                                                   // logit in base-2 units per accumulator unit
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int r = g8 + 8 * i;
-            const bool have = r < nrows && (RT == 16 || i == 0);
-            const char *qr = nullptr;
-            if (have) {
-                const int sq = p.spt ? first_seq + r / p.G : seq, gg = p.spt ? r % p.G : r;
-                qr = p.q + ((int64_t)sq * p.q_seq + (int64_t)(h * p.G + gg) * p.q_head) * 2;
-            }
-            float amax = 0.f;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                // slots 2 t4, 2 t4 + 1 and 2 t4 + 8, + 9 of step k: dims 16 k + slot, for 8-bit keys dims 16 k + 4 t4 + 0..3
-                const int d0 = 16 * k + (KEY8 ? 4 * t4 : 2 * t4), d1 = KEY8 ? d0 + 2 : d0 + 8;
-                qa[k][i] = have ? *reinterpret_cast<const uint32_t *>(qr + 2 * d0) : 0u;
-                qa[k][i + 2] = have ? *reinterpret_cast<const uint32_t *>(qr + 2 * d1) : 0u;
-                if (KEY8) {
-                    amax = fmaxf(amax, fmaxf(fmaxf(fabsf(bf16_lo(qa[k][i])), fabsf(bf16_hi(qa[k][i]))),
-                                             fmaxf(fabsf(bf16_lo(qa[k][i + 2])), fabsf(bf16_hi(qa[k][i + 2])))));
-                }
-            }
-            float back = 1.f;
-            if (KEY8) {
-                // f16 holds 11 bits down to 2^-14: with the row's largest entry brought to [1, 2) a bf16 entry is exact
-                // unless it is 2^14 times smaller than that one
-                amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-                amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-                int e = (int)((__float_as_uint(amax) >> 23) & 255u) - 127;
-                e = min(max(e, -126), 126);
-                if (amax == 0.f) e = 0;
-                const float by = __uint_as_float((uint32_t)(127 - e) << 23);
-                back = __uint_as_float((uint32_t)(127 + e) << 23);
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const uint32_t w = qa[k][i + 2 * j];
-                        qa[k][i + 2 * j] = f16_bits(bf16_lo(w) * by) | (f16_bits(bf16_hi(w) * by) << 16);
-                    }
-            }
-            if (i < NR) mul[i % NR] = p.scale * (p.k_scale ? __ldg(p.k_scale + h) : 1.f) * back;
+    // ---------------- copies: a cursor of their own, ST - 1 steps ahead ----------------
+    AttCursor pc = {sh.unit, 0, sh.start};
+    AttJob pj = {};
+    int pit = 0, page[NK], pstage = 0;                    // next step; the pages of its 16-row halves
+    uint32_t bad = 0;                                     // bits 2 i, 2 i + 1: these 16 rows of stage i are absent
+    bool more = true;
+    auto advance = [&]() {                                // to the next step, its pages looked up before they are needed
+        if (pit == 0 || pit == pj.kb) {
+            do more = att_next(p, sh, TILE, kAttUnitCost, pc, pj); while (more && pj.kb <= pj.ka);
+            pit = pj.ka;
         }
-
-        // ---------------- stream the rows ----------------
-        float o[16][4], m[NR], l[NR];
+        if (more && p.src.paged) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) { o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f; }
+            for (int half = 0; half < NK; ++half) {
+                const int64_t r = (int64_t)pit * TILE + warp * ROWS + 16 * half;
+                const int pg = p.src.page_shift >= 0 ? (int)r >> p.src.page_shift : (int)r / p.src.page_size;
+                page[half] = r < pj.len ? __ldg(p.src.page_table + (int64_t)pj.seq * p.src.max_pages_per_seq + pg) : 0;
+            }
+        }
+    };
+    auto issue = [&]() {
+        if (more) {
+            const uint32_t dst = ring + pstage * kAttStageBytes;
+            constexpr int es = KEY8 ? 1 : 2;
+            const int c = lane % kChunks, r0 = lane / kChunks;
+            uint32_t miss = 0;
 #pragma unroll
-        for (int i = 0; i < NR; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
-        const int nit = kb - ka;
-        // subtile `it` of this warp: rows row(it) .. row(it) + 15
-        auto row_of = [&](int it) { return (int64_t)(ka + it) * kAttTile + warp * kAttSub; };
-        auto page_of = [&](int it) -> int {
-            const int64_t r = row_of(it);
-            if (!p.src.paged || it >= nit || r >= len) return 0;
-            const int pg = p.src.page_shift >= 0 ? (int)r >> p.src.page_shift : (int)r / p.src.page_size;
-            return __ldg(p.src.page_table + (int64_t)seq * p.src.max_pages_per_seq + pg);
-        };
-        uint32_t bad = 0;                                                // bit i: the rows of stage i are absent
-        int page_next = page_of(0);
-        auto issue = [&](int it) {
-            const int64_t r = row_of(it);
-            const int stage = it % ST;
-            if (it < nit && r < len) {
-                int64_t base = (int64_t)p.layer * p.src.stride_layer + (int64_t)h * p.src.stride_head, step;
+            for (int half = 0; half < NK; ++half) {       // 16 rows each: they lie in one page
+                const int64_t r = (int64_t)pit * TILE + warp * ROWS + 16 * half;
+                int64_t base = (int64_t)p.layer * p.src.stride_layer + (int64_t)pj.h * p.src.stride_head, step;
                 bool ok = true;
                 if (p.src.paged) {
-                    ok = p.src.n_pages <= 0 || (page_next >= 0 && page_next < p.src.n_pages);
+                    ok = p.src.n_pages <= 0 || (page[half] >= 0 && page[half] < p.src.n_pages) || r >= pj.len;
                     const int off = (int)r - (p.src.page_shift >= 0 ? ((int)r >> p.src.page_shift) << p.src.page_shift
                                                                      : (int)r / p.src.page_size * p.src.page_size);
                     step = p.src.stride_slot;
-                    base += (ok ? (int64_t)page_next * p.src.stride_page : 0) + (int64_t)off * step;
+                    base += (int64_t)page[half] * p.src.stride_page + (int64_t)off * step;
                 } else {
                     step = p.src.stride_tok;
-                    base += (int64_t)seq * p.src.stride_seq + r * step;
+                    base += (int64_t)pj.seq * p.src.stride_seq + r * step;
                 }
-                bad = (bad & ~(1u << stage)) | (ok ? 0u : 1u << stage);
-                if (!ok && lane == 0 && p.device_status) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
-                const int have = ok ? (int)(len - r < kAttSub ? len - r : kAttSub) : 0;
-                const uint32_t dst = ring + stage * kStage;
-                constexpr int es = KEY8 ? 1 : 2;
-                const int c = lane % kChunks, r0 = lane / kChunks;
+                if (!ok) {
+                    miss |= 1u << half;
+                    if (lane == 0 && p.device_status) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
+                }
+                const int64_t left = pj.len - r;
+                const int have = !ok || left <= 0 ? 0 : (left < 16 ? (int)left : 16);
 #pragma unroll
-                for (int i = 0; i < kCopies; ++i) {
+                for (int i = 0; i < kCopies / NK; ++i) {
                     // rows behind the length (or absent ones) arrive as zeros and are not read
-                    const int row = i * (32 / kChunks) + r0;
-                    const uint32_t bytes = row < have ? 16u : 0u;
-                    const int64_t off = (base + (int64_t)(row < have ? row : 0) * step) * es + 16 * c;
+                    const int rr = i * (32 / kChunks) + r0, row = 16 * half + rr;
+                    const uint32_t bytes = rr < have ? 16u : 0u;
+                    const int64_t from = (rr < have ? (base + (int64_t)rr * step) * es : 0) + 16 * c;
                     const uint32_t to = dst + row * kRowBytes + (((c & 8) | ((c ^ row) & 7)) << 4);
-                    const int64_t from = have ? off : 16 * c;
                     cp_async16(to, p.src.k + from, bytes);
                     cp_async16(to + kHalf, p.src.v + from, bytes);
                 }
             }
-            page_next = page_of(it + 1);
-            cp_commit();
-        };
-        if (nit > 0) {
-#pragma unroll
-            for (int i = 0; i < ST - 1; ++i) issue(i);
+            bad = (bad & ~(3u << (2 * pstage))) | (miss << (2 * pstage));
+            ++pit;
+            advance();
         }
-        for (int it = 0; it < nit; ++it) {
-            cp_wait<ST - 2>();
-            __syncwarp();
-            const int64_t r0 = row_of(it);
-            const int stage = it % ST;
-            if (r0 < len && !((bad >> stage) & 1u)) {
-                const int have = len - r0 < kAttSub ? (int)(len - r0) : kAttSub;
-                const uint32_t kb_s = ring + stage * kStage, vb_s = kb_s + kHalf;
-                float sc[2][4];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) sc[j][0] = sc[j][1] = sc[j][2] = sc[j][3] = 0.f;
-                if (KEY8) {
-#pragma unroll
-                    for (int k = 0; k < 8; k += 2) {
-                        uint32_t f[4];
-                        const int row = (lane & 7) + (lane & 8), ch = k + (lane >> 4);
-                        ldmatrix_x4(f, kb_s + row * 128 + (((ch ^ row) & 7) << 4));
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            uint32_t b0, b1;
-                            e4m3x4_to_f16x2(f[j], b0, b1);
-                            const int kk = k + (j >> 1);
-                            mma16<true>(sc[j & 1], qa[kk][0], qa[kk][1], qa[kk][2], qa[kk][3], b0, b1);
-                        }
+        pstage = pstage + 1 == ST ? 0 : pstage + 1;
+        cp_commit();
+    };
+    advance();
+
+    AttCursor cur = {sh.unit, 0, sh.start};
+    AttJob j = {};
+    uint32_t qa[8][4];
+    float mul[NR];                                        // logit in base-2 units per accumulator unit
+    float o[16][4], m[NR], l[NR];
+    int it = 0, stage = 0, ahead = ST - 1;
+    for (;;) {
+        // the stage of the step before: read, or used and released in joining a unit
+        issue();
+        if (ahead > 0) { --ahead; continue; }
+        if (it == j.kb) {
+            // ---------------- the next unit ----------------
+            bool rows = false;
+            while (!rows && att_next(p, sh, TILE, kAttUnitCost, cur, j)) {
+                if (j.begins && tid == 0) p.rec[j.rec] = att_record(sh, j);
+                rows = j.kb > j.ka;
+                if (j.kt == 0 && j.begins && p.finish)    // no rows: zeros
+                    for (int i = tid; i < p.G * 16; i += kAttThreads) {
+                        const int hq = j.h * p.G + (i >> 4);
+                        *reinterpret_cast<uint4 *>(p.out + ((int64_t)j.seq * p.out_seq + (int64_t)hq * p.out_head) * 2 + 16 * (i & 15)) =
+                            make_uint4(0u, 0u, 0u, 0u);
+                        if (p.lse && (i & 15) == 0) p.lse[(int64_t)j.seq * p.H * p.G + hq] = -INFINITY;
                     }
-                } else {
+            }
+            if (!rows) break;
+            it = j.ka;
+            // ---------------- query rows as the A operand ----------------
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        uint32_t f[4];
-                        const int row = (lane & 7) + ((lane & 16) >> 1), ch = 2 * k + ((lane >> 3) & 1);
-                        ldmatrix_x4(f, kb_s + row * 256 + (((ch & 8) | ((ch ^ row) & 7)) << 4));
-                        mma16<false>(sc[0], qa[k][0], qa[k][1], qa[k][2], qa[k][3], f[0], f[1]);
-                        mma16<false>(sc[1], qa[k][0], qa[k][1], qa[k][2], qa[k][3], f[2], f[3]);
+            for (int i = 0; i < 2; ++i) {
+                const int r = g8 + 8 * i;
+                const bool have = r < j.nrows && (RT == 16 || i == 0);
+                const char *qr = nullptr;
+                if (have) {
+                    const int sq = p.spt ? j.first_seq + r / p.G : j.seq, gg = p.spt ? r % p.G : r;
+                    qr = p.q + ((int64_t)sq * p.q_seq + (int64_t)(j.h * p.G + gg) * p.q_head) * 2;
+                }
+                float amax = 0.f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    // slots 2 t4, 2 t4 + 1 and 2 t4 + 8, + 9 of step k: dims 16 k + slot, for 8-bit keys dims 16 k + 4 t4 + 0..3
+                    const int d0 = 16 * k + (KEY8 ? 4 * t4 : 2 * t4), d1 = KEY8 ? d0 + 2 : d0 + 8;
+                    qa[k][i] = have ? *reinterpret_cast<const uint32_t *>(qr + 2 * d0) : 0u;
+                    qa[k][i + 2] = have ? *reinterpret_cast<const uint32_t *>(qr + 2 * d1) : 0u;
+                    if (KEY8) {
+                        amax = fmaxf(amax, fmaxf(fmaxf(fabsf(bf16_lo(qa[k][i])), fabsf(bf16_hi(qa[k][i]))),
+                                                 fmaxf(fabsf(bf16_lo(qa[k][i + 2])), fabsf(bf16_hi(qa[k][i + 2])))));
                     }
                 }
-                // logits, running bound, weights; thread holds keys 8 j + 2 t4 + x of row g8 (+ 8)
-                float w[NR][4];
+                float back = 1.f;
+                if (KEY8) {
+                    // f16 holds 11 bits down to 2^-14: with the row's largest entry brought to [1, 2) a bf16 entry is exact
+                    // unless it is 2^14 times smaller than that one
+                    amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+                    amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+                    int e = (int)((__float_as_uint(amax) >> 23) & 255u) - 127;
+                    e = min(max(e, -126), 126);
+                    if (amax == 0.f) e = 0;
+                    const float by = __uint_as_float((uint32_t)(127 - e) << 23);
+                    back = __uint_as_float((uint32_t)(127 + e) << 23);
 #pragma unroll
-                for (int i = 0; i < NR; ++i) {
-                    float mx = -INFINITY;
+                    for (int k = 0; k < 8; ++k)
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const uint32_t w = qa[k][i + 2 * x];
+                            qa[k][i + 2 * x] = f16_bits(bf16_lo(w) * by) | (f16_bits(bf16_hi(w) * by) << 16);
+                        }
+                }
+                if (i < NR) mul[i % NR] = p.scale * (p.k_scale ? __ldg(p.k_scale + j.h) : 1.f) * back;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) { o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f; }
+#pragma unroll
+            for (int i = 0; i < NR; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
+        }
+
+        // ---------------- one step ----------------
+        cp_wait<ST - 1>();
+        __syncwarp();
+        const int64_t left = j.len - ((int64_t)it * TILE + warp * ROWS);
+        const int have = left < 0 ? 0 : (left < ROWS ? (int)left : ROWS);
+        const uint32_t miss = (bad >> (2 * stage)) & 3u;
+        const uint32_t kb_s = ring + stage * kAttStageBytes, vb_s = kb_s + kHalf;
+        // logits: 8 rows x 8 keys per accumulator (x 2: even and odd steps of 16 dims apart, shorter chains)
+        float sc[2 * NK][4];
+        if (KEY8) {
+#pragma unroll
+            for (int x = 0; x < 2 * NK; ++x) sc[x][0] = sc[x][1] = sc[x][2] = sc[x][3] = 0.f;
+#pragma unroll
+            for (int k = 0; k < 8; k += 2)
+#pragma unroll
+                for (int kg = 0; kg < NK; ++kg) {
+                    uint32_t f[4];
+                    const int row = 16 * kg + (lane & 7) + (lane & 8), ch = k + (lane >> 4);
+                    ldmatrix_x4(f, kb_s + row * 128 + (((ch ^ row) & 7) << 4));
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
-                        const int key = 8 * (x >> 1) + 2 * t4 + (x & 1);
-                        w[i][x] = key < have ? sc[x >> 1][2 * i + (x & 1)] * mul[i] : -INFINITY;
-                        mx = fmaxf(mx, w[i][x]);
-                    }
-                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-                    const bool raise = mx > m[i] + kAttLazy || (m[i] == -INFINITY && mx > m[i]);
-                    if (__any_sync(0xffffffffu, raise)) {
-                        const float by = raise ? ex2(m[i] - mx) : 1.f;   // 0 where there was no bound yet
-                        if (raise) m[i] = mx;
-                        l[i] *= by;
-#pragma unroll
-                        for (int n = 0; n < 16; ++n) {
-                            o[n][2 * i] *= by; o[n][2 * i + 1] *= by;
-                            if (RT == 8) { o[n][2] *= by; o[n][3] *= by; }
-                        }
-                    }
-                    const float ref = m[i] == -INFINITY ? 0.f : m[i];
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        w[i][x] = ex2(w[i][x] - ref);
-                        l[i] += w[i][x];
+                        uint32_t b0, b1;
+                        e4m3x4_to_f16x2(f[x], b0, b1);
+                        const int kk = k + (x >> 1);
+                        mma16<true>(sc[2 * kg + (x & 1)], qa[kk][0], qa[kk][1], qa[kk][2], qa[kk][3], b0, b1);
                     }
                 }
-                uint32_t ph[NR][2], pl[NR][2];
+        } else {
+            float sd[2][4];
 #pragma unroll
-                for (int i = 0; i < NR; ++i) {
-                    split16<KEY8>(w[i][0], w[i][1], ph[i][0], pl[i][0]);
-                    split16<KEY8>(w[i][2], w[i][3], ph[i][1], pl[i][1]);
-                }
-                auto pv = [&](float (&acc)[4], uint32_t b0, uint32_t b1) {
-                    if (RT == 8) {
-                        mma16<KEY8>(acc, ph[0][0], pl[0][0], ph[0][1], pl[0][1], b0, b1);
-                    } else {
-                        mma16<KEY8>(acc, ph[0][0], ph[NR - 1][0], ph[0][1], ph[NR - 1][1], b0, b1);
-                        mma16<KEY8>(acc, pl[0][0], pl[NR - 1][0], pl[0][1], pl[NR - 1][1], b0, b1);
-                    }
-                };
-                if (KEY8) {
+            for (int x = 0; x < 2; ++x) { sc[x][0] = sc[x][1] = sc[x][2] = sc[x][3] = 0.f; sd[x][0] = sd[x][1] = sd[x][2] = sd[x][3] = 0.f; }
 #pragma unroll
-                    for (int ch = 0; ch < 8; ch += 2) {
-                        uint32_t f[4];
-                        const int row = (lane & 7) + (lane & 8), cc = ch + (lane >> 4);
-                        ldmatrix_x4_t(f, vb_s + row * 128 + (((cc ^ row) & 7) << 4));
+            for (int k = 0; k < 8; ++k) {
+                uint32_t f[4];
+                const int row = (lane & 7) + ((lane & 16) >> 1), ch = 2 * k + ((lane >> 3) & 1);
+                ldmatrix_x4(f, kb_s + row * 256 + (((ch & 8) | ((ch ^ row) & 7)) << 4));
+                mma16<false>(k & 1 ? sd[0] : sc[0], qa[k][0], qa[k][1], qa[k][2], qa[k][3], f[0], f[1]);
+                mma16<false>(k & 1 ? sd[1] : sc[1], qa[k][0], qa[k][1], qa[k][2], qa[k][3], f[2], f[3]);
+            }
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            // bytes of a word: key 2 t4 dims (2 g8, 2 g8 + 1), key 2 t4 + 1 the same dims
-                            uint32_t e0, d0, e1, d1;
-                            e4m3x4_to_f16x2(__byte_perm(f[2 * j], 0, 0x3120), e0, d0);
-                            e4m3x4_to_f16x2(__byte_perm(f[2 * j + 1], 0, 0x3120), e1, d1);
-                            pv(o[2 * (ch + j)], e0, e1);
-                            pv(o[2 * (ch + j) + 1], d0, d1);
-                        }
-                    }
-                } else {
+            for (int x = 0; x < 2; ++x)
 #pragma unroll
-                    for (int n = 0; n < 16; n += 2) {
-                        uint32_t f[4];
-                        const int row = (lane & 7) + (lane & 8), cc = n + (lane >> 4);
-                        ldmatrix_x4_t(f, vb_s + row * 256 + (((cc & 8) | ((cc ^ row) & 7)) << 4));
-                        pv(o[n], f[0], f[1]);
-                        pv(o[n + 1], f[2], f[3]);
-                    }
+                for (int y = 0; y < 4; ++y) sc[x][y] += sd[x][y];
+        }
+        // running bound and weights; the thread holds keys 8 x + 2 t4, + 1 of row g8 (+ 8)
+        float w[NR][4 * NK];
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int x = 0; x < 4 * NK; ++x) {
+                const int key = 8 * (x >> 1) + 2 * t4 + (x & 1);
+                w[i][x] = key < have && !((miss >> (x >> 2)) & 1u) ? sc[x >> 1][2 * i + (x & 1)] * mul[i] : -INFINITY;
+                mx = fmaxf(mx, w[i][x]);
+            }
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+            const bool raise = mx > m[i] + kAttLazy || (m[i] == -INFINITY && mx > m[i]);
+            if (__any_sync(0xffffffffu, raise)) {
+                const float by = raise ? ex2(m[i] - mx) : 1.f;       // 0 where there was no bound yet
+                if (raise) m[i] = mx;
+                l[i] *= by;
+#pragma unroll
+                for (int n = 0; n < 16; ++n) {
+                    o[n][2 * i] *= by; o[n][2 * i + 1] *= by;
+                    if (RT == 8) { o[n][2] *= by; o[n][3] *= by; }
                 }
             }
-            __syncwarp();
-            issue(it + ST - 1);
+            const float ref = m[i] == -INFINITY ? 0.f : m[i];
+#pragma unroll
+            for (int x = 0; x < 4 * NK; ++x) {
+                w[i][x] = ex2(w[i][x] - ref);
+                l[i] += w[i][x];
+            }
         }
-        cp_wait<0>();
+#pragma unroll
+        for (int kg = 0; kg < NK; ++kg) {
+            uint32_t ph[NR][2], pl[NR][2];
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+                split16<KEY8>(w[i][4 * kg], w[i][4 * kg + 1], ph[i][0], pl[i][0]);
+                split16<KEY8>(w[i][4 * kg + 2], w[i][4 * kg + 3], ph[i][1], pl[i][1]);
+            }
+            auto pv = [&](float (&acc)[4], uint32_t b0, uint32_t b1) {
+                if (RT == 8) {
+                    mma16<KEY8>(acc, ph[0][0], pl[0][0], ph[0][1], pl[0][1], b0, b1);
+                } else {
+                    mma16<KEY8>(acc, ph[0][0], ph[NR - 1][0], ph[0][1], ph[NR - 1][1], b0, b1);
+                    mma16<KEY8>(acc, pl[0][0], pl[NR - 1][0], pl[0][1], pl[NR - 1][1], b0, b1);
+                }
+            };
+            const int row = 16 * kg + (lane & 7) + (lane & 8);
+            if (KEY8) {
+#pragma unroll
+                for (int ch = 0; ch < 8; ch += 2) {
+                    uint32_t f[4];
+                    const int cc = ch + (lane >> 4);
+                    ldmatrix_x4_t(f, vb_s + row * 128 + (((cc ^ row) & 7) << 4));
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        // bytes of a word: key 2 t4 dims (2 g8, 2 g8 + 1), key 2 t4 + 1 the same dims
+                        uint32_t e0, d0, e1, d1;
+                        e4m3x4_to_f16x2(__byte_perm(f[2 * x], 0, 0x3120), e0, d0);
+                        e4m3x4_to_f16x2(__byte_perm(f[2 * x + 1], 0, 0x3120), e1, d1);
+                        pv(o[2 * (ch + x)], e0, e1);
+                        pv(o[2 * (ch + x) + 1], d0, d1);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int n = 0; n < 16; n += 2) {
+                    uint32_t f[4];
+                    const int cc = n + (lane >> 4);
+                    ldmatrix_x4_t(f, vb_s + row * 256 + (((cc & 8) | ((cc ^ row) & 7)) << 4));
+                    pv(o[n], f[0], f[1]);
+                    pv(o[n + 1], f[2], f[3]);
+                }
+            }
+        }
+        __syncwarp();
+        uint8_t *used = dyn + (warp * ST + stage) * kAttStageBytes;
+        stage = stage + 1 == ST ? 0 : stage + 1;
+        if (++it < j.kb) continue;
 
-        // ---------------- join the warps ----------------
+        // ---------------- the unit's rows of this share are through: join the warps ----------------
+        // each leaves its sums in the stage it has just read, fragment by fragment, and takes a quarter of the dims of all
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
             l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
             l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-            if (t4 == 0) { stat[warp][g8 + 8 * i][0] = m[i]; stat[warp][g8 + 8 * i][1] = l[i]; }
+            if (t4 == 0) stat[warp][g8 + 8 * i] = make_float2(m[i], l[i]);
+#pragma unroll
+            for (int n = 0; n < 16; n += 2) {
+                float y[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    y[x] = o[n + (x >> 1)][2 * i + (x & 1)] + (RT == 8 ? o[n + (x >> 1)][2 + (x & 1)] : 0.f);
+                *reinterpret_cast<float4 *>(used + (i * 8 + n / 2) * 512 + lane * 16) = make_float4(y[0], y[1], y[2], y[3]);
+            }
         }
         __syncthreads();
-        float *red = reinterpret_cast<float *>(dyn);                     // [warps][RT][132]: the ring has been read
+        const float vs = p.v_scale ? __ldg(p.v_scale + j.h) : 1.f;
+        const bool final = j.complete && p.finish;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
             const int r = g8 + 8 * i;
-            float mm = stat[0][r][0];
+            float2 st[kAttWarps];
+            float mm = -INFINITY, ll = 0.f;
 #pragma unroll
-            for (int w2 = 1; w2 < kAttWarps; ++w2) mm = fmaxf(mm, stat[w2][r][0]);
-            const float by = m[i] == -INFINITY ? 0.f : ex2(m[i] - mm);
-            float *to = red + (warp * RT + r) * kAttRowPitch;
-#pragma unroll
-            for (int n = 0; n < 16; ++n) {
-                const int d0 = KEY8 ? 16 * (n >> 1) + 4 * t4 + (n & 1) : 8 * n + 2 * t4, d1 = d0 + (KEY8 ? 2 : 1);
-                to[d0] = (o[n][2 * i] + (RT == 8 ? o[n][2] : 0.f)) * by;
-                to[d1] = (o[n][2 * i + 1] + (RT == 8 ? o[n][3] : 0.f)) * by;
-            }
-        }
-        __syncthreads();
-        const float vs = p.v_scale ? __ldg(p.v_scale + h) : 1.f;
-        float *slot = p.slots + ((int64_t)blockIdx.x * 2 + (j.begins ? 1 : 0)) * (RT * kAttRowPitch);
-        for (int r = warp; r < nrows; r += kAttWarps) {
-            float mm = stat[0][r][0], ll = 0.f;
-#pragma unroll
-            for (int w2 = 1; w2 < kAttWarps; ++w2) mm = fmaxf(mm, stat[w2][r][0]);
-            float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int w2 = 0; w2 < kAttWarps; ++w2) { st[w2] = stat[w2][r]; mm = fmaxf(mm, st[w2].x); }
 #pragma unroll
             for (int w2 = 0; w2 < kAttWarps; ++w2) {
-                const float4 x = *reinterpret_cast<const float4 *>(red + (w2 * RT + r) * kAttRowPitch + 4 * lane);
-                a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
-                ll += stat[w2][r][0] == -INFINITY ? 0.f : stat[w2][r][1] * ex2(stat[w2][r][0] - mm);
+                st[w2].x = st[w2].x == -INFINITY ? 0.f : ex2(st[w2].x - mm);
+                ll += st[w2].y * st[w2].x;
             }
-            const int sq = p.spt ? first_seq + r / p.G : seq, hq = h * p.G + (p.spt ? r % p.G : r);
-            if (j.complete && p.finish) {
-                const float inv = ll == 0.f ? 0.f : vs / ll;
-                uint2 y = make_uint2(cvt_bf16x2(a.y * inv, a.x * inv), cvt_bf16x2(a.w * inv, a.z * inv));
-                *reinterpret_cast<uint2 *>(p.out + ((int64_t)sq * p.out_seq + (int64_t)hq * p.out_head) * 2 + 8 * lane) = y;
-                if (p.lse && lane == 0) p.lse[(int64_t)sq * p.H * p.G + hq] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.69314718f;
-            } else {
-                float *to = j.complete ? p.whole + ((int64_t)sq * p.H * p.G + hq) * kAttRowPitch : slot + r * kAttRowPitch;
-                *reinterpret_cast<float4 *>(to + 4 * lane) = make_float4(a.x * vs, a.y * vs, a.z * vs, a.w * vs);
-                if (lane == 0) *reinterpret_cast<float2 *>(to + kHeadDim) = make_float2(mm, ll);
+            const float by = final ? (ll == 0.f ? 0.f : vs / ll) : vs;
+            const int sq = p.spt ? j.first_seq + r / p.G : j.seq, hq = j.h * p.G + (p.spt ? r % p.G : r);
+            char *out = p.out + ((int64_t)sq * p.out_seq + (int64_t)hq * p.out_head) * 2;
+            float *to = j.complete ? p.whole + ((int64_t)sq * p.H * p.G + hq) * kAttRowPitch
+                                   : p.slots + (((int64_t)sh.worker * 2 + (j.tail ? 1 : 0)) * RT + r) * kAttRowPitch;
+#pragma unroll
+            for (int q2 = 0; q2 < 2; ++q2) {
+                const int q = 2 * warp + q2;               // fragments 2 q, 2 q + 1
+                float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int w2 = 0; w2 < kAttWarps; ++w2) {
+                    const float4 x = *reinterpret_cast<const float4 *>(used + (w2 - warp) * (ST * kAttStageBytes) + (i * 8 + q) * 512 + lane * 16);
+                    y.x += x.x * st[w2].x; y.y += x.y * st[w2].x; y.z += x.z * st[w2].x; y.w += x.w * st[w2].x;
+                }
+                y.x *= by; y.y *= by; y.z *= by; y.w *= by;
+                if (r >= j.nrows) continue;
+                if (KEY8) {                                // dims 16 q + 4 t4 + 0..3: even ones from fragment 2 q, odd ones from 2 q + 1
+                    const int d = 16 * q + 4 * t4;
+                    if (final) *reinterpret_cast<uint2 *>(out + 2 * d) = make_uint2(cvt_bf16x2(y.z, y.x), cvt_bf16x2(y.w, y.y));
+                    else *reinterpret_cast<float4 *>(to + d) = make_float4(y.x, y.z, y.y, y.w);
+                } else {                                   // dims 16 q + 2 t4 + 0, 1 and 8 further on
+                    const int d = 16 * q + 2 * t4;
+                    if (final) {
+                        *reinterpret_cast<uint32_t *>(out + 2 * d) = cvt_bf16x2(y.y, y.x);
+                        *reinterpret_cast<uint32_t *>(out + 2 * d + 16) = cvt_bf16x2(y.w, y.z);
+                    } else {
+                        *reinterpret_cast<float2 *>(to + d) = make_float2(y.x, y.y);
+                        *reinterpret_cast<float2 *>(to + d + 8) = make_float2(y.z, y.w);
+                    }
+                }
+            }
+            if (warp == 0 && t4 == 0 && r < j.nrows) {
+                if (!final) *reinterpret_cast<float2 *>(to + kHeadDim) = make_float2(mm, ll);
+                else if (p.lse) p.lse[(int64_t)sq * p.H * p.G + hq] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.69314718f;
             }
         }
-        __syncthreads();                                                 // the ring may be refilled
+        __syncthreads();                                   // the stages may be refilled
     }
+    cp_wait<0>();
 }
 
 // ----------------------------------------------------------------------------------------------
@@ -591,7 +674,7 @@ __global__ void __launch_bounds__(kMergeThreads) k_attend_merge(const MergeParam
         const int2 rc = is_own ? own : pre;
         const int k = is_own ? i : i - own.y;
         if (rc.y == 1) return a.whole + ((int64_t)s * p.H * p.G + hq) * kAttRowPitch;
-        return a.slots + (((int64_t)(rc.x + k) * 2 + (k == 0 ? 1 : 0)) * a.rows + (is_own ? 0 : row0) + g) * kAttRowPitch;
+        return a.slots + ((int64_t)(k == 0 ? rc.x : (rc.x & ~1) + 2 * k) * a.rows + (is_own ? 0 : row0) + g) * kAttRowPitch;
     };
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
     float mm = -INFINITY, ll = 0.f;

@@ -26,7 +26,9 @@
 namespace tri {
 
 constexpr int kPTile = 128;                               // cached rows per tile, query rows per tile
+constexpr int kPHalf = 64;                               // the weights of a tile are handed over in two halves, so that MMAs and softmax overlap
 constexpr int kPStages = 3;
+constexpr int kPUnitCost = 2, kPMinShare = 2;             // a unit's own cost and the least share, in tiles
 constexpr int kPBlock = kPTile * 128;                     // 128 rows x 64 bf16, one swizzled block
 constexpr int kPTileBytes = 2 * kPBlock;                  // dims 0..63 | dims 64..127
 constexpr int kPSoftWarps = 8;
@@ -38,16 +40,52 @@ __device__ __forceinline__ uint64_t tc_desc_sw128_n(uint32_t smem_addr)
 {
     return (uint64_t)((smem_addr >> 4) & 0x3fffu) | ((uint64_t)(kPBlock >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
-__device__ __forceinline__ void tc_ld32(uint32_t taddr, uint32_t (&r)[32])
+__device__ __forceinline__ void tc_ld64(uint32_t taddr, uint32_t (&r)[64])
 {
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,"
-        "%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
-          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
+        "%24,%25,%26,%27,%28,%29,%30,%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,"
+        "%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];\n"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
+          "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
+          "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
+          "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
+          "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
         : "r"(taddr));
+}
+__device__ __forceinline__ void tc_st64(uint32_t taddr, const uint32_t (&r)[64])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x64.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
+        "%24,%25,%26,%27,%28,%29,%30,%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,"
+        "%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63,%64};\n" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+        "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+        "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]),
+        "r"(r[32]), "r"(r[33]), "r"(r[34]), "r"(r[35]), "r"(r[36]), "r"(r[37]), "r"(r[38]), "r"(r[39]),
+        "r"(r[40]), "r"(r[41]), "r"(r[42]), "r"(r[43]), "r"(r[44]), "r"(r[45]), "r"(r[46]), "r"(r[47]),
+        "r"(r[48]), "r"(r[49]), "r"(r[50]), "r"(r[51]), "r"(r[52]), "r"(r[53]), "r"(r[54]), "r"(r[55]),
+        "r"(r[56]), "r"(r[57]), "r"(r[58]), "r"(r[59]), "r"(r[60]), "r"(r[61]), "r"(r[62]), "r"(r[63])
+        : "memory");
+}
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\nfma.rn.f32x2 d, a, b, c;\n"
+        "mov.b64 {%0, %1}, d;\n}\n" : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}\n"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
 }
 __device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16])
 {
@@ -85,7 +123,7 @@ __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sy
 
 struct PrefixBars {
     uint64_t kfull[kPStages], kempty[kPStages], vfull[kPStages], vempty[kPStages];
-    uint64_t sfull[2], pready[2], pvdone[2], q, ml;
+    uint64_t sfull[2], pready[4], q, ml;                  // per stream; per (stream, half of a tile's rows); block
 };
 
 __global__ void __launch_bounds__(kPThreads, 1)
@@ -98,25 +136,22 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
     __shared__ uint32_t absent[kPStages];                  // per stage: boxes of 16 rows whose page id is out of range
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const AttShare sh = att_share(p, kPTile);
-    if ((int)blockIdx.x >= sh.blocks) return;
+    const AttShare sh = att_share(p, kPTile, kPUnitCost, kPMinShare);
+    if (sh.worker >= sh.shares || sh.total == 0) return;
 
     const uint32_t base = (smem_u32(dyn) + 1023u) & ~1023u;
     const uint32_t sm_q = base, sm_k = base + kPTileBytes, sm_v = sm_k + kPStages * kPTileBytes;
     uint8_t *gq = dyn + (base - smem_u32(dyn)), *gv = gq + (1 + kPStages) * kPTileBytes;
     const uint32_t b_kfull = smem_u32(bars.kfull), b_kempty = smem_u32(bars.kempty), b_vfull = smem_u32(bars.vfull),
                    b_vempty = smem_u32(bars.vempty), b_sfull = smem_u32(bars.sfull), b_pready = smem_u32(bars.pready),
-                   b_pvdone = smem_u32(bars.pvdone), b_q = smem_u32(&bars.q), b_ml = smem_u32(&bars.ml);
+                   b_q = smem_u32(&bars.q), b_ml = smem_u32(&bars.ml);
     if (tid == 0) {
         for (int i = 0; i < kPStages; ++i) {
             mbar_init(b_kfull + 8 * i, 1); mbar_init(b_kempty + 8 * i, 1);
             mbar_init(b_vfull + 8 * i, 1); mbar_init(b_vempty + 8 * i, 1);
         }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(b_sfull + 8 * i, 1);
-            mbar_init(b_pready + 8 * i, kPSoftWarps / 2);
-            mbar_init(b_pvdone + 8 * i, 1);
-        }
+        for (int i = 0; i < 2; ++i) mbar_init(b_sfull + 8 * i, 1);
+        for (int i = 0; i < 4; ++i) mbar_init(b_pready + 8 * i, kPSoftWarps / 2);
         mbar_init(b_q, kPSoftWarps);
         mbar_init(b_ml, kPSoftWarps);
         gave_up = 0;
@@ -141,8 +176,8 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
         // ---------------- producer: lane = (matrix, box of 16 rows, half) is 2 x 16 x 1: K on lanes 0..15, V on 16..31 ----------
         const int sub = (lane & 15) >> 1, half = lane & 1;
         const bool is_v = lane >= 16;
-        while (!gave_up && att_next(p, sh, kPTile, cur, j)) {
-            const int n = j.kb - j.ka;
+        while (!gave_up && att_next(p, sh, kPTile, kPUnitCost, cur, j)) {
+            const int n = max(j.kb - j.ka, 0);
             auto locate = [&](int t, int &c1, int &c3) -> bool {          // false: the box's page id is out of range
                 const int64_t row = (int64_t)(j.ka + t) * kPTile + sub * kTileKeys;
                 c1 = (int)row; c3 = j.seq;
@@ -188,46 +223,51 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
         // ---------------- MMA issue ----------------
         constexpr uint32_t idesc_qk = tc_idesc_bf16(kPTile);                     // both operands K-major
         constexpr uint32_t idesc_pv = tc_idesc_bf16(kHeadDim) | (1u << 16);      // B (the values) N-major
-        int units = 0, cnt[2] = {0, 0};                    // tiles each stream had in earlier units
-        while (!gave_up && att_next(p, sh, kPTile, cur, j)) {
-            const int n = j.kb - j.ka;
+        int units = 0, cnt[2] = {0, 0};                    // tiles each stream had in earlier units (phases of pready)
+        while (!gave_up && att_next(p, sh, kPTile, kPUnitCost, cur, j)) {
+            const int n = max(j.kb - j.ka, 0);
             if (n == 0) continue;
             bool ok = __all_sync(0xffffffffu, mbar_wait_bounded(b_q, units & 1));
-            for (int t = -1; t < n && ok; ++t) {
-                if (t + 1 < n) {
-                    // logits of tile t + 1; their columns were last read by the MMAs of tile t - 1, issued before these
-                    const int i = done + t + 1, st = i % kPStages;
-                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(b_kfull + 8 * st, (i / kPStages) & 1));
+            // logits of tile t: into the columns whose weights the MMAs issued before have used up.  As MMAs complete in order,
+            // sfull says that the stream's accumulator rests, too; behind the stream's last tile it says nothing else
+            auto logits = [&](int t) -> bool {
+                const int i = done + t, st = i % kPStages;
+                if (!__all_sync(0xffffffffu, mbar_wait_bounded(b_kfull + 8 * st, (i / kPStages) & 1))) return false;
+                tc_fence_after();
+                if (lane == 0) {
+                    const uint32_t ka = sm_k + st * kPTileBytes, acc = tmem + 128 * (t & 1);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        tc_mma_bf16(acc, tc_desc_sw128(sm_q + (k >> 2) * kPBlock + (k & 3) * 32),
+                                    tc_desc_sw128(ka + (k >> 2) * kPBlock + (k & 3) * 32), idesc_qk, k > 0);
+                    tc_commit(b_sfull + 8 * (t & 1));
+                    tc_commit(b_kempty + 8 * st);
+                }
+                __syncwarp();
+                return true;
+            };
+            for (int t = 0; t < 2 && t < n && ok; ++t) ok = logits(t);
+            for (int t = 0; t < n && ok; ++t) {
+                // weights of tile t times its values, the upper half of its rows first (as the softmax delivers them), then
+                // the logits of the stream's next tile
+                const int i = done + t, st = i % kPStages, w = t & 1;
+                ok = mbar_wait_bounded(b_vfull + 8 * st, (i / kPStages) & 1);
+                for (int x = 1; x >= 0; --x) {
+                    ok = __all_sync(0xffffffffu, ok && mbar_wait_bounded(b_pready + 8 * (2 * w + x), (cnt[w] + (t >> 1)) & 1));
                     if (!ok) break;
                     tc_fence_after();
                     if (lane == 0) {
-                        const uint32_t ka = sm_k + st * kPTileBytes, acc = tmem + 128 * ((t + 1) & 1);
+                        const uint32_t va = sm_v + st * kPTileBytes + x * (kPHalf * 128), acc = tmem + 256 + 128 * w, pw = tmem + 128 * w + kPHalf * x;
 #pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            tc_mma_bf16(acc, tc_desc_sw128(sm_q + (k >> 2) * kPBlock + (k & 3) * 32),
-                                        tc_desc_sw128(ka + (k >> 2) * kPBlock + (k & 3) * 32), idesc_qk, k > 0);
-                        tc_commit(b_kempty + 8 * st);
-                        tc_commit(b_sfull + 8 * ((t + 1) & 1));
+                        for (int k = 0; k < 8; ++k)        // 4 steps of 16 rows with the weights, 4 with their rest
+                            tc_mma_bf16_ts(acc, pw + 32 * ((k & 3) >> 1) + 8 * (k & 1) + 4 * (k & 4), tc_desc_sw128_n(va + (k & 3) * 2048), idesc_pv,
+                                           t >= 2 || x == 0 || k > 0);
+                        if (x == 0) tc_commit(b_vempty + 8 * st);
+                        if (x == 0 && t + 2 >= n) tc_commit(b_sfull + 8 * w);
                     }
                     __syncwarp();
                 }
-                if (t < 0) continue;
-                // weights of tile t times its values
-                const int i = done + t, st = i % kPStages, w = t & 1;
-                ok = mbar_wait_bounded(b_vfull + 8 * st, (i / kPStages) & 1) &&
-                     mbar_wait_bounded(b_pready + 8 * w, (cnt[w] + (t >> 1)) & 1);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                tc_fence_after();
-                if (lane == 0) {
-                    const uint32_t va = sm_v + st * kPTileBytes, acc = tmem + 256 + 128 * w, pw = tmem + 128 * w;
-#pragma unroll
-                    for (int k = 0; k < 16; ++k)           // 8 steps of 16 rows with the weights, 8 with their rest
-                        tc_mma_bf16_ts(acc, pw + 32 * ((k & 7) >> 1) + 8 * (k & 1) + 2 * (k & 8), tc_desc_sw128_n(va + (k & 7) * 2048), idesc_pv, t >= 2 || k > 0);
-                    tc_commit(b_vempty + 8 * st);
-                    tc_commit(b_pvdone + 8 * w);
-                }
-                __syncwarp();
+                if (ok && t + 2 < n) ok = logits(t + 2);
             }
             done += n;
             cnt[0] += (n + 1) >> 1;
@@ -241,20 +281,26 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
         const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16, t_s = tmem + lane_base + 128 * w, t_o = tmem + lane_base + 256;
         const uint32_t flip = p.scale < 0.f ? 0x80008000u : 0u;            // a negative scale goes into the queries' signs
         const bool check_pages = p.src.paged && p.src.n_pages > 0;
-        int units = 0, cnt[2] = {0, 0};
-        while (!gave_up && att_next(p, sh, kPTile, cur, j)) {
-            if (j.begins && tid == 0) p.rec[j.rec] = j.record;
-            const int n = j.kb - j.ka;
+        int units = 0, phase[2] = {0, 0};                  // phases of sfull: one per tile, one more behind a unit's last
+        while (!gave_up && att_next(p, sh, kPTile, kPUnitCost, cur, j)) {
+            if (j.begins && tid == 0) p.rec[j.rec] = att_record(sh, j);
+            const int n = max(j.kb - j.ka, 0);
             if (n == 0) continue;
-            for (int i = tid; i < kPTile * 16; i += kPSoftWarps * 32) {
-                const int r = i >> 4, c = i & 15;
-                uint4 x = make_uint4(0u, 0u, 0u, 0u);
+            uint4 q[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int r = (tid >> 4) + 16 * i, c = tid & 15;
+                q[i] = make_uint4(0u, 0u, 0u, 0u);
                 if (r < j.nrows) {
                     const int sq = j.first_seq + r / p.G, g = r % p.G;
-                    x = *reinterpret_cast<const uint4 *>(p.q + ((int64_t)sq * p.q_seq + (int64_t)(j.h * p.G + g) * p.q_head) * 2 + 16 * c);
-                    x.x ^= flip; x.y ^= flip; x.z ^= flip; x.w ^= flip;
+                    q[i] = *reinterpret_cast<const uint4 *>(p.q + ((int64_t)sq * p.q_seq + (int64_t)(j.h * p.G + g) * p.q_head) * 2 + 16 * c);
+                    q[i].x ^= flip; q[i].y ^= flip; q[i].z ^= flip; q[i].w ^= flip;
                 }
-                *reinterpret_cast<uint4 *>(gq + (c >> 3) * kPBlock + sw128(r, c & 7)) = x;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int r = (tid >> 4) + 16 * i, c = tid & 15;
+                *reinterpret_cast<uint4 *>(gq + (c >> 3) * kPBlock + sw128(r, c & 7)) = q[i];
             }
             asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
             tc_fence_before();                             // the last unit's accumulators have been read
@@ -263,19 +309,46 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
 
             // base-2 logit = accumulator * mul (not 0: a masked logit is -infinity)
             const float mul = fmaxf(fabsf(p.scale) * (p.k_scale ? __ldg(p.k_scale + j.h) : 1.f), 1.17549435e-38f);
-            float m = -INFINITY, l = 0.f;
+            const float2 mul2 = make_float2(mul, mul);
+            float m = -INFINITY;
+            float2 l = make_float2(0.f, 0.f);              // sums of the even and of the odd rows
             bool ok = true;
+#pragma unroll 1
             for (int t = w; t < n; t += 2) {
                 const int i = done + t, st = i % kPStages;
                 const int64_t left = j.len - (int64_t)(j.ka + t) * kPTile;
-                const int have = left < kPTile ? (int)left : kPTile;
-                ok = mbar_wait_bounded(b_sfull + 8 * w, (cnt[w] + (t >> 1)) & 1);
-                if (have < kPTile || check_pages) ok = ok && mbar_wait_bounded(b_vfull + 8 * st, (i / kPStages) & 1);
+                const bool cut = left < kPTile;
+                ok = mbar_wait_bounded(b_sfull + 8 * w, (phase[w] + (t >> 1)) & 1);
+                if (cut || check_pages) ok = ok && mbar_wait_bounded(b_vfull + 8 * st, (i / kPStages) & 1);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                const uint32_t miss = check_pages ? absent[st] : 0u;
                 tc_fence_after();
-                if (have < kPTile || miss) {
+                const uint32_t miss = check_pages ? absent[st] : 0u;
+                const int have = cut ? (int)left : kPTile;
+                uint32_t s[kPHalf];
+                float top = -INFINITY;
+                // the row's largest logit: the lower half is read again below, the upper half stays in registers
+#pragma unroll 1
+                for (int x = 0; x < 2; ++x) {
+                    tc_ld64(t_s + kPHalf * x, s);
+                    tc_wait_ld();
+                    tc_loaded(s);
+                    if (cut || miss) {
+                        const int first = kPHalf * x;
+#pragma unroll
+                        for (int y = 0; y < kPHalf; ++y)
+                            if (first + y >= have || ((miss >> (4 * x + (y >> 4))) & 1u)) s[y] = 0xff800000u;
+                        if (x == 0) tc_st64(t_s, s);
+                    }
+                    float a = fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1])), b = fmaxf(__uint_as_float(s[2]), __uint_as_float(s[3]));
+#pragma unroll
+                    for (int y = 4; y < kPHalf; y += 4) {
+                        a = fmaxf(a, fmaxf(__uint_as_float(s[y]), __uint_as_float(s[y + 1])));
+                        b = fmaxf(b, fmaxf(__uint_as_float(s[y + 2]), __uint_as_float(s[y + 3])));
+                    }
+                    top = fmaxf(top, fmaxf(a, b));
+                }
+                if (cut || miss) {
                     // rows behind the length or of absent pages: no weight, and zeros for values (they may hold anything)
                     if (row >= have || ((miss >> (row >> 4)) & 1u)) {
 #pragma unroll
@@ -283,47 +356,15 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                             *reinterpret_cast<uint4 *>(gv + st * kPTileBytes + (c >> 3) * kPBlock + row * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
                     }
                     asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+                    tc_wait_st();
                 }
-                // 32 logits of the row at a time: the maximum over all four chunks first, the last two stay in registers
-                auto chunk = [&](int c, uint32_t (&r)[32]) {
-                    tc_wait_ld();
-                    tc_loaded(r);
-                    if (have < kPTile || miss) {
-#pragma unroll
-                        for (int x = 0; x < 32; ++x)
-                            if (32 * c + x >= have || ((miss >> (2 * c + (x >> 4))) & 1u)) r[x] = 0xff800000u;
-                    }
-                };
-                auto largest = [&](const uint32_t (&r)[32], float top) {
-#pragma unroll
-                    for (int x = 0; x < 32; ++x) top = fmaxf(top, __uint_as_float(r[x]));
-                    return top;
-                };
-                uint32_t sa[32], sb[32];
-                tc_ld32(t_s, sa);
-                tc_ld32(t_s + 32, sb);
-                chunk(0, sa);
-                float top = largest(sa, -INFINITY);
-                tc_ld32(t_s + 64, sa);
-                tc_loaded(sb);
-                if (have < kPTile || miss) chunk(1, sb);
-                top = largest(sb, top);
-                tc_ld32(t_s + 96, sb);
-                chunk(2, sa);
-                top = largest(sa, top);
-                tc_loaded(sb);
-                if (have < kPTile || miss) chunk(3, sb);
-                top = largest(sb, top);
                 top *= mul;
                 const bool raise = top > m + kAttLazy || (m == -INFINITY && top > m);
                 if (__any_sync(0xffffffffu, raise)) {
                     const float by = raise ? ex2(m - top) : 1.f;
                     if (raise) m = top;
-                    l *= by;
-                    if (t >= 2) {                          // an accumulator exists: wait until it rests, then rescale it
-                        ok = __all_sync(0xffffffffu, mbar_wait_bounded(b_pvdone + 8 * w, (cnt[w] + (t >> 1) - 1) & 1));
-                        if (!ok) break;
-                        tc_fence_after();
+                    l.x *= by; l.y *= by;
+                    if (t >= 2) {                          // an accumulator exists, and rests
 #pragma unroll 1
                         for (int c = 0; c < 8; ++c) {
                             uint32_t o[16];
@@ -331,53 +372,58 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                             tc_wait_ld();
                             tc_loaded(o);
 #pragma unroll
-                            for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * by);
+                            for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * by);
                             tc_st16(t_o + 128 * w + 16 * c, o);
                         }
                     }
                 }
                 const float ref = m == -INFINITY ? 0.f : m;
-                auto emit = [&](int c, const uint32_t (&r)[32]) {       // weights over the logits: 16 columns of bf16 pairs, 16 of their rest
-                    uint32_t hi[16], lo[16];
+                const float2 ref2 = make_float2(-ref, -ref), minus = make_float2(-1.f, -1.f);
+#pragma unroll 1
+                for (int x = 1; x >= 0; --x) {
+                    // weights over the logits: for each 32 rows 16 columns of bf16 pairs, then 16 of what their rounding left over
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) {
-                        const float a = ex2(fmaf(__uint_as_float(r[2 * x]), mul, -ref));
-                        const float b = ex2(fmaf(__uint_as_float(r[2 * x + 1]), mul, -ref));
-                        l += a + b;
-                        split16<false>(a, b, hi[x], lo[x]);
+                    for (int c = 0; c < kPHalf / 32; ++c) {
+                        uint32_t hi[16], lo[16];
+#pragma unroll
+                        for (int y = 0; y < 16; ++y) {
+                            float2 e = fma2(make_float2(__uint_as_float(s[32 * c + 2 * y]), __uint_as_float(s[32 * c + 2 * y + 1])), mul2, ref2);
+                            e.x = ex2(e.x);
+                            e.y = ex2(e.y);
+                            l = add2(l, e);
+                            hi[y] = cvt_bf16x2(e.y, e.x);
+                            const float2 rest = fma2(make_float2(bf16_lo(hi[y]), bf16_hi(hi[y])), minus, e);
+                            lo[y] = cvt_bf16x2(rest.y, rest.x);
+                        }
+                        tc_st16(t_s + kPHalf * x + 32 * c, hi);
+                        tc_st16(t_s + kPHalf * x + 32 * c + 16, lo);
                     }
-                    tc_st16(t_s + 32 * c, hi);
-                    tc_st16(t_s + 32 * c + 16, lo);
-                };
-                emit(2, sa);
-                tc_ld32(t_s, sa);
-                emit(3, sb);
-                tc_ld32(t_s + 32, sb);
-                chunk(0, sa);
-                emit(0, sa);
-                tc_loaded(sb);
-                if (have < kPTile || miss) chunk(1, sb);
-                emit(1, sb);
-                tc_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(b_pready + 8 * w);
+                    if (x == 1) {
+                        tc_ld64(t_s, s);
+                        tc_wait_ld();
+                        tc_loaded(s);
+                    }
+                    tc_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(b_pready + 8 * (2 * w + x));
+                }
             }
             done += n;
-            cnt[0] += (n + 1) >> 1;
-            cnt[1] += n >> 1;
+            phase[0] += ((n + 1) >> 1) + 1;
+            phase[1] += n >= 2 ? (n >> 1) + 1 : 0;
             // ---------------- join the two streams ----------------
-            // own stream first: the MMAs complete in order, so the other's barrier is then at most one phase behind its last
-            // (a parity wait cannot tell a phase from the one two before it)
-            for (int x = 0; x < 2 && ok; ++x) {
-                const int y = x == 0 ? w : 1 - w;
-                if (y == 0 || n >= 2) ok = mbar_wait_bounded(b_pvdone + 8 * y, (cnt[y] - 1) & 1);
+            // own stream first: a parity wait cannot tell a phase from the one two before it, and as the MMAs complete in
+            // order, the other stream's barrier is then at most its last phase behind
+            for (int z = 0; z < 2 && ok; ++z) {
+                const int y = z == 0 ? w : 1 - w;
+                if (y == 0 || n >= 2) ok = mbar_wait_bounded(b_sfull + 8 * y, (phase[y] - 1) & 1);
             }
             // (the columns of S and P are idle until the next unit's queries are announced: m and l pass through them)
             ok = __all_sync(0xffffffffu, ok);
             if (ok) {
                 tc_fence_after();
-                tc_st2(t_s, m, l);
+                tc_st2(t_s, m, l.x + l.y);
                 tc_wait_st();
                 tc_fence_before();
             }
@@ -397,7 +443,7 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
             const bool mine = row < j.nrows;
             const int sq = j.first_seq + (mine ? row : 0) / p.G, hq = j.h * p.G + row % p.G;
             float *to = j.complete ? p.whole + ((int64_t)sq * p.H * p.G + hq) * kAttRowPitch
-                                   : p.slots + (((int64_t)blockIdx.x * 2 + (j.begins ? 1 : 0)) * kPTile + row) * kAttRowPitch;
+                                   : p.slots + (((int64_t)sh.worker * 2 + (j.tail ? 1 : 0)) * kPTile + row) * kAttRowPitch;
 #pragma unroll 1
             for (int c = 0; c < 4; ++c) {                  // this group's half of the dims, 16 at a time
                 uint32_t a[16], b[16];
