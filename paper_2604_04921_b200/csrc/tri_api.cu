@@ -1262,11 +1262,29 @@ AttendPlan make_attend_plan(const tri_ctx *c, int32_t S, int32_t P)
     return a;
 }
 
-template <bool KEY8>
-void launch_attend(int rows, unsigned blocks, cudaStream_t st, const AttendParams &p)
+// A launch that may be set up, and where its kernel allows it started, while the kernel before it in the stream still runs.
+template <typename Kernel, typename Params>
+cudaError_t launch_under(Kernel kernel, unsigned blocks, unsigned threads, size_t smem, cudaStream_t st, const Params &p)
 {
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cfg.attrs = &attr; cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, p);
+}
+
+// under: behind a pass over prefixes, with which it shares nothing but the joining kernel
+template <bool KEY8>
+cudaError_t launch_attend(int rows, unsigned blocks, cudaStream_t st, const AttendParams &p, bool under)
+{
+    if (under)
+        return rows == 8 ? launch_under(k_attend<KEY8, 8>, blocks, kAttThreads, kAttRingBytes, st, p)
+                         : launch_under(k_attend<KEY8, 16>, blocks, kAttThreads, kAttRingBytes, st, p);
     if (rows == 8) k_attend<KEY8, 8><<<blocks, kAttThreads, kAttRingBytes, st>>>(p);
     else k_attend<KEY8, 16><<<blocks, kAttThreads, kAttRingBytes, st>>>(p);
+    return cudaGetLastError();
 }
 
 tri_status check_attend_cache(const tri_ctx *c, const tri_layer_cache *lc, int32_t n)
@@ -1306,6 +1324,12 @@ AttendParams attend_params(const tri_ctx *c, const tri_layer_cache *lc, int32_t 
     return p;
 }
 
+// Whether the line of steps that the passes cut into shares (at least 64 rows each, plus each unit's own cost) stays below 2^31.
+bool line_ok(const tri_ctx *c, const tri_cache_view *v, int64_t units)
+{
+    return units * c->desc.n_kv_heads * ((int64_t)v->n_max / 64 + 1 + kAttUnitCost) < ((int64_t)1 << 31);
+}
+
 tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, const int32_t *group_start,
                       const tri_layer_cache *src, int32_t S, const tri_attend_io *io, int32_t *device_status,
                       void *ws, size_t ws_bytes, cudaStream_t st)
@@ -1316,6 +1340,7 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
         !std::isfinite(io->scale))
         return TRI_ERR_INVALID_ARG;
     if ((r = check_device(c)) != TRI_OK) return r;
+    if (!line_ok(c, src->view, S) || (P > 0 && !line_ok(c, prefix->view, (int64_t)P + S / (16 / c->desc.group_size)))) return TRI_ERR_UNSUPPORTED;
     const AttendPlan pl = make_attend_plan(c, S, P);
     if (ws_bytes < pl.total) return TRI_ERR_WORKSPACE;
     char *w = (char *)ws;
@@ -1334,32 +1359,25 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
             if ((r = encode_key_map(c, prefix->view, P, c->desc.n_layers, &km)) != TRI_OK) return r;
             if ((r = encode_key_map(c, prefix->view, P, c->desc.n_layers, &vm, prefix->view->v)) != TRI_OK) return r;
             k_attend_prefix<<<(unsigned)c->n_sm, kPThreads, kPDynSmem, st>>>(km, vm, p);
+            TRI_CUDA(cudaGetLastError());
         } else if (prefix->view->k_kind == 3) {
-            launch_attend<true>(rows, (unsigned)pl.blocks, st, p);
+            TRI_CUDA(launch_attend<true>(rows, (unsigned)pl.blocks, st, p, false));
         } else {
-            launch_attend<false>(rows, (unsigned)pl.blocks, st, p);
+            TRI_CUDA(launch_attend<false>(rows, (unsigned)pl.blocks, st, p, false));
         }
-        if ((r = check_launch("k_attend (prefix)")) != TRI_OK) return r;
         mp.pre.rec = p.rec; mp.pre.slots = p.slots; mp.pre.whole = p.whole; mp.pre.rows = rows; mp.pre.spt = p.spt;
     }
     AttendParams p = attend_params(c, src, S, S, io, device_status);
     p.finish = P > 0 ? 0 : 1;
     p.rec = (int2 *)(w + pl.own_rec); p.slots = (float *)(w + pl.own_slots);
     p.whole = P > 0 ? (float *)(w + pl.own_whole) : nullptr;
-    if (src->view->k_kind == 3) launch_attend<true>(pl.own_rows, (unsigned)pl.blocks, st, p);
-    else launch_attend<false>(pl.own_rows, (unsigned)pl.blocks, st, p);
-    if ((r = check_launch("k_attend")) != TRI_OK) return r;
+    if (src->view->k_kind == 3) TRI_CUDA(launch_attend<true>(pl.own_rows, (unsigned)pl.blocks, st, p, P > 0));
+    else TRI_CUDA(launch_attend<false>(pl.own_rows, (unsigned)pl.blocks, st, p, P > 0));
 
     mp.own.rec = p.rec; mp.own.slots = p.slots; mp.own.whole = p.whole; mp.own.rows = pl.own_rows; mp.own.spt = 0;
     mp.S = S; mp.P = P; mp.H = H; mp.G = G; mp.group_start = group_start;
     mp.out = p.out; mp.out_seq = p.out_seq; mp.out_head = p.out_head; mp.lse = io->lse; mp.device_status = device_status;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(S * H)); cfg.blockDim = dim3(kMergeThreads); cfg.stream = st;
-    cfg.attrs = &attr; cfg.numAttrs = 1;
-    TRI_CUDA(cudaLaunchKernelEx(&cfg, k_attend_merge, mp));
+    TRI_CUDA(launch_under(k_attend_merge, (unsigned)(S * H), kMergeThreads, 0, st, mp));
     return TRI_OK;
 }
 

@@ -26,7 +26,6 @@ constexpr int kAttStages = 2, kAttStageBytes = 8192;             // K and V of 1
 constexpr int kAttRingBytes = kAttWarps * kAttStages * kAttStageBytes;
 template <bool KEY8> constexpr int kAttRows = KEY8 ? 32 : 16;    // rows of a warp's step; a tile is one step of all warps
 constexpr int kAttUnitCost = 2;                                  // a unit's own cost, in tiles
-constexpr int kAttMinShare = 1;                                  // tiles a share has at least (if there are that many)
 constexpr int kAttRowPitch = kHeadDim + 4;                       // floats per row of a part: 128 sums, m, l, two unused
 constexpr float kAttLazy = 8.0f;                                 // the bound m is raised when a logit passes it by this much
 
@@ -62,6 +61,8 @@ __device__ __forceinline__ int2 att_group(const int32_t *start, int S, int g)
     const int a = min(max(__ldg(start + g), 0), S), b = min(max(__ldg(start + g + 1), 0), S);
     return make_int2(a, max(b - a, 0));
 }
+// r / d for r < 256, 0 < d <= 16, with inv = 65536 / d + 1: the product's error r * d / 65536 never reaches the next integer.
+__device__ __forceinline__ int att_small_div(int r, int inv) { return (r * inv) >> 16; }
 __device__ __forceinline__ int att_row_tiles(const AttendParams &p, int seq)
 {
     if (p.spt == 0) return 1;
@@ -122,133 +123,128 @@ __device__ __forceinline__ float ex2(float x)
     return y;
 }
 
-// The share of one block: where it begins on the line and which unit lies there.
+// The share of one block: where it begins on the line and which unit lies there.  (The host refuses calls whose line
+// could pass 2^31 steps.)
 struct AttShare {
-    int64_t total, t0, t1;        // steps of the call; this worker's [t0, t1)
-    int64_t each;                 // steps per share; the first `longer` shares have one more
-    int32_t longer;
-    int64_t start;                // first step of the unit (all of its row tiles) below
-    int32_t shares, worker;       // blocks that get steps; this one
-    int32_t unit;                 // seq * H + h
+    int total, t0, t1;                // steps of the call; this block's [t0, t1)
+    int each, longer;                 // steps per share; the first `longer` shares have one more
+    int shares;                       // blocks that get steps
+    int seq, h, start;                // the unit at t0 and its first step (all of its row tiles)
 };
 // Where a block stands on the line, and what it finds there: tiles [ka, kb) of one unit and tile of query rows.
-struct AttCursor { int unit, rt; int64_t start; };
+struct AttCursor { int seq, h, rt, start; };
 struct AttJob {
     int seq, h, len, kt, ka, kb;      // tiles [ka, kb) of the unit's kt
     int first_seq, nrows;             // query rows: G of each sequence from first_seq on (prefixes), or of seq
     int rec;                          // index of the unit's record
-    int64_t rows0;                    // step of the unit's first tile
-    bool begins, tail, complete;      // the unit's first step is here; its part goes to the last slot; all tiles are here
+    int rows0;                        // step of the unit's first tile
+    bool begins, complete;            // the unit's first step is here (its part goes to the last slot); all tiles are here
 };
 
-// a / b for a >= 0, b > 0; the 64-bit division takes several hundred cycles, and steps rarely need it.
-__device__ __forceinline__ int64_t att_div(int64_t a, int64_t b)
+// The share of this block.  Where the heads of a sequence have equal lengths the sums run over sequences only.
+template <int TILE, int COST>
+__device__ __forceinline__ AttShare att_share(const AttendParams &p)
 {
-    return ((uint64_t)(a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
-}
-
-// The share of this block.  Units are entries seq * H + h; where the heads of a sequence have equal lengths the sums run
-// over sequences only.
-__device__ __forceinline__ AttShare att_share(const AttendParams &p, int tile_rows, int unit_cost, int min_share)
-{
-    __shared__ long long part_s[32], start_s;
-    __shared__ int unit_s;
+    __shared__ int part_s[32], found_s[3];
     const int tid = threadIdx.x, nth = blockDim.x, lane = tid & 31, warp = tid >> 5;
     const bool by_head = p.unit_lens != nullptr;
     const int n = by_head ? p.nseq * p.H : p.nseq, heads = by_head ? 1 : p.H;
-    const int per = (n + nth - 1) / nth;
+    const int per = n <= nth ? 1 : (n + nth - 1) / nth;
     const int a = min(tid * per, n), b = min(a + per, n);
-    auto cost = [&](int x) -> long long {                 // of one head
-        const int seq = by_head ? x / p.H : x, h = by_head ? x - seq * p.H : 0;
-        const long long kt = ((long long)att_len(p, seq, h) + tile_rows - 1) / tile_rows;
-        return (kt + unit_cost) * att_row_tiles(p, seq);
+    // steps of entry x, one head
+    auto cost = [&](int x) -> int {
+        const int len = by_head ? __ldg(p.unit_lens + x) : __ldg(p.src.seq_lens + x);
+        const int kt = (int)(((uint32_t)min(max(len, 0), p.src.n_max) + TILE - 1) / TILE);
+        return (kt + COST) * (p.spt ? att_row_tiles(p, by_head ? x / p.H : x) : 1);
     };
-    long long sum = 0;
-    for (int x = a; x < b; ++x) sum += cost(x) * heads;
-    long long incl = sum;
+    int sum = 0, c0 = 0;
+    for (int x = a; x < b; ++x) { c0 = cost(x); sum += c0 * heads; }
+    int incl = sum;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const long long o = __shfl_up_sync(0xffffffffu, incl, d);
+        const int o = __shfl_up_sync(0xffffffffu, incl, d);
         if (lane >= d) incl += o;
     }
     if (lane == 31) part_s[warp] = incl;
     __syncthreads();
-    long long before = 0, total = 0;
+    int before = 0, total = 0;
     for (int w = 0; w < nth / 32; ++w) {
         if (w < warp) before += part_s[w];
         total += part_s[w];
     }
     AttShare r;
     r.total = total;
-    const long long want = att_div(total, min_share), most = gridDim.x;
-    r.shares = (int)(want < 1 ? 1 : (want < most ? want : most));
-    r.each = att_div(total, r.shares);
-    r.longer = (int)(total - r.each * r.shares);
-    r.worker = (int)blockIdx.x;
-    const bool have = r.worker < r.shares && total > 0;
-    r.t0 = have ? r.worker * r.each + min(r.worker, r.longer) : total;
-    r.t1 = have ? r.t0 + r.each + (r.worker < r.longer ? 1 : 0) : total;
-    long long at = before + incl - sum;                   // this thread's entries: steps [at, at + sum)
+    r.shares = min(max(total, 1), (int)gridDim.x);
+    r.each = (int)((uint32_t)total / (uint32_t)r.shares);
+    r.longer = total - r.each * r.shares;
+    const int worker = (int)blockIdx.x;
+    const bool have = worker < r.shares && total > 0;
+    r.t0 = have ? worker * r.each + min(worker, r.longer) : total;
+    r.t1 = have ? r.t0 + r.each + (worker < r.longer ? 1 : 0) : total;
+    int at = before + incl - sum;                         // this thread's entries: steps [at, at + sum)
     if (r.t0 >= at && r.t0 < at + sum) {
         for (int x = a; x < b; ++x) {
-            const long long c = cost(x);
+            const int c = per == 1 ? c0 : cost(x);
             if (r.t0 < at + c * heads) {
-                const int skip = (int)att_div(r.t0 - at, c);
-                unit_s = by_head ? x : x * p.H + skip;
-                start_s = at + skip * c;
+                const int skip = by_head ? 0 : (int)((uint32_t)(r.t0 - at) / (uint32_t)c);
+                found_s[0] = by_head ? x / p.H : x;
+                found_s[1] = by_head ? x % p.H : skip;
+                found_s[2] = at + skip * c;
                 break;
             }
             at += c * heads;
         }
     }
     __syncthreads();
-    r.unit = have ? unit_s : p.nseq * p.H;
-    r.start = have ? start_s : total;
+    r.seq = have ? found_s[0] : p.nseq;
+    r.h = have ? found_s[1] : 0;
+    r.start = have ? found_s[2] : total;
     return r;
 }
 
 // Which block holds step t of the line.
-__device__ __forceinline__ int att_worker_of(const AttShare &r, int64_t t)
+__device__ __forceinline__ int att_block_of(const AttShare &r, int t)
 {
-    const int64_t split = r.longer * (r.each + 1);
-    return t < split ? (int)att_div(t, r.each + 1) : r.longer + (int)att_div(t - split, r.each);
+    const int split = r.longer * (r.each + 1);
+    return t < split ? (int)((uint32_t)t / (uint32_t)(r.each + 1)) : r.longer + (int)((uint32_t)(t - split) / (uint32_t)r.each);
 }
 
 // The record of a unit, made by the block that holds its first step: slot of its first part, number of parts.
 __device__ __forceinline__ int2 att_record(const AttShare &sh, const AttJob &j)
 {
     if (j.kt == 0) return make_int2(0, 0);
-    const int first = att_worker_of(sh, j.rows0);
-    return make_int2(2 * first + (first == sh.worker ? 1 : 0), att_worker_of(sh, j.rows0 + j.kt - 1) - first + 1);
+    const int here = (int)blockIdx.x;
+    if (j.complete) return make_int2(2 * here, 1);
+    const int first = j.rows0 < sh.t1 ? here : att_block_of(sh, j.rows0);
+    return make_int2(2 * first + (first == here ? 1 : 0), att_block_of(sh, j.rows0 + j.kt - 1) - first + 1);
 }
 
 // The next unit of a share; false at its end.  Units without rows come too, and units of which the share holds only the
 // steps that stand for their own cost (kb <= ka).
-__device__ __forceinline__ bool att_next(const AttendParams &p, const AttShare &sh, int tile_rows, int unit_cost, AttCursor &c, AttJob &j)
+template <int TILE, int COST>
+__device__ __forceinline__ bool att_next(const AttendParams &p, const AttShare &sh, AttCursor &c, AttJob &j)
 {
-    while (c.unit < p.nseq * p.H && c.start < sh.t1) {
-        j.seq = c.unit / p.H; j.h = c.unit - j.seq * p.H;
+    while (c.start < sh.t1 && c.seq < p.nseq) {
+        j.seq = c.seq; j.h = c.h;
         j.len = att_len(p, j.seq, j.h);
-        j.kt = (int)(((int64_t)j.len + tile_rows - 1) / tile_rows);
-        const int2 grp = p.spt ? att_group(p.group_start, p.S, j.seq) : make_int2(j.seq, 1);
-        const int rts = p.spt ? (grp.y + p.spt - 1) / p.spt : 1, rt = c.rt++;
-        const int64_t c1 = (int64_t)j.kt + unit_cost;
-        if (rt >= rts) {
-            c.start += c1 * rts;
-            ++c.unit;
+        j.kt = (int)(((uint32_t)j.len + TILE - 1) / TILE);
+        const int c1 = j.kt + COST, rt = c.rt;
+        int2 grp = make_int2(j.seq, 1);
+        int rts = 1;
+        if (p.spt) { grp = att_group(p.group_start, p.S, j.seq); rts = (grp.y + p.spt - 1) / p.spt; }
+        const int js = c.start, rows0 = js + COST, je = js + c1;             // the steps of this tile of query rows
+        if (rt < rts) c.start += c1;
+        if (++c.rt >= rts) {
             c.rt = 0;
-            continue;
+            if (++c.h == p.H) { c.h = 0; ++c.seq; }
         }
-        const int64_t js = c.start + rt * c1, rows0 = js + unit_cost, je = js + c1;      // the unit's steps; its first tile
-        if (je <= sh.t0) continue;
-        if (js >= sh.t1) return false;
+        if (rt >= rts || je <= sh.t0) continue;
         j.first_seq = grp.x + rt * p.spt;
         j.nrows = p.spt ? min(p.spt, grp.y - rt * p.spt) * p.G : p.G;
-        j.rec = p.spt ? att_tile_index(j.seq, grp.x, p.spt, rt) * p.H + j.h : c.unit;
-        j.ka = sh.t0 > rows0 ? (int)(sh.t0 - rows0) : 0;
-        j.kb = je > sh.t1 ? (sh.t1 > rows0 ? (int)(sh.t1 - rows0) : 0) : j.kt;
+        j.rec = p.spt ? att_tile_index(j.seq, grp.x, p.spt, rt) * p.H + j.h : j.seq * p.H + j.h;
+        j.ka = max(sh.t0 - rows0, 0);
+        j.kb = min(max(sh.t1 - rows0, 0), j.kt);
         j.begins = js >= sh.t0;
-        j.tail = js >= sh.t0;
         j.complete = j.ka == 0 && j.kb == j.kt;
         j.rows0 = rows0;
         return true;
@@ -272,26 +268,31 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
     const uint32_t ring = smem_u32(dyn) + warp * (ST * kAttStageBytes);
     grid_dependents_launch();                             // the joining kernel may be set up under this one
-    const AttShare sh = att_share(p, TILE, kAttUnitCost, kAttMinShare);
-    if (sh.worker >= sh.shares) return;
+    const AttShare sh = att_share<TILE, kAttUnitCost>(p);
+    if ((int)blockIdx.x >= sh.shares) return;
 
     // ---------------- copies: a cursor of their own, ST - 1 steps ahead ----------------
-    AttCursor pc = {sh.unit, 0, sh.start};
+    AttCursor pc = {sh.seq, sh.h, 0, sh.start};
     AttJob pj = {};
-    int pit = 0, page[NK], pstage = 0;                    // next step; the pages of its 16-row halves
+    int pit = 0, pstage = 0, page[NK], slot[NK];          // next step; page and first slot of its 16-row halves
     uint32_t bad = 0;                                     // bits 2 i, 2 i + 1: these 16 rows of stage i are absent
     bool more = true;
+    int64_t unit_base = 0;                                // first row of the unit; of page 0, where rows are paged
+    const int64_t step_row = p.src.paged ? p.src.stride_slot : p.src.stride_tok;
     auto advance = [&]() {                                // to the next step, its pages looked up before they are needed
-        if (pit == 0 || pit == pj.kb) {
-            do more = att_next(p, sh, TILE, kAttUnitCost, pc, pj); while (more && pj.kb <= pj.ka);
+        if (pit == pj.kb) {
+            do more = att_next<TILE, kAttUnitCost>(p, sh, pc, pj); while (more && pj.kb <= pj.ka);
             pit = pj.ka;
+            unit_base = (int64_t)p.layer * p.src.stride_layer + (int64_t)pj.h * p.src.stride_head +
+                        (p.src.paged ? 0 : (int64_t)pj.seq * p.src.stride_seq);
         }
         if (more && p.src.paged) {
 #pragma unroll
             for (int half = 0; half < NK; ++half) {
-                const int64_t r = (int64_t)pit * TILE + warp * ROWS + 16 * half;
-                const int pg = p.src.page_shift >= 0 ? (int)r >> p.src.page_shift : (int)r / p.src.page_size;
-                page[half] = r < pj.len ? __ldg(p.src.page_table + (int64_t)pj.seq * p.src.max_pages_per_seq + pg) : 0;
+                const uint32_t r = (uint32_t)pit * TILE + warp * ROWS + 16 * half;
+                const uint32_t pg = p.src.page_shift >= 0 ? r >> p.src.page_shift : r / (uint32_t)p.src.page_size;
+                page[half] = r < (uint32_t)pj.len ? __ldg(p.src.page_table + (int64_t)pj.seq * p.src.max_pages_per_seq + pg) : 0;
+                slot[half] = (int)(r - pg * (uint32_t)p.src.page_size);
             }
         }
     };
@@ -303,34 +304,31 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
             uint32_t miss = 0;
 #pragma unroll
             for (int half = 0; half < NK; ++half) {       // 16 rows each: they lie in one page
-                const int64_t r = (int64_t)pit * TILE + warp * ROWS + 16 * half;
-                int64_t base = (int64_t)p.layer * p.src.stride_layer + (int64_t)pj.h * p.src.stride_head, step;
-                bool ok = true;
+                const uint32_t r = (uint32_t)pit * TILE + warp * ROWS + 16 * half;
+                int have = r < (uint32_t)pj.len ? min(pj.len - (int)r, 16) : 0;
+                int64_t base = unit_base;
                 if (p.src.paged) {
-                    ok = p.src.n_pages <= 0 || (page[half] >= 0 && page[half] < p.src.n_pages) || r >= pj.len;
-                    const int off = (int)r - (p.src.page_shift >= 0 ? ((int)r >> p.src.page_shift) << p.src.page_shift
-                                                                     : (int)r / p.src.page_size * p.src.page_size);
-                    step = p.src.stride_slot;
-                    base += (int64_t)page[half] * p.src.stride_page + (int64_t)off * step;
+                    base += (int64_t)page[half] * p.src.stride_page + (int64_t)slot[half] * step_row;
+                    if (have && p.src.n_pages > 0 && (uint32_t)page[half] >= (uint32_t)p.src.n_pages) {
+                        have = 0;
+                        miss |= 1u << half;
+                        if (lane == 0 && p.device_status) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
+                    }
                 } else {
-                    step = p.src.stride_tok;
-                    base += (int64_t)pj.seq * p.src.stride_seq + r * step;
+                    base += (int64_t)r * step_row;
                 }
-                if (!ok) {
-                    miss |= 1u << half;
-                    if (lane == 0 && p.device_status) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
-                }
-                const int64_t left = pj.len - r;
-                const int have = !ok || left <= 0 ? 0 : (left < 16 ? (int)left : 16);
+                int64_t from = (base + r0 * step_row) * es;
+                const uint32_t to = dst + (16 * half + r0) * kRowBytes;
 #pragma unroll
                 for (int i = 0; i < kCopies / NK; ++i) {
                     // rows behind the length (or absent ones) arrive as zeros and are not read
-                    const int rr = i * (32 / kChunks) + r0, row = 16 * half + rr;
-                    const uint32_t bytes = rr < have ? 16u : 0u;
-                    const int64_t from = (rr < have ? (base + (int64_t)rr * step) * es : 0) + 16 * c;
-                    const uint32_t to = dst + row * kRowBytes + (((c & 8) | ((c ^ row) & 7)) << 4);
-                    cp_async16(to, p.src.k + from, bytes);
-                    cp_async16(to + kHalf, p.src.v + from, bytes);
+                    const int rr = i * (32 / kChunks) + r0;
+                    const bool there = rr < have;
+                    const int64_t at = (there ? from : 0) + 16 * c;
+                    const uint32_t off = i * (32 / kChunks) * kRowBytes + (((c & 8) | ((c ^ rr) & 7)) << 4);
+                    cp_async16(to + off, p.src.k + at, there ? 16u : 0u);
+                    cp_async16(to + kHalf + off, p.src.v + at, there ? 16u : 0u);
+                    from += (32 / kChunks) * step_row * es;
                 }
             }
             bad = (bad & ~(3u << (2 * pstage))) | (miss << (2 * pstage));
@@ -342,9 +340,10 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
     };
     advance();
 
-    AttCursor cur = {sh.unit, 0, sh.start};
+    AttCursor cur = {sh.seq, sh.h, 0, sh.start};
     AttJob j = {};
     uint32_t qa[8][4];
+    const int inv_g = 65536 / p.G + 1;
     float mul[NR];                                        // logit in base-2 units per accumulator unit
     float o[16][4], m[NR], l[NR];
     int it = 0, stage = 0, ahead = ST - 1;
@@ -355,7 +354,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
         if (it == j.kb) {
             // ---------------- the next unit ----------------
             bool rows = false;
-            while (!rows && att_next(p, sh, TILE, kAttUnitCost, cur, j)) {
+            while (!rows && att_next<TILE, kAttUnitCost>(p, sh, cur, j)) {
                 if (j.begins && tid == 0) p.rec[j.rec] = att_record(sh, j);
                 rows = j.kb > j.ka;
                 if (j.kt == 0 && j.begins && p.finish)    // no rows: zeros
@@ -375,7 +374,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
                 const bool have = r < j.nrows && (RT == 16 || i == 0);
                 const char *qr = nullptr;
                 if (have) {
-                    const int sq = p.spt ? j.first_seq + r / p.G : j.seq, gg = p.spt ? r % p.G : r;
+                    const int sr = p.spt ? att_small_div(r, inv_g) : 0, sq = p.spt ? j.first_seq + sr : j.seq, gg = r - sr * p.G;
                     qr = p.q + ((int64_t)sq * p.q_seq + (int64_t)(j.h * p.G + gg) * p.q_head) * 2;
                 }
                 float amax = 0.f;
@@ -420,8 +419,8 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
         // ---------------- one step ----------------
         cp_wait<ST - 1>();
         __syncwarp();
-        const int64_t left = j.len - ((int64_t)it * TILE + warp * ROWS);
-        const int have = left < 0 ? 0 : (left < ROWS ? (int)left : ROWS);
+        const uint32_t r0 = (uint32_t)it * TILE + warp * ROWS;
+        const int have = r0 < (uint32_t)j.len ? min(j.len - (int)r0, ROWS) : 0;
         const uint32_t miss = (bad >> (2 * stage)) & 3u;
         const uint32_t kb_s = ring + stage * kAttStageBytes, vb_s = kb_s + kHalf;
         // logits: 8 rows x 8 keys per accumulator (x 2: even and odd steps of 16 dims apart, shorter chains)
@@ -573,10 +572,10 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
                 ll += st[w2].y * st[w2].x;
             }
             const float by = final ? (ll == 0.f ? 0.f : vs / ll) : vs;
-            const int sq = p.spt ? j.first_seq + r / p.G : j.seq, hq = j.h * p.G + (p.spt ? r % p.G : r);
+            const int sr = p.spt ? att_small_div(r, inv_g) : 0, sq = p.spt ? j.first_seq + sr : j.seq, hq = j.h * p.G + r - sr * p.G;
             char *out = p.out + ((int64_t)sq * p.out_seq + (int64_t)hq * p.out_head) * 2;
             float *to = j.complete ? p.whole + ((int64_t)sq * p.H * p.G + hq) * kAttRowPitch
-                                   : p.slots + (((int64_t)sh.worker * 2 + (j.tail ? 1 : 0)) * RT + r) * kAttRowPitch;
+                                   : p.slots + (((int64_t)blockIdx.x * 2 + (j.begins ? 1 : 0)) * RT + r) * kAttRowPitch;
 #pragma unroll
             for (int q2 = 0; q2 < 2; ++q2) {
                 const int q = 2 * warp + q2;               // fragments 2 q, 2 q + 1
@@ -611,6 +610,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
         __syncthreads();                                   // the stages may be refilled
     }
     cp_wait<0>();
+    grid_dependency_wait();                               // not through before the pass over prefixes is, if one was launched before
 }
 
 // ----------------------------------------------------------------------------------------------
@@ -619,7 +619,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
 struct AttendPass {                // where a pass left its parts
     const int2 *rec;
     const float *slots, *whole;
-    int32_t rows;                  // query rows per slot
+    int32_t rows;                  // query rows per slot; 128: the sums of 4 dims of all rows, the next 4 dims, .., (m, l) of all rows
     int32_t spt;                   // prefixes: sequences per tile
 };
 
@@ -632,6 +632,8 @@ struct MergeParams {
     float *lse;
     int32_t *device_status;
 };
+
+constexpr int kMergeTile = 128;     // query rows per slot of k_attend_prefix, see AttendPass::rows
 
 // A block joins the G rows of one (sequence, KV head): 16 / G warps per row take its parts in turn, each lane four sums.
 // The kernel is launched while the pass before it still runs (programmatic dependent launch) and waits for it here.
@@ -648,11 +650,10 @@ __global__ void __launch_bounds__(kMergeThreads) k_attend_merge(const MergeParam
     int row0 = 0;
     if (p.pre.rec) {
         // the group of this sequence: the last one that starts at or before it
-        int lo = 0, hi = p.P;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (__ldg(p.group_start + mid) <= s) lo = mid; else hi = mid;
-        }
+        int lo = -1;
+        for (int b = 0; b < p.P; b += 32)
+            lo += __popc(__ballot_sync(0xffffffffu, b + lane < p.P && __ldg(p.group_start + min(b + lane, p.P - 1)) <= s));
+        lo = max(lo, 0);
         const int2 g = att_group(p.group_start, p.S, lo);
         if (s >= g.x && s < g.x + g.y) {
             const int rt = (s - g.x) / p.pre.spt;
@@ -667,22 +668,35 @@ __global__ void __launch_bounds__(kMergeThreads) k_attend_merge(const MergeParam
     const int wpr = kMergeWarps / p.G, g = warp / wpr, sub = warp - g * wpr;
     const bool active = g < p.G;
     const int64_t hq = (int64_t)h * p.G + g;
-    // part i: the own rows' parts in ascending order, then the prefix's
-    auto at = [&](int i) -> const float * {
+    // part i: the own rows' parts in ascending order, then the prefix's; its row, and where its (m, l) lie
+    const bool tiled = p.pre.rows == kMergeTile && pre.y > 1;
+    auto at = [&](int i, const float2 *&ml) -> const float * {
         const bool is_own = i < own.y;
         const AttendPass &a = is_own ? p.own : p.pre;
         const int2 rc = is_own ? own : pre;
-        const int k = is_own ? i : i - own.y;
-        if (rc.y == 1) return a.whole + ((int64_t)s * p.H * p.G + hq) * kAttRowPitch;
-        return a.slots + ((int64_t)(k == 0 ? rc.x : (rc.x & ~1) + 2 * k) * a.rows + (is_own ? 0 : row0) + g) * kAttRowPitch;
+        const int k = is_own ? i : i - own.y, row = is_own ? g : row0 + g;
+        const float *src;
+        if (rc.y == 1) {
+            src = a.whole + ((int64_t)s * p.H * p.G + hq) * kAttRowPitch;
+        } else {
+            src = a.slots + (int64_t)(k == 0 ? rc.x : (rc.x & ~1) + 2 * k) * a.rows * kAttRowPitch;
+            if (!is_own && tiled) {
+                ml = reinterpret_cast<const float2 *>(src + kMergeTile * kHeadDim) + row;
+                return src + 4 * row;
+            }
+            src += row * kAttRowPitch;
+        }
+        ml = reinterpret_cast<const float2 *>(src + kHeadDim);
+        return src;
     };
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
     float mm = -INFINITY, ll = 0.f;
     if (active) {
         for (int b = 0; b < parts; b += 32) {
             // summaries of up to 32 parts, one per lane, then their sums; a larger bound met on the way rescales what is there
-            const float *mine = b + lane < parts ? at(b + lane) : nullptr;
-            const float2 ml = mine ? *reinterpret_cast<const float2 *>(mine + kHeadDim) : make_float2(-INFINITY, 0.f);
+            const float2 *mlp = nullptr;
+            const float *mine = b + lane < parts ? at(b + lane, mlp) : nullptr;
+            const float2 ml = mine ? *mlp : make_float2(-INFINITY, 0.f);
             float top = fmaxf(mm, ml.x);
 #pragma unroll
             for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
@@ -699,7 +713,7 @@ __global__ void __launch_bounds__(kMergeThreads) k_attend_merge(const MergeParam
             for (int j = sub; j < n; j += wpr) {
                 const float *src = reinterpret_cast<const float *>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), j));
                 const float w = __shfl_sync(0xffffffffu, by, j);
-                const float4 x = *reinterpret_cast<const float4 *>(src + 4 * lane);
+                const float4 x = *reinterpret_cast<const float4 *>(src + lane * (tiled && b + j >= own.y ? 4 * kMergeTile : 4));
                 a.x += x.x * w; a.y += x.y * w; a.z += x.z * w; a.w += x.w * w;
             }
         }

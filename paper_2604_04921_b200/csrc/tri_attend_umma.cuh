@@ -28,7 +28,8 @@ namespace tri {
 constexpr int kPTile = 128;                               // cached rows per tile, query rows per tile
 constexpr int kPHalf = 64;                               // the weights of a tile are handed over in two halves, so that MMAs and softmax overlap
 constexpr int kPStages = 3;
-constexpr int kPUnitCost = 2, kPMinShare = 2;             // a unit's own cost and the least share, in tiles
+constexpr int kPUnitCost = 2;                             // a unit's own cost, in tiles
+static_assert(kPTile == kMergeTile, "slots are laid out for the joining kernel");
 constexpr int kPBlock = kPTile * 128;                     // 128 rows x 64 bf16, one swizzled block
 constexpr int kPTileBytes = 2 * kPBlock;                  // dims 0..63 | dims 64..127
 constexpr int kPSoftWarps = 8;
@@ -136,8 +137,9 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
     __shared__ uint32_t absent[kPStages];                  // per stage: boxes of 16 rows whose page id is out of range
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const AttShare sh = att_share(p, kPTile, kPUnitCost, kPMinShare);
-    if (sh.worker >= sh.shares || sh.total == 0) return;
+    grid_dependents_launch();                              // the pass over the sequences' own rows may start as blocks leave
+    const AttShare sh = att_share<kPTile, kPUnitCost>(p);
+    if ((int)blockIdx.x >= sh.shares || sh.total == 0) return;
 
     const uint32_t base = (smem_u32(dyn) + 1023u) & ~1023u;
     const uint32_t sm_q = base, sm_k = base + kPTileBytes, sm_v = sm_k + kPStages * kPTileBytes;
@@ -168,7 +170,7 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
     const uint32_t tmem = tmem_base_s;
     // columns: S/P of stream w at 128 w (weights: 64 columns, their rest: 64), O of stream w at 256 + 128 w
 
-    AttCursor cur = {sh.unit, 0, sh.start};
+    AttCursor cur = {sh.seq, sh.h, 0, sh.start};
     AttJob j;
     int done = 0;                                          // tiles of all earlier units of this block
 
@@ -176,7 +178,7 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
         // ---------------- producer: lane = (matrix, box of 16 rows, half) is 2 x 16 x 1: K on lanes 0..15, V on 16..31 ----------
         const int sub = (lane & 15) >> 1, half = lane & 1;
         const bool is_v = lane >= 16;
-        while (!gave_up && att_next(p, sh, kPTile, kPUnitCost, cur, j)) {
+        while (!gave_up && att_next<kPTile, kPUnitCost>(p, sh, cur, j)) {
             const int n = max(j.kb - j.ka, 0);
             auto locate = [&](int t, int &c1, int &c3) -> bool {          // false: the box's page id is out of range
                 const int64_t row = (int64_t)(j.ka + t) * kPTile + sub * kTileKeys;
@@ -224,7 +226,7 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
         constexpr uint32_t idesc_qk = tc_idesc_bf16(kPTile);                     // both operands K-major
         constexpr uint32_t idesc_pv = tc_idesc_bf16(kHeadDim) | (1u << 16);      // B (the values) N-major
         int units = 0, cnt[2] = {0, 0};                    // tiles each stream had in earlier units (phases of pready)
-        while (!gave_up && att_next(p, sh, kPTile, kPUnitCost, cur, j)) {
+        while (!gave_up && att_next<kPTile, kPUnitCost>(p, sh, cur, j)) {
             const int n = max(j.kb - j.ka, 0);
             if (n == 0) continue;
             bool ok = __all_sync(0xffffffffu, mbar_wait_bounded(b_q, units & 1));
@@ -281,8 +283,9 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
         const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16, t_s = tmem + lane_base + 128 * w, t_o = tmem + lane_base + 256;
         const uint32_t flip = p.scale < 0.f ? 0x80008000u : 0u;            // a negative scale goes into the queries' signs
         const bool check_pages = p.src.paged && p.src.n_pages > 0;
+        const int inv_g = 65536 / p.G + 1;
         int units = 0, phase[2] = {0, 0};                  // phases of sfull: one per tile, one more behind a unit's last
-        while (!gave_up && att_next(p, sh, kPTile, kPUnitCost, cur, j)) {
+        while (!gave_up && att_next<kPTile, kPUnitCost>(p, sh, cur, j)) {
             if (j.begins && tid == 0) p.rec[j.rec] = att_record(sh, j);
             const int n = max(j.kb - j.ka, 0);
             if (n == 0) continue;
@@ -292,7 +295,7 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                 const int r = (tid >> 4) + 16 * i, c = tid & 15;
                 q[i] = make_uint4(0u, 0u, 0u, 0u);
                 if (r < j.nrows) {
-                    const int sq = j.first_seq + r / p.G, g = r % p.G;
+                    const int sr = att_small_div(r, inv_g), sq = j.first_seq + sr, g = r - sr * p.G;
                     q[i] = *reinterpret_cast<const uint4 *>(p.q + ((int64_t)sq * p.q_seq + (int64_t)(j.h * p.G + g) * p.q_head) * 2 + 16 * c);
                     q[i].x ^= flip; q[i].y ^= flip; q[i].z ^= flip; q[i].w ^= flip;
                 }
@@ -441,9 +444,11 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
             const float m0 = __uint_as_float(s0[0]), m1 = __uint_as_float(s1[0]), mm = fmaxf(m0, m1);
             const float f0 = m0 == -INFINITY ? 0.f : ex2(m0 - mm), f1 = m1 == -INFINITY ? 0.f : ex2(m1 - mm);
             const bool mine = row < j.nrows;
-            const int sq = j.first_seq + (mine ? row : 0) / p.G, hq = j.h * p.G + row % p.G;
-            float *to = j.complete ? p.whole + ((int64_t)sq * p.H * p.G + hq) * kAttRowPitch
-                                   : p.slots + (((int64_t)sh.worker * 2 + (j.tail ? 1 : 0)) * kPTile + row) * kAttRowPitch;
+            const int sr = att_small_div(row, inv_g), sq = j.first_seq + sr, hq = j.h * p.G + row - sr * p.G;
+            // slots hold four dims of all rows, then the next four: a warp writes 512 bytes in a row
+            float *to = j.complete ? p.whole + ((int64_t)(mine ? sq : 0) * p.H * p.G + hq) * kAttRowPitch
+                                   : p.slots + ((int64_t)blockIdx.x * 2 + (j.begins ? 1 : 0)) * kPTile * kAttRowPitch + 4 * row;
+            const int quad = j.complete ? 4 : 4 * kPTile;
 #pragma unroll 1
             for (int c = 0; c < 4; ++c) {                  // this group's half of the dims, 16 at a time
                 uint32_t a[16], b[16];
@@ -458,10 +463,12 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                 if (mine) {
 #pragma unroll
                     for (int x = 0; x < 4; ++x)
-                        *reinterpret_cast<float4 *>(to + 64 * w + 16 * c + 4 * x) = make_float4(y[4 * x], y[4 * x + 1], y[4 * x + 2], y[4 * x + 3]);
+                        *reinterpret_cast<float4 *>(to + (16 * w + 4 * c + x) * quad) = make_float4(y[4 * x], y[4 * x + 1], y[4 * x + 2], y[4 * x + 3]);
                 }
             }
-            if (mine && w == 0) *reinterpret_cast<float2 *>(to + kHeadDim) = make_float2(mm, __uint_as_float(s0[1]) * f0 + __uint_as_float(s1[1]) * f1);
+            if (mine && w == 0)
+                *reinterpret_cast<float2 *>(j.complete ? to + kHeadDim : to - 4 * row + kPTile * kHeadDim + 2 * row) =
+                    make_float2(mm, __uint_as_float(s0[1]) * f0 + __uint_as_float(s1[1]) * f1);
             ++units;
         }
     }
