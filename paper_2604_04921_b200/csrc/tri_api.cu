@@ -1149,6 +1149,19 @@ tri_status check_layer_cache(const tri_ctx *c, const tri_layer_cache *lc, int32_
     return TRI_OK;
 }
 
+// A launch that may be set up, and where its kernel allows it started, while the kernel before it in the stream still runs.
+template <typename Kernel, typename Params>
+cudaError_t launch_under(Kernel kernel, unsigned blocks, unsigned threads, size_t smem, cudaStream_t st, const Params &p)
+{
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cfg.attrs = &attr; cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, p);
+}
+
 // Rows of `es`-byte elements that start on 16-byte boundaries.
 bool rows16_ok(const void *p, int64_t a, int64_t b, int64_t c, int es)
 {
@@ -1218,17 +1231,20 @@ extern "C" tri_status tri_append(tri_ctx *c, const tri_layer_cache *dst, int32_t
     p.ntiles = (int32_t)(((int64_t)rows->T + tt - 1) / tt);
     if ((int64_t)p.ntiles * S > 0x7fffffff) return TRI_ERR_UNSUPPORTED;
     int32_t *lens_out = new_lens ? new_lens + (dst->unit_lens ? (int64_t)dst->layer * S * H : 0) : nullptr;
-    p.new_lens = p.ntiles == 1 ? lens_out : nullptr;
+    // the lengths can be stored by the same launch unless blocks read what others store
+    const int64_t n_lens = (int64_t)S * (p.unit_lens ? H : 1);
+    const int32_t *lens_in = p.unit_lens ? p.unit_lens : dst->view->seq_lens;
+    const bool apart = !lens_out || (uintptr_t)(lens_out + n_lens) <= (uintptr_t)lens_in || (uintptr_t)(lens_in + n_lens) <= (uintptr_t)lens_out;
+    const bool later = !apart && p.ntiles > 1;
+    p.new_lens = later ? nullptr : lens_out;
     const unsigned blocks = (unsigned)(p.ntiles * S);
     cudaStream_t st = (cudaStream_t)stream;
     if (rows->kind == 0) launch_append<0>(dst->view->k_kind, c->desc.pair_layout == 1, blocks, tt, st, p);
     else launch_append<1>(dst->view->k_kind, c->desc.pair_layout == 1, blocks, tt, st, p);
     if ((r = check_launch("k_append")) != TRI_OK) return r;
-    if (lens_out && p.ntiles > 1) {
+    if (later) {
         p.new_lens = lens_out;
-        const int64_t n = (int64_t)S * (dst->unit_lens ? H : 1);
-        k_append_lens<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(p);
-        return check_launch("k_append_lens");
+        TRI_CUDA(launch_under(k_append_lens, (unsigned)((n_lens + 255) / 256), 256, 0, st, p));
     }
     return TRI_OK;
 }
@@ -1260,19 +1276,6 @@ AttendPlan make_attend_plan(const tri_ctx *c, int32_t S, int32_t P)
     a.pre_whole = o; o += P > 0 ? whole : 0;
     a.total = o;
     return a;
-}
-
-// A launch that may be set up, and where its kernel allows it started, while the kernel before it in the stream still runs.
-template <typename Kernel, typename Params>
-cudaError_t launch_under(Kernel kernel, unsigned blocks, unsigned threads, size_t smem, cudaStream_t st, const Params &p)
-{
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(blocks); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
-    cfg.attrs = &attr; cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
 // under: behind a pass over prefixes, with which it shares nothing but the joining kernel

@@ -29,7 +29,7 @@ struct AppendParams {
     const int32_t *n_new;
     const int64_t *pos;
     const double2 *turn;                         // [64] omega_f / 2 pi as hi + lo
-    int32_t *new_lens;                           // written here only when one block covers a whole sequence
+    int32_t *new_lens;                           // NULL where k_append_lens writes them
     int32_t *device_status;
 };
 
@@ -43,23 +43,34 @@ __device__ __forceinline__ int append_count(const AppendParams &p, int s)
     return p.n_new ? min(max(__ldg(p.n_new + s), 0), p.T) : p.T;
 }
 
-// The 16 components a lane owns of a row, as fp32.  SPLIT: components 8c..8c+7 and 64+8c..64+8c+7 (the two halves of 8
-// bands in the half-split layout), else 16c..16c+15.
+// The 16 components a lane owns of a row.  SPLIT: components 8c..8c+7 and 64+8c..64+8c+7 (the two halves of 8 bands in the
+// half-split layout), else 16c..16c+15.
+template <int KIND> struct Raw16 { uint4 v[KIND == 0 ? 2 : 4]; };
 template <int KIND, bool SPLIT>
-__device__ __forceinline__ void load16(const char *row, int c, float (&x)[16])
+__device__ __forceinline__ void load16(const char *row, int c, Raw16<KIND> &x)
 {
     const int first = SPLIT ? 8 * c : 16 * c, second = SPLIT ? 64 + 8 * c : 16 * c + 8;
-    if (KIND == 0) {
-        const uint4 a = *reinterpret_cast<const uint4 *>(row + 2 * first);
-        const uint4 b = *reinterpret_cast<const uint4 *>(row + 2 * second);
-        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) { x[2 * i] = bf16_lo(w[i]); x[2 * i + 1] = bf16_hi(w[i]); }
+    if constexpr (KIND == 0) {
+        x.v[0] = *reinterpret_cast<const uint4 *>(row + 2 * first);
+        x.v[1] = *reinterpret_cast<const uint4 *>(row + 2 * second);
     } else {
-        const float4 v[4] = {*reinterpret_cast<const float4 *>(row + 4 * first), *reinterpret_cast<const float4 *>(row + 4 * first + 16),
-                             *reinterpret_cast<const float4 *>(row + 4 * second), *reinterpret_cast<const float4 *>(row + 4 * second + 16)};
+        x.v[0] = *reinterpret_cast<const uint4 *>(row + 4 * first);
+        x.v[1] = *reinterpret_cast<const uint4 *>(row + 4 * first + 16);
+        x.v[2] = *reinterpret_cast<const uint4 *>(row + 4 * second);
+        x.v[3] = *reinterpret_cast<const uint4 *>(row + 4 * second + 16);
+    }
+}
+template <int KIND>
+__device__ __forceinline__ void widen16(const Raw16<KIND> &r, float (&x)[16])
+{
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { x[4 * i] = v[i].x; x[4 * i + 1] = v[i].y; x[4 * i + 2] = v[i].z; x[4 * i + 3] = v[i].w; }
+    for (int i = 0; i < (KIND == 0 ? 2 : 4); ++i) {
+        const uint32_t w[4] = {r.v[i].x, r.v[i].y, r.v[i].z, r.v[i].w};
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            if constexpr (KIND == 0) { x[8 * i + 2 * y] = bf16_lo(w[y]); x[8 * i + 2 * y + 1] = bf16_hi(w[y]); }
+            else x[4 * i + y] = __uint_as_float(w[y]);
+        }
     }
 }
 
@@ -117,6 +128,7 @@ __global__ void __launch_bounds__(kAppendThreads) k_append(const AppendParams p)
 
     const int tid = threadIdx.x, c = tid & 7;
     const int s = blockIdx.x / p.ntiles, t0 = (blockIdx.x - s * p.ntiles) * TT;
+    grid_dependents_launch();                                 // k_append_lens, where there is one, waits for this kernel itself
     const int n_new = append_count(p, s);
     const bool first = t0 == 0;
     if (first && tid == 0 && p.device_status && p.n_new) {
@@ -143,51 +155,70 @@ __global__ void __launch_bounds__(kAppendThreads) k_append(const AppendParams p)
         const bool pos_ok = at >= 0 && at <= 0x7fffffff;
         if (t < n_new && !pos_ok && p.device_status) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
         if (t < n_new && pos_ok) {
+            constexpr int in_es = KIND == 0 ? 2 : 4, U = KIND == 0 ? 4 : 2;      // rows in flight per lane
+            const int kv = p.v ? 2 * p.H : p.H;               // rows: H keys, H values, then the queries
+            const int rows = kv + (p.q ? p.H * p.G : 0);
+            // where head 0's row goes when all heads have the same length
+            int64_t slot0 = 0, off0 = -1;
+            if (!p.unit_lens) {
+                slot0 = (int64_t)append_len(p, s, 0) + t;
+                if (slot0 < p.dst.n_max) off0 = row_offset(p.dst, p.layer, s, 0, (int)slot0);
+            }
             float2 cs[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) cs[j] = cs_s[tt][8 * c + j];
-            constexpr int in_es = KIND == 0 ? 2 : 4;
-            const int kv = p.v ? 2 * p.H : p.H;               // rows: H keys, H values, then the queries
-            const int rows = kv + (p.q ? p.H * p.G : 0);
-#pragma unroll 2
-            for (int r = grp; r < rows; r += kGroups) {
-                float x[16];
-                if (r >= kv) {
-                    const int hq = r - kv;
-                    load16<KIND, SPLIT>(p.q + (s * p.qs_seq + t * p.qs_tok + hq * p.qs_head) * in_es, c, x);
-                    rotate16<SPLIT>(x, cs);
-                    store16<2, SPLIT>(p.q_out + (s * p.qo_seq + t * p.qo_tok + hq * p.qo_head) * 2, c, x);
-                    continue;
-                }
-                const bool is_k = r < p.H;
-                const int h = is_k ? r : r - p.H;
-                const int64_t slot = (int64_t)append_len(p, s, h) + t;
-                const int64_t off = slot < p.dst.n_max ? row_offset(p.dst, p.layer, s, h, (int)slot) : -1;
-                if (off < 0) {
-                    if (p.device_status) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
-                    continue;
-                }
-                const char *src = is_k ? p.k + (s * p.ks_seq + t * p.ks_tok + h * p.ks_head) * in_es
-                                       : p.v + (s * p.vs_seq + t * p.vs_tok + h * p.vs_head) * in_es;
-                load16<KIND, SPLIT>(src, c, x);
-                if (is_k && kRotateKeys) rotate16<SPLIT>(x, cs);
-                if (KK == 3) {
-                    const float *sc = is_k ? p.k_scale : p.v_scale;
-                    if (sc) {
-                        const float scale = __ldg(sc + h);
+            const char *q = p.q + (s * p.qs_seq + t * p.qs_tok) * in_es, *k = p.k + (s * p.ks_seq + t * p.ks_tok) * in_es,
+                       *v = p.v + (s * p.vs_seq + t * p.vs_tok) * in_es;
+            for (int r0 = grp; r0 < rows; r0 += U * kGroups) {
+                Raw16<KIND> raw[U];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) x[i] = __fdiv_rn(x[i], scale);
-                    }
+                for (int u = 0; u < U; ++u) {
+                    const int r = r0 + u * kGroups;
+                    if (r >= rows) break;
+                    const char *src = r < p.H ? k + r * p.ks_head * in_es : (r < kv ? v + (r - p.H) * p.vs_head * in_es : q + (r - kv) * p.qs_head * in_es);
+                    load16<KIND, SPLIT>(src, c, raw[u]);
                 }
-                if (is_k) store16<kES, SPLIT>(p.dst.k + off * kES, c, x);
-                else store16<vES, SPLIT>(p.dst.v + off * vES, c, x);
-                if (is_k && c == 0 && p.dst.positions)
-                    p.dst.positions[(((int64_t)p.layer * p.S + s) * p.H + h) * p.dst.n_max + slot] = (int32_t)at;
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int r = r0 + u * kGroups;
+                    if (r >= rows) break;
+                    float x[16];
+                    widen16<KIND>(raw[u], x);
+                    if (r >= kv) {
+                        rotate16<SPLIT>(x, cs);
+                        store16<2, SPLIT>(p.q_out + (s * p.qo_seq + t * p.qo_tok + (r - kv) * p.qo_head) * 2, c, x);
+                        continue;
+                    }
+                    const bool is_k = r < p.H;
+                    const int h = is_k ? r : r - p.H;
+                    int64_t slot = slot0, off = off0 == -1 ? -1 : off0 + h * p.dst.stride_head;
+                    if (p.unit_lens) {
+                        slot = (int64_t)append_len(p, s, h) + t;
+                        off = slot < p.dst.n_max ? row_offset(p.dst, p.layer, s, h, (int)slot) : -1;
+                    }
+                    if (off == -1) {                          // (offsets are multiples of 8 elements)
+                        if (p.device_status) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
+                        continue;
+                    }
+                    if (is_k && kRotateKeys) rotate16<SPLIT>(x, cs);
+                    if (KK == 3) {
+                        const float *sc = is_k ? p.k_scale : p.v_scale;
+                        if (sc) {
+                            const float scale = __ldg(sc + h);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) x[i] = __fdiv_rn(x[i], scale);
+                        }
+                    }
+                    if (is_k) store16<kES, SPLIT>(p.dst.k + off * kES, c, x);
+                    else store16<vES, SPLIT>(p.dst.v + off * vES, c, x);
+                    if (is_k && c == 0 && p.dst.positions)
+                        p.dst.positions[(((int64_t)p.layer * p.S + s) * p.H + h) * p.dst.n_max + slot] = (int32_t)at;
+                }
             }
         }
     }
-    // lengths: a block that covers its whole sequence is their only reader and stores them after its last read
-    if (p.new_lens) {
+    // lengths into another array, or by the block that covers its whole sequence, their only reader, after its last read
+    if (p.new_lens && first) {
         __syncthreads();
         const int n = p.unit_lens ? p.H : 1;
         for (int h = tid; h < n; h += kAppendThreads) {
@@ -197,9 +228,10 @@ __global__ void __launch_bounds__(kAppendThreads) k_append(const AppendParams p)
     }
 }
 
-// Lengths after an append whose blocks share sequences: a launch of its own, behind the one that reads them.
+// Lengths in place after an append whose blocks share sequences: a launch of its own, set up under the one that reads them.
 __global__ void __launch_bounds__(256) k_append_lens(const AppendParams p)
 {
+    grid_dependency_wait();
     const int n = p.unit_lens ? p.H : 1;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= (int64_t)p.S * n) return;

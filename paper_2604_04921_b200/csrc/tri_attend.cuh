@@ -72,9 +72,6 @@ __device__ __forceinline__ int att_row_tiles(const AttendParams &p, int seq)
 // index reaches P + S / spt + 1 whatever group_start holds.
 __device__ __forceinline__ int att_tile_index(int g, int first, int spt, int rt) { return g + first / spt + rt; }
 
-__device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
-__device__ __forceinline__ void grid_dependents_launch() { asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory"); }
-
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint32_t bytes)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
