@@ -72,9 +72,10 @@ __device__ __forceinline__ int att_row_tiles(const AttendParams &p, int seq)
 // index reaches P + S / spt + 1 whatever group_start holds.
 __device__ __forceinline__ int att_tile_index(int g, int first, int spt, int rt) { return g + first / spt + rt; }
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint32_t bytes)
+// 16 bytes (or zeros, bytes = 0) with an L2 policy.
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint32_t bytes, uint64_t policy)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;\n" ::"r"(dst), "l"(src), "r"(bytes), "l"(policy) : "memory");
 }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
 template <int N>
@@ -264,6 +265,11 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
     const uint32_t ring = smem_u32(dyn) + warp * (ST * kAttStageBytes);
+    // 16-byte chunk c of row r lies at chunk c ^ (r & 7) of its 128 bytes; as stages are multiples of 128 bytes, the chunk's
+    // number can be xor-ed into a lane's address.  Matrices of one load: keys as (8 keys, 2 chunks), values as (16 keys, 2 chunks)
+    const int krow = KEY8 ? (lane & 15) : (lane & 7) + ((lane & 16) >> 1), vrow = lane & 15;
+    const uint32_t klane = krow * kRowBytes + ((((KEY8 ? lane >> 4 : (lane >> 3) & 1) ^ krow) & 7) << 4);
+    const uint32_t vlane = vrow * kRowBytes + ((((lane >> 4) ^ vrow) & 7) << 4);
     grid_dependents_launch();                             // the joining kernel may be set up under this one
     const AttShare sh = att_share<TILE, kAttUnitCost>(p);
     if ((int)blockIdx.x >= sh.shares) return;
@@ -275,6 +281,10 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
     uint32_t bad = 0;                                     // bits 2 i, 2 i + 1: these 16 rows of stage i are absent
     bool more = true;
     int64_t unit_base = 0;                                // first row of the unit; of page 0, where rows are paged
+    // own rows are read once in a step: first to leave L2 (3 % faster on long batches); a prefix's tiles of query rows share them
+    uint64_t policy;
+    if (p.spt) asm("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;\n" : "=l"(policy));
+    else asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;\n" : "=l"(policy));
     const int64_t step_row = p.src.paged ? p.src.stride_slot : p.src.stride_tok;
     auto advance = [&]() {                                // to the next step, its pages looked up before they are needed
         if (pit == pj.kb) {
@@ -314,18 +324,29 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
                 } else {
                     base += (int64_t)r * step_row;
                 }
-                int64_t from = (base + r0 * step_row) * es;
+                int64_t from = (base + r0 * step_row) * es + 16 * c;
                 const uint32_t to = dst + (16 * half + r0) * kRowBytes;
+                constexpr int kRowsAtOnce = 32 / kChunks;
+                if (have == 16) {
 #pragma unroll
-                for (int i = 0; i < kCopies / NK; ++i) {
+                    for (int i = 0; i < kCopies / NK; ++i) {
+                        const uint32_t off = i * kRowsAtOnce * kRowBytes + (((c & 8) | ((c ^ (i * kRowsAtOnce + r0)) & 7)) << 4);
+                        cp_async16(to + off, p.src.k + from, 16u, policy);
+                        cp_async16(to + kHalf + off, p.src.v + from, 16u, policy);
+                        from += kRowsAtOnce * step_row * es;
+                    }
+                } else {
                     // rows behind the length (or absent ones) arrive as zeros and are not read
-                    const int rr = i * (32 / kChunks) + r0;
-                    const bool there = rr < have;
-                    const int64_t at = (there ? from : 0) + 16 * c;
-                    const uint32_t off = i * (32 / kChunks) * kRowBytes + (((c & 8) | ((c ^ rr) & 7)) << 4);
-                    cp_async16(to + off, p.src.k + at, there ? 16u : 0u);
-                    cp_async16(to + kHalf + off, p.src.v + at, there ? 16u : 0u);
-                    from += (32 / kChunks) * step_row * es;
+#pragma unroll 1
+                    for (int i = 0; i < kCopies / NK; ++i) {
+                        const int rr = i * kRowsAtOnce + r0;
+                        const bool there = rr < have;
+                        const int64_t at = there ? from : 16 * c;
+                        const uint32_t off = i * kRowsAtOnce * kRowBytes + (((c & 8) | ((c ^ rr) & 7)) << 4);
+                        cp_async16(to + off, p.src.k + at, there ? 16u : 0u, policy);
+                        cp_async16(to + kHalf + off, p.src.v + at, there ? 16u : 0u, policy);
+                        from += kRowsAtOnce * step_row * es;
+                    }
                 }
             }
             bad = (bad & ~(3u << (2 * pstage))) | (miss << (2 * pstage));
@@ -419,6 +440,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
         const uint32_t r0 = (uint32_t)it * TILE + warp * ROWS;
         const int have = r0 < (uint32_t)j.len ? min(j.len - (int)r0, ROWS) : 0;
         const uint32_t miss = (bad >> (2 * stage)) & 3u;
+        const bool cut = have < ROWS || miss;
         const uint32_t kb_s = ring + stage * kAttStageBytes, vb_s = kb_s + kHalf;
         // logits: 8 rows x 8 keys per accumulator (x 2: even and odd steps of 16 dims apart, shorter chains)
         float sc[2 * NK][4];
@@ -430,8 +452,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
 #pragma unroll
                 for (int kg = 0; kg < NK; ++kg) {
                     uint32_t f[4];
-                    const int row = 16 * kg + (lane & 7) + (lane & 8), ch = k + (lane >> 4);
-                    ldmatrix_x4(f, kb_s + row * 128 + (((ch ^ row) & 7) << 4));
+                    ldmatrix_x4(f, (kb_s + klane + 16 * kg * 128) ^ (k << 4));
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
                         uint32_t b0, b1;
@@ -447,8 +468,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 uint32_t f[4];
-                const int row = (lane & 7) + ((lane & 16) >> 1), ch = 2 * k + ((lane >> 3) & 1);
-                ldmatrix_x4(f, kb_s + row * 256 + (((ch & 8) | ((ch ^ row) & 7)) << 4));
+                ldmatrix_x4(f, (kb_s + klane + (k >> 2) * 128) ^ ((2 * k & 7) << 4));
                 mma16<false>(k & 1 ? sd[0] : sc[0], qa[k][0], qa[k][1], qa[k][2], qa[k][3], f[0], f[1]);
                 mma16<false>(k & 1 ? sd[1] : sc[1], qa[k][0], qa[k][1], qa[k][2], qa[k][3], f[2], f[3]);
             }
@@ -464,8 +484,11 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
             float mx = -INFINITY;
 #pragma unroll
             for (int x = 0; x < 4 * NK; ++x) {
-                const int key = 8 * (x >> 1) + 2 * t4 + (x & 1);
-                w[i][x] = key < have && !((miss >> (x >> 2)) & 1u) ? sc[x >> 1][2 * i + (x & 1)] * mul[i] : -INFINITY;
+                w[i][x] = sc[x >> 1][2 * i + (x & 1)] * mul[i];
+                if (cut) {
+                    const int key = 8 * (x >> 1) + 2 * t4 + (x & 1);
+                    if (key >= have || ((miss >> (x >> 2)) & 1u)) w[i][x] = -INFINITY;
+                }
                 mx = fmaxf(mx, w[i][x]);
             }
             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
@@ -504,13 +527,11 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
                     mma16<KEY8>(acc, pl[0][0], pl[NR - 1][0], pl[0][1], pl[NR - 1][1], b0, b1);
                 }
             };
-            const int row = 16 * kg + (lane & 7) + (lane & 8);
             if (KEY8) {
 #pragma unroll
                 for (int ch = 0; ch < 8; ch += 2) {
                     uint32_t f[4];
-                    const int cc = ch + (lane >> 4);
-                    ldmatrix_x4_t(f, vb_s + row * 128 + (((cc ^ row) & 7) << 4));
+                    ldmatrix_x4_t(f, (vb_s + vlane + 16 * kg * 128) ^ (ch << 4));
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
                         // bytes of a word: key 2 t4 dims (2 g8, 2 g8 + 1), key 2 t4 + 1 the same dims
@@ -525,8 +546,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
 #pragma unroll
                 for (int n = 0; n < 16; n += 2) {
                     uint32_t f[4];
-                    const int cc = n + (lane >> 4);
-                    ldmatrix_x4_t(f, vb_s + row * 256 + (((cc & 8) | ((cc ^ row) & 7)) << 4));
+                    ldmatrix_x4_t(f, (vb_s + vlane + (n >> 3) * 128) ^ ((n & 7) << 4));
                     pv(o[n], f[0], f[1]);
                     pv(o[n + 1], f[2], f[3]);
                 }
