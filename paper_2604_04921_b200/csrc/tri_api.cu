@@ -374,9 +374,9 @@ tri_status encode_fn(EncodeTiledFn *out)
     return TRI_OK;
 }
 
-// (rows: the keys of the view, or its values when given)
+// (rows: the keys of the view, or its values when given; boxes of 16 rows unless said otherwise)
 tri_status encode_key_map(const tri_ctx *c, const tri_cache_view *v, int32_t S, int32_t n_layers, CUtensorMap *out,
-                          void *rows = nullptr)
+                          void *rows = nullptr, int32_t box_rows = kTileKeys)
 {
     EncodeTiledFn fn;
     tri_status fs = encode_fn(&fn);
@@ -400,7 +400,7 @@ tri_status encode_key_map(const tri_ctx *c, const tri_cache_view *v, int32_t S, 
     }
     strides[1] = bytes(v->stride_head);
     strides[3] = bytes(v->stride_layer);
-    cuuint32_t box[5] = {(cuuint32_t)(key8 ? kHeadDim : kHeadDim / 2), kTileKeys, 1, 1, 1}, estr[5] = {1, 1, 1, 1, 1};
+    cuuint32_t box[5] = {(cuuint32_t)(key8 ? kHeadDim : kHeadDim / 2), (cuuint32_t)box_rows, 1, 1, 1}, estr[5] = {1, 1, 1, 1, 1};
     CUresult r = fn(out, key8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, rows ? rows : v->k, dims, strides, box, estr,
                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
@@ -1315,7 +1315,7 @@ AttendParams attend_params(const tri_ctx *c, const tri_layer_cache *lc, int32_t 
     const int32_t H = c->desc.n_kv_heads;
     AttendParams p;
     p.src = to_view(lc->view);
-    p.layer = lc->layer; p.nseq = n; p.H = H; p.G = c->desc.group_size; p.spt = 0; p.S = S;
+    p.layer = lc->layer; p.nseq = n; p.H = H; p.G = c->desc.group_size; p.spt = 0; p.S = S; p.box_rows = 0;
     p.unit_lens = lc->unit_lens ? lc->unit_lens + (int64_t)lc->layer * n * H : nullptr;
     p.k_scale = lc->k_scale ? lc->k_scale + (int64_t)lc->layer * H : nullptr;
     p.v_scale = lc->v_scale ? lc->v_scale + (int64_t)lc->layer * H : nullptr;
@@ -1359,8 +1359,12 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
         p.rec = (int2 *)(w + pl.pre_rec); p.slots = (float *)(w + pl.pre_slots); p.whole = (float *)(w + pl.pre_whole);
         if (umma) {
             CUtensorMap km, vm;
-            if ((r = encode_key_map(c, prefix->view, P, c->desc.n_layers, &km)) != TRI_OK) return r;
-            if ((r = encode_key_map(c, prefix->view, P, c->desc.n_layers, &vm, prefix->view->v)) != TRI_OK) return r;
+            const tri_cache_view *pv = prefix->view;
+            p.box_rows = kPTile;
+            if (pv->paged)
+                while (pv->page_size % p.box_rows) p.box_rows /= 2;      // pages are multiples of 16 rows
+            if ((r = encode_key_map(c, pv, P, c->desc.n_layers, &km, pv->k, p.box_rows)) != TRI_OK) return r;
+            if ((r = encode_key_map(c, pv, P, c->desc.n_layers, &vm, pv->v, p.box_rows)) != TRI_OK) return r;
             k_attend_prefix<<<(unsigned)c->n_sm, kPThreads, kPDynSmem, st>>>(km, vm, p);
             TRI_CUDA(cudaGetLastError());
         } else if (prefix->view->k_kind == 3) {

@@ -34,6 +34,7 @@ struct AttendParams {
     int32_t layer, nseq, H, G;                            // nseq: sequences (or prefixes) of src
     int32_t spt;                                          // prefixes: sequences per tile of query rows; own rows: 0
     int32_t S;                                            // sequences of the call
+    int32_t box_rows;                                     // k_attend_prefix: rows per copied box
     const int32_t *unit_lens;                             // [nseq][H] of this layer or NULL
     const float *k_scale, *v_scale;                       // [H] of this layer or NULL
     const int32_t *group_start;                           // [nseq + 1], prefixes only

@@ -2,10 +2,10 @@
 //
 // A prefix that n sequences share meets n * G query rows per KV head: up to 128 of them are one M = 128 tile, so every
 // cached row fetched from memory serves all of them.  Per tile of 128 cached rows:
-//   producer warp    bulk-tensor copies of the K and V rows (boxes of 16 rows x 64 dims, 128-byte swizzle) into rings of
-//                    three stages each; K is the K-major, V the N-major B operand as they lie
+//   producer warp    bulk-tensor copies of the K and V rows (boxes of 16..128 rows x 64 dims, 128-byte swizzle) into rings
+//                    of three stages each; K is the K-major, V the N-major B operand as they lie
 //   MMA warp         S = Q K^T (8 MMAs 128 x 128 x 16) into tensor memory, and one tile later O += P V with P taken from
-//                    tensor memory: the bf16 weights and, in a second sweep, the bf16 of what that rounding left over
+//                    tensor memory, bf16
 //   2 x 4 warps      softmax: each group of four takes every other tile with statistics and an accumulator O of its own
 //                    (two independent streams, so the groups never wait for each other); a thread owns one query row,
 //                    reads its 128 logits, raises its bound m only when a logit passes it by 2^8 (then O is rescaled in
@@ -104,13 +104,13 @@ __device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t (&r)[16])
         "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
-__device__ __forceinline__ void tc_ld2(uint32_t taddr, uint32_t (&r)[2])
+__device__ __forceinline__ void tc_ld4(uint32_t taddr, uint32_t (&r)[4])
 {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x2.b32 {%0,%1}, [%2];\n" : "=r"(r[0]), "=r"(r[1]) : "r"(taddr));
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];\n" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr));
 }
-__device__ __forceinline__ void tc_st2(uint32_t taddr, float a, float b)
+__device__ __forceinline__ void tc_st4f(uint32_t taddr, float a, float b, float c)
 {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1,%2};\n" ::"r"(taddr), "f"(a), "f"(b) : "memory");
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%3};\n" ::"r"(taddr), "f"(a), "f"(b), "f"(c) : "memory");
 }
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory"); }
 // Registers a tensor-memory load fills may be read only behind the wait: this keeps the compiler from moving a use before it.
@@ -164,26 +164,49 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
     }
+    AttCursor cur = {sh.seq, sh.h, 0, sh.start};
+    AttJob j;
+    int done = 0;                                          // tiles of all earlier units of this block
+    const int inv_g = 65536 / p.G + 1;
+    auto query_row = [&](const AttJob &u, int r) -> const char * {
+        const int sr = att_small_div(r, inv_g);
+        return p.q + ((int64_t)(u.first_seq + sr) * p.q_seq + (int64_t)(u.h * p.G + r - sr * p.G) * p.q_head) * 2;
+    };
+    // a unit's queries into L2, one 128-byte line per thread of the softmax warps: asked for behind 200 KB of copies in flight
+    // they would take microseconds
+    auto prefetch_queries = [&](const AttJob &u) {
+        if ((tid >> 1) < u.nrows) asm volatile("prefetch.global.L2 [%0];\n" ::"l"(query_row(u, tid >> 1) + (tid & 1) * 128));
+    };
+    // the next unit of the share that has rows here; `records`: of those passed over or found, where they begin here
+    auto next_rows = [&](bool records) -> bool {
+        while (att_next<kPTile, kPUnitCost>(p, sh, cur, j)) {
+            if (records && j.begins) p.rec[j.rec] = att_record(sh, j);
+            if (j.kb > j.ka) return true;
+        }
+        return false;
+    };
+    bool more = false;
+    if (warp < kPSoftWarps) {
+        more = next_rows(tid == 0);
+        if (more) prefetch_queries(j);
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_base_s;
     // columns: S/P of stream w at 128 w (weights: 64 columns, their rest: 64), O of stream w at 256 + 128 w
 
-    AttCursor cur = {sh.seq, sh.h, 0, sh.start};
-    AttJob j;
-    int done = 0;                                          // tiles of all earlier units of this block
-
     if (warp == kPSoftWarps) {
-        // ---------------- producer: lane = (matrix, box of 16 rows, half) is 2 x 16 x 1: K on lanes 0..15, V on 16..31 ----------
-        const int sub = (lane & 15) >> 1, half = lane & 1;
+        // ---------------- producer: K boxes on lanes 0..15 (box, half of the dims), V boxes on lanes 16..31 ----------------
+        // a box is `box` rows high: 128 where rows are contiguous, else the largest power of two up to 128 that divides a page
+        const int box = p.box_rows, sub = (lane & 15) >> 1, half = lane & 1, boxes = kPTile / box;
         const bool is_v = lane >= 16;
-        while (!gave_up && att_next<kPTile, kPUnitCost>(p, sh, cur, j)) {
-            const int n = max(j.kb - j.ka, 0);
+        while (!gave_up && next_rows(false)) {
+            const int n = j.kb - j.ka;
             auto locate = [&](int t, int &c1, int &c3) -> bool {          // false: the box's page id is out of range
-                const int64_t row = (int64_t)(j.ka + t) * kPTile + sub * kTileKeys;
+                const int64_t row = (int64_t)(j.ka + t) * kPTile + sub * box;
                 c1 = (int)row; c3 = j.seq;
-                if (!p.src.paged || t >= n || row >= j.len) return true;
+                if (!p.src.paged || t >= n || sub >= boxes || row >= j.len) return true;
                 const int pg = p.src.page_shift >= 0 ? (int)row >> p.src.page_shift : (int)row / p.src.page_size;
                 c3 = __ldg(p.src.page_table + (int64_t)j.seq * p.src.max_pages_per_seq + pg);
                 c1 = (int)row - pg * p.src.page_size;
@@ -194,13 +217,15 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
             for (int t = 0; t < n; ++t) {
                 const int i = done + t, st = i % kPStages;
                 const uint32_t par = ((i / kPStages) - 1) & 1;
-                const int64_t row0 = (int64_t)(j.ka + t) * kPTile;
-                const int nsub = (int)min((int64_t)(kPTile / kTileKeys), (j.len - row0 + kTileKeys - 1) / kTileKeys);
+                const int64_t left = j.len - (int64_t)(j.ka + t) * kPTile;
+                const int nsub = left >= kPTile ? boxes : (int)((left + box - 1) / box);
                 const uint32_t bad = __ballot_sync(0xffffffffu, !ok && sub < nsub && half == 0 && !is_v);
-                uint32_t mask = 0;
-                for (int x = 0; x < kPTile / kTileKeys; ++x) mask |= ((bad >> (2 * x)) & 1u) << x;
-                if (mask && lane == 0 && p.device_status) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
-                const uint32_t bytes = (uint32_t)(nsub - __popc(mask)) * kTileBytes;
+                uint32_t mask = 0;                         // of 16-row groups
+                if (bad) {
+                    for (int x = 0; x < kPTile / kTileKeys; ++x) mask |= ((bad >> (2 * (x * kTileKeys / box))) & 1u) << x;
+                    if (lane == 0 && p.device_status) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
+                }
+                const uint32_t bytes = (uint32_t)(nsub - __popc(bad)) * box * (kHeadDim * 2);
                 const bool mine = sub < nsub && ok;
                 // K first: its stage frees as soon as the logits of three tiles before are done
                 bool w = i < kPStages || mbar_wait_parked<20>(b_kempty + 8 * st, par);
@@ -208,14 +233,14 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                 if (lane == 0) mbar_expect_tx(b_kfull + 8 * st, bytes);
                 __syncwarp();
                 if (!is_v && mine)
-                    tma_load_5d(sm_k + st * kPTileBytes + half * kPBlock + sub * (kTileKeys * 128), &kmap, b_kfull + 8 * st,
+                    tma_load_5d(sm_k + st * kPTileBytes + half * kPBlock + sub * box * 128, &kmap, b_kfull + 8 * st,
                                 half * (kHeadDim / 2), c1, j.h, c3, p.layer);
                 w = i < kPStages || mbar_wait_parked<20>(b_vempty + 8 * st, par);
                 if (!__all_sync(0xffffffffu, w)) { gave_up = 1; break; }
                 if (lane == 0) { absent[st] = mask; mbar_expect_tx(b_vfull + 8 * st, bytes); }
                 __syncwarp();
                 if (is_v && mine)
-                    tma_load_5d(sm_v + st * kPTileBytes + half * kPBlock + sub * (kTileKeys * 128), &vmap, b_vfull + 8 * st,
+                    tma_load_5d(sm_v + st * kPTileBytes + half * kPBlock + sub * box * 128, &vmap, b_vfull + 8 * st,
                                 half * (kHeadDim / 2), c1, j.h, c3, p.layer);
                 ok = locate(t + 1, c1, c3);
             }
@@ -226,9 +251,8 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
         constexpr uint32_t idesc_qk = tc_idesc_bf16(kPTile);                     // both operands K-major
         constexpr uint32_t idesc_pv = tc_idesc_bf16(kHeadDim) | (1u << 16);      // B (the values) N-major
         int units = 0, cnt[2] = {0, 0};                    // tiles each stream had in earlier units (phases of pready)
-        while (!gave_up && att_next<kPTile, kPUnitCost>(p, sh, cur, j)) {
-            const int n = max(j.kb - j.ka, 0);
-            if (n == 0) continue;
+        while (!gave_up && next_rows(false)) {
+            const int n = j.kb - j.ka;
             bool ok = __all_sync(0xffffffffu, mbar_wait_bounded(b_q, units & 1));
             // logits of tile t: into the columns whose weights the MMAs issued before have used up.  As MMAs complete in order,
             // sfull says that the stream's accumulator rests, too; behind the stream's last tile it says nothing else
@@ -261,9 +285,8 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                     if (lane == 0) {
                         const uint32_t va = sm_v + st * kPTileBytes + x * (kPHalf * 128), acc = tmem + 256 + 128 * w, pw = tmem + 128 * w + kPHalf * x;
 #pragma unroll
-                        for (int k = 0; k < 8; ++k)        // 4 steps of 16 rows with the weights, 4 with their rest
-                            tc_mma_bf16_ts(acc, pw + 32 * ((k & 3) >> 1) + 8 * (k & 1) + 4 * (k & 4), tc_desc_sw128_n(va + (k & 3) * 2048), idesc_pv,
-                                           t >= 2 || x == 0 || k > 0);
+                        for (int k = 0; k < 4; ++k)
+                            tc_mma_bf16_ts(acc, pw + 8 * k, tc_desc_sw128_n(va + k * 2048), idesc_pv, t >= 2 || x == 0 || k > 0);
                         if (x == 0) tc_commit(b_vempty + 8 * st);
                         if (x == 0 && t + 2 >= n) tc_commit(b_sfull + 8 * w);
                     }
@@ -281,45 +304,43 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
         // ---------------- softmax: stream w takes tiles w, w + 2, ..; this thread owns query row `row` of its stream ----------
         const int w = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16, t_s = tmem + lane_base + 128 * w, t_o = tmem + lane_base + 256;
-        const uint32_t flip = p.scale < 0.f ? 0x80008000u : 0u;            // a negative scale goes into the queries' signs
         const bool check_pages = p.src.paged && p.src.n_pages > 0;
-        const int inv_g = 65536 / p.G + 1;
         int units = 0, phase[2] = {0, 0};                  // phases of sfull: one per tile, one more behind a unit's last
-        while (!gave_up && att_next<kPTile, kPUnitCost>(p, sh, cur, j)) {
-            if (j.begins && tid == 0) p.rec[j.rec] = att_record(sh, j);
-            const int n = max(j.kb - j.ka, 0);
-            if (n == 0) continue;
+        const uint32_t flip = p.scale < 0.f ? 0x80008000u : 0u;            // a negative scale goes into the queries' signs
+        while (!gave_up && more) {
+            const AttJob u = j;                            // (j runs ahead to the unit behind it)
+            const int n = u.kb - u.ka;
             uint4 q[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int r = (tid >> 4) + 16 * i, c = tid & 15;
-                q[i] = make_uint4(0u, 0u, 0u, 0u);
-                if (r < j.nrows) {
-                    const int sr = att_small_div(r, inv_g), sq = j.first_seq + sr, g = r - sr * p.G;
-                    q[i] = *reinterpret_cast<const uint4 *>(p.q + ((int64_t)sq * p.q_seq + (int64_t)(j.h * p.G + g) * p.q_head) * 2 + 16 * c);
-                    q[i].x ^= flip; q[i].y ^= flip; q[i].z ^= flip; q[i].w ^= flip;
-                }
+            for (int i = 0; i < 8; ++i) {                  // 16 bytes of 8 rows per thread
+                const int r = (tid >> 4) + 16 * i;
+                q[i] = r < u.nrows ? *reinterpret_cast<const uint4 *>(query_row(u, r) + 16 * (tid & 15)) : make_uint4(0u, 0u, 0u, 0u);
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int r = (tid >> 4) + 16 * i, c = tid & 15;
-                *reinterpret_cast<uint4 *>(gq + (c >> 3) * kPBlock + sw128(r, c & 7)) = q[i];
+                *reinterpret_cast<uint4 *>(gq + (c >> 3) * kPBlock + sw128(r, c & 7)) =
+                    make_uint4(q[i].x ^ flip, q[i].y ^ flip, q[i].z ^ flip, q[i].w ^ flip);
             }
             asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
             tc_fence_before();                             // the last unit's accumulators have been read
             __syncwarp();
             if (lane == 0) mbar_arrive(b_q);
+            more = next_rows(tid == 0);
+            if (more) prefetch_queries(j);
 
             // base-2 logit = accumulator * mul (not 0: a masked logit is -infinity)
-            const float mul = fmaxf(fabsf(p.scale) * (p.k_scale ? __ldg(p.k_scale + j.h) : 1.f), 1.17549435e-38f);
+            const float mul = fmaxf(fabsf(p.scale) * (p.k_scale ? __ldg(p.k_scale + u.h) : 1.f), 1.17549435e-38f);
             const float2 mul2 = make_float2(mul, mul);
             float m = -INFINITY;
-            float2 l = make_float2(0.f, 0.f);              // sums of the even and of the odd rows
+            // sums of the weights (even and odd rows) as they are, for the row's statistics, and as they enter the MMAs: o is
+            // divided by the latter, so that the roundings all but cancel
+            float2 l = make_float2(0.f, 0.f), lr = make_float2(0.f, 0.f);
             bool ok = true;
 #pragma unroll 1
             for (int t = w; t < n; t += 2) {
                 const int i = done + t, st = i % kPStages;
-                const int64_t left = j.len - (int64_t)(j.ka + t) * kPTile;
+                const int64_t left = u.len - (int64_t)(u.ka + t) * kPTile;
                 const bool cut = left < kPTile;
                 ok = mbar_wait_bounded(b_sfull + 8 * w, (phase[w] + (t >> 1)) & 1);
                 if (cut || check_pages) ok = ok && mbar_wait_bounded(b_vfull + 8 * st, (i / kPStages) & 1);
@@ -366,7 +387,7 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                 if (__any_sync(0xffffffffu, raise)) {
                     const float by = raise ? ex2(m - top) : 1.f;
                     if (raise) m = top;
-                    l.x *= by; l.y *= by;
+                    l.x *= by; l.y *= by; lr.x *= by; lr.y *= by;
                     if (t >= 2) {                          // an accumulator exists, and rests
 #pragma unroll 1
                         for (int c = 0; c < 8; ++c) {
@@ -381,25 +402,23 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                     }
                 }
                 const float ref = m == -INFINITY ? 0.f : m;
-                const float2 ref2 = make_float2(-ref, -ref), minus = make_float2(-1.f, -1.f);
+                const float2 ref2 = make_float2(-ref, -ref);
 #pragma unroll 1
                 for (int x = 1; x >= 0; --x) {
-                    // weights over the logits: for each 32 rows 16 columns of bf16 pairs, then 16 of what their rounding left over
+                    // weights over the logits of this half, 32 columns of bf16 pairs
 #pragma unroll
                     for (int c = 0; c < kPHalf / 32; ++c) {
-                        uint32_t hi[16], lo[16];
+                        uint32_t hi[16];
 #pragma unroll
                         for (int y = 0; y < 16; ++y) {
                             float2 e = fma2(make_float2(__uint_as_float(s[32 * c + 2 * y]), __uint_as_float(s[32 * c + 2 * y + 1])), mul2, ref2);
                             e.x = ex2(e.x);
                             e.y = ex2(e.y);
-                            l = add2(l, e);
                             hi[y] = cvt_bf16x2(e.y, e.x);
-                            const float2 rest = fma2(make_float2(bf16_lo(hi[y]), bf16_hi(hi[y])), minus, e);
-                            lo[y] = cvt_bf16x2(rest.y, rest.x);
+                            l = add2(l, e);
+                            lr = add2(lr, make_float2(bf16_lo(hi[y]), bf16_hi(hi[y])));
                         }
-                        tc_st16(t_s + kPHalf * x + 32 * c, hi);
-                        tc_st16(t_s + kPHalf * x + 32 * c + 16, lo);
+                        tc_st16(t_s + kPHalf * x + 16 * c, hi);
                     }
                     if (x == 1) {
                         tc_ld64(t_s, s);
@@ -422,11 +441,11 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                 const int y = z == 0 ? w : 1 - w;
                 if (y == 0 || n >= 2) ok = mbar_wait_bounded(b_sfull + 8 * y, (phase[y] - 1) & 1);
             }
-            // (the columns of S and P are idle until the next unit's queries are announced: m and l pass through them)
+            // (the columns of S and P are idle until the next unit's queries are announced: m, l and l / lr pass through them)
             ok = __all_sync(0xffffffffu, ok);
             if (ok) {
                 tc_fence_after();
-                tc_st2(t_s, m, l.x + l.y);
+                tc_st4f(t_s, m, l.x + l.y, lr.x + lr.y > 0.f ? (l.x + l.y) / (lr.x + lr.y) : 1.f);
                 tc_wait_st();
                 tc_fence_before();
             }
@@ -435,20 +454,21 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
             ok = __all_sync(0xffffffffu, ok && mbar_wait_bounded(b_ml, units & 1));
             if (!ok) { gave_up = 1; break; }
             tc_fence_after();
-            uint32_t s0[2], s1[2];
-            tc_ld2(tmem + lane_base, s0);
-            tc_ld2(tmem + lane_base + 128, s1);
+            uint32_t s0[4], s1[4];
+            tc_ld4(tmem + lane_base, s0);
+            tc_ld4(tmem + lane_base + 128, s1);
             tc_wait_ld();
             tc_loaded(s0);
             tc_loaded(s1);
             const float m0 = __uint_as_float(s0[0]), m1 = __uint_as_float(s1[0]), mm = fmaxf(m0, m1);
-            const float f0 = m0 == -INFINITY ? 0.f : ex2(m0 - mm), f1 = m1 == -INFINITY ? 0.f : ex2(m1 - mm);
-            const bool mine = row < j.nrows;
-            const int sr = att_small_div(row, inv_g), sq = j.first_seq + sr, hq = j.h * p.G + row - sr * p.G;
+            const float e0 = m0 == -INFINITY ? 0.f : ex2(m0 - mm), e1 = m1 == -INFINITY ? 0.f : ex2(m1 - mm);
+            const float f0 = e0 * __uint_as_float(s0[2]), f1 = e1 * __uint_as_float(s1[2]);
+            const bool mine = row < u.nrows;
+            const int sr = att_small_div(row, inv_g), sq = u.first_seq + sr, hq = u.h * p.G + row - sr * p.G;
             // slots hold four dims of all rows, then the next four: a warp writes 512 bytes in a row
-            float *to = j.complete ? p.whole + ((int64_t)(mine ? sq : 0) * p.H * p.G + hq) * kAttRowPitch
-                                   : p.slots + ((int64_t)blockIdx.x * 2 + (j.begins ? 1 : 0)) * kPTile * kAttRowPitch + 4 * row;
-            const int quad = j.complete ? 4 : 4 * kPTile;
+            float *to = u.complete ? p.whole + ((int64_t)(mine ? sq : 0) * p.H * p.G + hq) * kAttRowPitch
+                                   : p.slots + ((int64_t)blockIdx.x * 2 + (u.begins ? 1 : 0)) * kPTile * kAttRowPitch + 4 * row;
+            const int quad = u.complete ? 4 : 4 * kPTile;
 #pragma unroll 1
             for (int c = 0; c < 4; ++c) {                  // this group's half of the dims, 16 at a time
                 uint32_t a[16], b[16];
@@ -467,8 +487,8 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                 }
             }
             if (mine && w == 0)
-                *reinterpret_cast<float2 *>(j.complete ? to + kHeadDim : to - 4 * row + kPTile * kHeadDim + 2 * row) =
-                    make_float2(mm, __uint_as_float(s0[1]) * f0 + __uint_as_float(s1[1]) * f1);
+                *reinterpret_cast<float2 *>(u.complete ? to + kHeadDim : to - 4 * row + kPTile * kHeadDim + 2 * row) =
+                    make_float2(mm, __uint_as_float(s0[1]) * e0 + __uint_as_float(s1[1]) * e1);
             ++units;
         }
     }
