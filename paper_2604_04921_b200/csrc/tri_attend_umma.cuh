@@ -2,7 +2,7 @@
 //
 // A prefix that n sequences share meets n * G query rows per KV head: up to 128 of them are one M = 128 tile, so every
 // cached row fetched from memory serves all of them.  Per tile of 128 cached rows:
-//   producer warp    bulk-tensor copies of the K and V rows (boxes of 16..128 rows x 64 dims, 128-byte swizzle) into rings
+//   producer warps   bulk-tensor copies of the K and V rows (boxes of 16..128 rows x 64 dims, 128-byte swizzle) into rings
 //                    of three stages each; K is the K-major, V the N-major B operand as they lie
 //   MMA warp         S = Q K^T (8 MMAs 128 x 128 x 16) into tensor memory, and one tile later O += P V with P taken from
 //                    tensor memory, bf16
@@ -33,7 +33,7 @@ static_assert(kPTile == kMergeTile, "slots are laid out for the joining kernel")
 constexpr int kPBlock = kPTile * 128;                     // 128 rows x 64 bf16, one swizzled block
 constexpr int kPTileBytes = 2 * kPBlock;                  // dims 0..63 | dims 64..127
 constexpr int kPSoftWarps = 8;
-constexpr int kPThreads = (kPSoftWarps + 2) * 32;
+constexpr int kPThreads = (kPSoftWarps + 3) * 32;           // + K producer, V producer, MMA warp
 constexpr int kPDynSmem = (1 + 2 * kPStages) * kPTileBytes + 1024;      // Q, K ring, V ring
 
 // V as the B operand: N (dims) contiguous, 64-element chunks one block apart, groups of 8 cached rows 1024 bytes apart.
@@ -159,7 +159,7 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
         gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
-    if (warp == kPSoftWarps + 1) {                         // the MMA warp owns the tensor-memory allocation
+    if (warp == kPSoftWarps + 2) {                         // the MMA warp owns the tensor-memory allocation
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&tmem_base_s)), "r"(512)
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
@@ -196,11 +196,14 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
     const uint32_t tmem = tmem_base_s;
     // columns: S/P of stream w at 128 w (weights: 64 columns, their rest: 64), O of stream w at 256 + 128 w
 
-    if (warp == kPSoftWarps) {
-        // ---------------- producer: K boxes on lanes 0..15 (box, half of the dims), V boxes on lanes 16..31 ----------------
+    if (warp == kPSoftWarps || warp == kPSoftWarps + 1) {
+        // ---------------- producers: one warp for K, one for V, lane = (box, half of the dims) ----------------
+        // (one warp for both: its copies, 32 for 16-row boxes, are issued one by one and held a paged prefix back)
         // a box is `box` rows high: 128 where rows are contiguous, else the largest power of two up to 128 that divides a page
-        const int box = p.box_rows, sub = (lane & 15) >> 1, half = lane & 1, boxes = kPTile / box;
-        const bool is_v = lane >= 16;
+        const bool is_v = warp != kPSoftWarps;
+        const CUtensorMap *map = is_v ? &vmap : &kmap;
+        const uint32_t b_full = is_v ? b_vfull : b_kfull, b_empty = is_v ? b_vempty : b_kempty, ring = is_v ? sm_v : sm_k;
+        const int box = p.box_rows, sub = lane >> 1, half = lane & 1, boxes = kPTile / box;
         while (!gave_up && next_rows(false)) {
             const int n = j.kb - j.ka;
             auto locate = [&](int t, int &c1, int &c3) -> bool {          // false: the box's page id is out of range
@@ -219,34 +222,28 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                 const uint32_t par = ((i / kPStages) - 1) & 1;
                 const int64_t left = j.len - (int64_t)(j.ka + t) * kPTile;
                 const int nsub = left >= kPTile ? boxes : (int)((left + box - 1) / box);
-                const uint32_t bad = __ballot_sync(0xffffffffu, !ok && sub < nsub && half == 0 && !is_v);
+                const uint32_t bad = __ballot_sync(0xffffffffu, !ok && sub < nsub && half == 0);
                 uint32_t mask = 0;                         // of 16-row groups
                 if (bad) {
                     for (int x = 0; x < kPTile / kTileKeys; ++x) mask |= ((bad >> (2 * (x * kTileKeys / box))) & 1u) << x;
-                    if (lane == 0 && p.device_status) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
+                    if (lane == 0 && !is_v && p.device_status) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
                 }
                 const uint32_t bytes = (uint32_t)(nsub - __popc(bad)) * box * (kHeadDim * 2);
-                const bool mine = sub < nsub && ok;
-                // K first: its stage frees as soon as the logits of three tiles before are done
-                bool w = i < kPStages || mbar_wait_parked<20>(b_kempty + 8 * st, par);
+                const bool w = i < kPStages || mbar_wait_parked<20>(b_empty + 8 * st, par);
                 if (!__all_sync(0xffffffffu, w)) { gave_up = 1; break; }
-                if (lane == 0) mbar_expect_tx(b_kfull + 8 * st, bytes);
+                if (lane == 0) {
+                    if (is_v) absent[st] = mask;
+                    mbar_expect_tx(b_full + 8 * st, bytes);
+                }
                 __syncwarp();
-                if (!is_v && mine)
-                    tma_load_5d(sm_k + st * kPTileBytes + half * kPBlock + sub * box * 128, &kmap, b_kfull + 8 * st,
-                                half * (kHeadDim / 2), c1, j.h, c3, p.layer);
-                w = i < kPStages || mbar_wait_parked<20>(b_vempty + 8 * st, par);
-                if (!__all_sync(0xffffffffu, w)) { gave_up = 1; break; }
-                if (lane == 0) { absent[st] = mask; mbar_expect_tx(b_vfull + 8 * st, bytes); }
-                __syncwarp();
-                if (is_v && mine)
-                    tma_load_5d(sm_v + st * kPTileBytes + half * kPBlock + sub * box * 128, &vmap, b_vfull + 8 * st,
-                                half * (kHeadDim / 2), c1, j.h, c3, p.layer);
+                if (sub < nsub && ok)
+                    tma_load_5d(ring + st * kPTileBytes + half * kPBlock + sub * box * 128, map, b_full + 8 * st, half * (kHeadDim / 2), c1, j.h,
+                                c3, p.layer);
                 ok = locate(t + 1, c1, c3);
             }
             done += n;
         }
-    } else if (warp == kPSoftWarps + 1) {
+    } else if (warp == kPSoftWarps + 2) {
         // ---------------- MMA issue ----------------
         constexpr uint32_t idesc_qk = tc_idesc_bf16(kPTile);                     // both operands K-major
         constexpr uint32_t idesc_pv = tc_idesc_bf16(kHeadDim) | (1u << 16);      // B (the values) N-major
@@ -498,13 +495,11 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
     if (gave_up) {
         // a wait ran out: report it, and give copies still in flight one more bounded chance to land before the block exits
         if (tid == 0 && p.device_status) atomicExch(p.device_status, (int)TRI_ERR_TIMEOUT);
-        if (warp == kPSoftWarps)
-            for (int i = 0; i < 2 * kPStages; ++i) {
-                (void)mbar_wait_parked(b_kfull + 8 * (i % kPStages), (i / kPStages) & 1);
-                (void)mbar_wait_parked(b_vfull + 8 * (i % kPStages), (i / kPStages) & 1);
-            }
+        if (warp == kPSoftWarps || warp == kPSoftWarps + 1)
+            for (int i = 0; i < 2 * kPStages; ++i)
+                (void)mbar_wait_parked((warp == kPSoftWarps ? b_kfull : b_vfull) + 8 * (i % kPStages), (i / kPStages) & 1);
     }
-    if (warp == kPSoftWarps + 1) {
+    if (warp == kPSoftWarps + 2) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(512) : "memory");
     }
