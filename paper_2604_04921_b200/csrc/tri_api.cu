@@ -1298,11 +1298,13 @@ tri_status check_attend_cache(const tri_ctx *c, const tri_layer_cache *lc, int32
     return lc->view->v ? TRI_OK : TRI_ERR_INVALID_ARG;
 }
 
-// Whether the rows of a prefix can be addressed by the TMA unit: bf16, every stride that is used positive (a broadcast
-// head has stride 0) and below the unit's 2^40 bytes.
-bool prefix_umma_ok(const tri_ctx *c, const tri_cache_view *v, int32_t P)
+// Whether the 128-row tcgen05 pass takes the prefixes: more query rows per prefix on average than the one 16-row tile of
+// the mma.sync pass, which reads the rows once per tile (one 32K prefix, G = 4: 37 against 43 us at 4 or 8 rows, 39 against
+// 43 at 16, 49 against 44 at 32, 77 against 46 at 64), and rows the TMA unit can address: bf16, every stride that is used
+// positive (a broadcast head has stride 0) and below the unit's 2^40 bytes.
+bool prefix_umma_ok(const tri_ctx *c, const tri_cache_view *v, int32_t S, int32_t P)
 {
-    if (v->k_kind != 0) return false;
+    if (v->k_kind != 0 || (int64_t)S * c->desc.group_size <= (int64_t)16 * P) return false;
     auto ok = [](int64_t n, int64_t stride) { return n <= 1 || (stride > 0 && stride < ((int64_t)1 << 38)); };
     if (!ok(c->desc.n_kv_heads, v->stride_head) || !ok(c->desc.n_layers, v->stride_layer)) return false;
     return v->paged ? ok(2, v->stride_page) && ok(2, v->stride_slot) : ok(P, v->stride_seq) && ok(2, v->stride_tok);
@@ -1353,7 +1355,7 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
     mp.pre.rec = nullptr; mp.pre.slots = mp.pre.whole = nullptr; mp.pre.rows = 0; mp.pre.spt = 0;
     if (P > 0) {
         AttendParams p = attend_params(c, prefix, P, S, io, device_status);
-        const bool umma = prefix_umma_ok(c, prefix->view, P);
+        const bool umma = prefix_umma_ok(c, prefix->view, S, P);
         const int rows = umma ? kPTile : 16;
         p.spt = rows / G; p.group_start = group_start; p.finish = 0;
         p.rec = (int2 *)(w + pl.pre_rec); p.slots = (float *)(w + pl.pre_slots); p.whole = (float *)(w + pl.pre_whole);
@@ -1384,7 +1386,8 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
     mp.own.rec = p.rec; mp.own.slots = p.slots; mp.own.whole = p.whole; mp.own.rows = pl.own_rows; mp.own.spt = 0;
     mp.S = S; mp.P = P; mp.H = H; mp.G = G; mp.group_start = group_start;
     mp.out = p.out; mp.out_seq = p.out_seq; mp.out_head = p.out_head; mp.lse = io->lse; mp.device_status = device_status;
-    TRI_CUDA(launch_under(k_attend_merge, (unsigned)(S * H), kMergeThreads, 0, st, mp));
+    mp.rows = (int64_t)S * H < c->n_sm ? 1 : G;
+    TRI_CUDA(launch_under(k_attend_merge, (unsigned)((int64_t)S * H * (G / mp.rows)), kMergeThreads, 0, st, mp));
     return TRI_OK;
 }
 

@@ -644,6 +644,7 @@ struct AttendPass {                // where a pass left its parts
 struct MergeParams {
     AttendPass own, pre;           // pre.rec == NULL: no prefixes
     int32_t S, P, H, G;
+    int32_t rows;                  // query rows per block: G or 1
     const int32_t *group_start;
     char *out;
     int64_t out_seq, out_head;
@@ -653,16 +654,20 @@ struct MergeParams {
 
 constexpr int kMergeTile = 128;     // query rows per slot of k_attend_prefix, see AttendPass::rows
 
-// A block joins the G rows of one (sequence, KV head): 16 / G warps per row take its parts in turn, each lane four sums.
+// A block joins `rows` query rows of one (sequence, KV head): all G, or one where there are too few units to fill the GPU.
+// 16 / rows warps per row take its parts four at a time, each lane four sums, and are joined through shared memory.  Bound
+// by the latency of a chain of three L2 reads (record; parts; nothing more for up to 4 parts per warp).
 // The kernel is launched while the pass before it still runs (programmatic dependent launch) and waits for it here.
 constexpr int kMergeWarps = 16, kMergeThreads = 32 * kMergeWarps;
 
 __global__ void __launch_bounds__(kMergeThreads) k_attend_merge(const MergeParams p)
 {
     __shared__ float4 red[kMergeWarps][32];
-    const int s = blockIdx.x / p.H, h = blockIdx.x - s * p.H, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    __shared__ float2 red_ml[kMergeWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int per = p.G / p.rows, unit = blockIdx.x / per, s = unit / p.H, h = unit - s * p.H;
     grid_dependency_wait();
-    const int2 own = p.own.rec[blockIdx.x];
+    const int2 own = p.own.rec[unit];
     if (!p.pre.rec && own.y < 2) return;                                     // finished by its block
     int2 pre = make_int2(0, 0);
     int row0 = 0;
@@ -683,8 +688,8 @@ __global__ void __launch_bounds__(kMergeThreads) k_attend_merge(const MergeParam
                 if (__ldg(p.group_start + i) > __ldg(p.group_start + i + 1)) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
     }
     const int parts = own.y + pre.y;
-    const int wpr = kMergeWarps / p.G, g = warp / wpr, sub = warp - g * wpr;
-    const bool active = g < p.G;
+    const int wpr = kMergeWarps / p.rows, r = warp / wpr, sub = warp - r * wpr, g = ((int)blockIdx.x - unit * per) * p.rows + r;
+    const bool active = r < p.rows;
     const int64_t hq = (int64_t)h * p.G + g;
     // part i: the own rows' parts in ascending order, then the prefix's; its row, and where its (m, l) lie
     const bool tiled = p.pre.rows == kMergeTile && pre.y > 1;
@@ -709,40 +714,38 @@ __global__ void __launch_bounds__(kMergeThreads) k_attend_merge(const MergeParam
     };
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
     float mm = -INFINITY, ll = 0.f;
+    auto add = [&](float2 ml, float4 x) {                                    // one more summary
+        const float top = fmaxf(mm, ml.x);
+        const float old = mm == -INFINITY ? 0.f : ex2(mm - top), by = ml.x == -INFINITY ? 0.f : ex2(ml.x - top);
+        mm = top;
+        ll = ll * old + ml.y * by;
+        a.x = a.x * old + x.x * by; a.y = a.y * old + x.y * by; a.z = a.z * old + x.z * by; a.w = a.w * old + x.w * by;
+    };
     if (active) {
-        for (int b = 0; b < parts; b += 32) {
-            // summaries of up to 32 parts, one per lane, then their sums; a larger bound met on the way rescales what is there
-            const float2 *mlp = nullptr;
-            const float *mine = b + lane < parts ? at(b + lane, mlp) : nullptr;
-            const float2 ml = mine ? *mlp : make_float2(-INFINITY, 0.f);
-            float top = fmaxf(mm, ml.x);
+        for (int b = sub; b < parts; b += 4 * wpr) {
+            float2 ml[4];
+            float4 x[4];
 #pragma unroll
-            for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-            const float old = mm == -INFINITY ? 0.f : ex2(mm - top);
-            mm = top;
-            const float by = ml.x == -INFINITY ? 0.f : ex2(ml.x - mm);
-            float l = ml.y * by;
-#pragma unroll
-            for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
-            ll = ll * old + l;
-            a.x *= old; a.y *= old; a.z *= old; a.w *= old;
-            const int n = min(32, parts - b);
-#pragma unroll 4
-            for (int j = sub; j < n; j += wpr) {
-                const float *src = reinterpret_cast<const float *>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), j));
-                const float w = __shfl_sync(0xffffffffu, by, j);
-                const float4 x = *reinterpret_cast<const float4 *>(src + lane * (tiled && b + j >= own.y ? 4 * kMergeTile : 4));
-                a.x += x.x * w; a.y += x.y * w; a.z += x.z * w; a.w += x.w * w;
+            for (int k = 0; k < 4; ++k) {
+                const int i = b + k * wpr;
+                ml[k] = make_float2(-INFINITY, 0.f);
+                x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (i < parts) {
+                    const float2 *mlp;
+                    const float *src = at(i, mlp);
+                    ml[k] = *mlp;
+                    x[k] = *reinterpret_cast<const float4 *>(src + lane * (tiled && i >= own.y ? 4 * kMergeTile : 4));
+                }
             }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) add(ml[k], x[k]);
         }
         red[warp][lane] = a;
+        if (lane == 0) red_ml[warp] = make_float2(mm, ll);
     }
     __syncthreads();
     if (!active || sub != 0) return;
-    for (int w = 1; w < wpr; ++w) {
-        const float4 x = red[warp + w][lane];
-        a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
-    }
+    for (int w = 1; w < wpr; ++w) add(red_ml[warp + w], red[warp + w][lane]);
     const float inv = ll == 0.f ? 0.f : 1.f / ll;
     *reinterpret_cast<uint2 *>(p.out + ((int64_t)s * p.out_seq + hq * p.out_head) * 2 + 8 * lane) =
         make_uint2(cvt_bf16x2(a.y * inv, a.x * inv), cvt_bf16x2(a.w * inv, a.z * inv));
