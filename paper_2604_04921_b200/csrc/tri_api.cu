@@ -448,7 +448,8 @@ cudaError_t prepare_device()
     if ((e = allow_attend_smem<false, 16>()) != cudaSuccess) return e;
     if ((e = allow_attend_smem<true, 8>()) != cudaSuccess) return e;
     if ((e = allow_attend_smem<true, 16>()) != cudaSuccess) return e;
-    return cudaFuncSetAttribute(k_attend_prefix, cudaFuncAttributeMaxDynamicSharedMemorySize, kPDynSmem);
+    if ((e = cudaFuncSetAttribute(k_attend_prefix<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPDynSmem)) != cudaSuccess) return e;
+    return cudaFuncSetAttribute(k_attend_prefix<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPDynSmem);
 }
 
 // Every entry point that launches kernels runs on the device the context was created on.
@@ -1300,11 +1301,11 @@ tri_status check_attend_cache(const tri_ctx *c, const tri_layer_cache *lc, int32
 
 // Whether the 128-row tcgen05 pass takes the prefixes: more query rows per prefix on average than the one 16-row tile of
 // the mma.sync pass, which reads the rows once per tile (one 32K prefix, G = 4: 37 against 43 us at 4 or 8 rows, 39 against
-// 43 at 16, 49 against 44 at 32, 77 against 46 at 64), and rows the TMA unit can address: bf16, every stride that is used
-// positive (a broadcast head has stride 0) and below the unit's 2^40 bytes.
+// 43 at 16, 49 against 44 at 32, 77 against 46 at 64), and rows the TMA unit can address: every stride that is used positive
+// (a broadcast head has stride 0) and below the unit's 2^40 bytes.
 bool prefix_umma_ok(const tri_ctx *c, const tri_cache_view *v, int32_t S, int32_t P)
 {
-    if (v->k_kind != 0 || (int64_t)S * c->desc.group_size <= (int64_t)16 * P) return false;
+    if ((int64_t)S * c->desc.group_size <= (int64_t)16 * P) return false;
     auto ok = [](int64_t n, int64_t stride) { return n <= 1 || (stride > 0 && stride < ((int64_t)1 << 38)); };
     if (!ok(c->desc.n_kv_heads, v->stride_head) || !ok(c->desc.n_layers, v->stride_layer)) return false;
     return v->paged ? ok(2, v->stride_page) && ok(2, v->stride_slot) : ok(P, v->stride_seq) && ok(2, v->stride_tok);
@@ -1367,7 +1368,8 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
                 while (pv->page_size % p.box_rows) p.box_rows /= 2;      // pages are multiples of 16 rows
             if ((r = encode_key_map(c, pv, P, c->desc.n_layers, &km, pv->k, p.box_rows)) != TRI_OK) return r;
             if ((r = encode_key_map(c, pv, P, c->desc.n_layers, &vm, pv->v, p.box_rows)) != TRI_OK) return r;
-            k_attend_prefix<<<(unsigned)c->n_sm, kPThreads, kPDynSmem, st>>>(km, vm, p);
+            if (pv->k_kind == 3) k_attend_prefix<true><<<(unsigned)c->n_sm, kPThreads<true>, kPDynSmem, st>>>(km, vm, p);
+            else k_attend_prefix<false><<<(unsigned)c->n_sm, kPThreads<false>, kPDynSmem, st>>>(km, vm, p);
             TRI_CUDA(cudaGetLastError());
         } else if (prefix->view->k_kind == 3) {
             TRI_CUDA(launch_attend<true>(rows, (unsigned)pl.blocks, st, p, false));

@@ -11,6 +11,8 @@
 //                    reads its 128 logits, raises its bound m only when a logit passes it by 2^8 (then O is rescaled in
 //                    tensor memory), and writes the weights over the logits
 // Tensor memory: S/P of both streams (2 x 128 columns) and O of both (2 x 128), all of its 512 columns.
+// 8-bit rows: the producers' two warps per matrix widen the raw e4m3 rows to f16 on their way into the operand stages, and
+// the MMAs are f16 (queries scaled to f16 by a power of two per row, weights with 11 bits).
 // At the end of a unit's share the streams are joined and the part goes to the workspace, as in k_attend.
 //
 // What bounds it: with up to 128 rows per prefix, HBM (64 KB per 1.5 us and SM); the MMAs of a tile take 1536 cycles, the
@@ -27,14 +29,16 @@ namespace tri {
 
 constexpr int kPTile = 128;                               // cached rows per tile, query rows per tile
 constexpr int kPHalf = 64;                               // the weights of a tile are handed over in two halves, so that MMAs and softmax overlap
-constexpr int kPStages = 3;
+template <bool KEY8> constexpr int kPStages = KEY8 ? 2 : 3;     // operand stages of K and of V
 constexpr int kPUnitCost = 2;                             // a unit's own cost, in tiles
 static_assert(kPTile == kMergeTile, "slots are laid out for the joining kernel");
 constexpr int kPBlock = kPTile * 128;                     // 128 rows x 64 bf16, one swizzled block
 constexpr int kPTileBytes = 2 * kPBlock;                  // dims 0..63 | dims 64..127
 constexpr int kPSoftWarps = 8;
-constexpr int kPThreads = (kPSoftWarps + 3) * 32;           // + K producer, V producer, MMA warp
-constexpr int kPDynSmem = (1 + 2 * kPStages) * kPTileBytes + 1024;      // Q, K ring, V ring
+template <bool KEY8> constexpr int kPMoveWarps = KEY8 ? 4 : 2;    // producers (8 bits: and converters) of K, of V; then the MMA warp
+template <bool KEY8> constexpr int kPThreads = (kPSoftWarps + kPMoveWarps<KEY8> + 1) * 32;
+constexpr int kPRawBytes = kPTile * 128;                  // 128 rows of 128 e4m3 values
+constexpr int kPDynSmem = 7 * kPTileBytes + 1024;         // Q, K and V stages; 8 bits: two stages of raw rows each in place of one of them
 
 // V as the B operand: N (dims) contiguous, 64-element chunks one block apart, groups of 8 cached rows 1024 bytes apart.
 __device__ __forceinline__ uint64_t tc_desc_sw128_n(uint32_t smem_addr)
@@ -123,18 +127,24 @@ __device__ __forceinline__ void tc_loaded(uint32_t (&r)[N])
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
 
 struct PrefixBars {
-    uint64_t kfull[kPStages], kempty[kPStages], vfull[kPStages], vempty[kPStages];
+    uint64_t kfull[3], kempty[3], vfull[3], vempty[3];
     uint64_t sfull[2], pready[4], q, ml;                  // per stream; per (stream, half of a tile's rows); block
+    uint64_t rawfull[4], rawfree[4];                      // 8 bits: two stages of raw K, two of raw V
 };
+// Instruction descriptor of an f16 or bf16 MMA with M = 128, both operands K-major.
+__host__ __device__ constexpr uint32_t tc_idesc_16(bool f16, int ncol) { return f16 ? tc_idesc_bf16(ncol) & ~((1u << 7) | (1u << 10)) : tc_idesc_bf16(ncol); }
 
-__global__ void __launch_bounds__(kPThreads, 1)
+template <bool KEY8>
+__global__ void __launch_bounds__(kPThreads<KEY8>, 1)
 k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const AttendParams p)
 {
     extern __shared__ uint8_t dyn[];
     __shared__ __align__(8) PrefixBars bars;
     __shared__ uint32_t tmem_base_s;
     __shared__ volatile int gave_up;
-    __shared__ uint32_t absent[kPStages];                  // per stage: boxes of 16 rows whose page id is out of range
+    __shared__ uint32_t absent[3], absent_raw[2];          // per stage: groups of 16 rows whose page id is out of range
+    __shared__ float qscale_s[KEY8 ? kPTile : 1];          // 8 bits: power of two a query row was divided by
+    constexpr int ST = kPStages<KEY8>, kMmaWarp = kPSoftWarps + kPMoveWarps<KEY8>;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     grid_dependents_launch();                              // the pass over the sequences' own rows may start as blocks leave
@@ -142,16 +152,18 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
     if ((int)blockIdx.x >= sh.shares || sh.total == 0) return;
 
     const uint32_t base = (smem_u32(dyn) + 1023u) & ~1023u;
-    const uint32_t sm_q = base, sm_k = base + kPTileBytes, sm_v = sm_k + kPStages * kPTileBytes;
-    uint8_t *gq = dyn + (base - smem_u32(dyn)), *gv = gq + (1 + kPStages) * kPTileBytes;
+    const uint32_t sm_q = base, sm_k = base + kPTileBytes, sm_v = sm_k + ST * kPTileBytes;
+    uint8_t *gq = dyn + (base - smem_u32(dyn)), *gv = gq + (1 + ST) * kPTileBytes;
     const uint32_t b_kfull = smem_u32(bars.kfull), b_kempty = smem_u32(bars.kempty), b_vfull = smem_u32(bars.vfull),
                    b_vempty = smem_u32(bars.vempty), b_sfull = smem_u32(bars.sfull), b_pready = smem_u32(bars.pready),
                    b_q = smem_u32(&bars.q), b_ml = smem_u32(&bars.ml);
     if (tid == 0) {
-        for (int i = 0; i < kPStages; ++i) {
-            mbar_init(b_kfull + 8 * i, 1); mbar_init(b_kempty + 8 * i, 1);
-            mbar_init(b_vfull + 8 * i, 1); mbar_init(b_vempty + 8 * i, 1);
+        for (int i = 0; i < ST; ++i) {
+            mbar_init(b_kfull + 8 * i, KEY8 ? 2 : 1); mbar_init(b_kempty + 8 * i, 1);       // filled by a copy, or by two converter warps
+            mbar_init(b_vfull + 8 * i, KEY8 ? 2 : 1); mbar_init(b_vempty + 8 * i, 1);
         }
+        if (KEY8)
+            for (int i = 0; i < 4; ++i) { mbar_init(smem_u32(&bars.rawfull[i]), 1); mbar_init(smem_u32(&bars.rawfree[i]), 2); }
         for (int i = 0; i < 2; ++i) mbar_init(b_sfull + 8 * i, 1);
         for (int i = 0; i < 4; ++i) mbar_init(b_pready + 8 * i, kPSoftWarps / 2);
         mbar_init(b_q, kPSoftWarps);
@@ -159,7 +171,7 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
         gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
-    if (warp == kPSoftWarps + 2) {                         // the MMA warp owns the tensor-memory allocation
+    if (warp == kMmaWarp) {                         // the MMA warp owns the tensor-memory allocation
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&tmem_base_s)), "r"(512)
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
@@ -196,8 +208,105 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
     const uint32_t tmem = tmem_base_s;
     // columns: S/P of stream w at 128 w (weights: 64 columns, their rest: 64), O of stream w at 256 + 128 w
 
-    if (warp == kPSoftWarps || warp == kPSoftWarps + 1) {
-        // ---------------- producers: one warp for K, one for V, lane = (box, half of the dims) ----------------
+    if (KEY8 && warp >= kPSoftWarps && warp < kMmaWarp) {
+        // ---------------- 8 bits: two warps for K, two for V; the first of a pair issues the copies of raw rows two tiles ahead,
+        // each widens half of a tile's rows to f16 into the operand's stage (rows behind the length or absent become zeros) ----
+        const bool is_v = warp >= kPSoftWarps + 2, lead = ((warp - kPSoftWarps) & 1) == 0;
+        const uint32_t b_full = is_v ? b_vfull : b_kfull, b_empty = is_v ? b_vempty : b_kempty;
+        const uint32_t b_raw = smem_u32(&bars.rawfull[is_v ? 2 : 0]), b_free = smem_u32(&bars.rawfree[is_v ? 2 : 0]);
+        uint8_t *g_raw = gq + (1 + 2 * ST) * kPTileBytes + (is_v ? 2 * kPRawBytes : 0), *g_out = gq + (1 + (is_v ? ST : 0)) * kPTileBytes;
+        const uint32_t raw = smem_u32(g_raw);
+        const CUtensorMap *map = is_v ? &vmap : &kmap;
+        const int box = p.box_rows, boxes = kPTile / box;
+        AttCursor ahead = cur;
+        AttJob a;                                          // the unit whose rows are being asked for
+        int at = 0, asked = 0;
+        auto next_asked = [&]() -> bool {
+            while (att_next<kPTile, kPUnitCost>(p, sh, ahead, a))
+                if (a.kb > a.ka) return true;
+            return false;
+        };
+        bool open = lead && next_asked();
+        auto ask = [&]() -> bool {                         // raw rows of the share's next tile
+            if (!open) return true;
+            const int st = asked & 1;
+            if (asked >= 2 && !__all_sync(0xffffffffu, mbar_wait_parked<20>(b_free + 8 * st, ((asked >> 1) - 1) & 1))) return false;
+            const int64_t row = (int64_t)(a.ka + at) * kPTile + lane * box, left = a.len - (int64_t)(a.ka + at) * kPTile;
+            const int nsub = left >= kPTile ? boxes : (int)((left + box - 1) / box);
+            int c1 = (int)row, c3 = a.seq;
+            bool ok = true;
+            if (p.src.paged && lane < nsub) {
+                const int pg = p.src.page_shift >= 0 ? (int)row >> p.src.page_shift : (int)row / p.src.page_size;
+                c3 = __ldg(p.src.page_table + (int64_t)a.seq * p.src.max_pages_per_seq + pg);
+                c1 = (int)row - pg * p.src.page_size;
+                ok = p.src.n_pages <= 0 || (c3 >= 0 && c3 < p.src.n_pages);
+            }
+            const uint32_t bad = __ballot_sync(0xffffffffu, !ok);
+            if (lane == 0) {
+                uint32_t mask = 0;
+                if (bad) {
+                    for (int x = 0; x < kPTile / kTileKeys; ++x) mask |= ((bad >> (x * kTileKeys / box)) & 1u) << x;
+                    if (!is_v && p.device_status) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
+                }
+                if (is_v) absent_raw[st] = mask;
+                mbar_expect_tx(b_raw + 8 * st, (uint32_t)(nsub - __popc(bad)) * box * 128);
+            }
+            __syncwarp();
+            if (lane < nsub && ok) tma_load_5d(raw + st * kPRawBytes + lane * box * 128, map, b_raw + 8 * st, 0, c1, a.h, c3, p.layer);
+            ++asked;
+            if (++at == a.kb - a.ka) { at = 0; open = next_asked(); }
+            return true;
+        };
+        bool ok = ask() && ask();
+        while (ok && !gave_up && next_rows(false)) {
+            const int n = j.kb - j.ka;
+            for (int t = 0; t < n; ++t) {
+                const int i = done + t, st = i & 1;
+                ok = mbar_wait_parked<20>(b_raw + 8 * st, (i >> 1) & 1) && (i < 2 || mbar_wait_parked<20>(b_empty + 8 * st, ((i >> 1) - 1) & 1));
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                const int64_t left = j.len - (int64_t)(j.ka + t) * kPTile;
+                const int have = left < kPTile ? (int)left : kPTile;
+                const uint32_t miss = is_v ? absent_raw[st] : 0u;
+                const bool cut = is_v && (have < kPTile || miss);
+                if (is_v && lead && lane == 0) absent[st] = miss;
+                const uint8_t *src = g_raw + st * kPRawBytes;
+                uint8_t *dst = g_out + st * kPTileBytes;
+                // lane = (row of four, 16 values): 512 contiguous bytes in, four wavefronts per store out
+                const int c = lane & 7, first = (lead ? 0 : 64) + (lane >> 3);
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    uint4 x[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int r = first + 4 * (8 * b + k);
+                        x[k] = *reinterpret_cast<const uint4 *>(src + r * 128 + ((c ^ (r & 7)) << 4));
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int r = first + 4 * (8 * b + k);
+                        uint4 lo, hi;
+                        e4m3x4_to_f16x2(x[k].x, lo.x, lo.y);
+                        e4m3x4_to_f16x2(x[k].y, lo.z, lo.w);
+                        e4m3x4_to_f16x2(x[k].z, hi.x, hi.y);
+                        e4m3x4_to_f16x2(x[k].w, hi.z, hi.w);
+                        if (cut && (r >= have || ((miss >> (r >> 4)) & 1u))) { lo = make_uint4(0u, 0u, 0u, 0u); hi = lo; }
+                        uint8_t *to = dst + (c >> 2) * kPBlock;
+                        *reinterpret_cast<uint4 *>(to + sw128(r, 2 * c & 7)) = lo;
+                        *reinterpret_cast<uint4 *>(to + sw128(r, (2 * c + 1) & 7)) = hi;
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+                __syncwarp();
+                if (lane == 0) { mbar_arrive(b_full + 8 * st); mbar_arrive(b_free + 8 * st); }
+                ok = ask();
+                if (!ok) break;
+            }
+            done += n;
+        }
+        if (!ok) gave_up = 1;
+    } else if (!KEY8 && warp >= kPSoftWarps && warp < kMmaWarp) {
+        // ---------------- bf16 producers: one warp for K, one for V, lane = (box, half of the dims) ----------------
         // (one warp for both: its copies, 32 for 16-row boxes, are issued one by one and held a paged prefix back)
         // a box is `box` rows high: 128 where rows are contiguous, else the largest power of two up to 128 that divides a page
         const bool is_v = warp != kPSoftWarps;
@@ -218,8 +327,8 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
             int c1 = 0, c3 = 0;
             bool ok = locate(0, c1, c3);
             for (int t = 0; t < n; ++t) {
-                const int i = done + t, st = i % kPStages;
-                const uint32_t par = ((i / kPStages) - 1) & 1;
+                const int i = done + t, st = i % ST;
+                const uint32_t par = ((i / ST) - 1) & 1;
                 const int64_t left = j.len - (int64_t)(j.ka + t) * kPTile;
                 const int nsub = left >= kPTile ? boxes : (int)((left + box - 1) / box);
                 const uint32_t bad = __ballot_sync(0xffffffffu, !ok && sub < nsub && half == 0);
@@ -229,7 +338,7 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                     if (lane == 0 && !is_v && p.device_status) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
                 }
                 const uint32_t bytes = (uint32_t)(nsub - __popc(bad)) * box * (kHeadDim * 2);
-                const bool w = i < kPStages || mbar_wait_parked<20>(b_empty + 8 * st, par);
+                const bool w = i < ST || mbar_wait_parked<20>(b_empty + 8 * st, par);
                 if (!__all_sync(0xffffffffu, w)) { gave_up = 1; break; }
                 if (lane == 0) {
                     if (is_v) absent[st] = mask;
@@ -243,10 +352,10 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
             }
             done += n;
         }
-    } else if (warp == kPSoftWarps + 2) {
+    } else if (warp == kMmaWarp) {
         // ---------------- MMA issue ----------------
-        constexpr uint32_t idesc_qk = tc_idesc_bf16(kPTile);                     // both operands K-major
-        constexpr uint32_t idesc_pv = tc_idesc_bf16(kHeadDim) | (1u << 16);      // B (the values) N-major
+        constexpr uint32_t idesc_qk = tc_idesc_16(KEY8, kPTile);                 // both operands K-major
+        constexpr uint32_t idesc_pv = tc_idesc_16(KEY8, kHeadDim) | (1u << 16);  // B (the values) N-major
         int units = 0, cnt[2] = {0, 0};                    // tiles each stream had in earlier units (phases of pready)
         while (!gave_up && next_rows(false)) {
             const int n = j.kb - j.ka;
@@ -254,8 +363,8 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
             // logits of tile t: into the columns whose weights the MMAs issued before have used up.  As MMAs complete in order,
             // sfull says that the stream's accumulator rests, too; behind the stream's last tile it says nothing else
             auto logits = [&](int t) -> bool {
-                const int i = done + t, st = i % kPStages;
-                if (!__all_sync(0xffffffffu, mbar_wait_bounded(b_kfull + 8 * st, (i / kPStages) & 1))) return false;
+                const int i = done + t, st = i % ST;
+                if (!__all_sync(0xffffffffu, mbar_wait_bounded(b_kfull + 8 * st, (i / ST) & 1))) return false;
                 tc_fence_after();
                 if (lane == 0) {
                     const uint32_t ka = sm_k + st * kPTileBytes, acc = tmem + 128 * (t & 1);
@@ -273,8 +382,8 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
             for (int t = 0; t < n && ok; ++t) {
                 // weights of tile t times its values, the upper half of its rows first (as the softmax delivers them), then
                 // the logits of the stream's next tile
-                const int i = done + t, st = i % kPStages, w = t & 1;
-                ok = mbar_wait_bounded(b_vfull + 8 * st, (i / kPStages) & 1);
+                const int i = done + t, st = i % ST, w = t & 1;
+                ok = mbar_wait_bounded(b_vfull + 8 * st, (i / ST) & 1);
                 for (int x = 1; x >= 0; --x) {
                     ok = __all_sync(0xffffffffu, ok && mbar_wait_bounded(b_pready + 8 * (2 * w + x), (cnt[w] + (t >> 1)) & 1));
                     if (!ok) break;
@@ -316,8 +425,22 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int r = (tid >> 4) + 16 * i, c = tid & 15;
-                *reinterpret_cast<uint4 *>(gq + (c >> 3) * kPBlock + sw128(r, c & 7)) =
-                    make_uint4(q[i].x ^ flip, q[i].y ^ flip, q[i].z ^ flip, q[i].w ^ flip);
+                uint32_t x[4] = {q[i].x ^ flip, q[i].y ^ flip, q[i].z ^ flip, q[i].w ^ flip};
+                if (KEY8) {
+                    // to f16, the row's largest entry brought to [1, 2) (see k_attend)
+                    float amax = 0.f;
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) amax = fmaxf(amax, fmaxf(fabsf(bf16_lo(x[y])), fabsf(bf16_hi(x[y]))));
+#pragma unroll
+                    for (int d = 1; d < 16; d <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, d));
+                    int e = min(max((int)((__float_as_uint(amax) >> 23) & 255u) - 127, -126), 126);
+                    if (amax == 0.f) e = 0;
+                    const float by = __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) x[y] = f16_bits(bf16_lo(x[y]) * by) | (f16_bits(bf16_hi(x[y]) * by) << 16);
+                    if (c == 0) qscale_s[KEY8 ? r : 0] = __uint_as_float((uint32_t)(127 + e) << 23);
+                }
+                *reinterpret_cast<uint4 *>(gq + (c >> 3) * kPBlock + sw128(r, c & 7)) = make_uint4(x[0], x[1], x[2], x[3]);
             }
             asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
             tc_fence_before();                             // the last unit's accumulators have been read
@@ -327,20 +450,25 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
             if (more) prefetch_queries(j);
 
             // base-2 logit = accumulator * mul (not 0: a masked logit is -infinity)
-            const float mul = fmaxf(fabsf(p.scale) * (p.k_scale ? __ldg(p.k_scale + u.h) : 1.f), 1.17549435e-38f);
+            bool ok = true;
+            float mul = fabsf(p.scale) * (p.k_scale ? __ldg(p.k_scale + u.h) : 1.f);
+            if (KEY8) {
+                ok = __all_sync(0xffffffffu, mbar_wait_bounded(b_q, units & 1));        // the other warps' rows and scales, too
+                mul *= qscale_s[KEY8 ? row : 0];
+            }
+            mul = fmaxf(mul, 1.17549435e-38f);
             const float2 mul2 = make_float2(mul, mul);
             float m = -INFINITY;
             // sums of the weights (even and odd rows) as they are, for the row's statistics, and as they enter the MMAs: o is
             // divided by the latter, so that the roundings all but cancel
             float2 l = make_float2(0.f, 0.f), lr = make_float2(0.f, 0.f);
-            bool ok = true;
 #pragma unroll 1
-            for (int t = w; t < n; t += 2) {
-                const int i = done + t, st = i % kPStages;
+            for (int t = w; t < n && ok; t += 2) {
+                const int i = done + t, st = i % ST;
                 const int64_t left = u.len - (int64_t)(u.ka + t) * kPTile;
                 const bool cut = left < kPTile;
                 ok = mbar_wait_bounded(b_sfull + 8 * w, (phase[w] + (t >> 1)) & 1);
-                if (cut || check_pages) ok = ok && mbar_wait_bounded(b_vfull + 8 * st, (i / kPStages) & 1);
+                if (cut || check_pages) ok = ok && mbar_wait_bounded(b_vfull + 8 * st, (i / ST) & 1);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
@@ -371,7 +499,8 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                 }
                 if (cut || miss) {
                     // rows behind the length or of absent pages: no weight, and zeros for values (they may hold anything)
-                    if (row >= have || ((miss >> (row >> 4)) & 1u)) {
+                    // (8 bits: the converters have seen to the values)
+                    if (!KEY8 && (row >= have || ((miss >> (row >> 4)) & 1u))) {
 #pragma unroll
                         for (int c = 0; c < 16; ++c)
                             *reinterpret_cast<uint4 *>(gv + st * kPTileBytes + (c >> 3) * kPBlock + row * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
@@ -411,9 +540,13 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                             float2 e = fma2(make_float2(__uint_as_float(s[32 * c + 2 * y]), __uint_as_float(s[32 * c + 2 * y + 1])), mul2, ref2);
                             e.x = ex2(e.x);
                             e.y = ex2(e.y);
-                            hi[y] = cvt_bf16x2(e.y, e.x);
                             l = add2(l, e);
-                            lr = add2(lr, make_float2(bf16_lo(hi[y]), bf16_hi(hi[y])));
+                            if (KEY8) {                    // 11 bits in f16
+                                asm("cvt.rn.f16x2.f32 %0, %1, %2;\n" : "=r"(hi[y]) : "f"(e.y), "f"(e.x));
+                            } else {
+                                hi[y] = cvt_bf16x2(e.y, e.x);
+                                lr = add2(lr, make_float2(bf16_lo(hi[y]), bf16_hi(hi[y])));
+                            }
                         }
                         tc_st16(t_s + kPHalf * x + 16 * c, hi);
                     }
@@ -442,7 +575,7 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
             ok = __all_sync(0xffffffffu, ok);
             if (ok) {
                 tc_fence_after();
-                tc_st4f(t_s, m, l.x + l.y, lr.x + lr.y > 0.f ? (l.x + l.y) / (lr.x + lr.y) : 1.f);
+                tc_st4f(t_s, m, l.x + l.y, !KEY8 && lr.x + lr.y > 0.f ? (l.x + l.y) / (lr.x + lr.y) : 1.f);
                 tc_wait_st();
                 tc_fence_before();
             }
@@ -459,7 +592,8 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
             tc_loaded(s1);
             const float m0 = __uint_as_float(s0[0]), m1 = __uint_as_float(s1[0]), mm = fmaxf(m0, m1);
             const float e0 = m0 == -INFINITY ? 0.f : ex2(m0 - mm), e1 = m1 == -INFINITY ? 0.f : ex2(m1 - mm);
-            const float f0 = e0 * __uint_as_float(s0[2]), f1 = e1 * __uint_as_float(s1[2]);
+            const float vs = p.v_scale ? __ldg(p.v_scale + u.h) : 1.f;
+            const float f0 = e0 * __uint_as_float(s0[2]) * vs, f1 = e1 * __uint_as_float(s1[2]) * vs;
             const bool mine = row < u.nrows;
             const int sr = att_small_div(row, inv_g), sq = u.first_seq + sr, hq = u.h * p.G + row - sr * p.G;
             // slots hold four dims of all rows, then the next four: a warp writes 512 bytes in a row
@@ -496,10 +630,12 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
         // a wait ran out: report it, and give copies still in flight one more bounded chance to land before the block exits
         if (tid == 0 && p.device_status) atomicExch(p.device_status, (int)TRI_ERR_TIMEOUT);
         if (warp == kPSoftWarps || warp == kPSoftWarps + 1)
-            for (int i = 0; i < 2 * kPStages; ++i)
-                (void)mbar_wait_parked((warp == kPSoftWarps ? b_kfull : b_vfull) + 8 * (i % kPStages), (i / kPStages) & 1);
+            for (int i = 0; i < 2 * ST; ++i) {
+                const uint32_t full = KEY8 ? smem_u32(&bars.rawfull[warp == kPSoftWarps ? 0 : 2]) : (warp == kPSoftWarps ? b_kfull : b_vfull);
+                (void)mbar_wait_parked(full + 8 * (i % ST), (i / ST) & 1);
+            }
     }
-    if (warp == kPSoftWarps + 2) {
+    if (warp == kMmaWarp) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(512) : "memory");
     }
