@@ -416,31 +416,35 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
         while (!gave_up && more) {
             const AttJob u = j;                            // (j runs ahead to the unit behind it)
             const int n = u.kb - u.ka;
-            uint4 q[8];
+            constexpr int NQ = KEY8 ? 4 : 8;               // 16 bytes of 8 rows per thread, NQ rows at a time
+#pragma unroll 1
+            for (int q0 = 0; q0 < 8; q0 += NQ) {
+                uint4 q[NQ];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {                  // 16 bytes of 8 rows per thread
-                const int r = (tid >> 4) + 16 * i;
-                q[i] = r < u.nrows ? *reinterpret_cast<const uint4 *>(query_row(u, r) + 16 * (tid & 15)) : make_uint4(0u, 0u, 0u, 0u);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int r = (tid >> 4) + 16 * i, c = tid & 15;
-                uint32_t x[4] = {q[i].x ^ flip, q[i].y ^ flip, q[i].z ^ flip, q[i].w ^ flip};
-                if (KEY8) {
-                    // to f16, the row's largest entry brought to [1, 2) (see k_attend)
-                    float amax = 0.f;
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) amax = fmaxf(amax, fmaxf(fabsf(bf16_lo(x[y])), fabsf(bf16_hi(x[y]))));
-#pragma unroll
-                    for (int d = 1; d < 16; d <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, d));
-                    int e = min(max((int)((__float_as_uint(amax) >> 23) & 255u) - 127, -126), 126);
-                    if (amax == 0.f) e = 0;
-                    const float by = __uint_as_float((uint32_t)(127 - e) << 23);
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) x[y] = f16_bits(bf16_lo(x[y]) * by) | (f16_bits(bf16_hi(x[y]) * by) << 16);
-                    if (c == 0) qscale_s[KEY8 ? r : 0] = __uint_as_float((uint32_t)(127 + e) << 23);
+                for (int i = 0; i < NQ; ++i) {
+                    const int r = (tid >> 4) + 16 * (q0 + i);
+                    q[i] = r < u.nrows ? *reinterpret_cast<const uint4 *>(query_row(u, r) + 16 * (tid & 15)) : make_uint4(0u, 0u, 0u, 0u);
                 }
-                *reinterpret_cast<uint4 *>(gq + (c >> 3) * kPBlock + sw128(r, c & 7)) = make_uint4(x[0], x[1], x[2], x[3]);
+#pragma unroll
+                for (int i = 0; i < NQ; ++i) {
+                    const int r = (tid >> 4) + 16 * (q0 + i), c = tid & 15;
+                    uint32_t x[4] = {q[i].x ^ flip, q[i].y ^ flip, q[i].z ^ flip, q[i].w ^ flip};
+                    if (KEY8) {
+                        // to f16, the row's largest entry brought to [1, 2) (see k_attend)
+                        float amax = 0.f;
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) amax = fmaxf(amax, fmaxf(fabsf(bf16_lo(x[y])), fabsf(bf16_hi(x[y]))));
+#pragma unroll
+                        for (int d = 1; d < 16; d <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, d));
+                        int e = min(max((int)((__float_as_uint(amax) >> 23) & 255u) - 127, -126), 126);
+                        if (amax == 0.f) e = 0;
+                        const float by = __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) x[y] = f16_bits(bf16_lo(x[y]) * by) | (f16_bits(bf16_hi(x[y]) * by) << 16);
+                        if (c == 0) qscale_s[KEY8 ? r : 0] = __uint_as_float((uint32_t)(127 + e) << 23);
+                    }
+                    *reinterpret_cast<uint4 *>(gq + (c >> 3) * kPBlock + sw128(r, c & 7)) = make_uint4(x[0], x[1], x[2], x[3]);
+                }
             }
             asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
             tc_fence_before();                             // the last unit's accumulators have been read
