@@ -128,7 +128,8 @@ __global__ void __launch_bounds__(kAppendThreads) k_append(const AppendParams p)
 
     const int tid = threadIdx.x, c = tid & 7;
     const int s = blockIdx.x / p.ntiles, t0 = (blockIdx.x - s * p.ntiles) * TT;
-    grid_dependents_launch();                                 // k_append_lens, where there is one, waits for this kernel itself
+    grid_dependency_wait();                                   // set up under the kernel before it in the stream, as the next is under this one
+    grid_dependents_launch();
     const int n_new = append_count(p, s);
     const bool first = t0 == 0;
     if (first && tid == 0 && p.device_status && p.n_new) {
@@ -232,6 +233,7 @@ __global__ void __launch_bounds__(kAppendThreads) k_append(const AppendParams p)
 __global__ void __launch_bounds__(256) k_append_lens(const AppendParams p)
 {
     grid_dependency_wait();
+    grid_dependents_launch();
     const int n = p.unit_lens ? p.H : 1;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= (int64_t)p.S * n) return;

@@ -35,6 +35,7 @@ struct AttendParams {
     int32_t spt;                                          // prefixes: sequences per tile of query rows; own rows: 0
     int32_t S;                                            // sequences of the call
     int32_t box_rows;                                     // k_attend_prefix: rows per copied box
+    int32_t under;                                        // launched behind a pass over prefixes
     const int32_t *unit_lens;                             // [nseq][H] of this layer or NULL
     const float *k_scale, *v_scale;                       // [H] of this layer or NULL
     const int32_t *group_start;                           // [nseq + 1], prefixes only
@@ -271,7 +272,10 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
     const int krow = KEY8 ? (lane & 15) : (lane & 7) + ((lane & 16) >> 1), vrow = lane & 15;
     const uint32_t klane = krow * kRowBytes + ((((KEY8 ? lane >> 4 : (lane >> 3) & 1) ^ krow) & 7) << 4);
     const uint32_t vlane = vrow * kRowBytes + ((((lane >> 4) ^ vrow) & 7) << 4);
-    grid_dependents_launch();                             // the joining kernel may be set up under this one
+    // Set up under the kernel before it in the stream and waits for it here, except behind a pass over prefixes, whose blocks
+    // this pass's may follow one by one: that pass began behind everything this one reads, and it is waited for at the end.
+    if (!p.under) grid_dependency_wait();
+    grid_dependents_launch();
     const AttShare sh = att_share<TILE, kAttUnitCost>(p);
     if ((int)blockIdx.x >= sh.shares) return;
 
@@ -628,7 +632,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
         __syncthreads();                                   // the stages may be refilled
     }
     cp_wait<0>();
-    grid_dependency_wait();                               // not through before the pass over prefixes is, if one was launched before
+    if (p.under) grid_dependency_wait();                  // not through before the pass over prefixes is
 }
 
 // ----------------------------------------------------------------------------------------------
@@ -667,6 +671,7 @@ __global__ void __launch_bounds__(kMergeThreads) k_attend_merge(const MergeParam
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int per = p.G / p.rows, unit = blockIdx.x / per, s = unit / p.H, h = unit - s * p.H;
     grid_dependency_wait();
+    grid_dependents_launch();
     const int2 own = p.own.rec[unit];
     if (!p.pre.rec && own.y < 2) return;                                     // finished by its block
     int2 pre = make_int2(0, 0);

@@ -147,6 +147,7 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
     constexpr int ST = kPStages<KEY8>, kMmaWarp = kPSoftWarps + kPMoveWarps<KEY8>;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    grid_dependency_wait();                                // set up under the kernel before it in the stream
     grid_dependents_launch();                              // the pass over the sequences' own rows may start as blocks leave
     const AttShare sh = att_share<kPTile, kPUnitCost>(p);
     if ((int)blockIdx.x >= sh.shares || sh.total == 0) return;
