@@ -331,7 +331,8 @@ tri_status tri_calib_finalize(const void *state, int32_t n_heads, int32_t pair_l
  * and layouts); rows [0, length) of a unit are cached, where the length is view->seq_lens[s], or
  * unit_lens[(layer * S + s) * n_kv_heads + h] when unit_lens is given: after tri_compress_budgets the heads of a
  * sequence hold different numbers of rows, and its kept_cnt array is such an array.  A length below 0 counts as 0, one
- * above n_max as n_max.  S is the number of sequences of the view.
+ * above n_max as n_max.  All n_max rows of a unit (contiguous views), all slots of a page in the table (paged views) must
+ * be addressable: copies may touch rows behind the length, which are then not used.  S is the view's number of sequences.
  */
 typedef struct {
     const tri_cache_view *view;
@@ -374,8 +375,8 @@ typedef struct {
  *   queries  rotated likewise into q_out
  * Nothing else of the cache or of q_out is written, rows of padding tokens (t >= n_new[s]) are not read.
  *   new_lens  device [S], or [U] with unit_lens (this layer's entries), or NULL: receives length + n_new, at most
- *             n_max.  It may be the array the lengths come from; the layers of a step share the lengths, so hand it
- *             over with the step's last layer only.
+ *             n_max.  It may be the array the lengths come from (not n_new); the layers of a step share the lengths, so
+ *             hand it over with the step's last layer only.
  *   device_status  device int32[1] or NULL; set to TRI_ERR_DEVICE_CHECK if a row had no slot below n_max, a page id
  *             outside [0, n_pages) or a position outside [0, 2^31) -- such rows are skipped -- or if n_new[s] was
  *             outside [0, T] (the nearest bound counts)
@@ -388,7 +389,7 @@ tri_status tri_append(tri_ctx *ctx, const tri_layer_cache *dst, int32_t S, const
 typedef struct {
     const void *q;             /* device bf16 [S][H*G][128], 16-byte rows                                          */
     int64_t q_stride_seq, q_stride_head;
-    void *out;                 /* device bf16 [S][H*G][128], 16-byte rows; must not overlap q                      */
+    void *out;                 /* device bf16 [S][H*G][128], 16-byte rows; must not overlap q (out == q is refused) */
     int64_t out_stride_seq, out_stride_head;
     float *lse;                /* device fp32 [S][H*G] or NULL: log sum_n exp(logit_n), -infinity without rows      */
     float scale;               /* logit_n = scale * (q . k_n); finite                                              */
@@ -403,8 +404,11 @@ size_t tri_attend_workspace_bytes(const tri_ctx *ctx, int32_t S, int32_t P);
  * A unit without rows gives zeros.  Key formats 0 and 3; the pre-RoPE formats hold unrotated keys and are refused
  * (TRI_ERR_UNSUPPORTED), as is a cache without values (TRI_ERR_INVALID_ARG).  Rows at or behind the length are never
  * used, whatever they hold.  Logits, softmax statistics and sums are fp32; the weights of the sum over values enter
- * the tensor cores as a 16-bit value plus the 16-bit rest of it.  Sums are formed in a fixed order: equal inputs give
- * equal bits.  Any length up to 2^31 - 1; ragged batches are cut into equal shares over the GPU.
+ * the tensor cores as a 16-bit value plus the 16-bit rest of it (where more than 16 query rows share a prefix: rounded
+ * once, to bf16, over 8-bit values to f16).  Sums are formed in a fixed order: equal inputs give
+ * equal bits.  Ragged batches are cut into equal shares over the GPU; S * n_kv_heads * (n_max / 64 + 3) must stay below
+ * 2^31 (for prefixes, with P + S in place of S at most), else TRI_ERR_UNSUPPORTED.  An infinity among the values of a
+ * unit's rows makes the outputs of its component infinite or NaN.
  *   ws  device workspace of tri_attend_workspace_bytes(ctx, S, 0) bytes, 256-byte aligned; nothing in it has to be
  *       set, nothing is kept in it from call to call.  Calls that may overlap on the GPU need a workspace each.
  *   device_status  device int32[1] or NULL; TRI_ERR_DEVICE_CHECK if a kernel met a page id outside [0, n_pages): such

@@ -280,6 +280,8 @@ class LayerCache:
         self.device = view.k.device
         L, H = view.k.shape[0], view.k.shape[2]
         assert 0 <= layer < L
+        rows = view.k.shape[3] if view.page_table is None else view.page_table.shape[1] * view.k.shape[3]
+        assert self._cv.n_max <= rows, "n_max rows of every unit have to exist"
         self.n_layers, self.n_kv_heads = L, H
         S = view.k.shape[1] if view.page_table is None else view.page_table.shape[0]
         self.n_seqs = S

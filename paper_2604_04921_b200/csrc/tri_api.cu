@@ -431,6 +431,22 @@ cudaError_t allow_attend_smem()
     return cudaFuncSetAttribute(k_attend<KEY8, RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttRingBytes);
 }
 
+// Loads kernels that need no attribute, so that a program's first call may already be captured into a graph.
+template <typename... Kernels>
+cudaError_t load_kernels(Kernels... kernels)
+{
+    cudaFuncAttributes a;
+    cudaError_t e = cudaSuccess;
+    ((e = e == cudaSuccess ? cudaFuncGetAttributes(&a, kernels) : e), ...);
+    return e;
+}
+template <int KIND, int KK>
+cudaError_t load_append()
+{
+    return load_kernels(k_append<KIND, KK, false, 1>, k_append<KIND, KK, false, kAppendTokens>, k_append<KIND, KK, true, 1>,
+                        k_append<KIND, KK, true, kAppendTokens>);
+}
+
 cudaError_t prepare_device()
 {
     cudaError_t e;
@@ -448,6 +464,11 @@ cudaError_t prepare_device()
     if ((e = allow_attend_smem<false, 16>()) != cudaSuccess) return e;
     if ((e = allow_attend_smem<true, 8>()) != cudaSuccess) return e;
     if ((e = allow_attend_smem<true, 16>()) != cudaSuccess) return e;
+    if ((e = load_append<0, 0>()) != cudaSuccess || (e = load_append<0, 1>()) != cudaSuccess) return e;
+    if ((e = load_append<0, 2>()) != cudaSuccess || (e = load_append<0, 3>()) != cudaSuccess) return e;
+    if ((e = load_append<1, 0>()) != cudaSuccess || (e = load_append<1, 1>()) != cudaSuccess) return e;
+    if ((e = load_append<1, 2>()) != cudaSuccess || (e = load_append<1, 3>()) != cudaSuccess) return e;
+    if ((e = load_kernels(k_append_lens, k_attend_merge)) != cudaSuccess) return e;
     if ((e = cudaFuncSetAttribute(k_attend_prefix<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPDynSmem)) != cudaSuccess) return e;
     return cudaFuncSetAttribute(k_attend_prefix<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPDynSmem);
 }
@@ -1201,24 +1222,29 @@ extern "C" tri_status tri_append(tri_ctx *c, const tri_layer_cache *dst, int32_t
     if ((r = check_layer_cache(c, dst, S)) != TRI_OK) return r;
     if (!rows || rows->T <= 0 || rows->kind < 0 || rows->kind > 1) return TRI_ERR_INVALID_ARG;
     const int es = rows->kind == 0 ? 2 : 4;
-    if (!rows16_ok(rows->k, rows->k_stride_seq, rows->k_stride_tok, rows->k_stride_head, es)) return TRI_ERR_INVALID_ARG;
+    // (the stride of a dimension of size 1 is never used)
+    const int32_t H = c->desc.n_kv_heads, G = c->desc.group_size;
+    auto rows_ok = [&](const void *x, int64_t seq, int64_t tok, int64_t head, int32_t heads, int size) {
+        return rows16_ok(x, S > 1 ? seq : 0, rows->T > 1 ? tok : 0, heads > 1 ? head : 0, size);
+    };
+    if (!rows_ok(rows->k, rows->k_stride_seq, rows->k_stride_tok, rows->k_stride_head, H, es)) return TRI_ERR_INVALID_ARG;
     if ((rows->v != nullptr) != (dst->view->v != nullptr)) return TRI_ERR_INVALID_ARG;
-    if (rows->v && !rows16_ok(rows->v, rows->v_stride_seq, rows->v_stride_tok, rows->v_stride_head, es)) return TRI_ERR_INVALID_ARG;
+    if (rows->v && !rows_ok(rows->v, rows->v_stride_seq, rows->v_stride_tok, rows->v_stride_head, H, es)) return TRI_ERR_INVALID_ARG;
     if ((rows->q != nullptr) != (rows->q_out != nullptr)) return TRI_ERR_INVALID_ARG;
     if (rows->q) {
-        if (!rows16_ok(rows->q, rows->q_stride_seq, rows->q_stride_tok, rows->q_stride_head, es)) return TRI_ERR_INVALID_ARG;
-        if (!rows16_ok(rows->q_out, rows->qo_stride_seq, rows->qo_stride_tok, rows->qo_stride_head, 2)) return TRI_ERR_INVALID_ARG;
-        if (rows->q == rows->q_out && (rows->kind != 0 || rows->q_stride_seq != rows->qo_stride_seq ||
-                                       rows->q_stride_tok != rows->qo_stride_tok || rows->q_stride_head != rows->qo_stride_head))
+        if (!rows_ok(rows->q, rows->q_stride_seq, rows->q_stride_tok, rows->q_stride_head, H * G, es)) return TRI_ERR_INVALID_ARG;
+        if (!rows_ok(rows->q_out, rows->qo_stride_seq, rows->qo_stride_tok, rows->qo_stride_head, H * G, 2)) return TRI_ERR_INVALID_ARG;
+        if (rows->q == rows->q_out && (rows->kind != 0 || (S > 1 && rows->q_stride_seq != rows->qo_stride_seq) ||
+                                       (rows->T > 1 && rows->q_stride_tok != rows->qo_stride_tok) ||
+                                       (H * G > 1 && rows->q_stride_head != rows->qo_stride_head)))
             return TRI_ERR_INVALID_ARG;
     }
     if (!rows->pos && dst->unit_lens) return TRI_ERR_INVALID_ARG;
     if ((r = check_device(c)) != TRI_OK) return r;
 
-    const int32_t H = c->desc.n_kv_heads;
     AppendParams p;
     p.dst = to_view(dst->view);
-    p.layer = dst->layer; p.S = S; p.H = H; p.G = c->desc.group_size; p.T = rows->T;
+    p.layer = dst->layer; p.S = S; p.H = H; p.G = G; p.T = rows->T;
     p.unit_lens = dst->unit_lens ? dst->unit_lens + (int64_t)dst->layer * S * H : nullptr;
     p.k_scale = dst->k_scale ? dst->k_scale + (int64_t)dst->layer * H : nullptr;
     p.v_scale = dst->v_scale ? dst->v_scale + (int64_t)dst->layer * H : nullptr;
@@ -1235,7 +1261,11 @@ extern "C" tri_status tri_append(tri_ctx *c, const tri_layer_cache *dst, int32_t
     // the lengths can be stored by the same launch unless blocks read what others store
     const int64_t n_lens = (int64_t)S * (p.unit_lens ? H : 1);
     const int32_t *lens_in = p.unit_lens ? p.unit_lens : dst->view->seq_lens;
-    const bool apart = !lens_out || (uintptr_t)(lens_out + n_lens) <= (uintptr_t)lens_in || (uintptr_t)(lens_in + n_lens) <= (uintptr_t)lens_out;
+    auto disjoint = [&](const int32_t *a, int64_t n) {
+        return !lens_out || !a || (uintptr_t)(lens_out + n_lens) <= (uintptr_t)a || (uintptr_t)(a + n) <= (uintptr_t)lens_out;
+    };
+    if (!disjoint(rows->n_new, S)) return TRI_ERR_INVALID_ARG;
+    const bool apart = disjoint(lens_in, n_lens);
     const bool later = !apart && p.ntiles > 1;
     p.new_lens = later ? nullptr : lens_out;
     const unsigned blocks = (unsigned)(p.ntiles * S);
@@ -1336,7 +1366,9 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
 {
     tri_status r;
     if (!io || !ws || ((uintptr_t)ws & 255)) return TRI_ERR_INVALID_ARG;
-    if (!rows16_ok(io->q, io->q_stride_seq, io->q_stride_head, 0, 2) || !rows16_ok(io->out, io->out_stride_seq, io->out_stride_head, 0, 2) ||
+    const int32_t H = c->desc.n_kv_heads, G = c->desc.group_size;
+    if (!rows16_ok(io->q, S > 1 ? io->q_stride_seq : 0, H * G > 1 ? io->q_stride_head : 0, 0, 2) ||
+        !rows16_ok(io->out, S > 1 ? io->out_stride_seq : 0, H * G > 1 ? io->out_stride_head : 0, 0, 2) || io->q == io->out ||
         !std::isfinite(io->scale))
         return TRI_ERR_INVALID_ARG;
     if ((r = check_device(c)) != TRI_OK) return r;
@@ -1344,7 +1376,6 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
     const AttendPlan pl = make_attend_plan(c, S, P);
     if (ws_bytes < pl.total) return TRI_ERR_WORKSPACE;
     char *w = (char *)ws;
-    const int32_t H = c->desc.n_kv_heads, G = c->desc.group_size;
 
     MergeParams mp;
     mp.pre.rec = nullptr; mp.pre.slots = mp.pre.whole = nullptr; mp.pre.rows = 0; mp.pre.spt = 0;

@@ -27,7 +27,11 @@ constexpr int kAttRingBytes = kAttWarps * kAttStages * kAttStageBytes;
 template <bool KEY8> constexpr int kAttRows = KEY8 ? 32 : 16;    // rows of a warp's step; a tile is one step of all warps
 constexpr int kAttUnitCost = 2;                                  // a unit's own cost, in tiles
 constexpr int kAttRowPitch = kHeadDim + 4;                       // floats per row of a part: 128 sums, m, l, two unused
-constexpr float kAttLazy = 8.0f;                                 // the bound m is raised when a logit passes it by this much
+// A weight is 2^(x - m).  The bound m is raised, to kAttBelow under the largest logit, when one passes it by kAttAbove.  As
+// bf16 a weight has the range of fp32.  An f16 ends at 2^16 and 2^-24, and a million rows each 2^-26 of the largest are mass:
+// the largest weight is kept in [2^11, 2^15], so that what falls below the format is 2^-36 of it.
+template <bool F16> constexpr float kAttAbove = F16 ? 15.0f : 8.0f;
+template <bool F16> constexpr float kAttBelow = F16 ? 11.0f : 0.0f;
 
 struct AttendParams {
     View src;
@@ -498,8 +502,9 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
             }
             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-            const bool raise = mx > m[i] + kAttLazy || (m[i] == -INFINITY && mx > m[i]);
+            const bool raise = mx > m[i] + kAttAbove<KEY8> || (m[i] == -INFINITY && mx > m[i]);
             if (__any_sync(0xffffffffu, raise)) {
+                mx -= kAttBelow<KEY8>;
                 const float by = raise ? ex2(m[i] - mx) : 1.f;       // 0 where there was no bound yet
                 if (raise) m[i] = mx;
                 l[i] *= by;

@@ -8,7 +8,7 @@
 //                    tensor memory, bf16
 //   2 x 4 warps      softmax: each group of four takes every other tile with statistics and an accumulator O of its own
 //                    (two independent streams, so the groups never wait for each other); a thread owns one query row,
-//                    reads its 128 logits, raises its bound m only when a logit passes it by 2^8 (then O is rescaled in
+//                    reads its 128 logits, raises its bound m only when a weight would pass 2^8 (then O is rescaled in
 //                    tensor memory), and writes the weights over the logits
 // Tensor memory: S/P of both streams (2 x 128 columns) and O of both (2 x 128), all of its 512 columns.
 // 8-bit rows: the producers' two warps per matrix widen the raw e4m3 rows to f16 on their way into the operand stages, and
@@ -514,8 +514,9 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                     tc_wait_st();
                 }
                 top *= mul;
-                const bool raise = top > m + kAttLazy || (m == -INFINITY && top > m);
+                const bool raise = top > m + kAttAbove<KEY8> || (m == -INFINITY && top > m);
                 if (__any_sync(0xffffffffu, raise)) {
+                    top -= kAttBelow<KEY8>;
                     const float by = raise ? ex2(m - top) : 1.f;
                     if (raise) m = top;
                     l.x *= by; l.y *= by; lr.x *= by; lr.y *= by;

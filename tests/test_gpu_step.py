@@ -519,6 +519,151 @@ def test_shared_reports_descending_groups():
         assert int(status) == want, starts
 
 
+@pytest.mark.parametrize("scale", [1.0, -1.0, 0.0])
+@pytest.mark.parametrize("fmt,S", [("bf16", 20), ("e4m3", 20), ("bf16", 3)])
+def test_shared_ascending_and_descending_logits(fmt, S, scale):
+    """Keys ordered by their logit, 60 units apart over the prefix: the bound is raised tile after tile, or never again."""
+    H, G, n = 1, 4, 1000
+    for sign in (1.0, -1.0):
+        g = torch.Generator(device=DEV).manual_seed(2)
+        pc, c = Cache(1, 1, H, n, fmt), Cache(1, S, H, 4, fmt)
+        pc.fill(0, 0, 0, n, g)
+        for s in range(S):
+            c.fill(0, s, 0, s % 3, g)
+        pc.k.view({1: torch.uint8, 2: torch.int16}[pc.k.element_size()])[0, 0, 0, :, 0] = raw(
+            (sign * torch.linspace(-60, 60, n, device=DEV)).to(pc.k.dtype))
+        q = torch.zeros(S, H * G, D, dtype=torch.bfloat16, device=DEV)
+        q[..., 0], q[..., 1] = 1.0, torch.linspace(-1, 1, S, device=DEV)[:, None]
+        out, lse = torch.empty_like(q), torch.empty(S, H * G, device=DEV)
+        ctx, lens = context(1, H, G), int32([s % 3 for s in range(S)])
+        ctx.attend_shared(tb.LayerCache(pc.view(tb, seq_lens=int32([n])), 0), int32([0, S]), tb.LayerCache(c.view(tb, seq_lens=lens), 0),
+                          q, out, ctx.attend_workspace(S, 1), scale=scale, lse=lse)
+        torch.cuda.synchronize()
+        check_rows(out, lse, q, lambda s, h: tuple(torch.cat((pc.unit(a, 0, 0, 0, n), c.unit(b, 0, s, 0, s % 3)))
+                                                   for a, b in ((pc.k, c.k), (pc.v, c.v))), S, H, G, scale, extra=U_BF16)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("S", [1, 24])
+def test_many_small_weights_beside_a_large_one(fmt, S):
+    """60,000 rows whose weight is 2^-25.5 of one row's: together 0.13 % of the sum, below what an f16 resolves beside 1."""
+    H, G, n = 1, 4, 60000
+    c = Cache(1, S, H, 1, fmt)
+    pc = Cache(1, 1, H, n, fmt)
+    pc.k.zero_()
+    pc.v.copy_(torch.ones(1, device=DEV).to(pc.v.dtype).expand_as(pc.v))
+    pc.k[0, 0, 0, 7, 0] = 1.0
+    pc.v[0, 0, 0, 7] = 0.0
+    q = torch.zeros(S, H * G, D, dtype=torch.bfloat16, device=DEV)
+    q[..., 0] = 16.0
+    scale = 25.5 * math.log(2.0) / 16.0
+    ctx, out = context(1, H, G), torch.empty_like(q)
+    pre = tb.LayerCache(pc.view(tb, seq_lens=int32([n])), 0)
+    src = tb.LayerCache(c.view(tb, seq_lens=int32([0] * S)), 0)
+    ctx.attend_shared(pre, int32([0, S]), src, q, out, ctx.attend_workspace(S, 1), scale=scale)
+    torch.cuda.synchronize()
+    rows = (pc.unit(pc.k, 0, 0, 0, n), pc.unit(pc.v, 0, 0, 0, n))
+    check_rows(out, None, q, lambda s, h: rows, S, H, G, scale, extra=U_BF16)
+    if S == 1:
+        ctx.attend(pre, q, out, ctx.attend_workspace(1), scale=scale)
+        torch.cuda.synchronize()
+        check_rows(out, None, q, lambda s, h: rows, 1, H, G, scale)
+
+
+def test_shared_more_prefixes_than_a_warp():
+    P = 70
+    starts, s = [0], 0
+    for p in range(P):
+        s += p % 3
+        starts.append(s)
+    check_shared("bf16", 16, 1, 4, starts, [(11 * p) % 50 for p in range(P)], [(5 * i) % 9 for i in range(s + 2)])
+    check_shared("bf16", 16, 1, 16, starts, [(11 * p) % 50 for p in range(P)], [(5 * i) % 9 for i in range(s + 2)])
+
+
+@pytest.mark.parametrize("fmt,S", [("bf16", 3), ("bf16", 30), ("e4m3", 3), ("e4m3", 30)])
+def test_shared_reports_bad_pages_of_a_prefix(fmt, S):
+    H, G, n, page = 2, 4, 300, 32
+    g = torch.Generator(device=DEV).manual_seed(7)
+    pc, c = Cache(1, 1, H, n, fmt, page), Cache(1, S, H, 16, fmt, 16)
+    for h in range(H):
+        pc.fill(0, 0, h, n, g)
+        for s in range(S):
+            c.fill(0, s, h, 5, g)
+    rows = [(pc.unit(pc.k, 0, 0, h, n), pc.unit(pc.v, 0, 0, h, n)) for h in range(H)]
+    keep = torch.tensor([i for i in range(n) if i // page not in (0, 4, 9)], device=DEV)
+    pc.table[0, 0], pc.table[0, 4], pc.table[0, 9] = -1, pc.k.shape[1], 1 << 30
+    q = torch.randn(S, H * G, D, generator=g, device=DEV).to(torch.bfloat16)
+    out, status = torch.empty_like(q), torch.zeros(1, dtype=torch.int32, device=DEV)
+    ctx = context(1, H, G)
+    ctx.attend_shared(tb.LayerCache(pc.view(tb, seq_lens=int32([n])), 0), int32([0, S]),
+                      tb.LayerCache(c.view(tb, seq_lens=int32([5] * S)), 0), q, out, ctx.attend_workspace(S, 1), device_status=status)
+    torch.cuda.synchronize()
+    assert int(status) == 5
+    check_rows(out, None, q, lambda s, h: tuple(torch.cat((x[keep], c.unit(t, 0, s, h, 5))) for x, t in zip(rows[h], (c.k, c.v))),
+               S, H, G, D ** -0.5, extra=U_BF16)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+def test_shared_non_finite_queries_and_rows_stay_in_their_group(fmt):
+    H, G, S, n = 2, 4, 24, 150
+    g = torch.Generator(device=DEV).manual_seed(5)
+    pc, c = Cache(1, 2, H, n, fmt), Cache(1, S, H, 8, fmt)
+    for h in range(H):
+        for p in range(2):
+            pc.fill(0, p, h, n, g)
+        for s in range(S):
+            c.fill(0, s, h, 3, g)
+    pc.k[0, 1, 0, 70, 3] = float("nan")
+    q = torch.randn(S, H * G, D, generator=g, device=DEV).to(torch.bfloat16)
+    q[4, 5, 9] = float("nan")
+    out = torch.empty_like(q)
+    ctx = context(1, H, G)
+    ctx.attend_shared(tb.LayerCache(pc.view(tb, seq_lens=int32([n, n])), 0), int32([0, 13, S]),
+                      tb.LayerCache(c.view(tb, seq_lens=int32([3] * S)), 0), q, out, ctx.attend_workspace(S, 2))
+    torch.cuda.synchronize()
+    nan = out.isnan().any(-1)
+    want = torch.zeros_like(nan)
+    want[13:, :G] = True
+    want[4, 5] = True
+    assert torch.equal(nan, want) and bool(out[want].isnan().all())
+
+
+def test_heads_that_share_one_cache_by_a_stride_of_zero():
+    """Multi-query layouts as an expanded head: prefix and own rows, against the same rows copied out."""
+    H, G, S, n = 4, 4, 10, 200
+    g = torch.Generator(device=DEV).manual_seed(6)
+    k, v = (torch.randn(1, S, 1, n, D, generator=g, device=DEV).to(torch.bfloat16) for _ in range(2))
+    pk, pv = (torch.randn(1, 1, 1, n, D, generator=g, device=DEV).to(torch.bfloat16) for _ in range(2))
+    q = torch.randn(S, H * G, D, generator=g, device=DEV).to(torch.bfloat16)
+    ctx, lens, plens, starts = context(1, H, G), int32([20 * s for s in range(S)]), int32([n]), int32([0, S])
+    outs = []
+    for f in (lambda x: x.expand(-1, -1, H, -1, -1), lambda x: x.expand(-1, -1, H, -1, -1).contiguous()):
+        src, pre = tb.LayerCache(tb.CacheView(f(k), f(v), seq_lens=lens), 0), tb.LayerCache(tb.CacheView(f(pk), f(pv), seq_lens=plens), 0)
+        a, b = torch.empty_like(q), torch.empty_like(q)
+        ctx.attend(src, q, a, ctx.attend_workspace(S))
+        ctx.attend_shared(pre, starts, src, q, b, ctx.attend_workspace(S, 1))
+        outs.append((a, b))
+    torch.cuda.synchronize()
+    assert torch.equal(raw(outs[0][0]), raw(outs[1][0]))
+    check_rows(outs[0][1], None, q, lambda s, h: tuple(torch.cat((a[0, 0, 0].double(), b[0, s, 0, :20 * s].double()))
+                                                       for a, b in ((pk, k), (pv, v))), S, H, G, D ** -0.5, extra=U_BF16)
+
+
+def test_strides_of_single_dimensions_do_not_matter():
+    ctx, H, G = context(1, 1, 1), 1, 1
+    c = Cache(1, 1, 1, 8)
+    odd = torch.randn(D, device=DEV).to(torch.bfloat16)
+    x = odd.as_strided((1, 1, 1, D), (3, 5, 7, 1))
+    lens = int32([0])
+    lc = tb.LayerCache(c.view(tb, seq_lens=lens), 0)
+    qo = torch.empty_like(odd).as_strided((1, 1, 1, D), (1, 3, 5, 1))
+    ctx.append(lc, x, x, torch.tensor([0], device=DEV), q=x, q_out=qo, new_lens=lens)
+    out = torch.empty(D, dtype=torch.bfloat16, device=DEV).as_strided((1, 1, D), (3, 5, 1))
+    ctx.attend(lc, qo.as_strided((1, 1, D), (9, 11, 1)), out, ctx.attend_workspace(1))
+    torch.cuda.synchronize()
+    assert torch.equal(out.view(-1), odd) and torch.equal(c.k[0, 0, 0, 0], odd)
+
+
 # ------------------------------------------------------------------------------------------------
 # together, on streams, in graphs
 # ------------------------------------------------------------------------------------------------
@@ -593,6 +738,47 @@ def test_decode_loop_with_windowed_compression_eager_and_captured():
         torch.cuda.synchronize()
         assert torch.equal(raw(b.out), raw(outs[i])), i
     assert torch.equal(raw(a.k), raw(b.k)) and torch.equal(a.positions, b.positions) and torch.equal(a.lens, b.lens)
+
+
+FIRST_CALL = """
+import torch
+from paper_2604_04921_b200 import binding as tb
+ctx = tb.TriContext(1, 2, 4, torch.zeros(1, 8, 128), torch.ones(1, 8, 64))
+g = torch.Generator(device="cuda").manual_seed(0)
+k, v = (torch.randn(1, 20, 2, 64, 128, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+x = torch.randn(20, 1, 12, 128, generator=g, device="cuda").to(torch.bfloat16)
+lens, pos = torch.full((20,), 5, dtype=torch.int32, device="cuda"), torch.arange(20, device="cuda")
+q, out, both = torch.empty(20, 1, 8, 128, dtype=torch.bfloat16, device="cuda"), *(torch.empty(20, 8, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+lc = tb.LayerCache(tb.CacheView(k, v, seq_lens=lens), 0)
+ws, starts = ctx.attend_workspace(20, 20), torch.zeros(21, dtype=torch.int32, device="cuda")
+starts[1:] = 20
+x2 = x.clone()
+graph = torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.graph(graph):
+    x2.copy_(x)                                  # a memory copy before the first kernel, and one in between
+    ctx.append(lc, x2[:, :, 8:10], x2[:, :, 10:], pos, q=x2[:, :, :8], q_out=q, new_lens=lens)
+    x2.copy_(x)
+    ctx.attend(lc, q[:, 0], out, ws)
+    ctx.attend_shared(lc, starts, lc, q[:, 0], both, ws)
+graph.replay()
+torch.cuda.synchronize()
+a, b = out.clone(), both.clone()
+lens.fill_(5)
+ctx.append(lc, x[:, :, 8:10], x[:, :, 10:], pos, q=x[:, :, :8], q_out=q, new_lens=lens)
+ctx.attend(lc, q[:, 0], out, ws)
+ctx.attend_shared(lc, starts, lc, q[:, 0], both, ws)
+torch.cuda.synchronize()
+assert torch.equal(a, out) and torch.equal(b, both) and bool((lens == 6).all()) and bool(a.isfinite().all())
+print("same")
+"""
+
+
+def test_first_calls_of_a_process_inside_a_capture():
+    import subprocess
+    import sys
+    r = subprocess.run([sys.executable, "-c", FIRST_CALL], capture_output=True, text=True, timeout=300, cwd=str(tb._ROOT))
+    assert r.returncode == 0 and "same" in r.stdout, r.stderr[-2000:]
 
 
 def test_two_streams_with_a_workspace_each():
@@ -692,6 +878,11 @@ def test_refusals_of_the_c_interface():
     assert append(layer_cache(stride_tok=100)) == 1
     assert append(layer_cache(unit_lens=lens.data_ptr()), pos=None) == 1
     assert append(layer_cache(Cache(2, S, H, 32, page=16), page_size=8)) == 2
+    r = tb._AppendRows(k=x.data_ptr(), v=x.data_ptr(), kind=0, T=T, pos=pos.data_ptr(), n_new=lens.data_ptr())
+    for p in ("k", "v"):
+        for n, st in zip(("seq", "tok", "head"), x.stride()):
+            setattr(r, f"{p}_stride_{n}", st)
+    assert lib.tri_append(ctx._h, ctypes.byref(layer_cache()), S, ctypes.byref(r), lens.data_ptr(), None, None) == 1
 
     def attend(lc=None, S=S, bytes=None, w=None, h=ctx._h, **kw):
         io = tb._AttendIo(q.data_ptr(), *q.stride()[:2], out.data_ptr(), *out.stride()[:2], None, 0.1)
@@ -707,6 +898,8 @@ def test_refusals_of_the_c_interface():
     assert attend(q=None) == 1 and attend(out=None) == 1 and attend(q=q.data_ptr() + 2) == 1 and attend(q_stride_head=4) == 1
     assert attend(scale=float("nan")) == 1 and attend(scale=float("inf")) == 1
     assert attend(layer_cache(v=None)) == 1 and attend(layer_cache(seq_lens=None)) == 1 and attend(layer_cache(layer=2)) == 1
+    assert attend(out=q.data_ptr()) == 1
+    assert attend(layer_cache(n_max=2 ** 31 - 1), S=64) == 2                    # the line of steps would pass 2^31
     assert attend(layer_cache(k_kind=2)) == 2 and attend(layer_cache(Cache(2, S, H, 32, "f32"))) == 2
     assert lib.tri_attend_workspace_bytes(None, 1, 0) == 0 and lib.tri_attend_workspace_bytes(ctx._h, 0, 0) == 0
     assert lib.tri_attend_workspace_bytes(ctx._h, 1, -1) == 0
@@ -739,7 +932,7 @@ def test_refusals_of_the_binding():
                 lambda: ctx.append(lc, x, x, pos, new_lens=int32([0])), lambda: ctx.attend(lc, q[:1], q[:1], ws),
                 lambda: ctx.attend(lc, q.float(), q, ws), lambda: ctx.attend(lc, q.cpu(), q, ws),
                 lambda: ctx.attend(lc, q, q.clone(), ws.cpu()), lambda: ctx.attend(lc, q, q.clone(), ws, lse=q),
-                lambda: tb.LayerCache(c.view(tb), 0), lambda: tb.LayerCache(c.view(tb, seq_lens=int32([0, 0])), 1),
+                lambda: tb.LayerCache(c.view(tb), 0), lambda: tb.LayerCache(c.view(tb, seq_lens=int32([0, 0]), n_max=33), 0), lambda: tb.LayerCache(c.view(tb, seq_lens=int32([0, 0])), 1),
                 lambda: tb.LayerCache(c.view(tb, seq_lens=torch.zeros(2, dtype=torch.int32)), 0),
                 lambda: ctx.attend_shared(lc, int32([0, 1]), lc, q, q.clone(), ws)):
         with pytest.raises(AssertionError):
