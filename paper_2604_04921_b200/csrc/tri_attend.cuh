@@ -675,28 +675,28 @@ __global__ void __launch_bounds__(kMergeThreads) k_attend_merge(const MergeParam
     __shared__ float2 red_ml[kMergeWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int per = p.G / p.rows, unit = blockIdx.x / per, s = unit / p.H, h = unit - s * p.H;
-    grid_dependency_wait();
-    grid_dependents_launch();
-    const int2 own = p.own.rec[unit];
-    if (!p.pre.rec && own.y < 2) return;                                     // finished by its block
-    int2 pre = make_int2(0, 0);
-    int row0 = 0;
+    // the sequence's group, before the passes are waited for: they began behind whatever wrote group_start
+    int pre_rec = -1, row0 = 0;
     if (p.pre.rec) {
-        // the group of this sequence: the last one that starts at or before it
-        int lo = -1;
+        int lo = -1;                                                         // the last group that starts at or before it
         for (int b = 0; b < p.P; b += 32)
             lo += __popc(__ballot_sync(0xffffffffu, b + lane < p.P && __ldg(p.group_start + min(b + lane, p.P - 1)) <= s));
         lo = max(lo, 0);
         const int2 g = att_group(p.group_start, p.S, lo);
         if (s >= g.x && s < g.x + g.y) {
             const int rt = (s - g.x) / p.pre.spt;
-            pre = p.pre.rec[(int64_t)att_tile_index(lo, g.x, p.pre.spt, rt) * p.H + h];
+            pre_rec = att_tile_index(lo, g.x, p.pre.spt, rt) * p.H + h;
             row0 = (s - g.x - rt * p.pre.spt) * p.G;
         }
         if (blockIdx.x == 0 && p.device_status)
             for (int i = threadIdx.x; i < p.P; i += kMergeThreads)
                 if (__ldg(p.group_start + i) > __ldg(p.group_start + i + 1)) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
     }
+    grid_dependency_wait();
+    grid_dependents_launch();
+    const int2 own = p.own.rec[unit];
+    if (!p.pre.rec && own.y < 2) return;                                     // finished by its block
+    const int2 pre = pre_rec >= 0 ? p.pre.rec[pre_rec] : make_int2(0, 0);
     const int parts = own.y + pre.y;
     const int wpr = kMergeWarps / p.rows, r = warp / wpr, sub = warp - r * wpr, g = ((int)blockIdx.x - unit * per) * p.rows + r;
     const bool active = r < p.rows;
