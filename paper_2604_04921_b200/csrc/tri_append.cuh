@@ -12,6 +12,7 @@
 // band, and used from registers for every head.
 #pragma once
 #include "tri_score_tma.cuh"
+#include "tri_step.cuh"
 
 namespace tri {
 

@@ -18,6 +18,7 @@
 // so every block finds its share by a sum over them.
 #pragma once
 #include "tri_score_tma.cuh"
+#include "tri_step.cuh"
 
 namespace tri {
 

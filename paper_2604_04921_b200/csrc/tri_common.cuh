@@ -42,10 +42,6 @@ __device__ __forceinline__ int64_t row_offset(const View &w, int l, int s, int h
            (int64_t)(n - pg * w.page_size) * w.stride_slot;
 }
 
-// Programmatic dependent launch: waits for the kernels this launch depends on; lets a launch that depends on this kernel begin.
-__device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
-__device__ __forceinline__ void grid_dependents_launch() { asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory"); }
-
 // Order-preserving image of an fp32 in uint32: a > b  <=>  key(a) > key(b) (for non-NaN values); -0.0 and
 // +0.0 are equal scores and get the same image.  Never 0 for a non-NaN input.
 __device__ __forceinline__ uint32_t float_key(float x)
