@@ -428,6 +428,8 @@ cudaError_t allow_umma_smem()
 template <bool KEY8, int RT>
 cudaError_t allow_attend_smem()
 {
+    cudaError_t e = cudaFuncSetAttribute(k_attend<KEY8, RT, kAttCluster>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttRingBytes);
+    if (e != cudaSuccess) return e;
     return cudaFuncSetAttribute(k_attend<KEY8, RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttRingBytes);
 }
 
@@ -1171,18 +1173,26 @@ tri_status check_layer_cache(const tri_ctx *c, const tri_layer_cache *lc, int32_
     return TRI_OK;
 }
 
+template <typename Kernel, typename... Params>
+cudaError_t launch_clusters(Kernel kernel, unsigned cluster, unsigned blocks, unsigned threads, size_t smem, cudaStream_t st, const Params &...p)
+{
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cfg.attrs = attr; cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, p...);
+}
+
 // A launch that may be set up and started while the kernel before it in the stream still runs: the kernel itself waits for
 // that one (grid_dependency_wait) before it touches memory.  Takes about a microsecond off each launch of a chain.
 template <typename Kernel, typename... Params>
 cudaError_t launch_under(Kernel kernel, unsigned blocks, unsigned threads, size_t smem, cudaStream_t st, const Params &...p)
 {
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(blocks); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
-    cfg.attrs = &attr; cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, p...);
+    return launch_clusters(kernel, 1, blocks, threads, smem, st, p...);
 }
 
 // Rows of `es`-byte elements that start on 16-byte boundaries.
@@ -1315,6 +1325,13 @@ cudaError_t launch_attend(int rows, unsigned blocks, cudaStream_t st, const Atte
                      : launch_under(k_attend<KEY8, 16>, blocks, kAttThreads, kAttRingBytes, st, p);
 }
 
+template <bool KEY8>
+cudaError_t launch_attend_clusters(int rows, unsigned units, cudaStream_t st, const AttendParams &p)
+{
+    return rows == 8 ? launch_clusters(k_attend<KEY8, 8, kAttCluster>, kAttCluster, units * kAttCluster, kAttThreads, kAttRingBytes, st, p)
+                     : launch_clusters(k_attend<KEY8, 16, kAttCluster>, kAttCluster, units * kAttCluster, kAttThreads, kAttRingBytes, st, p);
+}
+
 tri_status check_attend_cache(const tri_ctx *c, const tri_layer_cache *lc, int32_t n)
 {
     tri_status r = check_layer_cache(c, lc, n);
@@ -1406,6 +1423,11 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
     p.finish = P > 0 ? 0 : 1; p.under = P > 0 ? 1 : 0;
     p.rec = (int2 *)(w + pl.own_rec); p.slots = (float *)(w + pl.own_slots);
     p.whole = P > 0 ? (float *)(w + pl.own_whole) : nullptr;
+    if (P == 0 && (int64_t)S * H * kAttCluster <= pl.blocks && src->view->n_max <= kAttClusterRows) {
+        if (src->view->k_kind == 3) TRI_CUDA(launch_attend_clusters<true>(pl.own_rows, (unsigned)(S * H), st, p));
+        else TRI_CUDA(launch_attend_clusters<false>(pl.own_rows, (unsigned)(S * H), st, p));
+        return TRI_OK;
+    }
     if (src->view->k_kind == 3) TRI_CUDA(launch_attend<true>(pl.own_rows, (unsigned)pl.blocks, st, p));
     else TRI_CUDA(launch_attend<false>(pl.own_rows, (unsigned)pl.blocks, st, p));
 

@@ -17,6 +17,8 @@
 // first unit and one for its last, and k_attend_merge joins them in a fixed order.  The lengths are on the device only,
 // so every block finds its share by a sum over them.
 #pragma once
+#include <cuda_bf16.h>
+
 #include "tri_score_tma.cuh"
 #include "tri_step.cuh"
 
@@ -27,6 +29,10 @@ constexpr int kAttStages = 2, kAttStageBytes = 8192;             // K and V of 1
 constexpr int kAttRingBytes = kAttWarps * kAttStages * kAttStageBytes;
 template <bool KEY8> constexpr int kAttRows = KEY8 ? 32 : 16;    // rows of a warp's step; a tile is one step of all warps
 constexpr int kAttUnitCost = 2;                                  // a unit's own cost, in tiles
+// Few units with room for few rows go to clusters of 8 blocks, one unit each, in one launch: for one sequence of 8 heads
+// 5.2 against 7.9 us at 600 rows, 6.9 against 9.0 at 2,176, equal at 4,352, 13.4 against 11.4 at 8,192, where cutting the
+// unit over the whole GPU wins.  (The lengths are on the device: the rule goes by the view's capacity.)
+constexpr int kAttCluster = 8, kAttClusterRows = 4352;
 constexpr int kAttRowPitch = kHeadDim + 4;                       // floats per row of a part: 128 sums, m, l, two unused
 // A weight is 2^(x - m).  The bound m is raised, to kAttBelow under the largest logit, when one passes it by kAttAbove.  As
 // bf16 a weight has the range of fp32.  An f16 ends at 2^16 and 2^-24, and a million rows each 2^-26 of the largest are mass:
@@ -260,7 +266,9 @@ __device__ __forceinline__ bool att_next(const AttendParams &p, const AttShare &
 // KEY8: e4m3 rows, widened exactly to f16 (the queries are brought to f16 by a power of two per row).
 // RT = 8: at most 8 query rows; the rest of the rounded weights rides in the upper 8 rows of the 16-row MMA, for free.
 // RT = 16: up to 16 query rows; that rest takes a second MMA.
-template <bool KEY8, int RT>
+// CL > 0: a cluster of CL blocks takes one unit, cuts it evenly, and joins its parts through distributed shared memory: one
+// launch and no workspace where there are few short units.
+template <bool KEY8, int RT, int CL = 0>
 __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const AttendParams p)
 {
     constexpr int ST = kAttStages, ROWS = kAttRows<KEY8>, NK = ROWS / 16, TILE = kAttWarps * ROWS;
@@ -269,6 +277,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
     constexpr int NR = RT / 8;                            // query rows per thread
     extern __shared__ __align__(128) uint8_t dyn[];
     __shared__ float2 stat[kAttWarps][RT];
+    __shared__ __align__(16) float part[CL ? RT : 1][kAttRowPitch];      // this block's sums, and (m, l)
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
     const uint32_t ring = smem_u32(dyn) + warp * (ST * kAttStageBytes);
@@ -281,8 +290,29 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
     // this pass's may follow one by one: that pass began behind everything this one reads, and it is waited for at the end.
     if (!p.under) grid_dependency_wait();
     grid_dependents_launch();
-    const AttShare sh = att_share<TILE, kAttUnitCost>(p);
-    if ((int)blockIdx.x >= sh.shares) return;
+    AttShare sh = {};
+    int rank = 0;
+    if constexpr (CL == 0) {
+        sh = att_share<TILE, kAttUnitCost>(p);
+        if ((int)blockIdx.x >= sh.shares) return;
+    } else {
+        asm volatile("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(rank));
+        sh.seq = (int)blockIdx.x / CL / p.H; sh.h = (int)blockIdx.x / CL - sh.seq * p.H;
+        if (tid < RT) { part[CL ? tid : 0][kHeadDim] = -INFINITY; part[CL ? tid : 0][kHeadDim + 1] = 0.f; }      // no rows so far
+    }
+    auto next_unit = [&](AttCursor &c, AttJob &u) -> bool {
+        if constexpr (CL == 0) {
+            return att_next<TILE, kAttUnitCost>(p, sh, c, u);
+        } else {
+            if (c.rt) return false;
+            c.rt = 1;
+            u.seq = c.seq; u.h = c.h; u.nrows = p.G; u.first_seq = c.seq; u.len = att_len(p, c.seq, c.h);
+            u.kt = (int)(((uint32_t)u.len + TILE - 1) / TILE);
+            u.ka = rank * u.kt / CL; u.kb = (rank + 1) * u.kt / CL;
+            u.begins = u.complete = false;
+            return true;
+        }
+    };
 
     // ---------------- copies: a cursor of their own, ST - 1 steps ahead ----------------
     AttCursor pc = {sh.seq, sh.h, 0, sh.start};
@@ -298,7 +328,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
     const int64_t step_row = p.src.paged ? p.src.stride_slot : p.src.stride_tok;
     auto advance = [&]() {                                // to the next step, its pages looked up before they are needed
         if (pit == pj.kb) {
-            do more = att_next<TILE, kAttUnitCost>(p, sh, pc, pj); while (more && pj.kb <= pj.ka);
+            do more = next_unit(pc, pj); while (more && pj.kb <= pj.ka);
             pit = pj.ka;
             unit_base = (int64_t)p.layer * p.src.stride_layer + (int64_t)pj.h * p.src.stride_head +
                         (p.src.paged ? 0 : (int64_t)pj.seq * p.src.stride_seq);
@@ -382,7 +412,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
         if (it == j.kb) {
             // ---------------- the next unit ----------------
             bool rows = false;
-            while (!rows && att_next<TILE, kAttUnitCost>(p, sh, cur, j)) {
+            while (!rows && next_unit(cur, j)) {
                 if (j.begins && tid == 0) p.rec[j.rec] = att_record(sh, j);
                 rows = j.kb > j.ka;
                 if (j.kt == 0 && j.begins && p.finish)    // no rows: zeros
@@ -602,8 +632,9 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
             const float by = final ? (ll == 0.f ? 0.f : vs / ll) : vs;
             const int sr = p.spt ? att_small_div(r, inv_g) : 0, sq = p.spt ? j.first_seq + sr : j.seq, hq = j.h * p.G + r - sr * p.G;
             char *out = p.out + ((int64_t)sq * p.out_seq + (int64_t)hq * p.out_head) * 2;
-            float *to = j.complete ? p.whole + ((int64_t)sq * p.H * p.G + hq) * kAttRowPitch
-                                   : p.slots + (((int64_t)blockIdx.x * 2 + (j.begins ? 1 : 0)) * RT + r) * kAttRowPitch;
+            float *to = CL ? part[CL ? r : 0]
+                           : (j.complete ? p.whole + ((int64_t)sq * p.H * p.G + hq) * kAttRowPitch
+                                         : p.slots + (((int64_t)blockIdx.x * 2 + (j.begins ? 1 : 0)) * RT + r) * kAttRowPitch);
 #pragma unroll
             for (int q2 = 0; q2 < 2; ++q2) {
                 const int q = 2 * warp + q2;               // fragments 2 q, 2 q + 1
@@ -638,6 +669,37 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
         __syncthreads();                                   // the stages may be refilled
     }
     cp_wait<0>();
+    if constexpr (CL > 0) {
+        // every block of the cluster joins 128 / CL dims of all rows
+        constexpr int DIMS = kHeadDim / (CL ? CL : 1);
+        asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+        for (int i = tid; i < p.G * DIMS; i += kAttThreads) {
+            const int r = i / DIMS, d = rank * DIMS + i % DIMS;
+            float x[CL], pm[CL], pl[CL], mm = -INFINITY;
+#pragma unroll
+            for (int b = 0; b < CL; ++b) {
+                const uint32_t row = smem_u32(part[r]);
+                uint32_t peer;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(peer) : "r"(row), "r"(b));
+                asm volatile("ld.shared::cluster.f32 %0, [%1];\n" : "=f"(x[b]) : "r"(peer + 4 * d));
+                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];\n" : "=f"(pm[b]), "=f"(pl[b]) : "r"(peer + 4 * kHeadDim));
+                mm = fmaxf(mm, pm[b]);
+            }
+            float y = 0.f, ll = 0.f;
+#pragma unroll
+            for (int b = 0; b < CL; ++b) {
+                if (pm[b] == -INFINITY && !(pl[b] != pl[b])) continue;         // no rows there (a NaN sum stays)
+                const float by = pm[b] == -INFINITY ? 1.f : ex2(pm[b] - mm);
+                y += x[b] * by;
+                ll += pl[b] * by;
+            }
+            const int hq = sh.h * p.G + r;
+            *reinterpret_cast<__nv_bfloat16 *>(p.out + ((int64_t)sh.seq * p.out_seq + (int64_t)hq * p.out_head) * 2 + 2 * d) =
+                __float2bfloat16_rn(ll == 0.f ? 0.f : y / ll);
+            if (p.lse && d == 0) p.lse[(int64_t)sh.seq * p.H * p.G + hq] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.69314718f;
+        }
+        asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");   // peers have read
+    }
     if (p.under) grid_dependency_wait();                  // not through before the pass over prefixes is
 }
 

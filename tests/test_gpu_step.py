@@ -268,6 +268,21 @@ def test_attend_group_sizes_and_edge_lengths(fmt, G):
     check_attend(fmt, 16, "heads", 2, G, EDGES, scales=fmt == "e4m3", seed=G)
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("G", [1, 4, 7, 8, 16])
+@pytest.mark.parametrize("S,rows", [(40, None), (5, 6000)])
+def test_attend_edge_lengths_where_units_are_cut_over_the_gpu(fmt, G, S, rows):
+    """More units than clusters of blocks hold at a time, or room for more rows than they take."""
+    check_attend(fmt, 16, "heads", 2, G, [EDGES[(5 * s) % len(EDGES)] for s in range(S)], scales=fmt == "e4m3", seed=G, rows=rows)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("n", [63, 64, 65, 511, 512, 513, 1024, 2176, 4351, 4352, 4353])
+def test_attend_few_units_around_the_cluster_limits(fmt, n):
+    check_attend(fmt, 0, "tokens", 1, 4, [n], seed=n)
+    check_attend(fmt, 16, "heads", 2, 12, [n // 2, n, 0], per_head=False, seed=n)
+
+
 @pytest.mark.parametrize("fmt,page,order", [("bf16", 0, "heads"), ("bf16", 0, "tokens"), ("bf16", 0, "padded"),
                                             ("bf16", 48, "heads"), ("bf16", 64, "tokens"), ("bf16", 32, "padded"),
                                             ("e4m3", 0, "heads"), ("e4m3", 0, "tokens"), ("e4m3", 48, "padded")])
