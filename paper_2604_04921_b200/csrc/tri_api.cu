@@ -428,7 +428,7 @@ cudaError_t allow_umma_smem()
 template <bool KEY8, int RT>
 cudaError_t allow_attend_smem()
 {
-    cudaError_t e = cudaFuncSetAttribute(k_attend<KEY8, RT, kAttCluster>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttRingBytes);
+    cudaError_t e = cudaFuncSetAttribute(k_attend_cluster<KEY8, RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttRingBytes);
     if (e != cudaSuccess) return e;
     return cudaFuncSetAttribute(k_attend<KEY8, RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttRingBytes);
 }
@@ -1326,10 +1326,10 @@ cudaError_t launch_attend(int rows, unsigned blocks, cudaStream_t st, const Atte
 }
 
 template <bool KEY8>
-cudaError_t launch_attend_clusters(int rows, unsigned units, cudaStream_t st, const AttendParams &p)
+cudaError_t launch_attend_clusters(int rows, unsigned units, cudaStream_t st, const AttendParams &p, const AttendParams &pre)
 {
-    return rows == 8 ? launch_clusters(k_attend<KEY8, 8, kAttCluster>, kAttCluster, units * kAttCluster, kAttThreads, kAttRingBytes, st, p)
-                     : launch_clusters(k_attend<KEY8, 16, kAttCluster>, kAttCluster, units * kAttCluster, kAttThreads, kAttRingBytes, st, p);
+    return rows == 8 ? launch_clusters(k_attend_cluster<KEY8, 8>, kAttCluster, units * kAttCluster, kAttThreads, kAttRingBytes, st, p, pre)
+                     : launch_clusters(k_attend_cluster<KEY8, 16>, kAttCluster, units * kAttCluster, kAttThreads, kAttRingBytes, st, p, pre);
 }
 
 tri_status check_attend_cache(const tri_ctx *c, const tri_layer_cache *lc, int32_t n)
@@ -1394,6 +1394,23 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
     if (ws_bytes < pl.total) return TRI_ERR_WORKSPACE;
     char *w = (char *)ws;
 
+    // few short units, prefixes included: one launch (the rows of a prefix are then read for each of its sequences, from L2)
+    if ((int64_t)S * H * kAttCluster <= pl.blocks &&
+        (int64_t)src->view->n_max + (P > 0 ? prefix->view->n_max : 0) <= kAttClusterRows &&
+        (P == 0 || prefix->view->k_kind == src->view->k_kind)) {
+        AttendParams p = attend_params(c, src, S, S, io, device_status), pre = p;
+        p.finish = 1;
+        p.rec = nullptr; p.slots = p.whole = nullptr;
+        pre.nseq = 0;
+        if (P > 0) {
+            pre = attend_params(c, prefix, P, S, io, device_status);
+            pre.group_start = group_start;
+        }
+        if (src->view->k_kind == 3) TRI_CUDA(launch_attend_clusters<true>(pl.own_rows, (unsigned)(S * H), st, p, pre));
+        else TRI_CUDA(launch_attend_clusters<false>(pl.own_rows, (unsigned)(S * H), st, p, pre));
+        return TRI_OK;
+    }
+
     MergeParams mp;
     mp.pre.rec = nullptr; mp.pre.slots = mp.pre.whole = nullptr; mp.pre.rows = 0; mp.pre.spt = 0;
     if (P > 0) {
@@ -1423,11 +1440,6 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
     p.finish = P > 0 ? 0 : 1; p.under = P > 0 ? 1 : 0;
     p.rec = (int2 *)(w + pl.own_rec); p.slots = (float *)(w + pl.own_slots);
     p.whole = P > 0 ? (float *)(w + pl.own_whole) : nullptr;
-    if (P == 0 && (int64_t)S * H * kAttCluster <= pl.blocks && src->view->n_max <= kAttClusterRows) {
-        if (src->view->k_kind == 3) TRI_CUDA(launch_attend_clusters<true>(pl.own_rows, (unsigned)(S * H), st, p));
-        else TRI_CUDA(launch_attend_clusters<false>(pl.own_rows, (unsigned)(S * H), st, p));
-        return TRI_OK;
-    }
     if (src->view->k_kind == 3) TRI_CUDA(launch_attend<true>(pl.own_rows, (unsigned)pl.blocks, st, p));
     else TRI_CUDA(launch_attend<false>(pl.own_rows, (unsigned)pl.blocks, st, p));
 

@@ -81,6 +81,14 @@ __device__ __forceinline__ int att_row_tiles(const AttendParams &p, int seq)
     if (p.spt == 0) return 1;
     return (att_group(p.group_start, p.S, seq).y + p.spt - 1) / p.spt;
 }
+// The last group that starts at or before a sequence (0 if none does); the warp's lanes look at 32 starts at a time.
+__device__ __forceinline__ int att_group_of(const int32_t *start, int groups, int seq, int lane)
+{
+    int g = -1;
+    for (int b = 0; b < groups; b += 32)
+        g += __popc(__ballot_sync(0xffffffffu, b + lane < groups && __ldg(start + min(b + lane, groups - 1)) <= seq));
+    return max(g, 0);
+}
 // Index of tile `rt` of group g in units before the head is added: the tiles of ascending groups never collide, and no
 // index reaches P + S / spt + 1 whatever group_start holds.
 __device__ __forceinline__ int att_tile_index(int g, int first, int spt, int rt) { return g + first / spt + rt; }
@@ -150,6 +158,7 @@ struct AttJob {
     int rec;                          // index of the unit's record
     int rows0;                        // step of the unit's first tile
     bool begins, complete;            // the unit's first step is here (its part goes to the last slot); all tiles are here
+    bool of_prefix;                   // in a cluster: rows of the sequence's prefix, not its own
 };
 
 // The share of this block.  Where the heads of a sequence have equal lengths the sums run over sequences only.
@@ -267,9 +276,10 @@ __device__ __forceinline__ bool att_next(const AttendParams &p, const AttShare &
 // RT = 8: at most 8 query rows; the rest of the rounded weights rides in the upper 8 rows of the 16-row MMA, for free.
 // RT = 16: up to 16 query rows; that rest takes a second MMA.
 // CL > 0: a cluster of CL blocks takes one unit, cuts it evenly, and joins its parts through distributed shared memory: one
-// launch and no workspace where there are few short units.
-template <bool KEY8, int RT, int CL = 0>
-__global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const AttendParams p)
+// launch and no workspace where there are few short units.  `pre` (pre.nseq > 0): the prefixes; a unit is then the rows of
+// its sequence's prefix, if it has one, and its own.
+template <bool KEY8, int RT, int CL>
+__device__ __forceinline__ void attend_block(const AttendParams &p, const AttendParams &pre)
 {
     constexpr int ST = kAttStages, ROWS = kAttRows<KEY8>, NK = ROWS / 16, TILE = kAttWarps * ROWS;
     constexpr int kRowBytes = KEY8 ? 128 : 256, kHalf = ROWS * kRowBytes;                             // K | V
@@ -290,8 +300,12 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
     // this pass's may follow one by one: that pass began behind everything this one reads, and it is waited for at the end.
     if (!p.under) grid_dependency_wait();
     grid_dependents_launch();
+    auto params_of = [&](const AttJob &u) -> const AttendParams & {
+        if constexpr (CL == 0) return p;
+        else return u.of_prefix ? pre : p;
+    };
     AttShare sh = {};
-    int rank = 0;
+    int rank = 0, group = -1;                             // in a cluster: this block's number, the sequence's prefix
     if constexpr (CL == 0) {
         sh = att_share<TILE, kAttUnitCost>(p);
         if ((int)blockIdx.x >= sh.shares) return;
@@ -299,14 +313,24 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
         asm volatile("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(rank));
         sh.seq = (int)blockIdx.x / CL / p.H; sh.h = (int)blockIdx.x / CL - sh.seq * p.H;
         if (tid < RT) { part[CL ? tid : 0][kHeadDim] = -INFINITY; part[CL ? tid : 0][kHeadDim + 1] = 0.f; }      // no rows so far
+        if (pre.nseq > 0) {
+            group = att_group_of(pre.group_start, pre.nseq, sh.seq, lane);
+            const int2 g = att_group(pre.group_start, pre.S, group);
+            if (sh.seq < g.x || sh.seq >= g.x + g.y) group = -1;
+            if (blockIdx.x == 0 && p.device_status)
+                for (int i = tid; i < pre.nseq; i += kAttThreads)
+                    if (__ldg(pre.group_start + i) > __ldg(pre.group_start + i + 1)) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
+        }
     }
     auto next_unit = [&](AttCursor &c, AttJob &u) -> bool {
         if constexpr (CL == 0) {
             return att_next<TILE, kAttUnitCost>(p, sh, c, u);
         } else {
-            if (c.rt) return false;
-            c.rt = 1;
-            u.seq = c.seq; u.h = c.h; u.nrows = p.G; u.first_seq = c.seq; u.len = att_len(p, c.seq, c.h);
+            if (c.rt == 0 && group < 0) c.rt = 1;
+            if (c.rt > 1) return false;
+            u.of_prefix = c.rt++ == 0;
+            u.seq = u.of_prefix ? group : c.seq; u.h = c.h; u.nrows = p.G; u.first_seq = c.seq;
+            u.len = att_len(params_of(u), u.seq, c.h);
             u.kt = (int)(((uint32_t)u.len + TILE - 1) / TILE);
             u.ka = rank * u.kt / CL; u.kb = (rank + 1) * u.kt / CL;
             u.begins = u.complete = false;
@@ -325,26 +349,30 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
     uint64_t policy;
     if (p.spt) asm("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;\n" : "=l"(policy));
     else asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;\n" : "=l"(policy));
-    const int64_t step_row = p.src.paged ? p.src.stride_slot : p.src.stride_tok;
+    int64_t step_row = 0;                                 // elements between rows
     auto advance = [&]() {                                // to the next step, its pages looked up before they are needed
         if (pit == pj.kb) {
             do more = next_unit(pc, pj); while (more && pj.kb <= pj.ka);
             pit = pj.ka;
-            unit_base = (int64_t)p.layer * p.src.stride_layer + (int64_t)pj.h * p.src.stride_head +
-                        (p.src.paged ? 0 : (int64_t)pj.seq * p.src.stride_seq);
+            const AttendParams &a = params_of(pj);
+            step_row = a.src.paged ? a.src.stride_slot : a.src.stride_tok;
+            unit_base = (int64_t)a.layer * a.src.stride_layer + (int64_t)pj.h * a.src.stride_head +
+                        (a.src.paged ? 0 : (int64_t)pj.seq * a.src.stride_seq);
         }
-        if (more && p.src.paged) {
+        const AttendParams &a = params_of(pj);
+        if (more && a.src.paged) {
 #pragma unroll
             for (int half = 0; half < NK; ++half) {
                 const uint32_t r = (uint32_t)pit * TILE + warp * ROWS + 16 * half;
-                const uint32_t pg = p.src.page_shift >= 0 ? r >> p.src.page_shift : r / (uint32_t)p.src.page_size;
-                page[half] = r < (uint32_t)pj.len ? __ldg(p.src.page_table + (int64_t)pj.seq * p.src.max_pages_per_seq + pg) : 0;
-                slot[half] = (int)(r - pg * (uint32_t)p.src.page_size);
+                const uint32_t pg = a.src.page_shift >= 0 ? r >> a.src.page_shift : r / (uint32_t)a.src.page_size;
+                page[half] = r < (uint32_t)pj.len ? __ldg(a.src.page_table + (int64_t)pj.seq * a.src.max_pages_per_seq + pg) : 0;
+                slot[half] = (int)(r - pg * (uint32_t)a.src.page_size);
             }
         }
     };
     auto issue = [&]() {
         if (more) {
+            const View &src = params_of(pj).src;
             const uint32_t dst = ring + pstage * kAttStageBytes;
             constexpr int es = KEY8 ? 1 : 2;
             const int c = lane % kChunks, r0 = lane / kChunks;
@@ -354,9 +382,9 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
                 const uint32_t r = (uint32_t)pit * TILE + warp * ROWS + 16 * half;
                 int have = r < (uint32_t)pj.len ? min(pj.len - (int)r, 16) : 0;
                 int64_t base = unit_base;
-                if (p.src.paged) {
-                    base += (int64_t)page[half] * p.src.stride_page + (int64_t)slot[half] * step_row;
-                    if (have && p.src.n_pages > 0 && (uint32_t)page[half] >= (uint32_t)p.src.n_pages) {
+                if (src.paged) {
+                    base += (int64_t)page[half] * src.stride_page + (int64_t)slot[half] * step_row;
+                    if (have && src.n_pages > 0 && (uint32_t)page[half] >= (uint32_t)src.n_pages) {
                         have = 0;
                         miss |= 1u << half;
                         if (lane == 0 && p.device_status) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
@@ -371,8 +399,8 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
 #pragma unroll
                     for (int i = 0; i < kCopies / NK; ++i) {
                         const uint32_t off = i * kRowsAtOnce * kRowBytes + (((c & 8) | ((c ^ (i * kRowsAtOnce + r0)) & 7)) << 4);
-                        cp_async16(to + off, p.src.k + from, 16u, policy);
-                        cp_async16(to + kHalf + off, p.src.v + from, 16u, policy);
+                        cp_async16(to + off, src.k + from, 16u, policy);
+                        cp_async16(to + kHalf + off, src.v + from, 16u, policy);
                         from += kRowsAtOnce * step_row * es;
                     }
                 } else {
@@ -383,8 +411,8 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
                         const bool there = rr < have;
                         const int64_t at = there ? from : 16 * c;
                         const uint32_t off = i * kRowsAtOnce * kRowBytes + (((c & 8) | ((c ^ rr) & 7)) << 4);
-                        cp_async16(to + off, p.src.k + at, there ? 16u : 0u, policy);
-                        cp_async16(to + kHalf + off, p.src.v + at, there ? 16u : 0u, policy);
+                        cp_async16(to + off, src.k + at, there ? 16u : 0u, policy);
+                        cp_async16(to + kHalf + off, src.v + at, there ? 16u : 0u, policy);
                         from += kRowsAtOnce * step_row * es;
                     }
                 }
@@ -402,7 +430,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
     AttJob j = {};
     uint32_t qa[8][4];
     const int inv_g = 65536 / p.G + 1;
-    float mul[NR];                                        // logit in base-2 units per accumulator unit
+    float mul[NR], k_scale = 1.f;                         // logit in base-2 units per accumulator unit
     float o[16][4], m[NR], l[NR];
     int it = 0, stage = 0, ahead = ST - 1;
     for (;;) {
@@ -432,7 +460,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
                 const bool have = r < j.nrows && (RT == 16 || i == 0);
                 const char *qr = nullptr;
                 if (have) {
-                    const int sr = p.spt ? att_small_div(r, inv_g) : 0, sq = p.spt ? j.first_seq + sr : j.seq, gg = r - sr * p.G;
+                    const int sr = p.spt ? att_small_div(r, inv_g) : 0, sq = j.first_seq + sr, gg = r - sr * p.G;
                     qr = p.q + ((int64_t)sq * p.q_seq + (int64_t)(j.h * p.G + gg) * p.q_head) * 2;
                 }
                 float amax = 0.f;
@@ -466,12 +494,15 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
                             qa[k][i + 2 * x] = f16_bits(bf16_lo(w) * by) | (f16_bits(bf16_hi(w) * by) << 16);
                         }
                 }
-                if (i < NR) mul[i % NR] = p.scale * (p.k_scale ? __ldg(p.k_scale + j.h) : 1.f) * back;
+                if (i < NR) mul[i % NR] = p.scale * back;
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) { o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f; }
 #pragma unroll
             for (int i = 0; i < NR; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
+            k_scale = params_of(j).k_scale ? __ldg(params_of(j).k_scale + j.h) : 1.f;
+#pragma unroll
+            for (int i = 0; i < NR; ++i) mul[i] *= k_scale;
         }
 
         // ---------------- one step ----------------
@@ -597,6 +628,26 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
         uint8_t *used = dyn + (warp * ST + stage) * kAttStageBytes;
         stage = stage + 1 == ST ? 0 : stage + 1;
         if (++it < j.kb) continue;
+        float vs = params_of(j).v_scale ? __ldg(params_of(j).v_scale + j.h) : 1.f;
+        if constexpr (CL > 0) {
+            // the prefix's rows are through: the sequence's own go on with the same sums, in units of their own scales
+            const float k_before = k_scale, v_before = vs;
+            bool own = false;
+            while (!own && next_unit(cur, j)) own = j.kb > j.ka;
+            if (own) {
+                it = j.ka;
+                k_scale = params_of(j).k_scale ? __ldg(params_of(j).k_scale + j.h) : 1.f;
+                vs = params_of(j).v_scale ? __ldg(params_of(j).v_scale + j.h) : 1.f;
+                const float k_by = k_scale / k_before, v_by = v_before / vs;
+#pragma unroll
+                for (int i = 0; i < NR; ++i) mul[i] *= k_by;
+#pragma unroll
+                for (int n = 0; n < 16; ++n)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) o[n][x] *= v_by;
+                continue;
+            }
+        }
 
         // ---------------- the unit's rows of this share are through: join the warps ----------------
         // each leaves its sums in the stage it has just read, fragment by fragment, and takes a quarter of the dims of all
@@ -615,7 +666,6 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
             }
         }
         __syncthreads();
-        const float vs = p.v_scale ? __ldg(p.v_scale + j.h) : 1.f;
         const bool final = j.complete && p.finish;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
@@ -630,7 +680,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
                 ll += st[w2].y * st[w2].x;
             }
             const float by = final ? (ll == 0.f ? 0.f : vs / ll) : vs;
-            const int sr = p.spt ? att_small_div(r, inv_g) : 0, sq = p.spt ? j.first_seq + sr : j.seq, hq = j.h * p.G + r - sr * p.G;
+            const int sr = p.spt ? att_small_div(r, inv_g) : 0, sq = j.first_seq + sr, hq = j.h * p.G + r - sr * p.G;
             char *out = p.out + ((int64_t)sq * p.out_seq + (int64_t)hq * p.out_head) * 2;
             float *to = CL ? part[CL ? r : 0]
                            : (j.complete ? p.whole + ((int64_t)sq * p.H * p.G + hq) * kAttRowPitch
@@ -666,6 +716,7 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
                 else if (p.lse) p.lse[(int64_t)sq * p.H * p.G + hq] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.69314718f;
             }
         }
+        if constexpr (CL > 0) break;                       // (j may be an empty job by now)
         __syncthreads();                                   // the stages may be refilled
     }
     cp_wait<0>();
@@ -701,6 +752,18 @@ __global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const A
         asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");   // peers have read
     }
     if (p.under) grid_dependency_wait();                  // not through before the pass over prefixes is
+}
+
+template <bool KEY8, int RT>
+__global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM) k_attend(const __grid_constant__ AttendParams p)
+{
+    attend_block<KEY8, RT, 0>(p, p);
+}
+template <bool KEY8, int RT>
+__global__ void __launch_bounds__(kAttThreads, kAttBlocksPerSM)
+k_attend_cluster(const __grid_constant__ AttendParams p, const __grid_constant__ AttendParams pre)
+{
+    attend_block<KEY8, RT, kAttCluster>(p, pre);
 }
 
 // ----------------------------------------------------------------------------------------------
@@ -741,10 +804,7 @@ __global__ void __launch_bounds__(kMergeThreads) k_attend_merge(const MergeParam
     // the sequence's group, before the passes are waited for: they began behind whatever wrote group_start
     int pre_rec = -1, row0 = 0;
     if (p.pre.rec) {
-        int lo = -1;                                                         // the last group that starts at or before it
-        for (int b = 0; b < p.P; b += 32)
-            lo += __popc(__ballot_sync(0xffffffffu, b + lane < p.P && __ldg(p.group_start + min(b + lane, p.P - 1)) <= s));
-        lo = max(lo, 0);
+        const int lo = att_group_of(p.group_start, p.P, s, lane);
         const int2 g = att_group(p.group_start, p.S, lo);
         if (s >= g.x && s < g.x + g.y) {
             const int rt = (s - g.x) / p.pre.spt;

@@ -434,13 +434,14 @@ def test_attend_and_append_past_32_bit_offsets():
 # ------------------------------------------------------------------------------------------------
 # shared prefixes
 # ------------------------------------------------------------------------------------------------
-def check_shared(fmt, page, H, G, starts, plens, lens, pfmt=None, ppage=None, per_head=False, seed=0, order="heads"):
+def check_shared(fmt, page, H, G, starts, plens, lens, pfmt=None, ppage=None, per_head=False, seed=0, order="heads",
+                 rows=None):
     S, P, L, layer = len(lens), len(plens), 2, 1
     g = torch.Generator(device=DEV).manual_seed(seed)
     pfmt, ppage = pfmt or fmt, page if ppage is None else ppage
     pu = plens if per_head else [[n] * H for n in plens]
     c = Cache(L, S, H, max(1, max(lens)), fmt, page, order, seed=seed)
-    pc = Cache(L, P, H, max(1, max(max(r) for r in pu)), pfmt, ppage, order, seed=seed + 1)
+    pc = Cache(L, P, H, rows or max(1, max(max(r) for r in pu)), pfmt, ppage, order, seed=seed + 1)
     for h in range(H):
         for s in range(S):
             c.fill(layer, s, h, lens[s], g)
@@ -516,9 +517,38 @@ def test_shared_long_prefix(fmt):
     check_shared(fmt, 0, 1, 8, [0, 24], [9001], [10 * s for s in range(24)], seed=21)
 
 
-def test_shared_reports_descending_groups():
+# The same with room for more rows than clusters of blocks take: passes over prefixes and own rows, then joined.
+ROOM = 6000
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("G", [1, 3, 4, 5, 8, 16])
+def test_shared_in_passes_group_sizes(fmt, G):
+    check_shared(fmt, 16, 2, G, [0, 1, 6, 6, 9], [300, 65, 40, 128], [0, 5, 17, 64, 1, 0, 130, 2, 33], seed=G, rows=ROOM)
+    check_shared(fmt, 16, 1, G, [0, 24, 25], [300, 140], [(7 * s) % 30 for s in range(25)], seed=G, rows=ROOM)
+
+
+@pytest.mark.parametrize("fmt,page,order", [("bf16", 0, "heads"), ("bf16", 0, "tokens"), ("bf16", 48, "padded"), ("bf16", 128, "heads"),
+                                            ("e4m3", 0, "heads"), ("e4m3", 64, "tokens"), ("e4m3", 48, "padded")])
+@pytest.mark.parametrize("S", [3, 30])
+def test_shared_in_passes_layouts(fmt, page, order, S):
+    check_shared(fmt, page, 2, 4, [0, S], [1000], [3 * s for s in range(S)], order=order, rows=ROOM)
+
+
+@pytest.mark.parametrize("a,b", [("bf16", "e4m3"), ("e4m3", "bf16")])
+@pytest.mark.parametrize("S", [5, 40])
+def test_shared_in_passes_formats_lengths_per_head_and_empty_parts(a, b, S):
+    lens = [(7 * s) % 40 for s in range(S)]
+    check_shared(a, 16, 2, 4, [0, S - 2, S], [200, 77], lens, pfmt=b, ppage=0, rows=ROOM)
+    check_shared(a, 16, 3, 4, [0, S - 2, S], [[200, 0, 77], [1, 64, 129]], lens, per_head=True, rows=ROOM)
+    check_shared(a, 16, 2, 4, [1, S - 2, S - 2, S - 1], [100, 0, 30], lens, rows=ROOM)
+    check_shared(a, 16, 1, 4, [0, S], [0], [0] * S, rows=ROOM)
+
+
+@pytest.mark.parametrize("rows", [32, ROOM])
+def test_shared_reports_descending_groups(rows):
     ctx, S, P = context(1, 1, 4), 4, 3
-    c, pc = Cache(1, S, 1, 16), Cache(1, P, 1, 32)
+    c, pc = Cache(1, S, 1, 16), Cache(1, P, 1, rows)
     g = torch.Generator(device=DEV).manual_seed(1)
     for s in range(S):
         c.fill(0, s, 0, 16, g)
@@ -534,18 +564,19 @@ def test_shared_reports_descending_groups():
         assert int(status) == want, starts
 
 
+@pytest.mark.parametrize("rows", [1000, ROOM])
 @pytest.mark.parametrize("scale", [1.0, -1.0, 0.0])
 @pytest.mark.parametrize("fmt,S", [("bf16", 20), ("e4m3", 20), ("bf16", 3)])
-def test_shared_ascending_and_descending_logits(fmt, S, scale):
+def test_shared_ascending_and_descending_logits(fmt, S, scale, rows):
     """Keys ordered by their logit, 60 units apart over the prefix: the bound is raised tile after tile, or never again."""
     H, G, n = 1, 4, 1000
     for sign in (1.0, -1.0):
         g = torch.Generator(device=DEV).manual_seed(2)
-        pc, c = Cache(1, 1, H, n, fmt), Cache(1, S, H, 4, fmt)
+        pc, c = Cache(1, 1, H, rows, fmt), Cache(1, S, H, 4, fmt)
         pc.fill(0, 0, 0, n, g)
         for s in range(S):
             c.fill(0, s, 0, s % 3, g)
-        pc.k.view({1: torch.uint8, 2: torch.int16}[pc.k.element_size()])[0, 0, 0, :, 0] = raw(
+        pc.k.view({1: torch.uint8, 2: torch.int16}[pc.k.element_size()])[0, 0, 0, :n, 0] = raw(
             (sign * torch.linspace(-60, 60, n, device=DEV)).to(pc.k.dtype))
         q = torch.zeros(S, H * G, D, dtype=torch.bfloat16, device=DEV)
         q[..., 0], q[..., 1] = 1.0, torch.linspace(-1, 1, S, device=DEV)[:, None]
@@ -595,11 +626,12 @@ def test_shared_more_prefixes_than_a_warp():
     check_shared("bf16", 16, 1, 16, starts, [(11 * p) % 50 for p in range(P)], [(5 * i) % 9 for i in range(s + 2)])
 
 
+@pytest.mark.parametrize("rows", [300, ROOM])
 @pytest.mark.parametrize("fmt,S", [("bf16", 3), ("bf16", 30), ("e4m3", 3), ("e4m3", 30)])
-def test_shared_reports_bad_pages_of_a_prefix(fmt, S):
+def test_shared_reports_bad_pages_of_a_prefix(fmt, S, rows):
     H, G, n, page = 2, 4, 300, 32
     g = torch.Generator(device=DEV).manual_seed(7)
-    pc, c = Cache(1, 1, H, n, fmt, page), Cache(1, S, H, 16, fmt, 16)
+    pc, c = Cache(1, 1, H, rows, fmt, page), Cache(1, S, H, 16, fmt, 16)
     for h in range(H):
         pc.fill(0, 0, h, n, g)
         for s in range(S):
@@ -618,11 +650,12 @@ def test_shared_reports_bad_pages_of_a_prefix(fmt, S):
                S, H, G, D ** -0.5, extra=U_BF16)
 
 
+@pytest.mark.parametrize("H,rows", [(2, 150), (1, 150), (2, ROOM)])
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
-def test_shared_non_finite_queries_and_rows_stay_in_their_group(fmt):
-    H, G, S, n = 2, 4, 24, 150
+def test_shared_non_finite_queries_and_rows_stay_in_their_group(fmt, H, rows):
+    G, S, n = 4, 24, 150
     g = torch.Generator(device=DEV).manual_seed(5)
-    pc, c = Cache(1, 2, H, n, fmt), Cache(1, S, H, 8, fmt)
+    pc, c = Cache(1, 2, H, rows, fmt), Cache(1, S, H, 8, fmt)
     for h in range(H):
         for p in range(2):
             pc.fill(0, p, h, n, g)
@@ -630,7 +663,7 @@ def test_shared_non_finite_queries_and_rows_stay_in_their_group(fmt):
             c.fill(0, s, h, 3, g)
     pc.k[0, 1, 0, 70, 3] = float("nan")
     q = torch.randn(S, H * G, D, generator=g, device=DEV).to(torch.bfloat16)
-    q[4, 5, 9] = float("nan")
+    q[4, H * G - 3, 9] = float("nan")
     out = torch.empty_like(q)
     ctx = context(1, H, G)
     ctx.attend_shared(tb.LayerCache(pc.view(tb, seq_lens=int32([n, n])), 0), int32([0, 13, S]),
@@ -639,7 +672,7 @@ def test_shared_non_finite_queries_and_rows_stay_in_their_group(fmt):
     nan = out.isnan().any(-1)
     want = torch.zeros_like(nan)
     want[13:, :G] = True
-    want[4, 5] = True
+    want[4, H * G - 3] = True
     assert torch.equal(nan, want) and bool(out[want].isnan().all())
 
 
