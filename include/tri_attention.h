@@ -392,7 +392,7 @@ typedef struct {
     void *out;                 /* device bf16 [S][H*G][128], 16-byte rows; must not overlap q (out == q is refused) */
     int64_t out_stride_seq, out_stride_head;
     float *lse;                /* device fp32 [S][H*G] or NULL: log sum_n exp(logit_n), -infinity without rows      */
-    float scale;               /* logit_n = scale * (q . k_n); finite                                              */
+    float scale;               /* logit_n = scale * (q . k_n); finite, and times log2 e too                         */
 } tri_attend_io;
 
 /* Bytes of device workspace the calls below need for S sequences and P prefixes (0: tri_attend); 0 for bad arguments. */

@@ -1386,7 +1386,7 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
     const int32_t H = c->desc.n_kv_heads, G = c->desc.group_size;
     if (!rows16_ok(io->q, S > 1 ? io->q_stride_seq : 0, H * G > 1 ? io->q_stride_head : 0, 0, 2) ||
         !rows16_ok(io->out, S > 1 ? io->out_stride_seq : 0, H * G > 1 ? io->out_stride_head : 0, 0, 2) || io->q == io->out ||
-        !std::isfinite(io->scale))
+        !std::isfinite(io->scale * 1.44269504f))
         return TRI_ERR_INVALID_ARG;
     if ((r = check_device(c)) != TRI_OK) return r;
     if (!line_ok(c, src->view, S) || (P > 0 && !line_ok(c, prefix->view, (int64_t)P + S / (16 / c->desc.group_size)))) return TRI_ERR_UNSUPPORTED;
@@ -1412,7 +1412,7 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
     }
 
     MergeParams mp;
-    mp.pre.rec = nullptr; mp.pre.slots = mp.pre.whole = nullptr; mp.pre.rows = 0; mp.pre.spt = 0;
+    mp.pre.rec = nullptr; mp.pre.slots = mp.pre.whole = nullptr; mp.pre.blocks = mp.pre.rows = 0; mp.pre.spt = 0;
     if (P > 0) {
         AttendParams p = attend_params(c, prefix, P, S, io, device_status);
         const bool umma = prefix_umma_ok(c, prefix->view, S, P);
@@ -1434,7 +1434,7 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
         } else {
             TRI_CUDA(launch_attend<false>(rows, (unsigned)pl.blocks, st, p));
         }
-        mp.pre.rec = p.rec; mp.pre.slots = p.slots; mp.pre.whole = p.whole; mp.pre.rows = rows; mp.pre.spt = p.spt;
+        mp.pre.rec = p.rec; mp.pre.slots = p.slots; mp.pre.whole = p.whole; mp.pre.blocks = umma ? c->n_sm : pl.blocks; mp.pre.rows = rows; mp.pre.spt = p.spt;
     }
     AttendParams p = attend_params(c, src, S, S, io, device_status);
     p.finish = P > 0 ? 0 : 1; p.under = P > 0 ? 1 : 0;
@@ -1443,7 +1443,7 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
     if (src->view->k_kind == 3) TRI_CUDA(launch_attend<true>(pl.own_rows, (unsigned)pl.blocks, st, p));
     else TRI_CUDA(launch_attend<false>(pl.own_rows, (unsigned)pl.blocks, st, p));
 
-    mp.own.rec = p.rec; mp.own.slots = p.slots; mp.own.whole = p.whole; mp.own.rows = pl.own_rows; mp.own.spt = 0;
+    mp.own.rec = p.rec; mp.own.slots = p.slots; mp.own.whole = p.whole; mp.own.blocks = pl.blocks; mp.own.rows = pl.own_rows; mp.own.spt = 0;
     mp.S = S; mp.P = P; mp.H = H; mp.G = G; mp.group_start = group_start;
     mp.out = p.out; mp.out_seq = p.out_seq; mp.out_head = p.out_head; mp.lse = io->lse; mp.device_status = device_status;
     mp.rows = (int64_t)S * H < c->n_sm ? 1 : G;

@@ -161,7 +161,8 @@ struct AttJob {
     bool of_prefix;                   // in a cluster: rows of the sequence's prefix, not its own
 };
 
-// The share of this block.  Where the heads of a sequence have equal lengths the sums run over sequences only.
+// The share of this block.  Where the heads of a sequence have equal lengths the sums run over sequences only.  Groups that
+// descend, and so overlap, could make the line longer than the host has checked: no block gets a share then.
 template <int TILE, int COST>
 __device__ __forceinline__ AttShare att_share(const AttendParams &p)
 {
@@ -177,8 +178,15 @@ __device__ __forceinline__ AttShare att_share(const AttendParams &p)
         const int kt = (int)(((uint32_t)min(max(len, 0), p.src.n_max) + TILE - 1) / TILE);
         return (kt + COST) * (p.spt ? att_row_tiles(p, by_head ? x / p.H : x) : 1);
     };
-    int sum = 0, c0 = 0;
-    for (int x = a; x < b; ++x) { c0 = cost(x); sum += c0 * heads; }
+    int sum = 0, c0 = 0, descends = 0;
+    for (int x = a; x < b; ++x) {
+        c0 = cost(x);
+        sum += c0 * heads;
+        if (p.spt) {
+            const int g = by_head ? x / p.H : x;
+            descends |= __ldg(p.group_start + g) > __ldg(p.group_start + g + 1);
+        }
+    }
     int incl = sum;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -186,12 +194,13 @@ __device__ __forceinline__ AttShare att_share(const AttendParams &p)
         if (lane >= d) incl += o;
     }
     if (lane == 31) part_s[warp] = incl;
-    __syncthreads();
+    descends = __syncthreads_or(descends);
     int before = 0, total = 0;
     for (int w = 0; w < nth / 32; ++w) {
         if (w < warp) before += part_s[w];
         total += part_s[w];
     }
+    if (descends) total = 0;
     AttShare r;
     r.total = total;
     r.shares = min(max(total, 1), (int)gridDim.x);
@@ -772,6 +781,7 @@ k_attend_cluster(const __grid_constant__ AttendParams p, const __grid_constant__
 struct AttendPass {                // where a pass left its parts
     const int2 *rec;
     const float *slots, *whole;
+    int32_t blocks;                // of the pass
     int32_t rows;                  // query rows per slot; 128: the sums of 4 dims of all rows, the next 4 dims, .., (m, l) of all rows
     int32_t spt;                   // prefixes: sequences per tile
 };
@@ -819,7 +829,9 @@ __global__ void __launch_bounds__(kMergeThreads) k_attend_merge(const MergeParam
     grid_dependents_launch();
     const int2 own = p.own.rec[unit];
     if (!p.pre.rec && own.y < 2) return;                                     // finished by its block
-    const int2 pre = pre_rec >= 0 ? p.pre.rec[pre_rec] : make_int2(0, 0);
+    int2 pre = pre_rec >= 0 ? p.pre.rec[pre_rec] : make_int2(0, 0);
+    // groups that descend have no records: whatever lies there names no slot outside the workspace
+    if ((uint32_t)pre.y > (uint32_t)p.pre.blocks || (uint32_t)(pre.x >> 1) > (uint32_t)(p.pre.blocks - pre.y)) pre = make_int2(0, 0);
     const int parts = own.y + pre.y;
     const int wpr = kMergeWarps / p.rows, r = warp / wpr, sub = warp - r * wpr, g = ((int)blockIdx.x - unit * per) * p.rows + r;
     const bool active = r < p.rows;

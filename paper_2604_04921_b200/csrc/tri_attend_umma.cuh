@@ -1,4 +1,4 @@
-// Attention of many query rows over a shared prefix on the 5th-generation tensor cores (bf16 rows).
+// Attention of many query rows over a shared prefix on the 5th-generation tensor cores.
 //
 // A prefix that n sequences share meets n * G query rows per KV head: up to 128 of them are one M = 128 tile, so every
 // cached row fetched from memory serves all of them.  Per tile of 128 cached rows:
@@ -15,9 +15,10 @@
 // the MMAs are f16 (queries scaled to f16 by a power of two per row, weights with 11 bits).
 // At the end of a unit's share the streams are joined and the part goes to the workspace, as in k_attend.
 //
-// What bounds it: with up to 128 rows per prefix, HBM (64 KB per 1.5 us and SM); the MMAs of a tile take 1536 cycles, the
-// exponentials 1024, against about 2800 cycles for its rows.  With more rows the tiles of one prefix share its rows
-// through L2 and the MMAs bound it.
+// What bounds it: with up to 128 query rows per prefix, HBM: a tile's 64 KB take about 2800 cycles per multiprocessor, its
+// MMAs 1024 (as issued, one by one, 1600), the exponentials 1024.  One prefix of 256K rows, 128 query rows per head: 6.7 TB/s.
+// With more query rows the tiles of one prefix share its rows through L2 and the issue of the MMAs bounds it.  Start, drain
+// and join cost about 15 us, which is what counts on short prefixes.
 //
 // Every wait is bounded; one that runs out sets TRI_ERR_TIMEOUT, all roles leave their loops and the tensor memory is
 // released at the common exit.
@@ -28,7 +29,7 @@
 namespace tri {
 
 constexpr int kPTile = 128;                               // cached rows per tile, query rows per tile
-constexpr int kPHalf = 64;                               // the weights of a tile are handed over in two halves, so that MMAs and softmax overlap
+constexpr int kPHalf = 64;                                // the weights of a tile are handed over in two halves, so that MMAs and softmax overlap
 template <bool KEY8> constexpr int kPStages = KEY8 ? 2 : 3;     // operand stages of K and of V
 constexpr int kPUnitCost = 2;                             // a unit's own cost, in tiles
 static_assert(kPTile == kMergeTile, "slots are laid out for the joining kernel");
@@ -172,7 +173,7 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
         gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
-    if (warp == kMmaWarp) {                         // the MMA warp owns the tensor-memory allocation
+    if (warp == kMmaWarp) {                                // the MMA warp owns the tensor-memory allocation
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&tmem_base_s)), "r"(512)
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
@@ -207,7 +208,7 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_base_s;
-    // columns: S/P of stream w at 128 w (weights: 64 columns, their rest: 64), O of stream w at 256 + 128 w
+    // columns: S of stream w at 128 w, P of its halves in the first 32 columns of either half, O of stream w at 256 + 128 w
 
     if (KEY8 && warp >= kPSoftWarps && warp < kMmaWarp) {
         // ---------------- 8 bits: two warps for K, two for V; the first of a pair issues the copies of raw rows two tiles ahead,
@@ -504,7 +505,7 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                 }
                 if (cut || miss) {
                     // rows behind the length or of absent pages: no weight, and zeros for values (they may hold anything)
-                    // (8 bits: the converters have seen to the values)
+                    // (8 bits: the converters have seen to the values' rows)
                     if (!KEY8 && (row >= have || ((miss >> (row >> 4)) & 1u))) {
 #pragma unroll
                         for (int c = 0; c < 16; ++c)

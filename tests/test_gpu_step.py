@@ -564,6 +564,38 @@ def test_shared_reports_descending_groups(rows):
         assert int(status) == want, starts
 
 
+@pytest.mark.parametrize("S,P", [(4096, 512), (64, 2048)])
+def test_shared_descending_groups_of_long_prefixes_take_no_work(S, P):
+    # all even groups are the whole batch: (4096, 512) would be 2^31 steps and more, which no unit's place may wrap around
+    ctx, H, n = context(1, 8, 4), 8, 2 ** 20
+    page = torch.zeros(1, 1, H, 1024, D, dtype=torch.bfloat16, device=DEV)
+    table = torch.zeros(P, n // 1024, dtype=torch.int32, device=DEV)
+    pre = tb.LayerCache(tb.CacheView(page, page, page_table=table, n_max=n, seq_lens=int32([n] * P)), 0)
+    c = Cache(1, S, H, 16)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    for s in (0, S - 1):
+        for h in range(H):
+            c.fill(0, s, h, 16, g)
+    src = tb.LayerCache(c.view(tb, seq_lens=int32([16] + [0] * (S - 2) + [16])), 0)
+    q = torch.randn(S, 4 * H, D, generator=g, device=DEV).to(torch.bfloat16)
+    out, status = torch.empty_like(q), int32([0])
+    ws = ctx.attend_workspace(S, P)
+    for fill in (0, 1, 127, 255):
+        ws.fill_(fill)
+        status.zero_()
+        ctx.attend_shared(pre, int32([0, S] * (P // 2) + [S]), src, q, out, ws, device_status=status)
+        torch.cuda.synchronize()
+        assert int(status) == 5
+    # the context goes on: the same call without prefixes of any sequence
+    status.zero_()
+    ctx.attend_shared(pre, int32([0] * (P + 1)), src, q, out, ws, device_status=status)
+    alone = torch.empty_like(q)
+    ctx.attend(src, q, alone, ws)
+    torch.cuda.synchronize()
+    # (the same sums; divided before or after the join, so that a rounding to bf16 may fall to the neighbour, 2 U apart)
+    assert int(status) == 0 and bool(((out.float() - alone.float()).abs() <= 2 * U_BF16 * alone.float().abs()).all())
+
+
 @pytest.mark.parametrize("rows", [1000, ROOM])
 @pytest.mark.parametrize("scale", [1.0, -1.0, 0.0])
 @pytest.mark.parametrize("fmt,S", [("bf16", 20), ("e4m3", 20), ("bf16", 3)])
@@ -946,6 +978,7 @@ def test_refusals_of_the_c_interface():
     assert attend(q=None) == 1 and attend(out=None) == 1 and attend(q=q.data_ptr() + 2) == 1 and attend(q_stride_head=4) == 1
     assert attend(scale=float("nan")) == 1 and attend(scale=float("inf")) == 1
     assert attend(layer_cache(v=None)) == 1 and attend(layer_cache(seq_lens=None)) == 1 and attend(layer_cache(layer=2)) == 1
+    assert attend(scale=3e38) == 1                                              # times log2 e: beyond fp32
     assert attend(out=q.data_ptr()) == 1
     assert attend(layer_cache(n_max=2 ** 31 - 1), S=64) == 2                    # the line of steps would pass 2^31
     assert attend(layer_cache(k_kind=2)) == 2 and attend(layer_cache(Cache(2, S, H, 32, "f32"))) == 2
