@@ -135,6 +135,13 @@ __device__ __forceinline__ void split16(float lower, float upper, uint32_t &hi, 
         lo = cvt_bf16x2(upper - bf16_hi(hi), lower - bf16_lo(hi));
     }
 }
+// An 8 x 8 matrix of 16-bit values held as a fragment (row lane / 4, columns 2 (lane % 4), + 1), transposed.
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x)
+{
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(y) : "r"(x));
+    return y;
+}
 __device__ __forceinline__ float ex2(float x)
 {
     float y;
@@ -282,18 +289,23 @@ __device__ __forceinline__ bool att_next(const AttendParams &p, const AttShare &
 }
 
 // KEY8: e4m3 rows, widened exactly to f16 (the queries are brought to f16 by a power of two per row).
-// RT = 8: at most 8 query rows; the rest of the rounded weights rides in the upper 8 rows of the 16-row MMA, for free.
-// RT = 16: up to 16 query rows; that rest takes a second MMA.
+// RT = 8: at most 8 query rows.  bf16: they are rows of A; the rest of the rounded weights rides in the upper 8 rows of the
+// 16-row MMA, for free.  e4m3, where widening leaves less room for waiting: the products are formed transposed (TR), keys and
+// dimensions as the 16 rows of A, the query rows as the 8 columns.  Logits then take half the MMAs, the sums half the
+// registers, and the rest of the weights a second MMA: 64 x 8 units of 0..4K rows 63.4 us against 67.9.  (16-row steps at
+// 4 blocks per multiprocessor 65.2, 32-row steps at 3 blocks 63.1; the copies alone 58.)
+// RT = 16: up to 16 query rows are rows of A; the rest of the weights takes a second MMA.
 // CL > 0: a cluster of CL blocks takes one unit, cuts it evenly, and joins its parts through distributed shared memory: one
 // launch and no workspace where there are few short units.  `pre` (pre.nseq > 0): the prefixes; a unit is then the rows of
 // its sequence's prefix, if it has one, and its own.
 template <bool KEY8, int RT, int CL>
 __device__ __forceinline__ void attend_block(const AttendParams &p, const AttendParams &pre)
 {
+    constexpr bool TR = KEY8 && RT == 8;
     constexpr int ST = kAttStages, ROWS = kAttRows<KEY8>, NK = ROWS / 16, TILE = kAttWarps * ROWS;
     constexpr int kRowBytes = KEY8 ? 128 : 256, kHalf = ROWS * kRowBytes;                             // K | V
     constexpr int kChunks = kRowBytes / 16, kCopies = ROWS * kChunks / 32;
-    constexpr int NR = RT / 8;                            // query rows per thread
+    constexpr int NR = TR ? 2 : RT / 8;                   // query rows per thread
     extern __shared__ __align__(128) uint8_t dyn[];
     __shared__ float2 stat[kAttWarps][RT];
     __shared__ __align__(16) float part[CL ? RT : 1][kAttRowPitch];      // this block's sums, and (m, l)
@@ -440,7 +452,7 @@ __device__ __forceinline__ void attend_block(const AttendParams &p, const Attend
     uint32_t qa[8][4];
     const int inv_g = 65536 / p.G + 1;
     float mul[NR], k_scale = 1.f;                         // logit in base-2 units per accumulator unit
-    float o[16][4], m[NR], l[NR];
+    float o[TR ? 8 : 16][4], m[NR], l[NR];
     int it = 0, stage = 0, ahead = ST - 1;
     for (;;) {
         // the stage of the step before: read, or used and released in joining a unit
@@ -503,10 +515,16 @@ __device__ __forceinline__ void attend_block(const AttendParams &p, const Attend
                             qa[k][i + 2 * x] = f16_bits(bf16_lo(w) * by) | (f16_bits(bf16_hi(w) * by) << 16);
                         }
                 }
-                if (i < NR) mul[i % NR] = p.scale * back;
+                if (TR) {
+                    if (i == 0)
+#pragma unroll
+                        for (int x = 0; x < NR; ++x) mul[x] = p.scale * __shfl_sync(0xffffffffu, back, (2 * t4 + x) * 4);
+                } else if (i < NR) {
+                    mul[i % NR] = p.scale * back;
+                }
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) { o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f; }
+            for (int i = 0; i < (TR ? 8 : 16); ++i) { o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f; }
 #pragma unroll
             for (int i = 0; i < NR; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
             k_scale = params_of(j).k_scale ? __ldg(params_of(j).k_scale + j.h) : 1.f;
@@ -522,114 +540,197 @@ __device__ __forceinline__ void attend_block(const AttendParams &p, const Attend
         const uint32_t miss = (bad >> (2 * stage)) & 3u;
         const bool cut = have < ROWS || miss;
         const uint32_t kb_s = ring + stage * kAttStageBytes, vb_s = kb_s + kHalf;
-        // logits: 8 rows x 8 keys per accumulator (x 2: even and odd steps of 16 dims apart, shorter chains)
-        float sc[2 * NK][4];
-        if (KEY8) {
+        if constexpr (TR) {
+            // logits transposed: 16 keys x 8 query rows per accumulator (x 2: even and odd steps of 16 dims, shorter chains); the
+            // thread holds keys g8, g8 + 8 of query rows 2 t4, 2 t4 + 1
+            float w[NK][4];
 #pragma unroll
-            for (int x = 0; x < 2 * NK; ++x) sc[x][0] = sc[x][1] = sc[x][2] = sc[x][3] = 0.f;
+            for (int kg = 0; kg < NK; ++kg) {
+                float odd[4] = {0.f, 0.f, 0.f, 0.f};
+                w[kg][0] = w[kg][1] = w[kg][2] = w[kg][3] = 0.f;
 #pragma unroll
-            for (int k = 0; k < 8; k += 2)
-#pragma unroll
-                for (int kg = 0; kg < NK; ++kg) {
-                    uint32_t f[4];
+                for (int k = 0; k < 8; k += 2) {
+                    uint32_t f[4], a[8];
                     ldmatrix_x4(f, (kb_s + klane + 16 * kg * 128) ^ (k << 4));
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        uint32_t b0, b1;
-                        e4m3x4_to_f16x2(f[x], b0, b1);
-                        const int kk = k + (x >> 1);
-                        mma16<true>(sc[2 * kg + (x & 1)], qa[kk][0], qa[kk][1], qa[kk][2], qa[kk][3], b0, b1);
-                    }
+                    for (int x = 0; x < 4; ++x) e4m3x4_to_f16x2(f[x], a[2 * x], a[2 * x + 1]);
+                    mma16<true>(w[kg], a[0], a[2], a[1], a[3], qa[k][0], qa[k][2]);
+                    mma16<true>(odd, a[4], a[6], a[5], a[7], qa[k + 1][0], qa[k + 1][2]);
                 }
-        } else {
-            float sd[2][4];
 #pragma unroll
-            for (int x = 0; x < 2; ++x) { sc[x][0] = sc[x][1] = sc[x][2] = sc[x][3] = 0.f; sd[x][0] = sd[x][1] = sd[x][2] = sd[x][3] = 0.f; }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                uint32_t f[4];
-                ldmatrix_x4(f, (kb_s + klane + (k >> 2) * 128) ^ ((2 * k & 7) << 4));
-                mma16<false>(k & 1 ? sd[0] : sc[0], qa[k][0], qa[k][1], qa[k][2], qa[k][3], f[0], f[1]);
-                mma16<false>(k & 1 ? sd[1] : sc[1], qa[k][0], qa[k][1], qa[k][2], qa[k][3], f[2], f[3]);
-            }
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int y = 0; y < 4; ++y) sc[x][y] += sd[x][y];
-        }
-        // running bound and weights; the thread holds keys 8 x + 2 t4, + 1 of row g8 (+ 8)
-        float w[NR][4 * NK];
-#pragma unroll
-        for (int i = 0; i < NR; ++i) {
-            float mx = -INFINITY;
-#pragma unroll
-            for (int x = 0; x < 4 * NK; ++x) {
-                w[i][x] = sc[x >> 1][2 * i + (x & 1)] * mul[i];
-                if (cut) {
-                    const int key = 8 * (x >> 1) + 2 * t4 + (x & 1);
-                    if (key >= have || ((miss >> (x >> 2)) & 1u)) w[i][x] = -INFINITY;
-                }
-                mx = fmaxf(mx, w[i][x]);
-            }
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-            const bool raise = mx > m[i] + kAttAbove<KEY8> || (m[i] == -INFINITY && mx > m[i]);
-            if (__any_sync(0xffffffffu, raise)) {
-                mx -= kAttBelow<KEY8>;
-                const float by = raise ? ex2(m[i] - mx) : 1.f;       // 0 where there was no bound yet
-                if (raise) m[i] = mx;
-                l[i] *= by;
-#pragma unroll
-                for (int n = 0; n < 16; ++n) {
-                    o[n][2 * i] *= by; o[n][2 * i + 1] *= by;
-                    if (RT == 8) { o[n][2] *= by; o[n][3] *= by; }
+                for (int x = 0; x < 4; ++x) {
+                    w[kg][x] = (w[kg][x] + odd[x]) * mul[x & 1];
+                    if (cut && (16 * kg + g8 + 8 * (x >> 1) >= have || ((miss >> kg) & 1u))) w[kg][x] = -INFINITY;
                 }
             }
-            const float ref = m[i] == -INFINITY ? 0.f : m[i];
-#pragma unroll
-            for (int x = 0; x < 4 * NK; ++x) {
-                w[i][x] = ex2(w[i][x] - ref);
-                l[i] += w[i][x];
-            }
-        }
-#pragma unroll
-        for (int kg = 0; kg < NK; ++kg) {
-            uint32_t ph[NR][2], pl[NR][2];
+            // the bound is looked at by a vote and searched for only when it has to be raised
+            float mx[NR];
+            bool raise = false;
 #pragma unroll
             for (int i = 0; i < NR; ++i) {
-                split16<KEY8>(w[i][4 * kg], w[i][4 * kg + 1], ph[i][0], pl[i][0]);
-                split16<KEY8>(w[i][4 * kg + 2], w[i][4 * kg + 3], ph[i][1], pl[i][1]);
+                mx[i] = fmaxf(w[0][i], w[0][i + 2]);
+#pragma unroll
+                for (int kg = 1; kg < NK; ++kg) mx[i] = fmaxf(mx[i], fmaxf(w[kg][i], w[kg][i + 2]));
+                raise = raise || mx[i] > m[i] + kAttAbove<KEY8>;
             }
-            auto pv = [&](float (&acc)[4], uint32_t b0, uint32_t b1) {
-                if (RT == 8) {
-                    mma16<KEY8>(acc, ph[0][0], pl[0][0], ph[0][1], pl[0][1], b0, b1);
-                } else {
-                    mma16<KEY8>(acc, ph[0][0], ph[NR - 1][0], ph[0][1], ph[NR - 1][1], b0, b1);
-                    mma16<KEY8>(acc, pl[0][0], pl[NR - 1][0], pl[0][1], pl[NR - 1][1], b0, b1);
+            if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+                for (int i = 0; i < NR; ++i) {
+                    mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 4));
+                    mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 8));
+                    mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 16));
+                    if (mx[i] > m[i] + kAttAbove<KEY8>) {
+                        mx[i] -= kAttBelow<KEY8>;
+                        const float by = ex2(m[i] - mx[i]);          // 0 where there was no bound yet
+                        m[i] = mx[i];
+                        l[i] *= by;
+#pragma unroll
+                        for (int n = 0; n < 8; ++n) { o[n][i] *= by; o[n][i + 2] *= by; }
+                    }
                 }
-            };
-            if (KEY8) {
+            }
+            // weights, and transposed into the B operand: 16 keys x 8 query rows
+            uint32_t ph[NK][2], pl[NK][2];
+#pragma unroll
+            for (int kg = 0; kg < NK; ++kg) {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    w[kg][x] = ex2(w[kg][x] - (m[x & 1] == -INFINITY ? 0.f : m[x & 1]));
+                    l[x & 1] += w[kg][x];
+                }
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    split16<true>(w[kg][2 * x], w[kg][2 * x + 1], ph[kg][x], pl[kg][x]);
+                    ph[kg][x] = transpose8x8(ph[kg][x]);
+                    pl[kg][x] = transpose8x8(pl[kg][x]);
+                }
+            }
+#pragma unroll
+            for (int kg = 0; kg < NK; ++kg)
 #pragma unroll
                 for (int ch = 0; ch < 8; ch += 2) {
                     uint32_t f[4];
                     ldmatrix_x4_t(f, (vb_s + vlane + 16 * kg * 128) ^ (ch << 4));
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        // bytes of a word: key 2 t4 dims (2 g8, 2 g8 + 1), key 2 t4 + 1 the same dims
+                        // bytes of a word: key 2 t4 dims (2 g8, 2 g8 + 1), key 2 t4 + 1 the same dims; even dims are rows 0..7
                         uint32_t e0, d0, e1, d1;
                         e4m3x4_to_f16x2(__byte_perm(f[2 * x], 0, 0x3120), e0, d0);
                         e4m3x4_to_f16x2(__byte_perm(f[2 * x + 1], 0, 0x3120), e1, d1);
-                        pv(o[2 * (ch + x)], e0, e1);
-                        pv(o[2 * (ch + x) + 1], d0, d1);
+                        mma16<true>(o[ch + x], e0, d0, e1, d1, ph[kg][0], ph[kg][1]);
+                        mma16<true>(o[ch + x], e0, d0, e1, d1, pl[kg][0], pl[kg][1]);
                     }
                 }
-            } else {
+        } else {
+            // logits: 8 rows x 8 keys per accumulator (x 2: even and odd steps of 16 dims apart, shorter chains)
+            float sc[2 * NK][4];
+            if (KEY8) {
 #pragma unroll
-                for (int n = 0; n < 16; n += 2) {
+                for (int x = 0; x < 2 * NK; ++x) sc[x][0] = sc[x][1] = sc[x][2] = sc[x][3] = 0.f;
+#pragma unroll
+                for (int k = 0; k < 8; k += 2)
+#pragma unroll
+                    for (int kg = 0; kg < NK; ++kg) {
+                        uint32_t f[4];
+                        ldmatrix_x4(f, (kb_s + klane + 16 * kg * 128) ^ (k << 4));
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            uint32_t b0, b1;
+                            e4m3x4_to_f16x2(f[x], b0, b1);
+                            const int kk = k + (x >> 1);
+                            mma16<true>(sc[2 * kg + (x & 1)], qa[kk][0], qa[kk][1], qa[kk][2], qa[kk][3], b0, b1);
+                        }
+                    }
+            } else {
+                float sd[2][4];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) { sc[x][0] = sc[x][1] = sc[x][2] = sc[x][3] = 0.f; sd[x][0] = sd[x][1] = sd[x][2] = sd[x][3] = 0.f; }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
                     uint32_t f[4];
-                    ldmatrix_x4_t(f, (vb_s + vlane + (n >> 3) * 128) ^ ((n & 7) << 4));
-                    pv(o[n], f[0], f[1]);
-                    pv(o[n + 1], f[2], f[3]);
+                    ldmatrix_x4(f, (kb_s + klane + (k >> 2) * 128) ^ ((2 * k & 7) << 4));
+                    mma16<false>(k & 1 ? sd[0] : sc[0], qa[k][0], qa[k][1], qa[k][2], qa[k][3], f[0], f[1]);
+                    mma16<false>(k & 1 ? sd[1] : sc[1], qa[k][0], qa[k][1], qa[k][2], qa[k][3], f[2], f[3]);
+                }
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) sc[x][y] += sd[x][y];
+            }
+            // running bound and weights; the thread holds keys 8 x + 2 t4, + 1 of row g8 (+ 8)
+            float w[NR][4 * NK];
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+                float mx = -INFINITY;
+#pragma unroll
+                for (int x = 0; x < 4 * NK; ++x) {
+                    w[i][x] = sc[x >> 1][2 * i + (x & 1)] * mul[i];
+                    if (cut) {
+                        const int key = 8 * (x >> 1) + 2 * t4 + (x & 1);
+                        if (key >= have || ((miss >> (x >> 2)) & 1u)) w[i][x] = -INFINITY;
+                    }
+                    mx = fmaxf(mx, w[i][x]);
+                }
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+                const bool raise = mx > m[i] + kAttAbove<KEY8> || (m[i] == -INFINITY && mx > m[i]);
+                if (__any_sync(0xffffffffu, raise)) {
+                    mx -= kAttBelow<KEY8>;
+                    const float by = raise ? ex2(m[i] - mx) : 1.f;       // 0 where there was no bound yet
+                    if (raise) m[i] = mx;
+                    l[i] *= by;
+#pragma unroll
+                    for (int n = 0; n < 16; ++n) {
+                        o[n][2 * i] *= by; o[n][2 * i + 1] *= by;
+                        if (RT == 8) { o[n][2] *= by; o[n][3] *= by; }
+                    }
+                }
+                const float ref = m[i] == -INFINITY ? 0.f : m[i];
+#pragma unroll
+                for (int x = 0; x < 4 * NK; ++x) {
+                    w[i][x] = ex2(w[i][x] - ref);
+                    l[i] += w[i][x];
+                }
+            }
+#pragma unroll
+            for (int kg = 0; kg < NK; ++kg) {
+                uint32_t ph[NR][2], pl[NR][2];
+#pragma unroll
+                for (int i = 0; i < NR; ++i) {
+                    split16<KEY8>(w[i][4 * kg], w[i][4 * kg + 1], ph[i][0], pl[i][0]);
+                    split16<KEY8>(w[i][4 * kg + 2], w[i][4 * kg + 3], ph[i][1], pl[i][1]);
+                }
+                auto pv = [&](float (&acc)[4], uint32_t b0, uint32_t b1) {
+                    if (RT == 8) {
+                        mma16<KEY8>(acc, ph[0][0], pl[0][0], ph[0][1], pl[0][1], b0, b1);
+                    } else {
+                        mma16<KEY8>(acc, ph[0][0], ph[NR - 1][0], ph[0][1], ph[NR - 1][1], b0, b1);
+                        mma16<KEY8>(acc, pl[0][0], pl[NR - 1][0], pl[0][1], pl[NR - 1][1], b0, b1);
+                    }
+                };
+                if (KEY8) {
+#pragma unroll
+                    for (int ch = 0; ch < 8; ch += 2) {
+                        uint32_t f[4];
+                        ldmatrix_x4_t(f, (vb_s + vlane + 16 * kg * 128) ^ (ch << 4));
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            // bytes of a word: key 2 t4 dims (2 g8, 2 g8 + 1), key 2 t4 + 1 the same dims
+                            uint32_t e0, d0, e1, d1;
+                            e4m3x4_to_f16x2(__byte_perm(f[2 * x], 0, 0x3120), e0, d0);
+                            e4m3x4_to_f16x2(__byte_perm(f[2 * x + 1], 0, 0x3120), e1, d1);
+                            pv(o[2 * (ch + x)], e0, e1);
+                            pv(o[2 * (ch + x) + 1], d0, d1);
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int n = 0; n < 16; n += 2) {
+                        uint32_t f[4];
+                        ldmatrix_x4_t(f, (vb_s + vlane + (n >> 3) * 128) ^ ((n & 7) << 4));
+                        pv(o[n], f[0], f[1]);
+                        pv(o[n + 1], f[2], f[3]);
+                    }
                 }
             }
         }
@@ -651,7 +752,7 @@ __device__ __forceinline__ void attend_block(const AttendParams &p, const Attend
 #pragma unroll
                 for (int i = 0; i < NR; ++i) mul[i] *= k_by;
 #pragma unroll
-                for (int n = 0; n < 16; ++n)
+                for (int n = 0; n < (TR ? 8 : 16); ++n)
 #pragma unroll
                     for (int x = 0; x < 4; ++x) o[n][x] *= v_by;
                 continue;
@@ -660,69 +761,128 @@ __device__ __forceinline__ void attend_block(const AttendParams &p, const Attend
 
         // ---------------- the unit's rows of this share are through: join the warps ----------------
         // each leaves its sums in the stage it has just read, fragment by fragment, and takes a quarter of the dims of all
+        if constexpr (TR) {
 #pragma unroll
-        for (int i = 0; i < NR; ++i) {
-            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-            if (t4 == 0) stat[warp][g8 + 8 * i] = make_float2(m[i], l[i]);
+            for (int i = 0; i < NR; ++i) {
+                l[i] += __shfl_xor_sync(0xffffffffu, l[i], 4);
+                l[i] += __shfl_xor_sync(0xffffffffu, l[i], 8);
+                l[i] += __shfl_xor_sync(0xffffffffu, l[i], 16);
+                if (g8 == 0) stat[warp][2 * t4 + i] = make_float2(m[i], l[i]);
+            }
 #pragma unroll
-            for (int n = 0; n < 16; n += 2) {
-                float y[4];
+            for (int n = 0; n < 8; ++n) *reinterpret_cast<float4 *>(used + n * 512 + lane * 16) = make_float4(o[n][0], o[n][1], o[n][2], o[n][3]);
+        } else {
 #pragma unroll
-                for (int x = 0; x < 4; ++x)
-                    y[x] = o[n + (x >> 1)][2 * i + (x & 1)] + (RT == 8 ? o[n + (x >> 1)][2 + (x & 1)] : 0.f);
-                *reinterpret_cast<float4 *>(used + (i * 8 + n / 2) * 512 + lane * 16) = make_float4(y[0], y[1], y[2], y[3]);
+            for (int i = 0; i < NR; ++i) {
+                l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+                l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+                if (t4 == 0) stat[warp][g8 + 8 * i] = make_float2(m[i], l[i]);
+#pragma unroll
+                for (int n = 0; n < 16; n += 2) {
+                    float y[4];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        y[x] = o[n + (x >> 1)][2 * i + (x & 1)] + (RT == 8 ? o[n + (x >> 1)][2 + (x & 1)] : 0.f);
+                    *reinterpret_cast<float4 *>(used + (i * 8 + n / 2) * 512 + lane * 16) = make_float4(y[0], y[1], y[2], y[3]);
+                }
             }
         }
         __syncthreads();
         const bool final = j.complete && p.finish;
+        if constexpr (TR) {
+            float4 y[2];                                   // dims 16 n + 2 g8, + 1 of query rows 2 t4, + 1, for n = 2 warp, + 1
+            y[0] = y[1] = make_float4(0.f, 0.f, 0.f, 0.f);
+            float mm[NR], ll[NR], st[kAttWarps][NR];
 #pragma unroll
-        for (int i = 0; i < NR; ++i) {
-            const int r = g8 + 8 * i;
-            float2 st[kAttWarps];
-            float mm = -INFINITY, ll = 0.f;
+            for (int i = 0; i < NR; ++i) {
+                mm[i] = -INFINITY; ll[i] = 0.f;
 #pragma unroll
-            for (int w2 = 0; w2 < kAttWarps; ++w2) { st[w2] = stat[w2][r]; mm = fmaxf(mm, st[w2].x); }
-#pragma unroll
-            for (int w2 = 0; w2 < kAttWarps; ++w2) {
-                st[w2].x = st[w2].x == -INFINITY ? 0.f : ex2(st[w2].x - mm);
-                ll += st[w2].y * st[w2].x;
-            }
-            const float by = final ? (ll == 0.f ? 0.f : vs / ll) : vs;
-            const int sr = p.spt ? att_small_div(r, inv_g) : 0, sq = j.first_seq + sr, hq = j.h * p.G + r - sr * p.G;
-            char *out = p.out + ((int64_t)sq * p.out_seq + (int64_t)hq * p.out_head) * 2;
-            float *to = CL ? part[CL ? r : 0]
-                           : (j.complete ? p.whole + ((int64_t)sq * p.H * p.G + hq) * kAttRowPitch
-                                         : p.slots + (((int64_t)blockIdx.x * 2 + (j.begins ? 1 : 0)) * RT + r) * kAttRowPitch);
-#pragma unroll
-            for (int q2 = 0; q2 < 2; ++q2) {
-                const int q = 2 * warp + q2;               // fragments 2 q, 2 q + 1
-                float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int w2 = 0; w2 < kAttWarps; ++w2) mm[i] = fmaxf(mm[i], stat[w2][2 * t4 + i].x);
 #pragma unroll
                 for (int w2 = 0; w2 < kAttWarps; ++w2) {
-                    const float4 x = *reinterpret_cast<const float4 *>(used + (w2 - warp) * (ST * kAttStageBytes) + (i * 8 + q) * 512 + lane * 16);
-                    y.x += x.x * st[w2].x; y.y += x.y * st[w2].x; y.z += x.z * st[w2].x; y.w += x.w * st[w2].x;
-                }
-                y.x *= by; y.y *= by; y.z *= by; y.w *= by;
-                if (r >= j.nrows) continue;
-                if (KEY8) {                                // dims 16 q + 4 t4 + 0..3: even ones from fragment 2 q, odd ones from 2 q + 1
-                    const int d = 16 * q + 4 * t4;
-                    if (final) *reinterpret_cast<uint2 *>(out + 2 * d) = make_uint2(cvt_bf16x2(y.z, y.x), cvt_bf16x2(y.w, y.y));
-                    else *reinterpret_cast<float4 *>(to + d) = make_float4(y.x, y.z, y.y, y.w);
-                } else {                                   // dims 16 q + 2 t4 + 0, 1 and 8 further on
-                    const int d = 16 * q + 2 * t4;
-                    if (final) {
-                        *reinterpret_cast<uint32_t *>(out + 2 * d) = cvt_bf16x2(y.y, y.x);
-                        *reinterpret_cast<uint32_t *>(out + 2 * d + 16) = cvt_bf16x2(y.w, y.z);
-                    } else {
-                        *reinterpret_cast<float2 *>(to + d) = make_float2(y.x, y.y);
-                        *reinterpret_cast<float2 *>(to + d + 8) = make_float2(y.z, y.w);
-                    }
+                    const float2 ml = stat[w2][2 * t4 + i];
+                    st[w2][i] = ml.x == -INFINITY ? 0.f : ex2(ml.x - mm[i]);
+                    ll[i] += ml.y * st[w2][i];
                 }
             }
-            if (warp == 0 && t4 == 0 && r < j.nrows) {
-                if (!final) *reinterpret_cast<float2 *>(to + kHeadDim) = make_float2(mm, ll);
-                else if (p.lse) p.lse[(int64_t)sq * p.H * p.G + hq] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.69314718f;
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int w2 = 0; w2 < kAttWarps; ++w2) {
+                    const float4 z = *reinterpret_cast<const float4 *>(used + (w2 - warp) * (ST * kAttStageBytes) + (2 * warp + x) * 512 + lane * 16);
+                    y[x].x += z.x * st[w2][0]; y[x].y += z.y * st[w2][1]; y[x].z += z.z * st[w2][0]; y[x].w += z.w * st[w2][1];
+                }
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+                const int r = 2 * t4 + i;
+                if (r >= j.nrows) continue;
+                const float by = final ? (ll[i] == 0.f ? 0.f : vs / ll[i]) : vs;
+                const int hq = j.h * p.G + r;
+                char *out = p.out + ((int64_t)j.first_seq * p.out_seq + (int64_t)hq * p.out_head) * 2;
+                float *to = CL ? part[CL ? r : 0]
+                               : (j.complete ? p.whole + ((int64_t)j.first_seq * p.H * p.G + hq) * kAttRowPitch
+                                             : p.slots + (((int64_t)blockIdx.x * 2 + (j.begins ? 1 : 0)) * RT + r) * kAttRowPitch);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int d = 16 * (2 * warp + x) + 2 * g8;
+                    const float lower = (i ? y[x].y : y[x].x) * by, upper = (i ? y[x].w : y[x].z) * by;
+                    if (final) *reinterpret_cast<uint32_t *>(out + 2 * d) = cvt_bf16x2(upper, lower);
+                    else *reinterpret_cast<float2 *>(to + d) = make_float2(lower, upper);
+                }
+                if (warp == 0 && g8 == 0) {
+                    if (!final) *reinterpret_cast<float2 *>(to + kHeadDim) = make_float2(mm[i], ll[i]);
+                    else if (p.lse) p.lse[(int64_t)j.first_seq * p.H * p.G + hq] = ll[i] == 0.f ? -INFINITY : (mm[i] + log2f(ll[i])) * 0.69314718f;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+                const int r = g8 + 8 * i;
+                float2 st[kAttWarps];
+                float mm = -INFINITY, ll = 0.f;
+#pragma unroll
+                for (int w2 = 0; w2 < kAttWarps; ++w2) { st[w2] = stat[w2][r]; mm = fmaxf(mm, st[w2].x); }
+#pragma unroll
+                for (int w2 = 0; w2 < kAttWarps; ++w2) {
+                    st[w2].x = st[w2].x == -INFINITY ? 0.f : ex2(st[w2].x - mm);
+                    ll += st[w2].y * st[w2].x;
+                }
+                const float by = final ? (ll == 0.f ? 0.f : vs / ll) : vs;
+                const int sr = p.spt ? att_small_div(r, inv_g) : 0, sq = j.first_seq + sr, hq = j.h * p.G + r - sr * p.G;
+                char *out = p.out + ((int64_t)sq * p.out_seq + (int64_t)hq * p.out_head) * 2;
+                float *to = CL ? part[CL ? r : 0]
+                               : (j.complete ? p.whole + ((int64_t)sq * p.H * p.G + hq) * kAttRowPitch
+                                             : p.slots + (((int64_t)blockIdx.x * 2 + (j.begins ? 1 : 0)) * RT + r) * kAttRowPitch);
+#pragma unroll
+                for (int q2 = 0; q2 < 2; ++q2) {
+                    const int q = 2 * warp + q2;               // fragments 2 q, 2 q + 1
+                    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int w2 = 0; w2 < kAttWarps; ++w2) {
+                        const float4 x = *reinterpret_cast<const float4 *>(used + (w2 - warp) * (ST * kAttStageBytes) + (i * 8 + q) * 512 + lane * 16);
+                        y.x += x.x * st[w2].x; y.y += x.y * st[w2].x; y.z += x.z * st[w2].x; y.w += x.w * st[w2].x;
+                    }
+                    y.x *= by; y.y *= by; y.z *= by; y.w *= by;
+                    if (r >= j.nrows) continue;
+                    if (KEY8) {                                // dims 16 q + 4 t4 + 0..3: even ones from fragment 2 q, odd ones from 2 q + 1
+                        const int d = 16 * q + 4 * t4;
+                        if (final) *reinterpret_cast<uint2 *>(out + 2 * d) = make_uint2(cvt_bf16x2(y.z, y.x), cvt_bf16x2(y.w, y.y));
+                        else *reinterpret_cast<float4 *>(to + d) = make_float4(y.x, y.z, y.y, y.w);
+                    } else {                                   // dims 16 q + 2 t4 + 0, 1 and 8 further on
+                        const int d = 16 * q + 2 * t4;
+                        if (final) {
+                            *reinterpret_cast<uint32_t *>(out + 2 * d) = cvt_bf16x2(y.y, y.x);
+                            *reinterpret_cast<uint32_t *>(out + 2 * d + 16) = cvt_bf16x2(y.w, y.z);
+                        } else {
+                            *reinterpret_cast<float2 *>(to + d) = make_float2(y.x, y.y);
+                            *reinterpret_cast<float2 *>(to + d + 8) = make_float2(y.z, y.w);
+                        }
+                    }
+                }
+                if (warp == 0 && t4 == 0 && r < j.nrows) {
+                    if (!final) *reinterpret_cast<float2 *>(to + kHeadDim) = make_float2(mm, ll);
+                    else if (p.lse) p.lse[(int64_t)sq * p.H * p.G + hq] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.69314718f;
+                }
             }
         }
         if constexpr (CL > 0) break;                       // (j may be an empty job by now)
