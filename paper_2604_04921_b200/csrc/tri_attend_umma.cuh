@@ -150,9 +150,6 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     grid_dependency_wait();                                // set up under the kernel before it in the stream
     grid_dependents_launch();                              // the pass over the sequences' own rows may start as blocks leave
-    const AttShare sh = att_share<kPTile, kPUnitCost>(p);
-    if ((int)blockIdx.x >= sh.shares || sh.total == 0) return;
-
     const uint32_t base = (smem_u32(dyn) + 1023u) & ~1023u;
     const uint32_t sm_q = base, sm_k = base + kPTileBytes, sm_v = sm_k + ST * kPTileBytes;
     uint8_t *gq = dyn + (base - smem_u32(dyn)), *gv = gq + (1 + ST) * kPTileBytes;
@@ -173,6 +170,10 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
         gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
+    // (the barriers are set up before its synchronisations, so that the producers may begin behind it)
+    const AttShare sh = att_share<kPTile, kPUnitCost>(p);
+    if ((int)blockIdx.x >= sh.shares || sh.total == 0) return;
+
     if (warp == kMmaWarp) {                                // the MMA warp owns the tensor-memory allocation
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&tmem_base_s)), "r"(512)
                      : "memory");
@@ -204,9 +205,12 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
         more = next_rows(tid == 0);
         if (more) prefetch_queries(j);
     }
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
+    // tensor memory is there; the producers have no part in it and are at work
+    if (warp < kPSoftWarps || warp == kMmaWarp) {
+        tc_fence_before();
+        asm volatile("bar.sync 2, %0;\n" ::"n"(32 * (kPSoftWarps + 1)) : "memory");
+        tc_fence_after();
+    }
     const uint32_t tmem = tmem_base_s;
     // columns: S of stream w at 128 w, P of its halves in the first 32 columns of either half, O of stream w at 256 + 128 w
 

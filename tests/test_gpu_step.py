@@ -535,6 +535,13 @@ def test_shared_in_passes_layouts(fmt, page, order, S):
     check_shared(fmt, page, 2, 4, [0, S], [1000], [3 * s for s in range(S)], order=order, rows=ROOM)
 
 
+@pytest.mark.parametrize("fmt,page", [("bf16", 0), ("bf16", 16), ("e4m3", 0), ("e4m3", 16)])
+@pytest.mark.parametrize("n", [1, 15, 50, 127, 128])
+def test_shared_in_passes_prefixes_shorter_than_a_tile(fmt, page, n):
+    check_shared(fmt, page, 2, 4, [0, 30, 31], [n, n], [1 + s % 3 for s in range(31)], seed=n)
+    check_shared(fmt, page, 2, 16, [0, 31], [n], [s % 3 for s in range(31)], seed=n)
+
+
 @pytest.mark.parametrize("a,b", [("bf16", "e4m3"), ("e4m3", "bf16")])
 @pytest.mark.parametrize("S", [5, 40])
 def test_shared_in_passes_formats_lengths_per_head_and_empty_parts(a, b, S):
