@@ -36,12 +36,12 @@ struct AppendParams {
 
 __device__ __forceinline__ int append_len(const AppendParams &p, int s, int h)
 {
-    const int n = p.unit_lens ? p.unit_lens[(int64_t)s * p.H + h] : p.dst.seq_lens[s];   // plain loads: new_lens may be this array
+    const int n = p.unit_lens ? p.unit_lens[(int64_t)s * p.H + h] : p.dst.seq_lens[s];
     return min(max(n, 0), p.dst.n_max);
 }
 __device__ __forceinline__ int append_count(const AppendParams &p, int s)
 {
-    return p.n_new ? min(max(__ldg(p.n_new + s), 0), p.T) : p.T;
+    return p.n_new ? min(max(p.n_new[s], 0), p.T) : p.T;
 }
 
 // The 16 components a lane owns of a row.  SPLIT: components 8c..8c+7 and 64+8c..64+8c+7 (the two halves of 8 bands in the
@@ -134,11 +134,11 @@ __global__ void __launch_bounds__(kAppendThreads) k_append(const AppendParams p)
     const int n_new = append_count(p, s);
     const bool first = t0 == 0;
     if (first && tid == 0 && p.device_status && p.n_new) {
-        const int raw = __ldg(p.n_new + s);
+        const int raw = p.n_new[s];
         if (raw < 0 || raw > p.T) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
     }
     if (t0 < n_new) {
-        const int64_t p0 = p.pos ? __ldg(p.pos + s) : (int64_t)append_len(p, s, 0);
+        const int64_t p0 = p.pos ? p.pos[s] : (int64_t)append_len(p, s, 0);
         for (int i = tid; i < TT * kBands; i += kAppendThreads) {
             const int f = i & (kBands - 1);
             const double2 w = p.turn[f];
@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(kAppendThreads) k_append(const AppendParams p)
             int64_t slot0 = 0, off0 = -1;
             if (!p.unit_lens) {
                 slot0 = (int64_t)append_len(p, s, 0) + t;
-                if (slot0 < p.dst.n_max) off0 = row_offset(p.dst, p.layer, s, 0, (int)slot0);
+                if (slot0 < p.dst.n_max) off0 = step_row_offset(p.dst, p.layer, s, 0, (int)slot0);
             }
             float2 cs[8];
 #pragma unroll
@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(kAppendThreads) k_append(const AppendParams p)
                     int64_t slot = slot0, off = off0 == -1 ? -1 : off0 + h * p.dst.stride_head;
                     if (p.unit_lens) {
                         slot = (int64_t)append_len(p, s, h) + t;
-                        off = slot < p.dst.n_max ? row_offset(p.dst, p.layer, s, h, (int)slot) : -1;
+                        off = slot < p.dst.n_max ? step_row_offset(p.dst, p.layer, s, h, (int)slot) : -1;
                     }
                     if (off == -1) {                          // (offsets are multiples of 8 elements)
                         if (p.device_status) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(kAppendThreads) k_append(const AppendParams p)
                     if (KK == 3) {
                         const float *sc = is_k ? p.k_scale : p.v_scale;
                         if (sc) {
-                            const float scale = __ldg(sc + h);
+                            const float scale = sc[h];
 #pragma unroll
                             for (int i = 0; i < 16; ++i) x[i] = __fdiv_rn(x[i], scale);
                         }

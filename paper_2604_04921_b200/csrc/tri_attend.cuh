@@ -65,13 +65,15 @@ struct AttendParams {
 
 __device__ __forceinline__ int att_len(const AttendParams &p, int seq, int h)
 {
-    const int n = p.unit_lens ? __ldg(p.unit_lens + (int64_t)seq * p.H + h) : __ldg(p.src.seq_lens + seq);
+    const int n = ld_here(p.unit_lens ? p.unit_lens + (int64_t)seq * p.H + h : p.src.seq_lens + seq);
     return min(max(n, 0), p.src.n_max);
 }
-// Sequences [first, first + count) of a group.
+// Sequences [first, first + count) of a group.  (STRONG: before the kernel has waited, see ld_relaxed.)
+template <bool STRONG = false>
 __device__ __forceinline__ int2 att_group(const int32_t *start, int S, int g)
 {
-    const int a = min(max(__ldg(start + g), 0), S), b = min(max(__ldg(start + g + 1), 0), S);
+    const int a0 = STRONG ? ld_relaxed(start + g) : ld_here(start + g), b0 = STRONG ? ld_relaxed(start + g + 1) : ld_here(start + g + 1);
+    const int a = min(max(a0, 0), S), b = min(max(b0, 0), S);
     return make_int2(a, max(b - a, 0));
 }
 // r / d for r < 256, 0 < d <= 16, with inv = 65536 / d + 1: the product's error r * d / 65536 never reaches the next integer.
@@ -82,11 +84,14 @@ __device__ __forceinline__ int att_row_tiles(const AttendParams &p, int seq)
     return (att_group(p.group_start, p.S, seq).y + p.spt - 1) / p.spt;
 }
 // The last group that starts at or before a sequence (0 if none does); the warp's lanes look at 32 starts at a time.
+template <bool STRONG = false>
 __device__ __forceinline__ int att_group_of(const int32_t *start, int groups, int seq, int lane)
 {
     int g = -1;
-    for (int b = 0; b < groups; b += 32)
-        g += __popc(__ballot_sync(0xffffffffu, b + lane < groups && __ldg(start + min(b + lane, groups - 1)) <= seq));
+    for (int b = 0; b < groups; b += 32) {
+        const int32_t *at = start + min(b + lane, groups - 1);
+        g += __popc(__ballot_sync(0xffffffffu, b + lane < groups && (STRONG ? ld_relaxed(at) : ld_here(at)) <= seq));
+    }
     return max(g, 0);
 }
 // Index of tile `rt` of group g in units before the head is added: the tiles of ascending groups never collide, and no
@@ -179,9 +184,11 @@ __device__ __forceinline__ AttShare att_share(const AttendParams &p)
     const int n = by_head ? p.nseq * p.H : p.nseq, heads = by_head ? 1 : p.H;
     const int per = n <= nth ? 1 : (n + nth - 1) / nth;
     const int a = min(tid * per, n), b = min(a + per, n);
-    // steps of entry x, one head
+    // steps of entry x, one head.  Where the pass does not wait for its predecessor the thread's first length is acquired; with
+    // the barrier below every other load of the block follows thread 0's.
     auto cost = [&](int x) -> int {
-        const int len = by_head ? __ldg(p.unit_lens + x) : __ldg(p.src.seq_lens + x);
+        const int32_t *at = (by_head ? p.unit_lens : p.src.seq_lens) + x;
+        const int len = p.under && x == a ? ld_acquire(at) : ld_here(at);
         const int kt = (int)(((uint32_t)min(max(len, 0), p.src.n_max) + TILE - 1) / TILE);
         return (kt + COST) * (p.spt ? att_row_tiles(p, by_head ? x / p.H : x) : 1);
     };
@@ -191,7 +198,7 @@ __device__ __forceinline__ AttShare att_share(const AttendParams &p)
         sum += c0 * heads;
         if (p.spt) {
             const int g = by_head ? x / p.H : x;
-            descends |= __ldg(p.group_start + g) > __ldg(p.group_start + g + 1);
+            descends |= p.group_start[g] > p.group_start[g + 1];
         }
     }
     int incl = sum;
@@ -318,7 +325,7 @@ __device__ __forceinline__ void attend_block(const AttendParams &p, const Attend
     const uint32_t klane = krow * kRowBytes + ((((KEY8 ? lane >> 4 : (lane >> 3) & 1) ^ krow) & 7) << 4);
     const uint32_t vlane = vrow * kRowBytes + ((((lane >> 4) ^ vrow) & 7) << 4);
     // Set up under the kernel before it in the stream and waits for it here, except behind a pass over prefixes, whose blocks
-    // this pass's may follow one by one: that pass began behind everything this one reads, and it is waited for at the end.
+    // this pass's may follow one by one: that pass is waited for at the end, and att_share's first load orders the others.
     if (!p.under) grid_dependency_wait();
     grid_dependents_launch();
     auto params_of = [&](const AttJob &u) -> const AttendParams & {
@@ -340,7 +347,7 @@ __device__ __forceinline__ void attend_block(const AttendParams &p, const Attend
             if (sh.seq < g.x || sh.seq >= g.x + g.y) group = -1;
             if (blockIdx.x == 0 && p.device_status)
                 for (int i = tid; i < pre.nseq; i += kAttThreads)
-                    if (__ldg(pre.group_start + i) > __ldg(pre.group_start + i + 1)) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
+                    if (pre.group_start[i] > pre.group_start[i + 1]) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
         }
     }
     auto next_unit = [&](AttCursor &c, AttJob &u) -> bool {
@@ -386,7 +393,7 @@ __device__ __forceinline__ void attend_block(const AttendParams &p, const Attend
             for (int half = 0; half < NK; ++half) {
                 const uint32_t r = (uint32_t)pit * TILE + warp * ROWS + 16 * half;
                 const uint32_t pg = a.src.page_shift >= 0 ? r >> a.src.page_shift : r / (uint32_t)a.src.page_size;
-                page[half] = r < (uint32_t)pj.len ? __ldg(a.src.page_table + (int64_t)pj.seq * a.src.max_pages_per_seq + pg) : 0;
+                page[half] = r < (uint32_t)pj.len ? ld_here(a.src.page_table + (int64_t)pj.seq * a.src.max_pages_per_seq + pg) : 0;
                 slot[half] = (int)(r - pg * (uint32_t)a.src.page_size);
             }
         }
@@ -527,7 +534,7 @@ __device__ __forceinline__ void attend_block(const AttendParams &p, const Attend
             for (int i = 0; i < (TR ? 8 : 16); ++i) { o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f; }
 #pragma unroll
             for (int i = 0; i < NR; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
-            k_scale = params_of(j).k_scale ? __ldg(params_of(j).k_scale + j.h) : 1.f;
+            k_scale = params_of(j).k_scale ? params_of(j).k_scale[j.h] : 1.f;
 #pragma unroll
             for (int i = 0; i < NR; ++i) mul[i] *= k_scale;
         }
@@ -738,7 +745,7 @@ __device__ __forceinline__ void attend_block(const AttendParams &p, const Attend
         uint8_t *used = dyn + (warp * ST + stage) * kAttStageBytes;
         stage = stage + 1 == ST ? 0 : stage + 1;
         if (++it < j.kb) continue;
-        float vs = params_of(j).v_scale ? __ldg(params_of(j).v_scale + j.h) : 1.f;
+        float vs = params_of(j).v_scale ? params_of(j).v_scale[j.h] : 1.f;
         if constexpr (CL > 0) {
             // the prefix's rows are through: the sequence's own go on with the same sums, in units of their own scales
             const float k_before = k_scale, v_before = vs;
@@ -746,8 +753,8 @@ __device__ __forceinline__ void attend_block(const AttendParams &p, const Attend
             while (!own && next_unit(cur, j)) own = j.kb > j.ka;
             if (own) {
                 it = j.ka;
-                k_scale = params_of(j).k_scale ? __ldg(params_of(j).k_scale + j.h) : 1.f;
-                vs = params_of(j).v_scale ? __ldg(params_of(j).v_scale + j.h) : 1.f;
+                k_scale = params_of(j).k_scale ? params_of(j).k_scale[j.h] : 1.f;
+                vs = params_of(j).v_scale ? params_of(j).v_scale[j.h] : 1.f;
                 const float k_by = k_scale / k_before, v_by = v_before / vs;
 #pragma unroll
                 for (int i = 0; i < NR; ++i) mul[i] *= k_by;
@@ -971,22 +978,22 @@ __global__ void __launch_bounds__(kMergeThreads) k_attend_merge(const MergeParam
     __shared__ float2 red_ml[kMergeWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int per = p.G / p.rows, unit = blockIdx.x / per, s = unit / p.H, h = unit - s * p.H;
-    // the sequence's group, before the passes are waited for: they began behind whatever wrote group_start
+    // the sequence's group, before the passes are waited for: they began behind whatever wrote group_start (see ld_relaxed)
     int pre_rec = -1, row0 = 0;
     if (p.pre.rec) {
-        const int lo = att_group_of(p.group_start, p.P, s, lane);
-        const int2 g = att_group(p.group_start, p.S, lo);
+        const int lo = att_group_of<true>(p.group_start, p.P, s, lane);
+        const int2 g = att_group<true>(p.group_start, p.S, lo);
         if (s >= g.x && s < g.x + g.y) {
             const int rt = (s - g.x) / p.pre.spt;
             pre_rec = att_tile_index(lo, g.x, p.pre.spt, rt) * p.H + h;
             row0 = (s - g.x - rt * p.pre.spt) * p.G;
         }
-        if (blockIdx.x == 0 && p.device_status)
-            for (int i = threadIdx.x; i < p.P; i += kMergeThreads)
-                if (__ldg(p.group_start + i) > __ldg(p.group_start + i + 1)) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
     }
     grid_dependency_wait();
     grid_dependents_launch();
+    if (p.pre.rec && blockIdx.x == 0 && p.device_status)
+        for (int i = threadIdx.x; i < p.P; i += kMergeThreads)
+            if (p.group_start[i] > p.group_start[i + 1]) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
     const int2 own = p.own.rec[unit];
     if (!p.pre.rec && own.y < 2) return;                                     // finished by its block
     int2 pre = pre_rec >= 0 ? p.pre.rec[pre_rec] : make_int2(0, 0);

@@ -243,7 +243,7 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
             bool ok = true;
             if (p.src.paged && lane < nsub) {
                 const int pg = p.src.page_shift >= 0 ? (int)row >> p.src.page_shift : (int)row / p.src.page_size;
-                c3 = __ldg(p.src.page_table + (int64_t)a.seq * p.src.max_pages_per_seq + pg);
+                c3 = ld_here(p.src.page_table + (int64_t)a.seq * p.src.max_pages_per_seq + pg);
                 c1 = (int)row - pg * p.src.page_size;
                 ok = p.src.n_pages <= 0 || (c3 >= 0 && c3 < p.src.n_pages);
             }
@@ -326,7 +326,7 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                 c1 = (int)row; c3 = j.seq;
                 if (!p.src.paged || t >= n || sub >= boxes || row >= j.len) return true;
                 const int pg = p.src.page_shift >= 0 ? (int)row >> p.src.page_shift : (int)row / p.src.page_size;
-                c3 = __ldg(p.src.page_table + (int64_t)j.seq * p.src.max_pages_per_seq + pg);
+                c3 = ld_here(p.src.page_table + (int64_t)j.seq * p.src.max_pages_per_seq + pg);
                 c1 = (int)row - pg * p.src.page_size;
                 return p.src.n_pages <= 0 || (c3 >= 0 && c3 < p.src.n_pages);
             };
@@ -461,7 +461,7 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
 
             // base-2 logit = accumulator * mul (not 0: a masked logit is -infinity)
             bool ok = true;
-            float mul = fabsf(p.scale) * (p.k_scale ? __ldg(p.k_scale + u.h) : 1.f);
+            float mul = fabsf(p.scale) * (p.k_scale ? p.k_scale[u.h] : 1.f);
             if (KEY8) {
                 ok = __all_sync(0xffffffffu, mbar_wait_bounded(b_q, units & 1));        // the other warps' rows and scales, too
                 mul *= qscale_s[KEY8 ? row : 0];
@@ -603,7 +603,7 @@ k_attend_prefix(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
             tc_loaded(s1);
             const float m0 = __uint_as_float(s0[0]), m1 = __uint_as_float(s1[0]), mm = fmaxf(m0, m1);
             const float e0 = m0 == -INFINITY ? 0.f : ex2(m0 - mm), e1 = m1 == -INFINITY ? 0.f : ex2(m1 - mm);
-            const float vs = p.v_scale ? __ldg(p.v_scale + u.h) : 1.f;
+            const float vs = p.v_scale ? p.v_scale[u.h] : 1.f;
             const float f0 = e0 * __uint_as_float(s0[2]) * vs, f1 = e1 * __uint_as_float(s1[2]) * vs;
             const bool mine = row < u.nrows;
             const int sr = att_small_div(row, inv_g), sq = u.first_seq + sr, hq = u.h * p.G + row - sr * p.G;

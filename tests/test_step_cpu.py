@@ -77,3 +77,11 @@ def test_reference_attention_merges_over_cuts():
     wa, wb = math.exp(la - m), math.exp(lb - m)
     assert torch.allclose((wa * a + wb * b) / (wa + wb), whole, atol=1e-12)
     assert abs(m + math.log(wa + wb) - lse) < 1e-12
+
+
+def test_step_kernels_read_nothing_through_the_read_only_path():
+    """They begin while their predecessor still runs; a read-only load may be moved before the wait for it."""
+    for name in ("tri_step.cuh", "tri_append.cuh", "tri_attend.cuh", "tri_attend_umma.cuh"):
+        with open(os.path.join(ROOT, "paper_2604_04921_b200", "csrc", name)) as f:
+            code = [line.split("//")[0] for line in f]
+        assert not [line for line in code if "__ldg" in line or ".nc." in line or " row_offset(" in line], name
