@@ -424,7 +424,7 @@ tri_status tri_attend(tri_ctx *ctx, const tri_layer_cache *src, int32_t S, const
  *   prefix       a cache view of P sequences, the prefixes; its format may differ from that of src
  *   group_start  device int32 [P + 1], ascending within [0, S]: prefix p belongs to the sequences group_start[p] <= s
  *                < group_start[p + 1]; the others have no prefix.  Entries outside [0, S] count as the nearest bound;
- *                if they descend, TRI_ERR_DEVICE_CHECK is set in device_status and the outputs are unspecified.
+ *                if they descend then, TRI_ERR_DEVICE_CHECK is set in device_status and the outputs are unspecified.
  *   ws           tri_attend_workspace_bytes(ctx, S, P) bytes
  * Queries must be rotated to positions behind the prefix, as the model would have them.
  */

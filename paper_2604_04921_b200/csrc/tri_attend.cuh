@@ -76,6 +76,12 @@ __device__ __forceinline__ int2 att_group(const int32_t *start, int S, int g)
     const int a = min(max(a0, 0), S), b = min(max(b0, 0), S);
     return make_int2(a, max(b - a, 0));
 }
+// Whether a group ends before it begins.  Boundaries outside [0, S] count as the nearest bound here, too: a group that descends
+// out there only is an empty one.
+__device__ __forceinline__ bool att_descends(const int32_t *start, int S, int g)
+{
+    return min(max(start[g], 0), S) > min(max(start[g + 1], 0), S);
+}
 // r / d for r < 256, 0 < d <= 16, with inv = 65536 / d + 1: the product's error r * d / 65536 never reaches the next integer.
 __device__ __forceinline__ int att_small_div(int r, int inv) { return (r * inv) >> 16; }
 __device__ __forceinline__ int att_row_tiles(const AttendParams &p, int seq)
@@ -198,7 +204,7 @@ __device__ __forceinline__ AttShare att_share(const AttendParams &p)
         sum += c0 * heads;
         if (p.spt) {
             const int g = by_head ? x / p.H : x;
-            descends |= p.group_start[g] > p.group_start[g + 1];
+            descends |= att_descends(p.group_start, p.S, g);
         }
     }
     int incl = sum;
@@ -347,7 +353,7 @@ __device__ __forceinline__ void attend_block(const AttendParams &p, const Attend
             if (sh.seq < g.x || sh.seq >= g.x + g.y) group = -1;
             if (blockIdx.x == 0 && p.device_status)
                 for (int i = tid; i < pre.nseq; i += kAttThreads)
-                    if (pre.group_start[i] > pre.group_start[i + 1]) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
+                    if (att_descends(pre.group_start, pre.S, i)) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
         }
     }
     auto next_unit = [&](AttCursor &c, AttJob &u) -> bool {
@@ -993,7 +999,7 @@ __global__ void __launch_bounds__(kMergeThreads) k_attend_merge(const MergeParam
     grid_dependents_launch();
     if (p.pre.rec && blockIdx.x == 0 && p.device_status)
         for (int i = threadIdx.x; i < p.P; i += kMergeThreads)
-            if (p.group_start[i] > p.group_start[i + 1]) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
+            if (att_descends(p.group_start, p.S, i)) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
     const int2 own = p.own.rec[unit];
     if (!p.pre.rec && own.y < 2) return;                                     // finished by its block
     int2 pre = pre_rec >= 0 ? p.pre.rec[pre_rec] : make_int2(0, 0);
