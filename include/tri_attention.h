@@ -375,12 +375,13 @@ typedef struct {
  *   queries  rotated likewise into q_out
  * Nothing else of the cache or of q_out is written, rows of padding tokens (t >= n_new[s]) are not read.
  *   new_lens  device [S], or [U] with unit_lens (this layer's entries), or NULL: receives length + n_new, at most
- *             n_max.  It may be the array the lengths come from (not n_new); the layers of a step share the lengths, so
- *             hand it over with the step's last layer only.
+ *             n_max.  It may be the array the lengths come from (hand it over with the last layer that shares the
+ *             lengths, then) or lie apart from it; one that overlaps it in part, or n_new or pos, is refused.
  *   device_status  device int32[1] or NULL; set to TRI_ERR_DEVICE_CHECK if a row had no slot below n_max, a page id
  *             outside [0, n_pages) or a position outside [0, 2^31) -- such rows are skipped -- or if n_new[s] was
  *             outside [0, T] (the nearest bound counts)
- * The rows must not overlap the cache, and two sequences must not append into one page.
+ * The rows must not overlap the cache, and two sequences must not append into one page.  Destinations that meet in one place (a
+ * cache whose heads or sequences are broadcast, strides of q_out below 128) are refused.
  */
 tri_status tri_append(tri_ctx *ctx, const tri_layer_cache *dst, int32_t S, const tri_append_rows *rows,
                       int32_t *new_lens, int32_t *device_status, void *stream);
@@ -389,7 +390,7 @@ tri_status tri_append(tri_ctx *ctx, const tri_layer_cache *dst, int32_t S, const
 typedef struct {
     const void *q;             /* device bf16 [S][H*G][128], 16-byte rows                                          */
     int64_t q_stride_seq, q_stride_head;
-    void *out;                 /* device bf16 [S][H*G][128], 16-byte rows; must not overlap q (out == q is refused) */
+    void *out;                 /* device bf16 [S][H*G][128], 16-byte rows apart; must not overlap q (out == q is refused) */
     int64_t out_stride_seq, out_stride_head;
     float *lse;                /* device fp32 [S][H*G] or NULL: log sum_n exp(logit_n), -infinity without rows      */
     float scale;               /* logit_n = scale * (q . k_n); finite, and times log2 e too                         */

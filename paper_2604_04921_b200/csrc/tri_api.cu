@@ -1201,6 +1201,10 @@ bool rows16_ok(const void *p, int64_t a, int64_t b, int64_t c, int es)
     return p && !((uintptr_t)p & 15) && (a * es) % 16 == 0 && (b * es) % 16 == 0 && (c * es) % 16 == 0;
 }
 
+// Rows that are written, `n` of them `stride` elements apart, lie side by side: a broadcast dimension, whose rows meet in one
+// place, would be written by several blocks at a time.
+bool rows_apart(int64_t n, int64_t stride) { return n <= 1 || stride >= kHeadDim || stride <= -kHeadDim; }
+
 template <int KIND, int KK, bool SPLIT>
 cudaError_t launch_append(unsigned blocks, int tt, cudaStream_t st, const AppendParams &p)
 {
@@ -1244,12 +1248,17 @@ extern "C" tri_status tri_append(tri_ctx *c, const tri_layer_cache *dst, int32_t
     if (rows->q) {
         if (!rows_ok(rows->q, rows->q_stride_seq, rows->q_stride_tok, rows->q_stride_head, H * G, es)) return TRI_ERR_INVALID_ARG;
         if (!rows_ok(rows->q_out, rows->qo_stride_seq, rows->qo_stride_tok, rows->qo_stride_head, H * G, 2)) return TRI_ERR_INVALID_ARG;
+        if (!rows_apart(S, rows->qo_stride_seq) || !rows_apart(rows->T, rows->qo_stride_tok) || !rows_apart(H * G, rows->qo_stride_head))
+            return TRI_ERR_INVALID_ARG;
         if (rows->q == rows->q_out && (rows->kind != 0 || (S > 1 && rows->q_stride_seq != rows->qo_stride_seq) ||
                                        (rows->T > 1 && rows->q_stride_tok != rows->qo_stride_tok) ||
                                        (H * G > 1 && rows->q_stride_head != rows->qo_stride_head)))
             return TRI_ERR_INVALID_ARG;
     }
     if (!rows->pos && dst->unit_lens) return TRI_ERR_INVALID_ARG;
+    const tri_cache_view *dv = dst->view;
+    if (!rows_apart(H, dv->stride_head) || !(dv->paged ? rows_apart(dv->n_pages == 1 ? 1 : 2, dv->stride_page) : rows_apart(S, dv->stride_seq)))
+        return TRI_ERR_INVALID_ARG;
     if ((r = check_device(c)) != TRI_OK) return r;
 
     AppendParams p;
@@ -1274,8 +1283,9 @@ extern "C" tri_status tri_append(tri_ctx *c, const tri_layer_cache *dst, int32_t
     auto disjoint = [&](const int32_t *a, int64_t n) {
         return !lens_out || !a || (uintptr_t)(lens_out + n_lens) <= (uintptr_t)a || (uintptr_t)(a + n) <= (uintptr_t)lens_out;
     };
-    if (!disjoint(rows->n_new, S)) return TRI_ERR_INVALID_ARG;
+    if (!disjoint(rows->n_new, S) || !disjoint((const int32_t *)rows->pos, 2 * (int64_t)S)) return TRI_ERR_INVALID_ARG;
     const bool apart = disjoint(lens_in, n_lens);
+    if (!apart && lens_out != lens_in) return TRI_ERR_INVALID_ARG;          // a block would store what another has yet to read
     const bool later = !apart && p.ntiles > 1;
     p.new_lens = later ? nullptr : lens_out;
     const unsigned blocks = (unsigned)(p.ntiles * S);
@@ -1386,6 +1396,7 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
     const int32_t H = c->desc.n_kv_heads, G = c->desc.group_size;
     if (!rows16_ok(io->q, S > 1 ? io->q_stride_seq : 0, H * G > 1 ? io->q_stride_head : 0, 0, 2) ||
         !rows16_ok(io->out, S > 1 ? io->out_stride_seq : 0, H * G > 1 ? io->out_stride_head : 0, 0, 2) || io->q == io->out ||
+        !rows_apart(S, io->out_stride_seq) || !rows_apart((int64_t)H * G, io->out_stride_head) ||
         !std::isfinite(io->scale * 1.44269504f))
         return TRI_ERR_INVALID_ARG;
     if ((r = check_device(c)) != TRI_OK) return r;
