@@ -319,6 +319,7 @@ class TriContext:
         self._h = None
         _check(L.tri_create(ctypes.byref(d), qc.data_ptr(), qn.data_ptr(), ctypes.byref(h)), "tri_create")
         self._h = h
+        self._dev = torch.cuda.current_device()              # where tri_create has put the context
 
     def close(self):
         if self._h is not None:
@@ -449,6 +450,7 @@ class TriContext:
     # -- the decode step around the round ----------------------------------------------------
     def _check_cache(self, c: LayerCache):
         assert c.n_kv_heads == self.n_kv_heads and c.n_layers == self.n_layers, "the cache is of another model"
+        assert c._dev == self._dev, "the cache is not on the context's device"
 
     def append(self, dst: LayerCache, k: torch.Tensor, v: Optional[torch.Tensor], pos: Optional[torch.Tensor],
                q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,

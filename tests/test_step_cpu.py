@@ -85,3 +85,31 @@ def test_step_kernels_read_nothing_through_the_read_only_path():
         with open(os.path.join(ROOT, "paper_2604_04921_b200", "csrc", name)) as f:
             code = [line.split("//")[0] for line in f]
         assert not [line for line in code if "__ldg" in line or ".nc." in line or " row_offset(" in line], name
+
+
+@pytest.mark.parametrize("call", ["append", "attend", "attend_shared"])
+def test_caches_of_another_device_never_reach_the_library(call, monkeypatch):
+    """A cache in host memory is consistent in itself; only the context knows that its kernels could not read it."""
+    reached = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *a: reached.append(name) or 0
+    monkeypatch.setattr(tb, "lib", Library)
+    monkeypatch.setattr(tb, "_stream_on", lambda device: 0)
+    ctx = tb.TriContext.__new__(tb.TriContext)
+    ctx.n_layers, ctx.n_kv_heads, ctx.group_size, ctx._h, ctx._dev = 1, 2, 4, None, 0
+    c, lens = Cache(1, 3, 2, 16, device="cpu"), torch.zeros(3, dtype=torch.int32)
+    lc = tb.LayerCache(c.view(tb, seq_lens=lens), 0)
+    x, q = torch.zeros(3, 1, 2, 128, dtype=torch.bfloat16), torch.zeros(3, 8, 128, dtype=torch.bfloat16)
+    ws = torch.zeros(1 << 20, dtype=torch.uint8)
+    run = {"append": lambda: ctx.append(lc, x, x, torch.zeros(3, dtype=torch.int64)),
+           "attend": lambda: ctx.attend(lc, q, q.clone(), ws),
+           "attend_shared": lambda: ctx.attend_shared(lc, torch.tensor([0, 3, 3, 3], dtype=torch.int32), lc, q, q.clone(), ws)}[call]
+    with pytest.raises(AssertionError):
+        run()
+    assert not reached
+    lc._dev = 0                                                       # (as if it were there: the rest of the arguments is not)
+    with pytest.raises(AssertionError):
+        run()
+    assert not reached
