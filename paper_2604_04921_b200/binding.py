@@ -459,7 +459,8 @@ class TriContext:
         """Append T tokens per sequence to one layer: k, v [S, T, H, 128] (bf16 or fp32, any strides with 16-byte rows),
         pre-RoPE; keys are rotated to positions pos[s] + t on the way (kept as they are in a pre-RoPE cache) and, if
         given, q [S, T, H * G, 128] into q_out (bf16).  n_new [S] int32: tokens each sequence brings, default T.
-        new_lens receives the lengths after the append and may be the array they come from (last layer of a step)."""
+        new_lens receives the lengths after the append: an array apart from the one they come from, given with every layer
+        and read by the step's attention, or that one itself, given with the last layer that shares the lengths."""
         self._check_cache(dst)
         dev, S, shape, dt = dst._dev, dst.n_seqs, k.shape, k.dtype
         T = shape[1]

@@ -113,3 +113,40 @@ def test_caches_of_another_device_never_reach_the_library(call, monkeypatch):
     with pytest.raises(AssertionError):
         run()
     assert not reached
+
+
+def test_the_documented_decode_step_attends_over_the_new_token():
+    """The README's decode step, run with a context that only keeps lengths: every layer's attention counts the appended row,
+    in the first step and in one behind it."""
+    with open(os.path.join(ROOT, "README.md")) as f:
+        blocks = [b.split("```")[0] for b in f.read().split("```python\n")[1:]]
+    code, = [b for b in blocks if "ctx.append(" in b]
+    L, S, H, G = 3, 2, 2, 4
+    c = Cache(L, S, H, 16, device="cpu")
+    seq_lens = torch.tensor([3, 9], dtype=torch.int32)
+    src = c.view(tb, seq_lens=seq_lens)
+    other = [tb.LayerCache(c.view(tb, seq_lens=torch.zeros(S, dtype=torch.int32)), l) for l in range(L)]
+    attended = []
+
+    class Lengths:
+        def append(self, cache, k, v, pos, q=None, q_out=None, n_new=None, new_lens=None):
+            if new_lens is not None:
+                new_lens.copy_(cache.view.seq_lens + 1)
+
+        def attend(self, cache, q, out, ws):
+            attended.append((cache.layer, cache.view.seq_lens.tolist()))
+
+        def attend_shared(self, prefix, starts, cache, q, out, ws):
+            self.attend(cache, q, out, ws)
+
+        def attend_workspace(self, S, n_prefixes=0):
+            return None
+    new = torch.zeros(S, 1, H, 128)
+    names = dict(tb=tb, torch=torch, ctx=Lengths(), src=src, seq_lens=seq_lens, k=c.k, v=c.v, q=new, k_new=new, v_new=new, q_new=new,
+                 q_rot=new, pos=torch.zeros(S), out=None, n_layers=L, S=S, after=other, prefix=other, starts=None, n_prefixes=1)
+    for step in range(2):
+        attended.clear()
+        exec(code, dict(names))
+        want = [4 + step, 10 + step]
+        assert {l for l, _ in attended} == set(range(L)) and all(n == want for _, n in attended), attended
+        assert seq_lens.tolist() == want
