@@ -405,23 +405,25 @@ size_t tri_attend_workspace_bytes(const tri_ctx *ctx, int32_t S, int32_t P);
  * A unit without rows gives zeros.  Key formats 0 and 3; the pre-RoPE formats hold unrotated keys and are refused
  * (TRI_ERR_UNSUPPORTED), as is a cache without values (TRI_ERR_INVALID_ARG).  Rows at or behind the length are never
  * used, whatever they hold.  Logits, softmax statistics and sums are fp32; the weights of the sum over values enter
- * the tensor cores as a 16-bit value plus the 16-bit rest of it (where more than 16 query rows share a prefix: rounded
- * once, to bf16, over 8-bit values to f16).  Sums are formed in a fixed order: equal inputs give
+ * the tensor cores as a 16-bit value plus the 16-bit rest of it (shared prefixes with S * G > 16 * P: rounded once, to
+ * bf16, which raises the error of bf16 outputs by up to 1.45 times, over 8-bit values to f16, which does not).  Sums are formed in a fixed order: equal inputs give
  * equal bits.  Ragged batches are cut into equal shares over the GPU; S * n_kv_heads * (n_max / 64 + 3) must stay below
  * 2^31 (for prefixes, with P + S in place of S at most), else TRI_ERR_UNSUPPORTED.  An infinity among the values of a
  * unit's rows makes the outputs of its component infinite or NaN.
  *   ws  device workspace of tri_attend_workspace_bytes(ctx, S, 0) bytes, 256-byte aligned; nothing in it has to be
  *       set, nothing is kept in it from call to call.  Calls that may overlap on the GPU need a workspace each.
  *   device_status  device int32[1] or NULL; TRI_ERR_DEVICE_CHECK if a kernel met a page id outside [0, n_pages): such
- *       rows count as absent.
+ *       rows count as absent.  tri_attend_shared also TRI_ERR_TIMEOUT if a bounded wait of the pass over prefixes ran out:
+ *       the outputs are unspecified then, and only device_status tells.
  */
 tri_status tri_attend(tri_ctx *ctx, const tri_layer_cache *src, int32_t S, const tri_attend_io *io,
                       int32_t *device_status, void *ws, size_t ws_bytes, void *stream);
 
 /*
  * The same for sequences that continue shared prefixes (several samples of one prompt): sequence s of group p attends
- * over the rows of prefix p and over its own rows, in one softmax, and the rows of a prefix are read for all sequences
- * of its group together.
+ * over the rows of prefix p and over its own rows, in one softmax.  The rows of a prefix are read for several sequences
+ * of its group together: for up to 128 query rows (sequences x G) where S * G > 16 * P, else for up to 16; in few short
+ * units for each sequence, from L2.  Prefixes without sequences count in P: hand over those in use.
  *   prefix       a cache view of P sequences, the prefixes; its format may differ from that of src
  *   group_start  device int32 [P + 1], ascending within [0, S]: prefix p belongs to the sequences group_start[p] <= s
  *                < group_start[p + 1]; the others have no prefix.  Entries outside [0, S] count as the nearest bound;

@@ -1350,10 +1350,14 @@ tri_status check_attend_cache(const tri_ctx *c, const tri_layer_cache *lc, int32
     return lc->view->v ? TRI_OK : TRI_ERR_INVALID_ARG;
 }
 
-// Whether the 128-row tcgen05 pass takes the prefixes: more query rows per prefix on average than the one 16-row tile of
-// the mma.sync pass, which reads the rows once per tile (one 32K prefix, G = 4: 37 against 43 us at 4 or 8 rows, 39 against
-// 43 at 16, 49 against 44 at 32, 77 against 46 at 64), and rows the TMA unit can address: every stride that is used positive
-// (a broadcast head has stride 0) and below the unit's 2^40 bytes.
+// Whether the 128-row tcgen05 pass takes the prefixes: more query rows per prefix on average than the one 16-row tile of the
+// mma.sync pass, which walks the rows once per tile.  16-row against 128-row pass, whole calls: one 32K prefix, 8 heads, G = 4,
+// bf16 33 against 41 us at 4 query rows, 35 / 42 at 16, 45 / 42 at 20, 47 / 42 at 32, 80 / 49 at 64; e4m3 29 / 44, 31 / 46, 41 / 48,
+// 42 / 48, 71 / 55.  The groups are on the device, so that the average counts prefixes without sequences, too: 16 prefixes of 8K
+// with 16 rows each 104 / 113..130 (e4m3 78 / 132) and 32 of them, one with 33 of 64 sequences at G = 8, 214 / 209..215 (174 /
+// 243), but one prefix of 32 sequences beside 7 unused ones 47 / 31..36 (45 / 34), one of 64 beside 63 unused 62 / 43 (57 / 42).
+// And rows the TMA unit can address: every stride that is used positive (a broadcast head has stride 0) and below the unit's
+// 2^40 bytes.
 bool prefix_umma_ok(const tri_ctx *c, const tri_cache_view *v, int32_t S, int32_t P)
 {
     if ((int64_t)S * c->desc.group_size <= (int64_t)16 * P) return false;
@@ -1457,6 +1461,9 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
     mp.own.rec = p.rec; mp.own.slots = p.slots; mp.own.whole = p.whole; mp.own.blocks = pl.blocks; mp.own.rows = pl.own_rows; mp.own.spt = 0;
     mp.S = S; mp.P = P; mp.H = H; mp.G = G; mp.group_start = group_start;
     mp.out = p.out; mp.out_seq = p.out_seq; mp.out_head = p.out_head; mp.lse = io->lse; mp.device_status = device_status;
+    // a query row per block, or all of a unit's: 8192 rows a unit, 8 units 12.1 against 14.5 us at G = 4 and 14.0 against 25.5 at
+    // G = 16, 32 units 26.6 / 26.9 and 31.2 / 31.6; between there and the limit the other side wins at large G (64 units 46.2 / 46.4
+    // and 54.8 / 49.9, 128 units 86.8 / 84.5 and 100.4 / 86.5)
     mp.rows = (int64_t)S * H < c->n_sm ? 1 : G;
     TRI_CUDA(launch_under(k_attend_merge, (unsigned)((int64_t)S * H * (G / mp.rows)), kMergeThreads, 0, st, mp));
     return TRI_OK;

@@ -19,6 +19,15 @@
 // MMAs 1024 (as issued, one by one, 1600), the exponentials 1024.  One prefix of 256K rows, 128 query rows per head: 6.7 TB/s.
 // With more query rows the tiles of one prefix share its rows through L2 and the issue of the MMAs bounds it.  Start, drain
 // and join cost about 15 us, which is what counts on short prefixes.
+// 8-bit rows are half the bytes but take as long (whole calls: 32 sequences on 32K rows 69.8 us, bf16 68.1; 64 on six prompts
+// 113.9, bf16 109.4): HBM does not bound them.  Not taken apart; the two converting warps per matrix stand between the copies
+// and the MMAs, and the MMAs as issued alone need more than the rows' 1400 cycles.
+//
+// Weights are rounded once, to bf16 (8-bit rows: f16), and the sum that divides is that of the rounded ones, which cancels the
+// part of the error that all rows share.  Error of the outputs against 64 bits, relative, where one rounding of the output makes
+// 1.65e-3: 1.68e-3 for values around a common centre of half their spread, 2.2e-3 to 2.4e-3 for values without one (1.8e-3 to
+// 2.0e-3 where few rows have the weight); 8-bit rows 1.67e-3.  The rest of a weight in a second MMA would take this off; it made
+// the MMAs 25 % longer.
 //
 // Every wait is bounded; one that runs out sets TRI_ERR_TIMEOUT, all roles leave their loops and the tensor memory is
 // released at the common exit.
