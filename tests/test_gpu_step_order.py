@@ -68,3 +68,24 @@ def test_append_then_attend_shared_back_to_back(fmt, page, S, T):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(raw(st.out), raw(want)), r
+
+
+def test_three_streams_append_and_attend_shared_at_once():
+    """Each with a cache and a workspace of its own, through the 16-row and the 128-row pass: the bits of each alone."""
+    jobs = [Step(S, "bf16", 16, 1, 12) for S in (3, 20, 33)]
+    want = []
+    for st in jobs:
+        st.run()
+        torch.cuda.synchronize()
+        want.append(st.out.clone())
+    streams = [torch.cuda.Stream() for _ in jobs]
+    for r in range(4):
+        for st in jobs:
+            st.out.zero_()
+        torch.cuda.synchronize()
+        for st, stream in zip(jobs, streams):
+            with torch.cuda.stream(stream):
+                st.run()
+        torch.cuda.synchronize()
+        for st, out in zip(jobs, want):
+            assert torch.equal(raw(st.out), raw(out)), (r, st.S)
