@@ -62,6 +62,8 @@ typedef struct {
 
 typedef struct tri_ctx tri_ctx;
 
+#define TRI_ROW4_BYTES 80      /* a cached row of 128 components in 4 bits (k_kind 5)                         */
+
 /*
  * Builds the per-model context on the current CUDA device: device copies of the calibration
  * statistics of Section 4.1 and the offset-averaged phasors (1/|D|) sum_delta e^{i omega_f delta}.
@@ -84,8 +86,8 @@ tri_status tri_destroy(tri_ctx *ctx);
  *                           row at  l*stride_layer + page*stride_page + h*stride_head + (n % page_size)*stride_slot
  */
 typedef struct {
-    void *k;                   /* keys: bf16 post-RoPE (k_kind 0), fp32 pre-RoPE (1), bf16 pre-RoPE (2), e4m3 post-RoPE (3) */
-    void *v;                   /* values, bf16 (e4m3 with k_kind 3), same strides as k; NULL = no value cache */
+    void *k;                   /* keys: bf16 post-RoPE (k_kind 0), fp32 pre-RoPE (1), bf16 pre-RoPE (2), e4m3 post-RoPE (3), 4 bits post-RoPE (5) */
+    void *v;                   /* values, bf16 (e4m3 with k_kind 3, 4 bits with k_kind 5), same strides as k; NULL = no value cache */
     int32_t k_kind;            /* 0: bf16 as cached by the model (post-RoPE) -- the fast path
                                   1: fp32 pre-RoPE vectors, scored in double (a slow reference-style path)
                                   2: bf16 pre-RoPE vectors (the k_f of Section 4.1 as they are), scored in fp32 with
@@ -96,7 +98,11 @@ typedef struct {
                                      by a unit's keys drops out of the z-score of Section 4.3).  Widened exactly to f16
                                      in registers, then the same contractions on f16 tensor-core MMAs.  Strides are
                                      multiples of 16 elements.  tri_compress_host does not take this format.
-                                  1 and 2 need `positions`, or slot = position                                   */
+                                  5: 4-bit post-RoPE keys and values, rows of TRI_ROW4_BYTES bytes as described at
+                                     tri_append.  Elements are bytes: strides are multiples of 16 and a row takes 80.
+                                     Taken by tri_append, tri_attend, tri_read and tri_compact; the calls that score keys
+                                     take what tri_read makes of them (TRI_ERR_UNSUPPORTED here)
+                                  1 and 2 need `positions`, or slot = position.  There is no format 4             */
     int32_t paged;
     int64_t stride_layer, stride_seq, stride_head, stride_tok;
     const int32_t *page_table; /* device [S][max_pages_per_seq]                                  */
@@ -369,8 +375,16 @@ typedef struct {
  *   keys     k_kind 0, 3: band f of the key is rotated by the angle p * omega_f (Section 2.1; the band layout is the
  *            context's pair_layout), in fp32 with the angle reduced in fp64, and rounded once to bf16 or e4m3;
  *            k_kind 1, 2: stored as they are (fp32, bf16), these caches hold pre-RoPE vectors
- *   values   rounded to the cache's format
+ *            k_kind 5: rotated likewise, in fp32, and quantised as below
+ *   values   rounded to the cache's format (k_kind 5: quantised as below)
  *   e4m3     round(x / scale) to nearest even, beyond +-448 to +-448, NaN to NaN
+ *   4 bits   (k_kind 5) each group of 32 components has a scale s and a centre c in bf16, and a component stands for
+ *            (code - 8) s + c.  With the group's smallest and largest value lo and hi: c = bf16((8 hi + 7 lo) / 15), s = the
+ *            smallest bf16 that is not below (hi - c) / 7 and (c - lo) / 8 (at least 2^-126, or 0 if both are 0), code =
+ *            8 + (x - c) / s, rounded to nearest even and kept within 0..15: no component is off by more than s / 2 and the
+ *            rounding of (x - c) / s.  A group with a NaN or an infinity becomes NaN throughout (c NaN, s 0).
+ *            A row is TRI_ROW4_BYTES bytes: component 32 g + 8 t + 2 i + h (g, t, i < 4, h < 2) in bits 4 (i + 4 h) .. + 3 of
+ *            the 32-bit word 4 t + g (little endian), the scales of the four groups from byte 64 on, the centres from byte 72 on.
  *   positions of the view, if any, receive p
  *   queries  rotated likewise into q_out
  * Nothing else of the cache or of q_out is written, rows of padding tokens (t >= n_new[s]) are not read.
@@ -385,6 +399,29 @@ typedef struct {
  */
 tri_status tri_append(tri_ctx *ctx, const tri_layer_cache *dst, int32_t S, const tri_append_rows *rows,
                       int32_t *new_lens, int32_t *device_status, void *stream);
+
+/* Where tri_read puts rows of one layer: up to T rows per sequence. */
+typedef struct {
+    void *k, *v;               /* device [S][T][H][128], rows on 16-byte boundaries, components contiguous, strides in
+                                  elements; either may be NULL, not both                                          */
+    int32_t kind;              /* 0: bf16, 1: fp32                                                                */
+    int32_t T;                 /* >= 1                                                                            */
+    int64_t k_stride_seq, k_stride_tok, k_stride_head;
+    int64_t v_stride_seq, v_stride_tok, v_stride_head;
+    const int32_t *first;      /* device [S] or NULL = 0: the slot row 0 of each sequence is read from (below 0: 0) */
+} tri_read_rows;
+
+/*
+ * Reads cached rows back: row t of unit (s, h) receives what slot first[s] + t stands for, for the slots below the unit's length
+ * and t < T.  The other rows are left as they are.  All key formats: bf16 and fp32 rows as they are, e4m3 times the scale of
+ * the head, 4-bit rows (code - 8) s + c; formed in fp32, rounded once to the output's type.  Keys come as they are cached, rotated
+ * or not.  With T at least the longest length the result is a contiguous cache of the same slots ([S][H][N][128] by its
+ * strides), which tri_score and the round take; with first = the lengths before an append it is what the append has stored.
+ *   device_status  device int32[1] or NULL; TRI_ERR_DEVICE_CHECK if a page id was outside [0, n_pages): such rows are skipped
+ * The outputs must not overlap the cache or each other; destinations that meet in one place are refused.
+ */
+tri_status tri_read(tri_ctx *ctx, const tri_layer_cache *src, int32_t S, const tri_read_rows *rows,
+                    int32_t *device_status, void *stream);
 
 /* Queries and outputs of an attention call: one query token per sequence, rotated like the cached keys. */
 typedef struct {
@@ -402,12 +439,14 @@ size_t tri_attend_workspace_bytes(const tri_ctx *ctx, int32_t S, int32_t P);
 /*
  * Attention of one decode step over one layer of the cache, compressed or not:
  *   out[s, h*G + g] = sum_n softmax_n(scale * q[s, h*G + g] . k_n) v_n     over the cached rows n of unit (s, h).
- * A unit without rows gives zeros.  Key formats 0 and 3; the pre-RoPE formats hold unrotated keys and are refused
+ * A unit without rows gives zeros.  Key formats 0, 3 and 5; the pre-RoPE formats hold unrotated keys and are refused
  * (TRI_ERR_UNSUPPORTED), as is a cache without values (TRI_ERR_INVALID_ARG).  Rows at or behind the length are never
  * used, whatever they hold.  Logits, softmax statistics and sums are fp32; the weights of the sum over values enter
  * the tensor cores as a 16-bit value plus the 16-bit rest of it (shared prefixes with S * G > 16 * P: rounded once, to
- * bf16, which raises the error of bf16 outputs by up to 1.45 times, over 8-bit values to f16, which does not).  Sums are formed in a fixed order: equal inputs give
- * equal bits.  Ragged batches are cut into equal shares over the GPU; S * n_kv_heads * (n_max / 64 + 3) must stay below
+ * bf16, which raises the error of bf16 outputs by up to 1.45 times, over 8-bit values to f16, which does not).  Over 4-bit
+ * values a weight is multiplied by the scale of its row and group and rounded once, to f16 (2^-12 of the weight, or 2^-36 of
+ * the largest weight times the largest scale of the unit so far where that is more); the centres are summed in fp32.  Sums
+ * are formed in a fixed order: equal inputs give equal bits.  Ragged batches are cut into equal shares over the GPU; S * n_kv_heads * (n_max / 64 + 3) must stay below
  * 2^31 (for prefixes, with P + S in place of S at most), else TRI_ERR_UNSUPPORTED.  An infinity among the values of a
  * unit's rows makes the outputs of its component infinite or NaN.
  *   ws  device workspace of tri_attend_workspace_bytes(ctx, S, 0) bytes, 256-byte aligned; nothing in it has to be
@@ -429,7 +468,8 @@ tri_status tri_attend(tri_ctx *ctx, const tri_layer_cache *src, int32_t S, const
  *                < group_start[p + 1]; the others have no prefix.  Entries outside [0, S] count as the nearest bound;
  *                if they descend then, TRI_ERR_DEVICE_CHECK is set in device_status and the outputs are unspecified.
  *   ws           tri_attend_workspace_bytes(ctx, S, P) bytes
- * Queries must be rotated to positions behind the prefix, as the model would have them.
+ * Queries must be rotated to positions behind the prefix, as the model would have them.  Key formats 0 and 3
+ * (TRI_ERR_UNSUPPORTED otherwise: a 4-bit cache is attended with tri_attend, and a prefix of its own joined by the lse).
  */
 tri_status tri_attend_shared(tri_ctx *ctx, const tri_layer_cache *prefix, int32_t P, const int32_t *group_start,
                              const tri_layer_cache *src, int32_t S, const tri_attend_io *io,

@@ -23,14 +23,15 @@ SOURCES = [_PKG / "csrc" / "tri_api.cu"]
 HEADERS = [_ROOT / "include" / "tri_attention.h", _PKG / "csrc" / "tri_common.cuh", _PKG / "csrc" / "tri_score.cuh",
            _PKG / "csrc" / "tri_score_pre.cuh", _PKG / "csrc" / "tri_score_tma.cuh", _PKG / "csrc" / "tri_score_umma.cuh", _PKG / "csrc" / "tri_calib.cuh", _PKG / "csrc" / "tri_calib_tma.cuh",
            _PKG / "csrc" / "tri_select.cuh", _PKG / "csrc" / "tri_compact.cuh",
-           _PKG / "csrc" / "tri_step.cuh", _PKG / "csrc" / "tri_append.cuh", _PKG / "csrc" / "tri_attend.cuh", _PKG / "csrc" / "tri_attend_umma.cuh"]
+           _PKG / "csrc" / "tri_step.cuh", _PKG / "csrc" / "tri_append.cuh", _PKG / "csrc" / "tri_attend.cuh", _PKG / "csrc" / "tri_attend_umma.cuh",
+           _PKG / "csrc" / "tri_row4.cuh", _PKG / "csrc" / "tri_attend4.cuh", _PKG / "csrc" / "tri_read.cuh"]
 
 EXPORTS = ["tri_create", "tri_destroy", "tri_workspace_bytes", "tri_score", "tri_select", "tri_compact",
            "tri_compress", "tri_select_budgets", "tri_compress_budgets", "tri_compress_windowed", "tri_compress_host", "tri_score_static", "tri_score_static_bytes", "tri_compress_launches", "tri_set_pipeline", "tri_set_score_kernel", "tri_last_cuda_error",
            "tri_profile_begin", "tri_profile_read", "tri_profile_end",
            "tri_calib_state_bytes", "tri_calib_workspace_bytes", "tri_calib_reset", "tri_calib_accumulate",
            "tri_calib_finalize", "tri_selftest_bounded_wait",
-           "tri_append", "tri_attend_workspace_bytes", "tri_attend", "tri_attend_shared"]
+           "tri_append", "tri_read", "tri_attend_workspace_bytes", "tri_attend", "tri_attend_shared"]
 
 STATUS = {0: "TRI_OK", 1: "TRI_ERR_INVALID_ARG", 2: "TRI_ERR_UNSUPPORTED", 3: "TRI_ERR_WORKSPACE",
           4: "TRI_ERR_CUDA", 5: "TRI_ERR_DEVICE_CHECK", 6: "TRI_ERR_TIMEOUT"}
@@ -92,15 +93,23 @@ class _AppendRows(ctypes.Structure):
                 ("n_new", ctypes.c_void_p), ("pos", ctypes.c_void_p)]
 
 
+class _ReadRows(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("kind", ctypes.c_int32), ("T", ctypes.c_int32),
+                ("k_stride_seq", ctypes.c_int64), ("k_stride_tok", ctypes.c_int64), ("k_stride_head", ctypes.c_int64),
+                ("v_stride_seq", ctypes.c_int64), ("v_stride_tok", ctypes.c_int64), ("v_stride_head", ctypes.c_int64),
+                ("first", ctypes.c_void_p)]
+
+
 class _AttendIo(ctypes.Structure):
     _fields_ = [("q", ctypes.c_void_p), ("q_stride_seq", ctypes.c_int64), ("q_stride_head", ctypes.c_int64),
                 ("out", ctypes.c_void_p), ("out_stride_seq", ctypes.c_int64), ("out_stride_head", ctypes.c_int64),
                 ("lse", ctypes.c_void_p), ("scale", ctypes.c_float)]
 
 
-# The same two structures in one packing step: these calls are made per layer and token, where every microsecond of the
+# The same structures in one packing step: these calls are made per layer and token, where every microsecond of the
 # host counts (setting 20 fields one by one takes 2 us, packing them 0.5 us).
 _pack_append = struct.Struct("@PPPiiqqqqqqqqqPqqqPP").pack
+_pack_read = struct.Struct("@PPiiqqqqqqP").pack
 _pack_attend = struct.Struct("@PqqPqqPfi").pack
 
 _lib = None
@@ -169,6 +178,8 @@ def lib():
     L.tri_selftest_bounded_wait.restype = ctypes.c_int
     L.tri_append.argtypes = [P, P, i32, P, P, P, P]          # structures as addresses or packed bytes
     L.tri_append.restype = ctypes.c_int
+    L.tri_read.argtypes = [P, P, i32, P, P, P]
+    L.tri_read.restype = ctypes.c_int
     L.tri_attend_workspace_bytes.argtypes = [P, i32, i32]
     L.tri_attend_workspace_bytes.restype = sz
     L.tri_attend.argtypes = [P, P, i32, P, P, P, sz, P]
@@ -212,6 +223,7 @@ def _status_addr(t: Optional[torch.Tensor], device: int) -> int:
 
 
 _SCALE = 128.0 ** -0.5
+ROW4_BYTES = 80            # a 4-bit row: 128 codes, then scale and centre of its four groups of 32 components
 
 
 @dataclasses.dataclass
@@ -219,6 +231,7 @@ class CacheView:
     """K/V cache as torch tensors plus the layout the C ABI needs.
 
     contiguous: k, v [L, S, H, N, 128];  paged: k, v [L, P, H, page_size, 128] + page_table [S, max_pages].
+    4-bit caches are uint8 tensors of 80-byte rows: [.., 80] in place of [.., 128].
     """
     k: torch.Tensor
     v: Optional[torch.Tensor]
@@ -230,16 +243,18 @@ class CacheView:
 
     def c_view(self) -> _CacheView:
         k = self.k
-        assert k.dim() == 5 and k.shape[-1] == 128 and k.stride(-1) == 1
+        row4 = k.dtype == torch.uint8                        # 4-bit keys and values: rows of bytes (k_kind 5)
+        assert k.dim() == 5 and k.shape[-1] == (ROW4_BYTES if row4 else 128) and k.stride(-1) == 1
         fp8 = k.dtype == torch.float8_e4m3fn                 # e4m3 keys come with e4m3 values (k_kind 3)
         if self.v is not None:
             assert self.v.shape == k.shape and self.v.stride() == k.stride()
-            assert self.v.dtype == (torch.float8_e4m3fn if fp8 else torch.bfloat16)
-        assert k.dtype in (torch.bfloat16, torch.float32, torch.float8_e4m3fn)
+            assert self.v.dtype == (k.dtype if fp8 or row4 else torch.bfloat16)
+        assert k.dtype in (torch.bfloat16, torch.float32, torch.float8_e4m3fn, torch.uint8)
+        assert not (row4 and self.pre_rope), "4-bit keys are cached post-RoPE"
         cv = _CacheView()
         cv.k = k.data_ptr()
         cv.v = self.v.data_ptr() if self.v is not None else None
-        cv.k_kind = 3 if fp8 else ((2 if self.pre_rope else 0) if k.dtype == torch.bfloat16 else 1)
+        cv.k_kind = 5 if row4 else 3 if fp8 else ((2 if self.pre_rope else 0) if k.dtype == torch.bfloat16 else 1)
         if self.page_table is None:
             cv.paged = 0
             cv.stride_layer, cv.stride_seq, cv.stride_head, cv.stride_tok = k.stride()[:4]
@@ -498,6 +513,35 @@ class TriContext:
         code = lib().tri_append(self._h, dst._ref, S, rows, lp, _status_addr(device_status, dev), _stream_on(dev))
         if code:
             _check(code, "tri_append")
+
+    def read(self, src: LayerCache, k: Optional[torch.Tensor], v: Optional[torch.Tensor] = None,
+             first: Optional[torch.Tensor] = None, device_status: Optional[torch.Tensor] = None):
+        """Read rows of one layer back: k, v [S, T, H, 128] (bf16 or fp32, any strides with 16-byte rows; either may be None)
+        receive what slots first[s] + t below each unit's length stand for; first [S] int32, default 0.  Other rows are left
+        as they are.  A [S, H, N, 128] tensor is passed as its transpose(1, 2)."""
+        self._check_cache(src)
+        dev, S = src._dev, src.n_seqs
+        some = k if k is not None else v
+        assert some is not None and (v is None or src.view.v is not None), "a cache without values has none to read"
+        shape, dt = some.shape, some.dtype
+        T = shape[1]
+        assert shape == (S, T, self.n_kv_heads, 128) and (dt is torch.bfloat16 or dt is torch.float32)
+        kp = ks = kt = kh = vp = vs = vt = vh = fp = 0
+        if k is not None:
+            ks, kt, kh, one = k.stride()
+            assert one == 1 and k.get_device() == dev
+            kp = k.data_ptr()
+        if v is not None:
+            vs, vt, vh, one = v.stride()
+            assert v.shape == shape and v.dtype is dt and one == 1 and v.get_device() == dev
+            vp = v.data_ptr()
+        if first is not None:
+            assert first.dtype is torch.int32 and first.numel() == S and first.is_contiguous() and first.get_device() == dev
+            fp = first.data_ptr()
+        rows = _pack_read(kp, vp, 0 if dt is torch.bfloat16 else 1, T, ks, kt, kh, vs, vt, vh, fp)
+        code = lib().tri_read(self._h, src._ref, S, rows, _status_addr(device_status, dev), _stream_on(dev))
+        if code:
+            _check(code, "tri_read")
 
     def attend_workspace_bytes(self, S: int, n_prefixes: int = 0) -> int:
         return int(lib().tri_attend_workspace_bytes(self._h, S, n_prefixes))

@@ -12,10 +12,12 @@
 
 #include "tri_append.cuh"
 #include "tri_attend.cuh"
+#include "tri_attend4.cuh"
 #include "tri_attend_umma.cuh"
 #include "tri_calib.cuh"
 #include "tri_calib_tma.cuh"
 #include "tri_compact.cuh"
+#include "tri_read.cuh"
 #include "tri_score.cuh"
 #include "tri_score_pre.cuh"
 #include "tri_score_tma.cuh"
@@ -322,25 +324,29 @@ View to_view(const tri_cache_view *v)
     return w;
 }
 
-// Bytes per key element / per value element of a view's format (fp8 caches hold V in fp8 too).
-int k_esize_of(int32_t k_kind) { return k_kind == 1 ? 4 : (k_kind == 3 ? 1 : 2); }
-int v_esize_of(int32_t k_kind) { return k_kind == 3 ? 1 : 2; }
+// Bytes per key element / per value element of a view's format (8-bit and 4-bit caches hold V likewise; elements of the latter are
+// bytes), and elements per row.
+int k_esize_of(int32_t k_kind) { return k_kind == 1 ? 4 : (k_kind >= 3 ? 1 : 2); }
+int v_esize_of(int32_t k_kind) { return k_kind >= 3 ? 1 : 2; }
+int row_elements(int32_t k_kind) { return k_kind == 5 ? kRow4Bytes : kHeadDim; }
 
-tri_status check_view(const tri_cache_view *v, bool need_lens)
+// rows4: whether the call takes 4-bit rows.
+tri_status check_view(const tri_cache_view *v, bool need_lens, bool rows4 = false)
 {
     if (!v || !v->k) return TRI_ERR_INVALID_ARG;
-    if (v->k_kind < 0 || v->k_kind > 3 || v->n_max <= 0) return TRI_ERR_INVALID_ARG;
+    if (v->k_kind < 0 || v->k_kind == 4 || v->k_kind > 5 || v->n_max <= 0) return TRI_ERR_INVALID_ARG;
+    if (v->k_kind == 5 && !rows4) return TRI_ERR_UNSUPPORTED;
     if (need_lens && !v->seq_lens) return TRI_ERR_INVALID_ARG;
     if (((uintptr_t)v->k & 15) || ((uintptr_t)v->v & 15)) return TRI_ERR_INVALID_ARG;
-    const int q = v->k_kind == 3 ? 16 : 8;            // strides in elements; every row starts on a 16-byte boundary
+    const int q = v->k_kind >= 3 ? 16 : 8, row = row_elements(v->k_kind);            // strides in elements; every row starts on a 16-byte boundary
     if (v->stride_layer % q || v->stride_head % q) return TRI_ERR_INVALID_ARG;
     if (v->paged) {
         if (!v->page_table || v->max_pages_per_seq <= 0 || v->page_size <= 0) return TRI_ERR_INVALID_ARG;
         if (v->page_size % kTileKeys) return TRI_ERR_UNSUPPORTED;
-        if (v->stride_page % q || v->stride_slot % q || v->stride_slot < kHeadDim) return TRI_ERR_INVALID_ARG;
+        if (v->stride_page % q || v->stride_slot % q || v->stride_slot < row) return TRI_ERR_INVALID_ARG;
         if ((int64_t)v->max_pages_per_seq * v->page_size < v->n_max) return TRI_ERR_INVALID_ARG;
     } else {
-        if (v->stride_seq % q || v->stride_tok % q || v->stride_tok < kHeadDim) return TRI_ERR_INVALID_ARG;
+        if (v->stride_seq % q || v->stride_tok % q || v->stride_tok < row) return TRI_ERR_INVALID_ARG;
     }
     return TRI_OK;
 }
@@ -433,6 +439,14 @@ cudaError_t allow_attend_smem()
     return cudaFuncSetAttribute(k_attend<KEY8, RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttRingBytes);
 }
 
+template <int RT>
+cudaError_t allow_attend4_smem()
+{
+    cudaError_t e = cudaFuncSetAttribute(k_attend4_cluster<RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kA4RingBytes);
+    if (e != cudaSuccess) return e;
+    return cudaFuncSetAttribute(k_attend4<RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kA4RingBytes);
+}
+
 // Loads kernels that need no attribute, so that a program's first call may already be captured into a graph.
 template <typename... Kernels>
 cudaError_t load_kernels(Kernels... kernels)
@@ -466,6 +480,10 @@ cudaError_t prepare_device()
     if ((e = allow_attend_smem<false, 16>()) != cudaSuccess) return e;
     if ((e = allow_attend_smem<true, 8>()) != cudaSuccess) return e;
     if ((e = allow_attend_smem<true, 16>()) != cudaSuccess) return e;
+    if ((e = allow_attend4_smem<8>()) != cudaSuccess || (e = allow_attend4_smem<16>()) != cudaSuccess) return e;
+    if ((e = load_append<0, 5>()) != cudaSuccess || (e = load_append<1, 5>()) != cudaSuccess) return e;
+    if ((e = load_kernels(k_read<0, 2>, k_read<1, 2>, k_read<2, 2>, k_read<3, 2>, k_read<5, 2>, k_read<0, 4>, k_read<1, 4>, k_read<2, 4>,
+                          k_read<3, 4>, k_read<5, 4>)) != cudaSuccess) return e;
     if ((e = load_append<0, 0>()) != cudaSuccess || (e = load_append<0, 1>()) != cudaSuccess) return e;
     if ((e = load_append<0, 2>()) != cudaSuccess || (e = load_append<0, 3>()) != cudaSuccess) return e;
     if ((e = load_append<1, 0>()) != cudaSuccess || (e = load_append<1, 1>()) != cudaSuccess) return e;
@@ -671,8 +689,8 @@ tri_status run_compact(tri_ctx *c, const tri_cache_view *src, const int32_t *kep
     p.S = S; p.H = c->desc.n_kv_heads; p.budget = budget; p.u0 = un.first;
     p.k_esize = k_esize_of(src->k_kind);
     p.v_esize = v_esize_of(src->k_kind);
-    p.k_vec = kHeadDim * p.k_esize / 16;
-    p.v_vec = (src->v && dst->v) ? kHeadDim * p.v_esize / 16 : 0;
+    p.k_vec = row_elements(src->k_kind) * p.k_esize / 16;
+    p.v_vec = (src->v && dst->v) ? row_elements(src->k_kind) * p.v_esize / 16 : 0;
     p.device_status = device_status;
     const bool rows16 = (src->k_kind == 0 || src->k_kind == 2) && p.v_vec != 0;     // bf16 K and V: the row-gather kernel applies
     const int U = un.count;
@@ -786,8 +804,8 @@ extern "C" tri_status tri_compact(tri_ctx *c, const tri_cache_view *src, const i
     tri_status r;
     if (!c || !kept_idx || !kept_cnt) return TRI_ERR_INVALID_ARG;
     if ((r = check_device(c)) != TRI_OK) return r;
-    if ((r = check_view(src, false)) != TRI_OK) return r;
-    if ((r = check_view(dst, false)) != TRI_OK) return r;
+    if ((r = check_view(src, false, true)) != TRI_OK) return r;
+    if ((r = check_view(dst, false, true)) != TRI_OK) return r;
     if ((r = check_common(c, S, src->n_max, budget)) != TRI_OK) return r;
     if (dst->n_max < budget && dst->n_max < src->n_max) return TRI_ERR_INVALID_ARG;
     if (src->k_kind != dst->k_kind) return TRI_ERR_INVALID_ARG;
@@ -1166,7 +1184,7 @@ tri_status check_layer_cache(const tri_ctx *c, const tri_layer_cache *lc, int32_
 {
     if (!c || !lc || !lc->view || S <= 0) return TRI_ERR_INVALID_ARG;
     tri_status r;
-    if ((r = check_view(lc->view, lc->unit_lens == nullptr)) != TRI_OK) return r;
+    if ((r = check_view(lc->view, lc->unit_lens == nullptr, true)) != TRI_OK) return r;
     if ((r = check_common(c, S, lc->view->n_max, 1)) != TRI_OK) return r;
     if (lc->layer < 0 || lc->layer >= c->desc.n_layers) return TRI_ERR_INVALID_ARG;
     if ((lc->k_scale || lc->v_scale) && lc->view->k_kind != 3) return TRI_ERR_INVALID_ARG;
@@ -1203,7 +1221,7 @@ bool rows16_ok(const void *p, int64_t a, int64_t b, int64_t c, int es)
 
 // Rows that are written, `n` of them `stride` elements apart, lie side by side: a broadcast dimension, whose rows meet in one
 // place, would be written by several blocks at a time.
-bool rows_apart(int64_t n, int64_t stride) { return n <= 1 || stride >= kHeadDim || stride <= -kHeadDim; }
+bool rows_apart(int64_t n, int64_t stride, int row = kHeadDim) { return n <= 1 || stride >= row || stride <= -row; }
 
 template <int KIND, int KK, bool SPLIT>
 cudaError_t launch_append(unsigned blocks, int tt, cudaStream_t st, const AppendParams &p)
@@ -1224,6 +1242,7 @@ cudaError_t launch_append(int kk, bool split, unsigned blocks, int tt, cudaStrea
     if (kk == 0) return launch_append<KIND, 0>(split, blocks, tt, st, p);
     if (kk == 1) return launch_append<KIND, 1>(split, blocks, tt, st, p);
     if (kk == 2) return launch_append<KIND, 2>(split, blocks, tt, st, p);
+    if (kk == 5) return launch_append<KIND, 5>(split, blocks, tt, st, p);
     return launch_append<KIND, 3>(split, blocks, tt, st, p);
 }
 
@@ -1257,7 +1276,9 @@ extern "C" tri_status tri_append(tri_ctx *c, const tri_layer_cache *dst, int32_t
     }
     if (!rows->pos && dst->unit_lens) return TRI_ERR_INVALID_ARG;
     const tri_cache_view *dv = dst->view;
-    if (!rows_apart(H, dv->stride_head) || !(dv->paged ? rows_apart(dv->n_pages == 1 ? 1 : 2, dv->stride_page) : rows_apart(S, dv->stride_seq)))
+    const int row = row_elements(dv->k_kind);
+    if (!rows_apart(H, dv->stride_head, row) ||
+        !(dv->paged ? rows_apart(dv->n_pages == 1 ? 1 : 2, dv->stride_page, row) : rows_apart(S, dv->stride_seq, row)))
         return TRI_ERR_INVALID_ARG;
     if ((r = check_device(c)) != TRI_OK) return r;
 
@@ -1301,9 +1322,61 @@ extern "C" tri_status tri_append(tri_ctx *c, const tri_layer_cache *dst, int32_t
 
 namespace {
 
+template <int OS>
+cudaError_t launch_read(int kk, unsigned blocks, cudaStream_t st, const ReadParams &p)
+{
+    if (kk == 0) return launch_under(k_read<0, OS>, blocks, kReadThreads, 0, st, p);
+    if (kk == 1) return launch_under(k_read<1, OS>, blocks, kReadThreads, 0, st, p);
+    if (kk == 2) return launch_under(k_read<2, OS>, blocks, kReadThreads, 0, st, p);
+    if (kk == 3) return launch_under(k_read<3, OS>, blocks, kReadThreads, 0, st, p);
+    return launch_under(k_read<5, OS>, blocks, kReadThreads, 0, st, p);
+}
+
+}  // namespace
+
+extern "C" tri_status tri_read(tri_ctx *c, const tri_layer_cache *src, int32_t S, const tri_read_rows *rows,
+                               int32_t *device_status, void *stream)
+{
+    tri_status r;
+    if ((r = check_layer_cache(c, src, S)) != TRI_OK) return r;
+    if (!rows || rows->T <= 0 || rows->kind < 0 || rows->kind > 1 || (!rows->k && !rows->v) || rows->k == rows->v) return TRI_ERR_INVALID_ARG;
+    if (rows->v && !src->view->v) return TRI_ERR_INVALID_ARG;
+    const int32_t H = c->desc.n_kv_heads, T = rows->T;
+    const int es = rows->kind == 0 ? 2 : 4;
+    auto rows_ok = [&](const void *x, int64_t seq, int64_t tok, int64_t head) {      // (the stride of a dimension of size 1 is never used)
+        return rows16_ok(x, S > 1 ? seq : 0, T > 1 ? tok : 0, H > 1 ? head : 0, es) && rows_apart(S, seq) && rows_apart(T, tok) && rows_apart(H, head);
+    };
+    if (rows->k && !rows_ok(rows->k, rows->k_stride_seq, rows->k_stride_tok, rows->k_stride_head)) return TRI_ERR_INVALID_ARG;
+    if (rows->v && !rows_ok(rows->v, rows->v_stride_seq, rows->v_stride_tok, rows->v_stride_head)) return TRI_ERR_INVALID_ARG;
+    if ((r = check_device(c)) != TRI_OK) return r;
+
+    ReadParams p;
+    p.src = to_view(src->view);
+    p.layer = src->layer; p.S = S; p.H = H; p.T = T;
+    p.tok_shift = 0;
+    while ((1 << p.tok_shift) < kReadTile && (1 << p.tok_shift) < T) ++p.tok_shift;
+    const int32_t toks = 1 << p.tok_shift, heads = kReadTile / toks;
+    p.tiles_t = (int32_t)(((int64_t)T + toks - 1) / toks);
+    p.tiles_h = (H + heads - 1) / heads;
+    p.unit_lens = src->unit_lens ? src->unit_lens + (int64_t)src->layer * S * H : nullptr;
+    p.k_scale = src->k_scale ? src->k_scale + (int64_t)src->layer * H : nullptr;
+    p.v_scale = src->v_scale ? src->v_scale + (int64_t)src->layer * H : nullptr;
+    p.k = (char *)rows->k; p.v = (char *)rows->v;
+    p.ks_seq = rows->k_stride_seq; p.ks_tok = rows->k_stride_tok; p.ks_head = rows->k_stride_head;
+    p.vs_seq = rows->v_stride_seq; p.vs_tok = rows->v_stride_tok; p.vs_head = rows->v_stride_head;
+    p.first = rows->first; p.device_status = device_status;
+    const int64_t blocks = (int64_t)p.tiles_t * p.tiles_h * S;
+    if (blocks > 0x7fffffff) return TRI_ERR_UNSUPPORTED;
+    if (rows->kind == 0) TRI_CUDA(launch_read<2>(src->view->k_kind, (unsigned)blocks, (cudaStream_t)stream, p));
+    else TRI_CUDA(launch_read<4>(src->view->k_kind, (unsigned)blocks, (cudaStream_t)stream, p));
+    return TRI_OK;
+}
+
+namespace {
+
 // Workspace of an attention call.
 struct AttendPlan {
-    int32_t blocks;                                    // grid of k_attend
+    int32_t blocks, blocks4;                           // grids of k_attend and k_attend4
     int32_t own_rows;                                  // query rows per slot of the own rows' pass
     size_t own_rec, own_slots, own_whole, pre_rec, pre_slots, pre_whole, total;
 };
@@ -1314,10 +1387,12 @@ AttendPlan make_attend_plan(const tri_ctx *c, int32_t S, int32_t P)
     const int32_t H = c->desc.n_kv_heads, G = c->desc.group_size;
     a.blocks = c->n_sm * kAttBlocksPerSM;
     a.own_rows = G <= 8 ? 8 : 16;
+    a.blocks4 = c->n_sm * (G <= 8 ? kA4BlocksPerSM<8> : kA4BlocksPerSM<16>);
+    const int32_t most = a.blocks > a.blocks4 ? a.blocks : a.blocks4;
     const size_t row = kAttRowPitch * sizeof(float), whole = align256((size_t)S * H * G * row);
     size_t o = 0;
     a.own_rec = o;   o += align256((size_t)S * H * sizeof(int2));
-    a.own_slots = o; o += align256((size_t)a.blocks * 2 * a.own_rows * row);
+    a.own_slots = o; o += align256((size_t)most * 2 * a.own_rows * row);
     a.own_whole = o; o += P > 0 ? whole : 0;
     // either pass over prefixes fits: tiles of 16 query rows, or of 128 with one block per multiprocessor
     a.pre_rec = o;   o += P > 0 ? align256(((size_t)P + S / (16 / G) + 2) * H * sizeof(int2)) : 0;
@@ -1342,11 +1417,25 @@ cudaError_t launch_attend_clusters(int rows, unsigned units, cudaStream_t st, co
                      : launch_clusters(k_attend_cluster<KEY8, 16>, kAttCluster, units * kAttCluster, kAttThreads, kAttRingBytes, st, p, pre);
 }
 
-tri_status check_attend_cache(const tri_ctx *c, const tri_layer_cache *lc, int32_t n)
+cudaError_t launch_attend4(int rows, unsigned blocks, cudaStream_t st, const AttendParams &p)
+{
+    return rows == 8 ? launch_under(k_attend4<8>, blocks, kA4Threads, kA4RingBytes, st, p)
+                     : launch_under(k_attend4<16>, blocks, kA4Threads, kA4RingBytes, st, p);
+}
+
+cudaError_t launch_attend4_clusters(int rows, unsigned units, cudaStream_t st, const AttendParams &p)
+{
+    return rows == 8 ? launch_clusters(k_attend4_cluster<8>, kAttCluster, units * kAttCluster, kA4Threads, kA4RingBytes, st, p)
+                     : launch_clusters(k_attend4_cluster<16>, kAttCluster, units * kAttCluster, kA4Threads, kA4RingBytes, st, p);
+}
+
+// rows4: whether the call takes 4-bit rows.
+tri_status check_attend_cache(const tri_ctx *c, const tri_layer_cache *lc, int32_t n, bool rows4)
 {
     tri_status r = check_layer_cache(c, lc, n);
     if (r != TRI_OK) return r;
-    if (lc->view->k_kind != 0 && lc->view->k_kind != 3) return TRI_ERR_UNSUPPORTED;
+    const int32_t kind = lc->view->k_kind;
+    if (kind != 0 && kind != 3 && !(kind == 5 && rows4)) return TRI_ERR_UNSUPPORTED;
     return lc->view->v ? TRI_OK : TRI_ERR_INVALID_ARG;
 }
 
@@ -1405,6 +1494,9 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
         return TRI_ERR_INVALID_ARG;
     if ((r = check_device(c)) != TRI_OK) return r;
     if (!line_ok(c, src->view, S) || (P > 0 && !line_ok(c, prefix->view, (int64_t)P + S / (16 / c->desc.group_size)))) return TRI_ERR_UNSUPPORTED;
+    const bool rows4 = src->view->k_kind == 5;
+    // (the kernel multiplies rows by the distance between them in 32 bits)
+    if (rows4 && (src->view->paged ? src->view->stride_slot : src->view->stride_tok) > 0x7fffffff) return TRI_ERR_UNSUPPORTED;
     const AttendPlan pl = make_attend_plan(c, S, P);
     if (ws_bytes < pl.total) return TRI_ERR_WORKSPACE;
     char *w = (char *)ws;
@@ -1421,7 +1513,8 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
             pre = attend_params(c, prefix, P, S, io, device_status);
             pre.group_start = group_start;
         }
-        if (src->view->k_kind == 3) TRI_CUDA(launch_attend_clusters<true>(pl.own_rows, (unsigned)(S * H), st, p, pre));
+        if (rows4) TRI_CUDA(launch_attend4_clusters(pl.own_rows, (unsigned)(S * H), st, p));
+        else if (src->view->k_kind == 3) TRI_CUDA(launch_attend_clusters<true>(pl.own_rows, (unsigned)(S * H), st, p, pre));
         else TRI_CUDA(launch_attend_clusters<false>(pl.own_rows, (unsigned)(S * H), st, p, pre));
         return TRI_OK;
     }
@@ -1455,10 +1548,12 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
     p.finish = P > 0 ? 0 : 1; p.under = P > 0 ? 1 : 0;
     p.rec = (int2 *)(w + pl.own_rec); p.slots = (float *)(w + pl.own_slots);
     p.whole = P > 0 ? (float *)(w + pl.own_whole) : nullptr;
-    if (src->view->k_kind == 3) TRI_CUDA(launch_attend<true>(pl.own_rows, (unsigned)pl.blocks, st, p));
+    const int32_t blocks = rows4 ? pl.blocks4 : pl.blocks;
+    if (rows4) TRI_CUDA(launch_attend4(pl.own_rows, (unsigned)blocks, st, p));
+    else if (src->view->k_kind == 3) TRI_CUDA(launch_attend<true>(pl.own_rows, (unsigned)pl.blocks, st, p));
     else TRI_CUDA(launch_attend<false>(pl.own_rows, (unsigned)pl.blocks, st, p));
 
-    mp.own.rec = p.rec; mp.own.slots = p.slots; mp.own.whole = p.whole; mp.own.blocks = pl.blocks; mp.own.rows = pl.own_rows; mp.own.spt = 0;
+    mp.own.rec = p.rec; mp.own.slots = p.slots; mp.own.whole = p.whole; mp.own.blocks = blocks; mp.own.rows = pl.own_rows; mp.own.spt = 0;
     mp.S = S; mp.P = P; mp.H = H; mp.G = G; mp.group_start = group_start;
     mp.out = p.out; mp.out_seq = p.out_seq; mp.out_head = p.out_head; mp.lse = io->lse; mp.device_status = device_status;
     // a query row per block, or all of a unit's: 8192 rows a unit, 8 units 12.1 against 14.5 us at G = 4 and 14.0 against 25.5 at
@@ -1480,7 +1575,7 @@ extern "C" size_t tri_attend_workspace_bytes(const tri_ctx *c, int32_t S, int32_
 extern "C" tri_status tri_attend(tri_ctx *c, const tri_layer_cache *src, int32_t S, const tri_attend_io *io,
                                  int32_t *device_status, void *ws, size_t ws_bytes, void *stream)
 {
-    const tri_status r = check_attend_cache(c, src, S);
+    const tri_status r = check_attend_cache(c, src, S, true);
     if (r != TRI_OK) return r;
     return run_attend(c, nullptr, 0, nullptr, src, S, io, device_status, ws, ws_bytes, (cudaStream_t)stream);
 }
@@ -1490,8 +1585,8 @@ extern "C" tri_status tri_attend_shared(tri_ctx *c, const tri_layer_cache *prefi
                                         int32_t *device_status, void *ws, size_t ws_bytes, void *stream)
 {
     tri_status r;
-    if ((r = check_attend_cache(c, src, S)) != TRI_OK) return r;
-    if ((r = check_attend_cache(c, prefix, P)) != TRI_OK) return r;
+    if ((r = check_attend_cache(c, src, S, false)) != TRI_OK) return r;
+    if ((r = check_attend_cache(c, prefix, P, false)) != TRI_OK) return r;
     if (!group_start) return TRI_ERR_INVALID_ARG;
     return run_attend(c, prefix, P, group_start, src, S, io, device_status, ws, ws_bytes, (cudaStream_t)stream);
 }

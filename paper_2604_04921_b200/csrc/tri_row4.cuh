@@ -1,0 +1,62 @@
+// Rows of 128 components in 4 bits: TRI_ROW4_BYTES bytes, as the header describes them at tri_append.
+//
+// Why this layout.  Word g of the 16-byte unit t holds components 8 t .. 8 t + 7 of group g, so that a lane of attention that
+// loads one unit has 8 components of each group, what a matrix instruction per group needs (see tri_attend4.cuh), and that 32 g +
+// 8 t .. + 7, one word, is a run of 16 bytes of a bf16 row.  In a word, nibbles i and i + 4 are neighbours 2 i, 2 i + 1: masked with
+// 0x000f000f << 4 i they are a pair of 16-bit values in order.  80 bytes is an odd number of 16-byte units: eight rows side by side
+// in shared memory are read without bank conflicts.
+#pragma once
+#include "tri_score_tma.cuh"
+
+namespace tri {
+
+constexpr int kRow4Bytes = TRI_ROW4_BYTES, kRow4Scales = 64, kRow4Centres = 72;
+
+__device__ __forceinline__ float min_nan(float a, float b)
+{
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;\n" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;\n" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// Scale and centre of a group from its smallest and largest value.  (8 hi + 7 lo) / 15 as (hi / 2 + 7 lo / 16) / (15 / 16), which
+// cannot overflow; with bf16 inputs every step up to the division is exact or rounded once, so that c is the correctly rounded
+// one.  A NaN or an infinity among the values makes c not finite.
+__device__ __forceinline__ void row4_group(float lo, float hi, float &s, float &c)
+{
+    c = bf16_lo(cvt_bf16x2(0.f, __fdiv_rn(fmaf(hi, 0.5f, lo * 0.4375f), 0.9375f)));
+    const float need = fmaxf(__fdiv_rn(hi - c, 7.f), (c - lo) * 0.125f);
+    // rounded up to bf16; the smallest normal number, where that is more
+    const uint32_t up = max((__float_as_uint(need) + 0xffffu) & 0xffff0000u, 0x00800000u);
+    s = need > 0.f ? __uint_as_float(up) : 0.f;
+    if (!(fabsf(c) < INFINITY)) { c = __uint_as_float(0x7fc00000u); s = 0.f; }
+}
+
+// The codes of 8 neighbouring components as a word.  Adding 1.5 * 2^23 + 8 rounds to the nearest integer (ties to even) and leaves
+// the code in the low bits of the sum; the sum of the shifted words carries a constant that is taken off at the end.
+__device__ __forceinline__ uint32_t row4_word(const float *x, float s, float c)
+{
+    const float by = s > 0.f ? s : 1.f;
+    uint32_t w = 0;
+#pragma unroll
+    for (int d = 0; d < 8; ++d) w += __float_as_uint(__fdiv_rn(x[d] - c, by) + (12582912.f + 8.f)) << 4 * ((d >> 1) + 4 * (d & 1));
+    return w - 0x4b400000u * 0x11111111u;                    // (1.5 * 2^23 has the bits 0x4b400000)
+}
+
+// The 8 components a word stands for.
+__device__ __forceinline__ void row4_values(uint32_t w, float s, float c, float *x)
+{
+#pragma unroll
+    for (int d = 0; d < 8; ++d) {
+        const uint32_t n = (w >> 4 * ((d >> 1) + 4 * (d & 1))) & 15u;
+        x[d] = fmaf(__uint_as_float(0x4b000000u | n) - 8388616.f, s, c);       // 2^23 + code, less 2^23 + 8
+    }
+}
+
+}  // namespace tri
