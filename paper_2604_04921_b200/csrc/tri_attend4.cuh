@@ -4,14 +4,17 @@
 //       q . k_n  = sum_g s_ng (sum_d q_d u_nd - 8 Q_g) + sum_g c_ng Q_g,      Q_g = sum of q over group g
 //       sum_n p_n v_n = sum_n (p_n s_ng) (u - 8) + sum_n p_n c_ng
 // so that the matrix instructions work on codes, and scales and centres are applied per row and group:
-//   logits   keys are the 16 rows of A, 8 query rows the columns of B.  A nibble or-ed under 0x4300 is the bf16 value 128 + u: 7
-//            integer instructions widen 8 codes, and the 128 + 8 is taken off by the accumulator's initial value, -136 Q_g.  (136 Q_g
-//            is rounded at 2^-24 of itself: some 2^-19 of the products' own sum.)  The queries are used as they are.  The centres take
-//            one matrix instruction more, bf16 against Q in three bf16 parts.
-//   sums     the 16 rows of A are components, its 16 columns cached rows.  A nibble or-ed under 0x6400 is the f16 value 1024 + u (16 u
-//            where it lies four bits further up, which saves the shift), and one f16 multiply-add makes u - 8 of it, exactly.  The
-//            weights p_n s_ng 2^-E are rounded once to f16; E keeps the largest scale of the rows so far below 1, and p is kept as in
-//            tri_attend.cuh, so that they use f16's range from 2^15 down.  The centres are summed in fp32.
+//   logits   keys are the 16 rows of A, 8 query rows the columns of B.  A nibble in 16 bits of its own is the f16 value u 2^-24, or
+//            u 2^-20 where it lies four bits further up: 5 integer instructions make operands of 8 codes (as bf16, with 128 or-ed in,
+//            7; as e4m3, whose matrix instructions sm_100a makes of conversions and f16 ones, 3 and 20 conversions).  A query row is
+//            brought to [2^14, 2^15) by a power of two and goes in as f16, a sixteenth of it where the codes are 16 times as large: a
+//            bf16 value is exact unless it is 2^28 times smaller than the row's largest.  Centres, and the 8 that each code is too
+//            large by, go through one and a half matrix instructions: c_ng against Q_g and s_ng against -8 Q_g, both in three bf16
+//            parts, that is to 24 bits.
+//   sums     the 16 rows of A are components, its 16 columns cached rows, operands likewise: A's upper 8 rows carry 16 times the lower
+//            ones.  8 times the weights' sum is taken off in the same accumulators, by a matrix of constants.  The weights p_n s_ng are rounded
+//            once to f16: the bound on the logits that p is taken against goes by the largest scale of the rows so far, too, so that
+//            they use f16's range from 2^15 down.  The centres are summed in fp32.
 //
 // What bounds it.  160 bytes per row and head: at HBM speed a multiprocessor gets 16 rows every 60 ns, and the instructions that turn
 // 16 x 256 codes into operands have to fit in there.  Copies are 16-byte asynchronous ones into a ring of stages that each warp keeps
@@ -22,40 +25,39 @@
 
 namespace tri {
 
-constexpr int kA4Warps = kAttWarps, kA4Threads = 32 * kA4Warps, kA4Rows = 32, kA4Stages = 2;
+constexpr int kA4Warps = kAttWarps, kA4Threads = 32 * kA4Warps, kA4Rows = 32, kA4Stages = 2;      // (one step ahead)
 constexpr int kA4Half = kA4Rows * kRow4Bytes, kA4StageBytes = 2 * kA4Half;                  // K | V
 constexpr int kA4RingBytes = kA4Warps * kA4Stages * kA4StageBytes;
 constexpr int kA4Tile = kA4Warps * kA4Rows;
 constexpr int kA4UnitCost = 2;                                   // a unit's own cost, in tiles
-template <int RT> constexpr int kA4BlocksPerSM = RT == 8 ? 4 : 2;
+template <int RT> constexpr int kA4BlocksPerSM = RT == 8 ? 3 : 2;
+constexpr uint32_t kLow = 0x000f000fu, kHigh = 0x00f000f0u;     // nibbles that are pairs of f16 values u 2^-24, u 2^-20
+constexpr uint32_t kLess = 0x80088008u, kLess16 = 0x80808080u;   // -8 2^-24, -8 2^-20
 static_assert(kA4StageBytes >= 8 * 512, "the sums of a warp fit into a stage");
 
-__device__ __forceinline__ void mma_bf16_from(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1,
-                                              float c0, float c1)
+__device__ __forceinline__ void mma_bf16_16816_new(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
     asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%10,%11};\n"
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
-// (w & mask) | bits, one instruction
-template <uint32_t MASK, uint32_t BITS>
-__device__ __forceinline__ uint32_t nibbles(uint32_t w)
+__device__ __forceinline__ void mma_bf16_1688_acc(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0)
+{
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};\n"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(b0));
+}
+__device__ __forceinline__ void mma_f16_16816_new(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ uint32_t cvt_f16x2(float upper, float lower)
 {
     uint32_t r;
-    asm("lop3.b32 %0, %1, %2, %3, 0xea;\n" : "=r"(r) : "r"(w), "n"(MASK), "r"(BITS));
-    return r;
-}
-__device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b)
-{
-    uint32_t r;
-    asm("sub.rn.f16x2 %0, %1, %2;\n" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
-__device__ __forceinline__ uint32_t fma_f16x2(uint32_t a, uint32_t b, uint32_t c)
-{
-    uint32_t r;
-    asm("fma.rn.f16x2 %0, %1, %2, %3;\n" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;\n" : "=r"(r) : "f"(upper), "f"(lower));
     return r;
 }
 __device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b)
@@ -88,7 +90,8 @@ __device__ __forceinline__ uint32_t pick(const uint4 &x, int i) { return i == 0 
 template <int RT, int CL>
 __device__ __forceinline__ void attend4_block(const AttendParams &p)
 {
-    constexpr int CT = RT / 8, ST = kA4Stages, ROWS = kA4Rows, NK = ROWS / 16, TILE = kA4Tile;
+    constexpr int CT = RT / 8, ST = kA4Stages, ROWS = kA4Rows, NK = 2, TILE = kA4Tile;
+    static_assert(ROWS == 16 * NK, "two tiles of 16 cached rows per step");
     extern __shared__ __align__(128) uint8_t dyn[];
     __shared__ float2 stat[kA4Warps][RT];
     __shared__ __align__(16) float part[CL ? RT : 1][kAttRowPitch];      // this block's sums, and (m, l)
@@ -113,139 +116,176 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
         sh.seq = (int)blockIdx.x / CL / p.H; sh.h = (int)blockIdx.x / CL - sh.seq * p.H;
         if (tid < RT) { part[CL ? tid : 0][kHeadDim] = -INFINITY; part[CL ? tid : 0][kHeadDim + 1] = 0.f; }      // no rows so far
     }
-    auto next_unit = [&](AttCursor &c, AttJob &u) -> bool {
+    // ---------------- the walk over the share's units, one step ahead of the sums ----------------
+    AttCursor cursor = {sh.seq, sh.h, 0, sh.start};
+    AttJob u = {};                                        // the unit that is being copied
+    // To the next unit with rows; units without rows, and those of which the share holds only their own cost, are settled here.
+    auto walk = [&]() -> bool {
         if constexpr (CL == 0) {
-            return att_next<TILE, kA4UnitCost>(p, sh, c, u);
+            while (att_next<TILE, kA4UnitCost>(p, sh, cursor, u)) {
+                if (u.begins && tid == 0) p.rec[u.rec] = att_record(sh, u);
+                if (u.kt == 0 && u.begins)                // no rows: zeros
+                    for (int i = tid; i < p.G * 16; i += kA4Threads) {
+                        const int hq = u.h * p.G + (i >> 4);
+                        *reinterpret_cast<uint4 *>(p.out + ((int64_t)u.seq * p.out_seq + (int64_t)hq * p.out_head) * 2 + 16 * (i & 15)) =
+                            make_uint4(0u, 0u, 0u, 0u);
+                        if (p.lse && (i & 15) == 0) p.lse[(int64_t)u.seq * p.H * p.G + hq] = -INFINITY;
+                    }
+                if (u.kb > u.ka) return true;
+            }
+            return false;
         } else {
-            if (c.rt++ > 0) return false;
-            u.seq = c.seq; u.h = c.h; u.nrows = p.G; u.first_seq = c.seq;
-            u.len = att_len(p, u.seq, c.h);
+            if (cursor.rt++ > 0) return false;
+            u.seq = cursor.seq; u.h = cursor.h;
+            u.len = att_len(p, u.seq, u.h);
             u.kt = (int)(((uint32_t)u.len + TILE - 1) / TILE);
             u.ka = rank * u.kt / CL; u.kb = (rank + 1) * u.kt / CL;
             u.begins = u.complete = false;
-            return true;
+            return u.kb > u.ka;
         }
     };
 
-    // ---------------- copies: a cursor of their own, ST - 1 steps ahead ----------------
-    AttCursor pc = {sh.seq, sh.h, 0, sh.start};
-    AttJob pj = {};
-    int pit = 0, pstage = 0, page[NK], slot[NK];          // next step; page and first slot of its 16-row halves
+    // ---------------- copies ----------------
+    int next = 0, stage = 0, page[NK] = {}, slot[NK] = {};        // next step to copy; page and first slot of its 16-row halves
     uint32_t bad = 0;                                     // bits 2 i, 2 i + 1: these 16 rows of stage i are absent
-    bool more = true;
     int64_t unit_base = 0;                                // first row of the unit; of page 0, where rows are paged
     uint64_t policy;                                      // rows are read once in a step: first to leave L2
     asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;\n" : "=l"(policy));
     const uint32_t step_row = (uint32_t)(p.src.paged ? p.src.stride_slot : p.src.stride_tok);      // bytes between rows (the host checks)
-    auto advance = [&]() {                                // to the next step, its pages looked up before they are needed
-        if (pit == pj.kb) {
-            do more = next_unit(pc, pj); while (more && pj.kb <= pj.ka);
-            pit = pj.ka;
-            unit_base = (int64_t)p.layer * p.src.stride_layer + (int64_t)pj.h * p.src.stride_head +
-                        (p.src.paged ? 0 : (int64_t)pj.seq * p.src.stride_seq);
-        }
-        if (more && p.src.paged) {
+    auto look_up = [&]() {                                // pages of the next step
+        if (!p.src.paged) return;
 #pragma unroll
-            for (int x = 0; x < NK; ++x) {
-                const uint32_t r = (uint32_t)pit * TILE + warp * ROWS + 16 * x;
-                const uint32_t pg = p.src.page_shift >= 0 ? r >> p.src.page_shift : r / (uint32_t)p.src.page_size;
-                page[x] = r < (uint32_t)pj.len ? ld_here(p.src.page_table + (int64_t)pj.seq * p.src.max_pages_per_seq + pg) : 0;
-                slot[x] = (int)(r - pg * (uint32_t)p.src.page_size);
-            }
+        for (int x = 0; x < NK; ++x) {
+            const uint32_t r = (uint32_t)next * TILE + warp * ROWS + 16 * x;
+            const uint32_t pg = p.src.page_shift >= 0 ? r >> p.src.page_shift : r / (uint32_t)p.src.page_size;
+            page[x] = r < (uint32_t)u.len ? ld_here(p.src.page_table + (int64_t)u.seq * p.src.max_pages_per_seq + pg) : 0;
+            slot[x] = (int)(r - pg * (uint32_t)p.src.page_size);
         }
     };
-    auto issue = [&]() {
-        if (more) {
-            const uint32_t dst = ring + pstage * kA4StageBytes + 16 * lane;
-            int64_t base[NK];
-            int have[NK];
-            uint32_t miss = 0;
+    auto begin_unit = [&]() {
+        next = u.ka;
+        unit_base = (int64_t)p.layer * p.src.stride_layer + (int64_t)u.h * p.src.stride_head + (p.src.paged ? 0 : (int64_t)u.seq * p.src.stride_seq);
+        look_up();
+    };
+    auto issue = [&](int to) {                            // the next step into stage `to`
+        const uint32_t dst = ring + to * kA4StageBytes + 16 * lane;
+        const uint32_t r = (uint32_t)next * TILE + warp * ROWS;
+        const int rows = r < (uint32_t)u.len ? min(u.len - (int)r, ROWS) : 0;
+        int have[NK] = {min(rows, 16), max(rows - 16, 0)};
+        int64_t base[NK];
+        uint32_t miss = 0;
+        if (p.src.paged) {
 #pragma unroll
             for (int x = 0; x < NK; ++x) {                // 16 rows each: they lie in one page
-                const uint32_t r = (uint32_t)pit * TILE + warp * ROWS + 16 * x;
-                have[x] = r < (uint32_t)pj.len ? min(pj.len - (int)r, 16) : 0;
-                base[x] = unit_base;
-                if (p.src.paged) {
-                    base[x] += (int64_t)page[x] * p.src.stride_page + (int64_t)slot[x] * p.src.stride_slot;
-                    if (have[x] && p.src.n_pages > 0 && (uint32_t)page[x] >= (uint32_t)p.src.n_pages) {
-                        have[x] = 0;
-                        miss |= 1u << x;
-                        if (lane == 0 && p.device_status) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
-                    }
-                } else {
-                    base[x] += (int64_t)r * p.src.stride_tok;
+                base[x] = unit_base + (int64_t)page[x] * p.src.stride_page + (int64_t)((uint64_t)(uint32_t)slot[x] * step_row);
+                if (have[x] && p.src.n_pages > 0 && (uint32_t)page[x] >= (uint32_t)p.src.n_pages) {
+                    have[x] = 0;
+                    miss |= 1u << x;
+                    if (lane == 0 && p.device_status) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
                 }
             }
-            // the 160 pieces of a stage's keys, 5 per row, go to the lanes in turn; rows behind the length (or absent ones)
-            // arrive as zeros and are not read
+        } else {
+            base[0] = unit_base + (int64_t)((uint64_t)r * step_row);
+            base[1] = base[0] + (int64_t)((uint64_t)16 * step_row);
+        }
+        // The 160 pieces of a stage's keys, 5 per row, go to the lanes in turn; where rows lie side by side, as they do in the
+        // stage, a piece's place in the copy is its place in the source.
+        if (rows == ROWS && miss == 0 && step_row == kRow4Bytes) {
+            const char *k0 = p.src.k + (base[0] + 16 * lane), *v0 = p.src.v + (base[0] + 16 * lane);
+            if (base[1] == base[0] + 16 * kRow4Bytes) {
 #pragma unroll
+                for (int i = 0; i < 5; ++i) {
+                    cp_async16(dst + 512 * i, k0 + 512 * i, 16u, policy);
+                    cp_async16(dst + kA4Half + 512 * i, v0 + 512 * i, 16u, policy);
+                }
+            } else {
+                const char *k1 = p.src.k + (base[1] + (16 * lane - 16 * kRow4Bytes)), *v1 = p.src.v + (base[1] + (16 * lane - 16 * kRow4Bytes));
+#pragma unroll
+                for (int i = 0; i < 5; ++i) {             // (piece 80 is the second half's first)
+                    const bool second = i == 2 ? lane >= 16 : i > 2;
+                    cp_async16(dst + 512 * i, (second ? k1 : k0) + 512 * i, 16u, policy);
+                    cp_async16(dst + kA4Half + 512 * i, (second ? v1 : v0) + 512 * i, 16u, policy);
+                }
+            }
+        } else {
+            // rows behind the length (or absent ones) arrive as zeros and are not read
+#pragma unroll 1
             for (int i = 0; i < 5; ++i) {
                 const int piece = 32 * i + lane, row = piece / 5, col = piece - 5 * row, x = row >> 4;
-                const bool there = (row & 15) < have[x == 0 ? 0 : NK - 1];
-                const int64_t at = there ? (x == 0 ? base[0] : base[NK - 1]) + (int64_t)((uint64_t)(uint32_t)(row & 15) * step_row) + 16 * col : 0;
+                const bool there = (row & 15) < (x == 0 ? have[0] : have[1]);
+                const int64_t at = there ? (x == 0 ? base[0] : base[1]) + (int64_t)((uint64_t)(uint32_t)(row & 15) * step_row) + 16 * col : 0;
                 cp_async16(dst + 512 * i, p.src.k + at, there ? 16u : 0u, policy);
                 cp_async16(dst + kA4Half + 512 * i, p.src.v + at, there ? 16u : 0u, policy);
             }
-            bad = (bad & ~(3u << (2 * pstage))) | (miss << (2 * pstage));
-            ++pit;
-            advance();
         }
-        pstage = pstage + 1 == ST ? 0 : pstage + 1;
-        cp_commit();
+        bad = (bad & ~(3u << (2 * to))) | (miss << (2 * to));
+        if (++next < u.kb) look_up();
     };
-    advance();
+    bool more = walk();
+    if (more) { begin_unit(); issue(0); }
+    cp_commit();
 
-    AttCursor cur = {sh.seq, sh.h, 0, sh.start};
-    AttJob j = {};
-    uint4 q[CT][4];                                       // components 32 g + 8 t4 .. + 7 of query row g8 (+ 8 ct)
-    uint32_t qsum[CT][2];                                 // Q in three bf16 parts, the B operand of the centres
-    float from[CT][4][2];                                 // -136 Q_g of query rows 2 t4, 2 t4 + 1
+    struct { int seq, h, len, it, kb; bool begins, complete; } j = {};      // the unit that is being summed
+    uint32_t q[CT][4][4];                                 // components 32 g + 8 t4 .. + 7 of query row g8 (+ 8 ct)
+    float mul[CT][2];                                     // logit in base-2 units per accumulator unit, query rows 2 t4, 2 t4 + 1
+    uint32_t qsum[CT][3];                                 // Q and -8 Q in three bf16 parts, B operands of centres and scales
     float o[CT][4][2][4], oc[CT][4][2], m[CT][2], l[CT][2];
-    float top = 0.f, down = 1.f;                          // 2^E, no scale of V so far is above it; 2^-E
-    int it = 0, stage = 0, ahead = ST - 1;
+    float top = 0.f, above = 0.f;                         // largest size of values so far, a power of two; 15 less its exponent
     for (;;) {
-        // the stage of the step before: read, or used and released in joining a unit
-        issue();
-        if (ahead > 0) { --ahead; continue; }
-        if (it == j.kb) {
-            // ---------------- the next unit ----------------
-            bool rows = false;
-            while (!rows && next_unit(cur, j)) {
-                if (j.begins && tid == 0) p.rec[j.rec] = att_record(sh, j);
-                rows = j.kb > j.ka;
-                if (j.kt == 0 && j.begins)                // no rows: zeros
-                    for (int i = tid; i < p.G * 16; i += kA4Threads) {
-                        const int hq = j.h * p.G + (i >> 4);
-                        *reinterpret_cast<uint4 *>(p.out + ((int64_t)j.seq * p.out_seq + (int64_t)hq * p.out_head) * 2 + 16 * (i & 15)) =
-                            make_uint4(0u, 0u, 0u, 0u);
-                        if (p.lse && (i & 15) == 0) p.lse[(int64_t)j.seq * p.H * p.G + hq] = -INFINITY;
-                    }
-            }
-            if (!rows) break;
-            it = j.ka;
+        if (j.it == j.kb) {
+            // ---------------- the next unit: the one whose first step has been copied ----------------
+            if (!more) break;
+            j = {u.seq, u.h, u.len, u.ka, u.kb, u.begins, u.complete};
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
                 const int r = g8 + 8 * ct;
                 const char *qr = p.q + ((int64_t)j.seq * p.q_seq + (int64_t)(j.h * p.G + r) * p.q_head) * 2 + 16 * t4;
-                float sum[4];
+                float x[4][8], amax = 0.f, sum[4];
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    q[ct][g] = r < p.G ? *reinterpret_cast<const uint4 *>(qr + 64 * g) : make_uint4(0u, 0u, 0u, 0u);
-                    const uint4 x = q[ct][g];
-                    sum[g] = ((bf16_lo(x.x) + bf16_hi(x.x)) + (bf16_lo(x.y) + bf16_hi(x.y))) + ((bf16_lo(x.z) + bf16_hi(x.z)) + (bf16_lo(x.w) + bf16_hi(x.w)));
+                    const uint4 raw = r < p.G ? *reinterpret_cast<const uint4 *>(qr + 64 * g) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        x[g][2 * i] = bf16_lo(pick(raw, i)); x[g][2 * i + 1] = bf16_hi(pick(raw, i));
+                        amax = fmaxf(amax, fmaxf(fabsf(x[g][2 * i]), fabsf(x[g][2 * i + 1])));
+                    }
+                }
+                amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+                amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+                const int e = min(max((int)(__float_as_uint(amax) >> 23) - 127, -113), 127);
+                const float by = __uint_as_float((uint32_t)(141 - e) << 23), back = p.scale * 0x1p10f * __uint_as_float((uint32_t)(127 + e) << 23);
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[g][i] *= by;
+                    // (i odd: against codes 16 times as large)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float part = i & 1 ? 0.0625f : 1.f;
+                        q[ct][g][i] = cvt_f16x2(x[g][2 * i + 1] * part, x[g][2 * i] * part);
+                    }
+                    sum[g] = ((x[g][0] + x[g][1]) + (x[g][2] + x[g][3])) + ((x[g][4] + x[g][5]) + (x[g][6] + x[g][7]));
                     sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], 1);
                     sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], 2);
-#pragma unroll
-                    for (int x2 = 0; x2 < 2; ++x2) from[ct][g][x2] = -136.f * __shfl_sync(0xffffffffu, sum[g], (2 * t4 + x2) * 4);
+                    sum[g] *= 0x1p-24f;                    // in units of the accumulators of codes u 2^-24
                 }
-                // slots 2 t4, 2 t4 + 1 of the first 8: groups (0, 1), (2, 3), their high parts, then their middle ones; of the second
-                // 8 the low parts, then nothing
+#pragma unroll
+                for (int i = 0; i < 2; ++i) mul[ct][i] = __shfl_sync(0xffffffffu, back, (2 * t4 + i) * 4);
+                // slots 2 t4, 2 t4 + 1 of the first 8: Q of groups (0, 1), (2, 3), the high parts, then the middle ones; of the second
+                // 8 the low parts, then -8 Q, the high parts; of the last 8 (with scales) its middle parts, then the low ones
+                auto split = [](float a, float b, uint32_t (&x)[3]) {
+                    x[0] = cvt_bf16x2(b, a);
+                    a -= bf16_lo(x[0]); b -= bf16_hi(x[0]);
+                    x[1] = cvt_bf16x2(b, a);
+                    x[2] = cvt_bf16x2(b - bf16_hi(x[1]), a - bf16_lo(x[1]));
+                };
                 const float a = t4 & 1 ? sum[2] : sum[0], b = t4 & 1 ? sum[3] : sum[1];
-                const uint32_t hi = cvt_bf16x2(b, a);
-                const float a1 = a - bf16_lo(hi), b1 = b - bf16_hi(hi);
-                const uint32_t mid = cvt_bf16x2(b1, a1);
-                qsum[ct][0] = t4 < 2 ? hi : mid;
-                qsum[ct][1] = t4 < 2 ? cvt_bf16x2(b1 - bf16_hi(mid), a1 - bf16_lo(mid)) : 0u;
+                uint32_t c3[3], s3[3];
+                split(a, b, c3);
+                split(-8.f * a, -8.f * b, s3);
+                qsum[ct][0] = t4 < 2 ? c3[0] : c3[1];
+                qsum[ct][1] = t4 < 2 ? c3[2] : s3[0];
+                qsum[ct][2] = t4 < 2 ? s3[1] : s3[2];
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
 #pragma unroll
@@ -255,13 +295,20 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
                 m[ct][0] = m[ct][1] = -INFINITY;
                 l[ct][0] = l[ct][1] = 0.f;
             }
-            top = 0.f; down = 1.f;
+            top = 0x1p-81f; above = kAttAbove<true> + 81.f;
         }
+        // the other stage has been read, or used and released in joining a unit
+        if (more && next == u.kb) {
+            more = walk();
+            if (more) begin_unit();
+        }
+        if (more) issue(stage ^ 1);
+        cp_commit();
 
         // ---------------- one step ----------------
         cp_wait<ST - 1>();
         __syncwarp();
-        const uint32_t r0 = (uint32_t)it * TILE + warp * ROWS;
+        const uint32_t r0 = (uint32_t)j.it * TILE + warp * ROWS;
         const int have = r0 < (uint32_t)j.len ? min(j.len - (int)r0, ROWS) : 0;
         const uint32_t miss = (bad >> (2 * stage)) & 3u;
         const bool cut = have < ROWS || miss;
@@ -274,24 +321,23 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
             const uint4 ka = lds128(at + 16 * t4), kb = lds128(at + 8 * kRow4Bytes + 16 * t4);
             const uint2 sa = lds64(at + kRow4Scales), sb = lds64(at + 8 * kRow4Bytes + kRow4Scales);
             const uint32_t ca = lds32(at + kRow4Centres + 4 * (t4 & 1)), cb = lds32(at + 8 * kRow4Bytes + kRow4Centres + 4 * (t4 & 1));
+            const uint32_t da = t4 & 1 ? sa.y : sa.x, db = t4 & 1 ? sb.y : sb.x;
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) mma_bf16_from(w[ct][kg], ca, cb, ca, cb, qsum[ct][0], qsum[ct][1], 0.f, 0.f);
+            for (int ct = 0; ct < CT; ++ct) {
+                mma_bf16_16816_new(w[ct][kg], ca, cb, t4 < 2 ? ca : da, t4 < 2 ? cb : db, qsum[ct][0], qsum[ct][1]);
+                mma_bf16_1688_acc(w[ct][kg], da, db, qsum[ct][2]);
+            }
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const uint32_t xa = pick(ka, g), xb = pick(kb, g);
-                uint32_t a[4], b[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    a[i] = nibbles<0x000f000fu, 0x43004300u>(xa >> 4 * i);
-                    b[i] = nibbles<0x000f000fu, 0x43004300u>(xb >> 4 * i);
-                }
+                const uint32_t xa8 = xa >> 8, xb8 = xb >> 8;
                 const float s0 = g & 1 ? bf16_hi(g < 2 ? sa.x : sa.y) : bf16_lo(g < 2 ? sa.x : sa.y);
                 const float s1 = g & 1 ? bf16_hi(g < 2 ? sb.x : sb.y) : bf16_lo(g < 2 ? sb.x : sb.y);
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
                     float acc[4];
-                    mma_bf16_from(acc, a[0], b[0], a[1], b[1], q[ct][g].x, q[ct][g].y, from[ct][g][0], from[ct][g][1]);
-                    mma_bf16_16816_acc(acc, a[2], b[2], a[3], b[3], q[ct][g].z, q[ct][g].w);
+                    mma_f16_16816_new(acc, xa & kLow, xb & kLow, xa & kHigh, xb & kHigh, q[ct][g][0], q[ct][g][1]);
+                    mma_f16_16816(acc, xa8 & kLow, xb8 & kLow, xa8 & kHigh, xb8 & kHigh, q[ct][g][2], q[ct][g][3]);
                     w[ct][kg][0] = fmaf(s0, acc[0], w[ct][kg][0]); w[ct][kg][1] = fmaf(s0, acc[1], w[ct][kg][1]);
                     w[ct][kg][2] = fmaf(s1, acc[2], w[ct][kg][2]); w[ct][kg][3] = fmaf(s1, acc[3], w[ct][kg][3]);
                 }
@@ -299,43 +345,38 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    w[ct][kg][x] *= p.scale;
-                    if (cut && (16 * kg + row_k + 8 * (x >> 1) >= have || ((miss >> kg) & 1u))) w[ct][kg][x] = -INFINITY;
-                }
+                for (int x = 0; x < 4; ++x) w[ct][kg][x] *= mul[ct][x & 1];
         }
-        // the bounds of weights and scales are looked at by a vote and searched for only when one has to be raised
-        uint2 vs[NK][2], vc[NK][2];                       // scales and centres of rows g8, g8 + 8 of V
-        uint32_t smax = 0;
+        if (cut) {
 #pragma unroll
-        for (int kg = 0; kg < NK; ++kg)
+            for (int kg = 0; kg < NK; ++kg)
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const uint32_t at = vb_s + klane + (16 * kg + 8 * x) * kRow4Bytes;
-                vs[kg][x] = lds64(at + kRow4Scales);
-                vc[kg][x] = lds64(at + kRow4Centres);
-                smax = max_bf16x2(smax, max_bf16x2(vs[kg][x].x, vs[kg][x].y));
-            }
-        float mx[CT][2], sm = fmaxf(bf16_lo(smax), bf16_hi(smax));
+                for (int x = 0; x < 4; ++x)
+                    if (16 * kg + row_k + 8 * (x >> 1) >= have || ((miss >> kg) & 1u))
+#pragma unroll
+                        for (int ct = 0; ct < CT; ++ct) w[ct][kg][x] = -INFINITY;
+        }
+        // The bound m on the logits, and `top` on the sizes of values: scales, and centres by 2^-30 (weights times centres stay below
+        // 2^45).  m keeps weights times top in [2^11, 2^15] where they are largest.  Both are looked at by a vote and searched for only
+        // when one has to be raised.
+        const uint4 par = lds128(vb_s + lane * kRow4Bytes + kRow4Scales);          // (of the lane's row of V)
+        const uint32_t s_max = max_bf16x2(par.x, par.y), c_max = max_bf16x2(par.z & 0x7fff7fffu, par.w & 0x7fff7fffu);
+        float mx[CT][2], sm = fmaxf(fmaxf(bf16_lo(s_max), bf16_hi(s_max)), fmaxf(bf16_lo(c_max), bf16_hi(c_max)) * 0x1p-30f);
         bool raise = sm > top;
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 mx[ct][i] = fmaxf(fmaxf(w[ct][0][i], w[ct][0][i + 2]), fmaxf(w[ct][NK - 1][i], w[ct][NK - 1][i + 2]));
-                raise = raise || mx[ct][i] > m[ct][i] + kAttAbove<true>;
+                raise = raise || mx[ct][i] > m[ct][i] + above;
             }
         if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
-            for (int d = 4; d < 32; d *= 2) sm = fmaxf(sm, __shfl_xor_sync(0xffffffffu, sm, d));
-            float by_s = 1.f;
+            for (int d = 1; d < 32; d *= 2) sm = fmaxf(sm, __shfl_xor_sync(0xffffffffu, sm, d));
             if (sm > top) {                               // (all lanes alike)
-                // the power of two above it; scales are 0 or at least 2^-126 and below 2^126
-                const uint32_t e = min(__float_as_uint(sm) >> 23, 252u) + 1;
-                const float up = __uint_as_float(e << 23);
-                by_s = top * __uint_as_float((254u - e) << 23);
-                top = up;
-                down = __uint_as_float((254u - e) << 23);
+                const int e = (int)min(__float_as_uint(sm) >> 23, 252u) - 126;
+                top = __uint_as_float((uint32_t)(e + 127) << 23);
+                above = kAttAbove<true> - (float)e;
             }
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
@@ -343,18 +384,17 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
                 for (int i = 0; i < 2; ++i) {
 #pragma unroll
                     for (int d = 4; d < 32; d *= 2) mx[ct][i] = fmaxf(mx[ct][i], __shfl_xor_sync(0xffffffffu, mx[ct][i], d));
-                    float by = 1.f;
-                    if (mx[ct][i] > m[ct][i] + kAttAbove<true>) {
-                        mx[ct][i] -= kAttBelow<true>;
-                        by = ex2(m[ct][i] - mx[ct][i]);           // 0 where there was no bound yet
-                        m[ct][i] = mx[ct][i];
-                        l[ct][i] *= by;
-                    }
+                    // the largest logit so far is at most m + above as it was, that is as far above m as the weights may reach
+                    float to = m[ct][i];
+                    if (mx[ct][i] > m[ct][i] + above) to = mx[ct][i] - above + (kAttAbove<true> - kAttBelow<true>);
+                    const float by = to == m[ct][i] ? 1.f : ex2(m[ct][i] - to);       // 0 where there was no bound yet
+                    m[ct][i] = to;
+                    l[ct][i] *= by;
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
                         oc[ct][g][i] *= by;
 #pragma unroll
-                        for (int y = 0; y < 2; ++y) { o[ct][g][y][i] *= by * by_s; o[ct][g][y][i + 2] *= by * by_s; }
+                        for (int y = 0; y < 2; ++y) { o[ct][g][y][i] *= by; o[ct][g][y][i + 2] *= by; }
                     }
                 }
         }
@@ -362,6 +402,13 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
         for (int kg = 0; kg < NK; ++kg) {
             // weights, times scales, and transposed into the B operand: 16 cached rows x 8 query rows for each group
             uint32_t pw[CT][4][2];
+            uint2 vs[2], vc[2];                           // scales and centres of rows g8, g8 + 8 of the tile
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const uint32_t row = vb_s + klane + (16 * kg + 8 * x) * kRow4Bytes;
+                vs[x] = lds64(row + kRow4Scales);
+                vc[x] = lds64(row + kRow4Centres);
+            }
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
                 float e[4];
@@ -374,14 +421,12 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
                 for (int g = 0; g < 4; ++g)
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        const uint32_t s2 = g < 2 ? vs[kg][x].x : vs[kg][x].y, c2 = g < 2 ? vc[kg][x].x : vc[kg][x].y;
+                        const uint32_t s2 = g < 2 ? vs[x].x : vs[x].y, c2 = g < 2 ? vc[x].x : vc[x].y;
                         const float c = g & 1 ? bf16_hi(c2) : bf16_lo(c2);
-                        const float s = (g & 1 ? bf16_hi(s2) : bf16_lo(s2)) * down;
+                        const float s = g & 1 ? bf16_hi(s2) : bf16_lo(s2);
                         oc[ct][g][0] = fmaf(e[2 * x], c, oc[ct][g][0]);
                         oc[ct][g][1] = fmaf(e[2 * x + 1], c, oc[ct][g][1]);
-                        uint32_t h2;
-                        asm("cvt.rn.f16x2.f32 %0, %1, %2;\n" : "=r"(h2) : "f"(e[2 * x + 1] * s), "f"(e[2 * x] * s));
-                        pw[ct][g][x] = transpose8x8(h2);
+                        pw[ct][g][x] = transpose8x8(cvt_f16x2(e[2 * x + 1] * s, e[2 * x] * s));
                     }
             }
             const uint32_t at = vb_s + vlane + 16 * kg * kRow4Bytes;
@@ -389,27 +434,21 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 // four components of rows (t4, t4 + 4) and of rows (t4 + 8, t4 + 12)
-                const uint32_t u = __byte_perm(pick(v0, g), pick(v1, g), half), x = __byte_perm(pick(v2, g), pick(v3, g), half);
-                const uint32_t u8 = u >> 8, x8 = x >> 8;
-                const uint32_t a0 = sub_f16x2(nibbles<0x000f000fu, 0x64006400u>(u), 0x64086408u);                         // 1032
-                const uint32_t a1 = fma_f16x2(nibbles<0x00f000f0u, 0x64006400u>(u), 0x2c002c00u, 0xd480d480u);            // 1/16, -72
-                const uint32_t a2 = sub_f16x2(nibbles<0x000f000fu, 0x64006400u>(x), 0x64086408u);
-                const uint32_t a3 = fma_f16x2(nibbles<0x00f000f0u, 0x64006400u>(x), 0x2c002c00u, 0xd480d480u);
-                const uint32_t b0 = sub_f16x2(nibbles<0x000f000fu, 0x64006400u>(u8), 0x64086408u);
-                const uint32_t b1 = fma_f16x2(nibbles<0x00f000f0u, 0x64006400u>(u8), 0x2c002c00u, 0xd480d480u);
-                const uint32_t b2 = sub_f16x2(nibbles<0x000f000fu, 0x64006400u>(x8), 0x64086408u);
-                const uint32_t b3 = fma_f16x2(nibbles<0x00f000f0u, 0x64006400u>(x8), 0x2c002c00u, 0xd480d480u);
+                const uint32_t xa = __byte_perm(pick(v0, g), pick(v1, g), half), xb = __byte_perm(pick(v2, g), pick(v3, g), half);
+                const uint32_t xa8 = xa >> 8, xb8 = xb >> 8;
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
-                    mma_f16_16816(o[ct][g][0], a0, a1, a2, a3, pw[ct][g][0], pw[ct][g][1]);
-                    mma_f16_16816(o[ct][g][1], b0, b1, b2, b3, pw[ct][g][0], pw[ct][g][1]);
+                    mma_f16_16816(o[ct][g][0], kLess, kLess16, kLess, kLess16, pw[ct][g][0], pw[ct][g][1]);
+                    mma_f16_16816(o[ct][g][1], kLess, kLess16, kLess, kLess16, pw[ct][g][0], pw[ct][g][1]);
+                    mma_f16_16816(o[ct][g][0], xa & kLow, xa & kHigh, xb & kLow, xb & kHigh, pw[ct][g][0], pw[ct][g][1]);
+                    mma_f16_16816(o[ct][g][1], xa8 & kLow, xa8 & kHigh, xb8 & kLow, xb8 & kHigh, pw[ct][g][0], pw[ct][g][1]);
                 }
             }
         }
         __syncwarp();
         uint8_t *used = dyn + (warp * ST + stage) * kA4StageBytes;
-        stage = stage + 1 == ST ? 0 : stage + 1;
-        if (++it < j.kb) continue;
+        stage ^= 1;
+        if (++j.it < j.kb) continue;
 
         // ---------------- the unit's rows of this share are through: join the warps ----------------
         // per 8 query rows: each leaves its sums in the stage it has just read, fragment by fragment, and takes a group of all
@@ -431,8 +470,8 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
 #pragma unroll
                 for (int y = 0; y < 2; ++y)
                     *reinterpret_cast<float4 *>(used + (2 * g + y) * 512 + lane * 16) =
-                        make_float4(fmaf(o[ct][g][y][0], top, oc[ct][g][0]), fmaf(o[ct][g][y][1], top, oc[ct][g][1]),
-                                    fmaf(o[ct][g][y][2], top, oc[ct][g][0]), fmaf(o[ct][g][y][3], top, oc[ct][g][1]));
+                        make_float4(fmaf(o[ct][g][y][0], 0x1p24f, oc[ct][g][0]), fmaf(o[ct][g][y][1], 0x1p24f, oc[ct][g][1]),
+                                    fmaf(o[ct][g][y][2], 0x1p20f, oc[ct][g][0]), fmaf(o[ct][g][y][3], 0x1p20f, oc[ct][g][1]));
             __syncthreads();
             // components 32 warp + 8 (g8 / 2) + g8 % 2 + 0, 2, 4, 6 of query rows 2 t4, 2 t4 + 1 (+ 8 ct)
             float mm[2], ll[2], by[kA4Warps][2], z[2][4];
