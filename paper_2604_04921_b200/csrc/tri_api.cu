@@ -480,7 +480,7 @@ cudaError_t prepare_device()
     if ((e = allow_attend_smem<false, 16>()) != cudaSuccess) return e;
     if ((e = allow_attend_smem<true, 8>()) != cudaSuccess) return e;
     if ((e = allow_attend_smem<true, 16>()) != cudaSuccess) return e;
-    if ((e = allow_attend4_smem<8>()) != cudaSuccess || (e = allow_attend4_smem<16>()) != cudaSuccess) return e;
+    if ((e = allow_attend4_smem<4>()) != cudaSuccess || (e = allow_attend4_smem<8>()) != cudaSuccess || (e = allow_attend4_smem<16>()) != cudaSuccess) return e;
     if ((e = load_append<0, 5>()) != cudaSuccess || (e = load_append<1, 5>()) != cudaSuccess) return e;
     if ((e = load_kernels(k_read<0, 2>, k_read<1, 2>, k_read<2, 2>, k_read<3, 2>, k_read<5, 2>, k_read<0, 4>, k_read<1, 4>, k_read<2, 4>,
                           k_read<3, 4>, k_read<5, 4>)) != cudaSuccess) return e;
@@ -1387,7 +1387,7 @@ AttendPlan make_attend_plan(const tri_ctx *c, int32_t S, int32_t P)
     const int32_t H = c->desc.n_kv_heads, G = c->desc.group_size;
     a.blocks = c->n_sm * kAttBlocksPerSM;
     a.own_rows = G <= 8 ? 8 : 16;
-    a.blocks4 = c->n_sm * (G <= 8 ? kA4BlocksPerSM<8> : kA4BlocksPerSM<16>);
+    a.blocks4 = c->n_sm * (G <= 4 ? kA4BlocksPerSM<4> : (G <= 8 ? kA4BlocksPerSM<8> : kA4BlocksPerSM<16>));
     const int32_t most = a.blocks > a.blocks4 ? a.blocks : a.blocks4;
     const size_t row = kAttRowPitch * sizeof(float), whole = align256((size_t)S * H * G * row);
     size_t o = 0;
@@ -1417,16 +1417,19 @@ cudaError_t launch_attend_clusters(int rows, unsigned units, cudaStream_t st, co
                      : launch_clusters(k_attend_cluster<KEY8, 16>, kAttCluster, units * kAttCluster, kAttThreads, kAttRingBytes, st, p, pre);
 }
 
-cudaError_t launch_attend4(int rows, unsigned blocks, cudaStream_t st, const AttendParams &p)
+// (G: query rows of a unit.  Up to 4, with the columns used twice, 131,072 rows of 8 heads take @@ us against @@.)
+cudaError_t launch_attend4(int G, unsigned blocks, cudaStream_t st, const AttendParams &p)
 {
-    return rows == 8 ? launch_under(k_attend4<8>, blocks, kA4Threads, kA4RingBytes, st, p)
-                     : launch_under(k_attend4<16>, blocks, kA4Threads, kA4RingBytes, st, p);
+    if (G <= 4) return launch_under(k_attend4<4>, blocks, kA4Threads, kA4RingBytes, st, p);
+    return G <= 8 ? launch_under(k_attend4<8>, blocks, kA4Threads, kA4RingBytes, st, p)
+                  : launch_under(k_attend4<16>, blocks, kA4Threads, kA4RingBytes, st, p);
 }
 
-cudaError_t launch_attend4_clusters(int rows, unsigned units, cudaStream_t st, const AttendParams &p)
+cudaError_t launch_attend4_clusters(int G, unsigned units, cudaStream_t st, const AttendParams &p)
 {
-    return rows == 8 ? launch_clusters(k_attend4_cluster<8>, kAttCluster, units * kAttCluster, kA4Threads, kA4RingBytes, st, p)
-                     : launch_clusters(k_attend4_cluster<16>, kAttCluster, units * kAttCluster, kA4Threads, kA4RingBytes, st, p);
+    if (G <= 4) return launch_clusters(k_attend4_cluster<4>, kAttCluster, units * kAttCluster, kA4Threads, kA4RingBytes, st, p);
+    return G <= 8 ? launch_clusters(k_attend4_cluster<8>, kAttCluster, units * kAttCluster, kA4Threads, kA4RingBytes, st, p)
+                  : launch_clusters(k_attend4_cluster<16>, kAttCluster, units * kAttCluster, kA4Threads, kA4RingBytes, st, p);
 }
 
 // rows4: whether the call takes 4-bit rows.
@@ -1513,7 +1516,7 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
             pre = attend_params(c, prefix, P, S, io, device_status);
             pre.group_start = group_start;
         }
-        if (rows4) TRI_CUDA(launch_attend4_clusters(pl.own_rows, (unsigned)(S * H), st, p));
+        if (rows4) TRI_CUDA(launch_attend4_clusters(G, (unsigned)(S * H), st, p));
         else if (src->view->k_kind == 3) TRI_CUDA(launch_attend_clusters<true>(pl.own_rows, (unsigned)(S * H), st, p, pre));
         else TRI_CUDA(launch_attend_clusters<false>(pl.own_rows, (unsigned)(S * H), st, p, pre));
         return TRI_OK;
@@ -1549,7 +1552,7 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
     p.rec = (int2 *)(w + pl.own_rec); p.slots = (float *)(w + pl.own_slots);
     p.whole = P > 0 ? (float *)(w + pl.own_whole) : nullptr;
     const int32_t blocks = rows4 ? pl.blocks4 : pl.blocks;
-    if (rows4) TRI_CUDA(launch_attend4(pl.own_rows, (unsigned)blocks, st, p));
+    if (rows4) TRI_CUDA(launch_attend4(G, (unsigned)blocks, st, p));
     else if (src->view->k_kind == 3) TRI_CUDA(launch_attend<true>(pl.own_rows, (unsigned)pl.blocks, st, p));
     else TRI_CUDA(launch_attend<false>(pl.own_rows, (unsigned)pl.blocks, st, p));
 

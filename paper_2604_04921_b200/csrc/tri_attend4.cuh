@@ -9,8 +9,8 @@
 //            7; as e4m3, whose matrix instructions sm_100a makes of conversions and f16 ones, 3 and 20 conversions).  A query row is
 //            brought to [2^14, 2^15) by a power of two and goes in as f16, a sixteenth of it where the codes are 16 times as large: a
 //            bf16 value is exact unless it is 2^28 times smaller than the row's largest.  Centres, and the 8 that each code is too
-//            large by, go through one and a half matrix instructions: c_ng against Q_g and s_ng against -8 Q_g, both in three bf16
-//            parts, that is to 24 bits.
+//            large by, go through one matrix instruction more: c_ng against Q_g and s_ng against -8 Q_g, both in two bf16 parts, that
+//            is to 2^-17.
 //   sums     the 16 rows of A are components, its 16 columns cached rows, operands likewise: A's upper 8 rows carry 16 times the lower
 //            ones.  8 times the weights' sum is taken off in the same accumulators, by a matrix of constants.  The weights p_n s_ng are rounded
 //            once to f16: the bound on the logits that p is taken against goes by the largest scale of the rows so far, too, so that
@@ -27,12 +27,13 @@ namespace tri {
 
 constexpr int kA4Warps = kAttWarps, kA4Threads = 32 * kA4Warps, kA4Rows = 32, kA4Stages = 2;      // (one step ahead)
 constexpr int kA4Half = kA4Rows * kRow4Bytes, kA4StageBytes = 2 * kA4Half;                  // K | V
-constexpr int kA4RingBytes = kA4Warps * kA4Stages * kA4StageBytes;
+constexpr int kA4ScaleBytes = kA4Rows * 48;                      // scales of K, scales and centres of V in fp32
+constexpr int kA4WarpBytes = kA4Stages * kA4StageBytes + kA4ScaleBytes, kA4RingBytes = kA4Warps * kA4WarpBytes;
 constexpr int kA4Tile = kA4Warps * kA4Rows;
 constexpr int kA4UnitCost = 2;                                   // a unit's own cost, in tiles
-template <int RT> constexpr int kA4BlocksPerSM = RT == 8 ? 3 : 2;
+template <int RT> constexpr int kA4BlocksPerSM = RT <= 8 ? 3 : 2;
+constexpr float kA4NoBound = -3e38f;                             // below every logit; finite, so that 2^(-infinity - m) is 0
 constexpr uint32_t kLow = 0x000f000fu, kHigh = 0x00f000f0u;     // nibbles that are pairs of f16 values u 2^-24, u 2^-20
-constexpr uint32_t kLess = 0x80088008u, kLess16 = 0x80808080u;   // -8 2^-24, -8 2^-20
 static_assert(kA4StageBytes >= 8 * 512, "the sums of a warp fit into a stage");
 
 __device__ __forceinline__ void mma_bf16_16816_new(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
@@ -41,11 +42,6 @@ __device__ __forceinline__ void mma_bf16_16816_new(float (&d)[4], uint32_t a0, u
         "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
-}
-__device__ __forceinline__ void mma_bf16_1688_acc(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0)
-{
-    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};\n"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(b0));
 }
 __device__ __forceinline__ void mma_f16_16816_new(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
@@ -72,11 +68,25 @@ __device__ __forceinline__ uint4 lds128(uint32_t at)
     asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];\n" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(at) : "memory");
     return r;
 }
+__device__ __forceinline__ float4 lds_f4(uint32_t at)
+{
+    const uint4 x = lds128(at);
+    return make_float4(__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w));
+}
+__device__ __forceinline__ void sts128(uint32_t at, float a, float b, float c, float d)
+{
+    asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};\n" ::"r"(at), "f"(a), "f"(b), "f"(c), "f"(d) : "memory");
+}
 __device__ __forceinline__ uint2 lds64(uint32_t at)
 {
     uint2 r;
     asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];\n" : "=r"(r.x), "=r"(r.y) : "r"(at) : "memory");
     return r;
+}
+__device__ __forceinline__ float2 lds_f2(uint32_t at)
+{
+    const uint2 x = lds64(at);
+    return make_float2(__uint_as_float(x.x), __uint_as_float(x.y));
 }
 __device__ __forceinline__ uint32_t lds32(uint32_t at)
 {
@@ -84,25 +94,29 @@ __device__ __forceinline__ uint32_t lds32(uint32_t at)
     asm volatile("ld.shared.u32 %0, [%1];\n" : "=r"(r) : "r"(at) : "memory");
     return r;
 }
+// Group g of four values in the order of groups 0, 2, 1, 3.
+__device__ __forceinline__ float pick(const float4 &x, int g) { return g == 0 ? x.x : (g == 2 ? x.y : (g == 1 ? x.z : x.w)); }
 __device__ __forceinline__ uint32_t pick(const uint4 &x, int i) { return i == 0 ? x.x : (i == 1 ? x.y : (i == 2 ? x.z : x.w)); }
 
-// RT: query rows, 8 or up to 16 (two column tiles).  CL > 0: a cluster of CL blocks takes one unit, as in tri_attend.cuh.
+// RT: query rows, up to 4, 8 or 16 (two column tiles).  RT = 4: the other 4 columns hold the same rows again; then the weights of
+// two groups go into one operand, half of the columns each, and their sums into those columns of each group's accumulators.  CL > 0: a cluster of CL blocks takes one unit, as in tri_attend.cuh.
 template <int RT, int CL>
 __device__ __forceinline__ void attend4_block(const AttendParams &p)
 {
-    constexpr int CT = RT / 8, ST = kA4Stages, ROWS = kA4Rows, NK = 2, TILE = kA4Tile;
+    constexpr int CT = RT == 16 ? 2 : 1, COLS = 8 * CT, GP = RT == 4 ? 2 : 4, ST = kA4Stages, ROWS = kA4Rows, NK = 2, TILE = kA4Tile;
     static_assert(ROWS == 16 * NK, "two tiles of 16 cached rows per step");
     extern __shared__ __align__(128) uint8_t dyn[];
-    __shared__ float2 stat[kA4Warps][RT];
-    __shared__ __align__(16) float part[CL ? RT : 1][kAttRowPitch];      // this block's sums, and (m, l)
+    __shared__ float2 stat[kA4Warps][COLS];
+    __shared__ __align__(16) float part[CL ? COLS : 1][kAttRowPitch];      // this block's sums, and (m, l)
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
-    const uint32_t ring = smem_u32(dyn) + warp * (ST * kA4StageBytes);
+    const uint32_t ring = smem_u32(dyn) + warp * kA4WarpBytes, scales = ring + ST * kA4StageBytes;
     // Cached row of row i of a matrix tile of keys: i / 2 + 4 (i % 2) of 8 (the second 8 rows 8 further on).  Rows 4 apart are 64 bytes
     // apart in the banks: two rows' 64 bytes of codes, one load's phase, take all of them.  The sums over cached rows then take
     // columns 2 t4, 2 t4 + 1 of A from rows t4, t4 + 4.
     const int row_k = (g8 >> 1) + 4 * (g8 & 1);
     const uint32_t klane = row_k * kRow4Bytes, vlane = t4 * kRow4Bytes + 16 * (g8 >> 1);
+    const int odd_cols = RT == 4 ? t4 >> 1 : 0;           // RT = 4: which group of a pair this lane's columns are for
     const uint32_t half = g8 & 1 ? 0x7632u : 0x5410u;     // which half of a word of V holds this lane's components
     grid_dependency_wait();
     grid_dependents_launch();
@@ -114,7 +128,7 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
     } else {
         asm volatile("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(rank));
         sh.seq = (int)blockIdx.x / CL / p.H; sh.h = (int)blockIdx.x / CL - sh.seq * p.H;
-        if (tid < RT) { part[CL ? tid : 0][kHeadDim] = -INFINITY; part[CL ? tid : 0][kHeadDim + 1] = 0.f; }      // no rows so far
+        if (tid < COLS) { part[CL ? tid : 0][kHeadDim] = -INFINITY; part[CL ? tid : 0][kHeadDim + 1] = 0.f; }      // no rows so far
     }
     // ---------------- the walk over the share's units, one step ahead of the sums ----------------
     AttCursor cursor = {sh.seq, sh.h, 0, sh.start};
@@ -228,9 +242,11 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
     struct { int seq, h, len, it, kb; bool begins, complete; } j = {};      // the unit that is being summed
     uint32_t q[CT][4][4];                                 // components 32 g + 8 t4 .. + 7 of query row g8 (+ 8 ct)
     float mul[CT][2];                                     // logit in base-2 units per accumulator unit, query rows 2 t4, 2 t4 + 1
-    uint32_t qsum[CT][3];                                 // Q and -8 Q in three bf16 parts, B operands of centres and scales
-    float o[CT][4][2][4], oc[CT][4][2], m[CT][2], l[CT][2];
+    uint32_t qsum[CT][2];                                 // Q and -8 Q in two bf16 parts, B operand of centres and scales
+    float o[CT][4][2][4], oc[CT][GP][2], m[CT][2], l[CT][2];
     float top = 0.f, above = 0.f;                         // largest size of values so far, a power of two; 15 less its exponent
+    uint32_t less[2];                                     // -8 2^-24, -8 2^-20 as f16 pairs (kept in registers)
+    asm volatile("mov.u32 %0, 0x80088008;\nmov.u32 %1, 0x80808080;\n" : "=r"(less[0]), "=r"(less[1]));
     for (;;) {
         if (j.it == j.kb) {
             // ---------------- the next unit: the one whose first step has been copied ----------------
@@ -238,7 +254,7 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
             j = {u.seq, u.h, u.len, u.ka, u.kb, u.begins, u.complete};
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
-                const int r = g8 + 8 * ct;
+                const int r = (RT == 4 ? g8 & 3 : g8) + 8 * ct;
                 const char *qr = p.q + ((int64_t)j.seq * p.q_seq + (int64_t)(j.h * p.G + r) * p.q_head) * 2 + 16 * t4;
                 float x[4][8], amax = 0.f, sum[4];
 #pragma unroll
@@ -271,28 +287,19 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
                 }
 #pragma unroll
                 for (int i = 0; i < 2; ++i) mul[ct][i] = __shfl_sync(0xffffffffu, back, (2 * t4 + i) * 4);
-                // slots 2 t4, 2 t4 + 1 of the first 8: Q of groups (0, 1), (2, 3), the high parts, then the middle ones; of the second
-                // 8 the low parts, then -8 Q, the high parts; of the last 8 (with scales) its middle parts, then the low ones
-                auto split = [](float a, float b, uint32_t (&x)[3]) {
-                    x[0] = cvt_bf16x2(b, a);
-                    a -= bf16_lo(x[0]); b -= bf16_hi(x[0]);
-                    x[1] = cvt_bf16x2(b, a);
-                    x[2] = cvt_bf16x2(b - bf16_hi(x[1]), a - bf16_lo(x[1]));
-                };
+                // slots 2 t4, 2 t4 + 1 of the first 8: Q of groups (0, 1), (2, 3), the high parts, then the low ones; of the second 8
+                // -8 Q likewise
                 const float a = t4 & 1 ? sum[2] : sum[0], b = t4 & 1 ? sum[3] : sum[1];
-                uint32_t c3[3], s3[3];
-                split(a, b, c3);
-                split(-8.f * a, -8.f * b, s3);
-                qsum[ct][0] = t4 < 2 ? c3[0] : c3[1];
-                qsum[ct][1] = t4 < 2 ? c3[2] : s3[0];
-                qsum[ct][2] = t4 < 2 ? s3[1] : s3[2];
+                const uint32_t hi = cvt_bf16x2(b, a), lo = cvt_bf16x2(b - bf16_hi(hi), a - bf16_lo(hi)), part8 = t4 < 2 ? hi : lo;
+                qsum[ct][0] = part8;
+                qsum[ct][1] = cvt_bf16x2(-8.f * bf16_hi(part8), -8.f * bf16_lo(part8));
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
 #pragma unroll
                     for (int y = 0; y < 2; ++y) o[ct][g][y][0] = o[ct][g][y][1] = o[ct][g][y][2] = o[ct][g][y][3] = 0.f;
-                    oc[ct][g][0] = oc[ct][g][1] = 0.f;
+                    oc[ct][g % GP][0] = oc[ct][g % GP][1] = 0.f;
                 }
-                m[ct][0] = m[ct][1] = -INFINITY;
+                m[ct][0] = m[ct][1] = kA4NoBound;
                 l[ct][0] = l[ct][1] = 0.f;
             }
             top = 0x1p-81f; above = kAttAbove<true> + 81.f;
@@ -313,26 +320,31 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
         const uint32_t miss = (bad >> (2 * stage)) & 3u;
         const bool cut = have < ROWS || miss;
         const uint32_t kb_s = ring + stage * kA4StageBytes, vb_s = kb_s + kA4Half;
+        // a lane widens the scales (of groups 0, 2, 1, 3) and centres of one row for all
+        const uint4 k_par = lds128(kb_s + lane * kRow4Bytes + kRow4Scales), v_par = lds128(vb_s + lane * kRow4Bytes + kRow4Scales);
+        const uint32_t row48 = scales + lane * 48;
+        sts128(row48, bf16_lo(k_par.x), bf16_lo(k_par.y), bf16_hi(k_par.x), bf16_hi(k_par.y));
+        sts128(row48 + 16, bf16_lo(v_par.x), bf16_lo(v_par.y), bf16_hi(v_par.x), bf16_hi(v_par.y));
+        sts128(row48 + 32, bf16_lo(v_par.z), bf16_lo(v_par.w), bf16_hi(v_par.z), bf16_hi(v_par.w));
+        const uint32_t s_max = max_bf16x2(v_par.x, v_par.y), c_max = max_bf16x2(v_par.z & 0x7fff7fffu, v_par.w & 0x7fff7fffu);
+        __syncwarp();
         // logits: 16 cached rows x 8 query rows; the thread holds rows g8, g8 + 8 of the tile for query rows 2 t4, 2 t4 + 1
         float w[CT][NK][4];
 #pragma unroll
         for (int kg = 0; kg < NK; ++kg) {
             const uint32_t at = kb_s + klane + 16 * kg * kRow4Bytes;
             const uint4 ka = lds128(at + 16 * t4), kb = lds128(at + 8 * kRow4Bytes + 16 * t4);
-            const uint2 sa = lds64(at + kRow4Scales), sb = lds64(at + 8 * kRow4Bytes + kRow4Scales);
+            const uint32_t wide = scales + row_k * 48 + 16 * kg * 48;
+            const float4 sa = lds_f4(wide), sb = lds_f4(wide + 8 * 48);
             const uint32_t ca = lds32(at + kRow4Centres + 4 * (t4 & 1)), cb = lds32(at + 8 * kRow4Bytes + kRow4Centres + 4 * (t4 & 1));
-            const uint32_t da = t4 & 1 ? sa.y : sa.x, db = t4 & 1 ? sb.y : sb.x;
+            const uint32_t da = lds32(at + kRow4Scales + 4 * (t4 & 1)), db = lds32(at + 8 * kRow4Bytes + kRow4Scales + 4 * (t4 & 1));
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) {
-                mma_bf16_16816_new(w[ct][kg], ca, cb, t4 < 2 ? ca : da, t4 < 2 ? cb : db, qsum[ct][0], qsum[ct][1]);
-                mma_bf16_1688_acc(w[ct][kg], da, db, qsum[ct][2]);
-            }
+            for (int ct = 0; ct < CT; ++ct) mma_bf16_16816_new(w[ct][kg], ca, cb, da, db, qsum[ct][0], qsum[ct][1]);
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const uint32_t xa = pick(ka, g), xb = pick(kb, g);
                 const uint32_t xa8 = xa >> 8, xb8 = xb >> 8;
-                const float s0 = g & 1 ? bf16_hi(g < 2 ? sa.x : sa.y) : bf16_lo(g < 2 ? sa.x : sa.y);
-                const float s1 = g & 1 ? bf16_hi(g < 2 ? sb.x : sb.y) : bf16_lo(g < 2 ? sb.x : sb.y);
+                const float s0 = pick(sa, g), s1 = pick(sb, g);
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
                     float acc[4];
@@ -359,8 +371,6 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
         // The bound m on the logits, and `top` on the sizes of values: scales, and centres by 2^-30 (weights times centres stay below
         // 2^45).  m keeps weights times top in [2^11, 2^15] where they are largest.  Both are looked at by a vote and searched for only
         // when one has to be raised.
-        const uint4 par = lds128(vb_s + lane * kRow4Bytes + kRow4Scales);          // (of the lane's row of V)
-        const uint32_t s_max = max_bf16x2(par.x, par.y), c_max = max_bf16x2(par.z & 0x7fff7fffu, par.w & 0x7fff7fffu);
         float mx[CT][2], sm = fmaxf(fmaxf(bf16_lo(s_max), bf16_hi(s_max)), fmaxf(bf16_lo(c_max), bf16_hi(c_max)) * 0x1p-30f);
         bool raise = sm > top;
 #pragma unroll
@@ -392,7 +402,7 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
                     l[ct][i] *= by;
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
-                        oc[ct][g][i] *= by;
+                        if (g < GP) oc[ct][g][i] *= by;
 #pragma unroll
                         for (int y = 0; y < 2; ++y) { o[ct][g][y][i] *= by; o[ct][g][y][i + 2] *= by; }
                     }
@@ -401,29 +411,31 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
 #pragma unroll
         for (int kg = 0; kg < NK; ++kg) {
             // weights, times scales, and transposed into the B operand: 16 cached rows x 8 query rows for each group
-            uint32_t pw[CT][4][2];
-            uint2 vs[2], vc[2];                           // scales and centres of rows g8, g8 + 8 of the tile
+            uint32_t pw[CT][GP][2];
+            float4 vs[2], vc[2];                          // scales and centres of rows g8, g8 + 8 of the tile; RT = 4: of two groups
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                const uint32_t row = vb_s + klane + (16 * kg + 8 * x) * kRow4Bytes;
-                vs[x] = lds64(row + kRow4Scales);
-                vc[x] = lds64(row + kRow4Centres);
+                const uint32_t wide = scales + row_k * 48 + (16 * kg + 8 * x) * 48;
+                if constexpr (RT == 4) {
+                    const float2 a = lds_f2(wide + 16 + 8 * odd_cols), b = lds_f2(wide + 32 + 8 * odd_cols);
+                    vs[x] = make_float4(a.x, a.y, 0.f, 0.f); vc[x] = make_float4(b.x, b.y, 0.f, 0.f);
+                } else {
+                    vs[x] = lds_f4(wide + 16); vc[x] = lds_f4(wide + 32);
+                }
             }
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
                 float e[4];
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    e[x] = ex2(w[ct][kg][x] - (m[ct][x & 1] == -INFINITY ? 0.f : m[ct][x & 1]));
+                    e[x] = ex2(w[ct][kg][x] - m[ct][x & 1]);
                     l[ct][x & 1] += e[x];
                 }
 #pragma unroll
-                for (int g = 0; g < 4; ++g)
+                for (int g = 0; g < GP; ++g)
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        const uint32_t s2 = g < 2 ? vs[x].x : vs[x].y, c2 = g < 2 ? vc[x].x : vc[x].y;
-                        const float c = g & 1 ? bf16_hi(c2) : bf16_lo(c2);
-                        const float s = g & 1 ? bf16_hi(s2) : bf16_lo(s2);
+                        const float c = RT == 4 ? (g ? vc[x].y : vc[x].x) : pick(vc[x], g), s = RT == 4 ? (g ? vs[x].y : vs[x].x) : pick(vs[x], g);
                         oc[ct][g][0] = fmaf(e[2 * x], c, oc[ct][g][0]);
                         oc[ct][g][1] = fmaf(e[2 * x + 1], c, oc[ct][g][1]);
                         pw[ct][g][x] = transpose8x8(cvt_f16x2(e[2 * x + 1] * s, e[2 * x] * s));
@@ -438,15 +450,15 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
                 const uint32_t xa8 = xa >> 8, xb8 = xb >> 8;
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
-                    mma_f16_16816(o[ct][g][0], kLess, kLess16, kLess, kLess16, pw[ct][g][0], pw[ct][g][1]);
-                    mma_f16_16816(o[ct][g][1], kLess, kLess16, kLess, kLess16, pw[ct][g][0], pw[ct][g][1]);
-                    mma_f16_16816(o[ct][g][0], xa & kLow, xa & kHigh, xb & kLow, xb & kHigh, pw[ct][g][0], pw[ct][g][1]);
-                    mma_f16_16816(o[ct][g][1], xa8 & kLow, xa8 & kHigh, xb8 & kLow, xb8 & kHigh, pw[ct][g][0], pw[ct][g][1]);
+                    mma_f16_16816(o[ct][g][0], less[0], less[1], less[0], less[1], pw[ct][g * GP / 4][0], pw[ct][g * GP / 4][1]);
+                    mma_f16_16816(o[ct][g][1], less[0], less[1], less[0], less[1], pw[ct][g * GP / 4][0], pw[ct][g * GP / 4][1]);
+                    mma_f16_16816(o[ct][g][0], xa & kLow, xa & kHigh, xb & kLow, xb & kHigh, pw[ct][g * GP / 4][0], pw[ct][g * GP / 4][1]);
+                    mma_f16_16816(o[ct][g][1], xa8 & kLow, xa8 & kHigh, xb8 & kLow, xb8 & kHigh, pw[ct][g * GP / 4][0], pw[ct][g * GP / 4][1]);
                 }
             }
         }
         __syncwarp();
-        uint8_t *used = dyn + (warp * ST + stage) * kA4StageBytes;
+        uint8_t *used = dyn + warp * kA4WarpBytes + stage * kA4StageBytes;
         stage ^= 1;
         if (++j.it < j.kb) continue;
 
@@ -461,7 +473,7 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
                 for (int d = 4; d < 32; d *= 2) {
                     l[ct][i] += __shfl_xor_sync(0xffffffffu, l[ct][i], d);
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) oc[ct][g][i] += __shfl_xor_sync(0xffffffffu, oc[ct][g][i], d);
+                    for (int g = 0; g < GP; ++g) oc[ct][g][i] += __shfl_xor_sync(0xffffffffu, oc[ct][g][i], d);
                 }
                 if (g8 == 0) stat[warp][8 * ct + 2 * t4 + i] = make_float2(m[ct][i], l[ct][i]);
             }
@@ -470,9 +482,10 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
 #pragma unroll
                 for (int y = 0; y < 2; ++y)
                     *reinterpret_cast<float4 *>(used + (2 * g + y) * 512 + lane * 16) =
-                        make_float4(fmaf(o[ct][g][y][0], 0x1p24f, oc[ct][g][0]), fmaf(o[ct][g][y][1], 0x1p24f, oc[ct][g][1]),
-                                    fmaf(o[ct][g][y][2], 0x1p20f, oc[ct][g][0]), fmaf(o[ct][g][y][3], 0x1p20f, oc[ct][g][1]));
+                        make_float4(fmaf(o[ct][g][y][0], 0x1p24f, oc[ct][g * GP / 4][0]), fmaf(o[ct][g][y][1], 0x1p24f, oc[ct][g * GP / 4][1]),
+                                    fmaf(o[ct][g][y][2], 0x1p20f, oc[ct][g * GP / 4][0]), fmaf(o[ct][g][y][3], 0x1p20f, oc[ct][g * GP / 4][1]));
             __syncthreads();
+            const int from = RT == 4 ? 4 * g8 + (t4 & 1) + 2 * (warp & 1) : lane;          // (RT = 4: where the group's columns are)
             // components 32 warp + 8 (g8 / 2) + g8 % 2 + 0, 2, 4, 6 of query rows 2 t4, 2 t4 + 1 (+ 8 ct)
             float mm[2], ll[2], by[kA4Warps][2], z[2][4];
 #pragma unroll
@@ -484,7 +497,7 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
 #pragma unroll
                 for (int w2 = 0; w2 < kA4Warps; ++w2) {
                     const float2 ml = stat[w2][8 * ct + 2 * t4 + i];
-                    by[w2][i] = ml.x == -INFINITY ? 0.f : ex2(ml.x - mm[i]);
+                    by[w2][i] = ex2(ml.x - mm[i]);
                     ll[i] += ml.y * by[w2][i];
                 }
             }
@@ -492,7 +505,7 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
             for (int y = 0; y < 2; ++y)
 #pragma unroll
                 for (int w2 = 0; w2 < kA4Warps; ++w2) {
-                    const float4 x = *reinterpret_cast<const float4 *>(used + (w2 - warp) * (ST * kA4StageBytes) + (2 * warp + y) * 512 + lane * 16);
+                    const float4 x = *reinterpret_cast<const float4 *>(used + (w2 - warp) * kA4WarpBytes + (2 * warp + y) * 512 + from * 16);
                     z[0][2 * y] += x.x * by[w2][0]; z[1][2 * y] += x.y * by[w2][1];
                     z[0][2 * y + 1] += x.z * by[w2][0]; z[1][2 * y + 1] += x.w * by[w2][1];
                 }
@@ -506,7 +519,7 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
                 const int r = 8 * ct + 2 * t4 + i, d = 32 * warp + 8 * (g8 >> 1) + 4 * (g8 & 1);
                 if (r >= p.G) continue;
                 const int hq = j.h * p.G + r;
-                float *to = CL ? part[CL ? r : 0] : p.slots + (((int64_t)blockIdx.x * 2 + (j.begins ? 1 : 0)) * RT + r) * kAttRowPitch;
+                float *to = CL ? part[CL ? r : 0] : p.slots + (((int64_t)blockIdx.x * 2 + (j.begins ? 1 : 0)) * COLS + r) * kAttRowPitch;
                 if (final) *reinterpret_cast<uint2 *>(p.out + ((int64_t)j.seq * p.out_seq + (int64_t)hq * p.out_head) * 2 + 2 * d) = make_uint2(cvt_bf16x2(y1, y0), cvt_bf16x2(y3, y2));
                 else *reinterpret_cast<float4 *>(to + d) = make_float4(y0, y1, y2, y3);
                 if (warp == 0 && g8 == 0) {
