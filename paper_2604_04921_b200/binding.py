@@ -106,6 +106,9 @@ class _AttendIo(ctypes.Structure):
                 ("lse", ctypes.c_void_p), ("scale", ctypes.c_float)]
 
 
+# A view in one packing step (setting its 17 fields one by one takes 5 us).
+_pack_view = struct.Struct("@PPiiqqqqPiiiqqPPi0q").pack
+
 # The same structures in one packing step: these calls are made per layer and token, where every microsecond of the
 # host counts (setting 20 fields one by one takes 2 us, packing them 0.5 us).
 _pack_append = struct.Struct("@PPPiiqqqqqqqqqPqqqPP").pack
@@ -242,41 +245,37 @@ class CacheView:
     pre_rope: bool = False                        # bf16 keys are pre-RoPE vectors (k_kind 2); fp32 keys always are
 
     def c_view(self) -> _CacheView:
-        k = self.k
-        row4 = k.dtype == torch.uint8                        # 4-bit keys and values: rows of bytes (k_kind 5)
-        assert k.dim() == 5 and k.shape[-1] == (ROW4_BYTES if row4 else 128) and k.stride(-1) == 1
-        fp8 = k.dtype == torch.float8_e4m3fn                 # e4m3 keys come with e4m3 values (k_kind 3)
-        if self.v is not None:
-            assert self.v.shape == k.shape and self.v.stride() == k.stride()
-            assert self.v.dtype == (k.dtype if fp8 or row4 else torch.bfloat16)
-        assert k.dtype in (torch.bfloat16, torch.float32, torch.float8_e4m3fn, torch.uint8)
+        k, v, dt = self.k, self.v, self.k.dtype
+        row4, fp8 = dt is torch.uint8, dt is torch.float8_e4m3fn     # 4-bit rows of bytes (k_kind 5); e4m3 (k_kind 3): keys and values alike
+        shape, strides = k.shape, k.stride()
+        assert k.dim() == 5
+        _, d1, _, d3, width = shape
+        sl, s1, sh, s3, one = strides
+        assert width == (ROW4_BYTES if row4 else 128) and one == 1
+        if v is not None:
+            assert v.shape == shape and v.stride() == strides and v.dtype is (dt if fp8 or row4 else torch.bfloat16)
+        assert row4 or fp8 or dt is torch.bfloat16 or dt is torch.float32
         assert not (row4 and self.pre_rope), "4-bit keys are cached post-RoPE"
-        cv = _CacheView()
-        cv.k = k.data_ptr()
-        cv.v = self.v.data_ptr() if self.v is not None else None
-        cv.k_kind = 5 if row4 else 3 if fp8 else ((2 if self.pre_rope else 0) if k.dtype == torch.bfloat16 else 1)
+        kind = 5 if row4 else 3 if fp8 else ((2 if self.pre_rope else 0) if dt is torch.bfloat16 else 1)
+        ss = st = sp = sslot = pages = per = size = n_pages = sl_addr = pos_addr = 0
         if self.page_table is None:
-            cv.paged = 0
-            cv.stride_layer, cv.stride_seq, cv.stride_head, cv.stride_tok = k.stride()[:4]
-            cv.n_max = k.shape[3] if self.n_max is None else self.n_max
+            ss, st, n_max = s1, s3, d3
         else:
             pt = self.page_table
-            assert pt.dtype == torch.int32 and pt.is_contiguous()
-            cv.paged = 1
-            cv.stride_layer, cv.stride_page, cv.stride_head, cv.stride_slot = k.stride()[:4]
-            cv.page_table = pt.data_ptr()
-            cv.max_pages_per_seq = pt.shape[1]
-            cv.page_size = k.shape[3]
-            cv.n_pages = k.shape[1]
-            cv.n_max = pt.shape[1] * k.shape[3] if self.n_max is None else self.n_max
+            assert pt.dtype is torch.int32 and pt.is_contiguous()
+            sp, sslot, pages, per, size, n_pages = s1, s3, pt.data_ptr(), pt.shape[1], d3, d1
+            n_max = per * size
+        if self.n_max is not None:
+            n_max = self.n_max
         if self.seq_lens is not None:
             assert self.seq_lens.dtype == torch.int32 and self.seq_lens.is_contiguous()
-            cv.seq_lens = self.seq_lens.data_ptr()
+            sl_addr = self.seq_lens.data_ptr()
         if self.positions is not None:
             assert self.positions.dtype == torch.int32 and self.positions.is_contiguous()
-            assert self.positions.shape[-1] == cv.n_max
-            cv.positions = self.positions.data_ptr()
-        return cv
+            assert self.positions.shape[-1] == n_max
+            pos_addr = self.positions.data_ptr()
+        return _CacheView.from_buffer_copy(_pack_view(k.data_ptr(), _addr(v) or 0, kind, int(self.page_table is not None), sl, ss, sh, st, pages, per,
+                                                      size, n_pages, sp, sslot, sl_addr, pos_addr, n_max))
 
 
 class LayerCache:
@@ -415,8 +414,8 @@ class TriContext:
         cs, cd = src.c_view(), dst.c_view()
         assert kept_idx.dtype == torch.int32 and kept_idx.numel() == self.units(S) * budget
         assert kept_cnt.dtype == torch.int32 and kept_cnt.numel() == self.units(S)
-        _check(lib().tri_compact(self._h, ctypes.byref(cs), _ptr(kept_idx), _ptr(kept_cnt), S, budget,
-                                 ctypes.byref(cd), _ptr(new_seq_lens), _stream()), "tri_compact")
+        _check(lib().tri_compact(self._h, ctypes.byref(cs), kept_idx.data_ptr(), kept_cnt.data_ptr(), S, budget,
+                                 ctypes.byref(cd), _addr(new_seq_lens), _stream_on(torch.cuda.current_device())), "tri_compact")
 
     def compress(self, src: CacheView, cur_pos: torch.Tensor, budget: int, dst: CacheView, ws: torch.Tensor,
                  kept_idx: Optional[torch.Tensor] = None, kept_cnt: Optional[torch.Tensor] = None,

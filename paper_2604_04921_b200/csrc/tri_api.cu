@@ -679,6 +679,18 @@ bool two_pass_compaction(const tri_cache_view *src, const tri_cache_view *dst)
     return aliases(src, dst) && src->k_kind != 1 && src->v && dst->v;
 }
 
+template <int PIECES>
+void launch_compact(bool in_place, int U, int32_t budget, cudaStream_t st, const CompactParams &p)
+{
+    const dim3 grid(U, (budget + RowShape<PIECES>::kRowsPerBlock - 1) / RowShape<PIECES>::kRowsPerBlock);
+    if (in_place) {
+        k_compact_inplace_rows<PIECES><<<U, kInplaceThreads, 0, st>>>(p);
+        if (!p.whole) k_gather_rows<true, PIECES><<<grid, kGatherThreads, 0, st>>>(p);
+    } else {
+        k_gather_rows<false, PIECES><<<grid, kGatherThreads, 0, st>>>(p);
+    }
+}
+
 tri_status run_compact(tri_ctx *c, const tri_cache_view *src, const int32_t *kept_idx, const int32_t *kept_cnt,
                        int32_t S, int32_t budget, const tri_cache_view *dst, int32_t *new_seq_lens,
                        int32_t *device_status, Units un, cudaStream_t st)
@@ -692,28 +704,24 @@ tri_status run_compact(tri_ctx *c, const tri_cache_view *src, const int32_t *kep
     p.k_vec = row_elements(src->k_kind) * p.k_esize / 16;
     p.v_vec = (src->v && dst->v) ? row_elements(src->k_kind) * p.v_esize / 16 : 0;
     p.device_status = device_status;
+    p.whole = 0;
     const bool rows16 = (src->k_kind == 0 || src->k_kind == 2) && p.v_vec != 0;     // bf16 K and V: the row-gather kernel applies
     const int U = un.count;
-    dim3 grid(U, (budget + kFastRowsPerBlock - 1) / kFastRowsPerBlock);
     const int pr = prof_open(c, 4, st);
-    if (aliases(src, dst)) {
-        // in place: the prefix whose sources lie inside the destination range goes tile by tile in one block
-        // per unit; everything behind it is a hazard-free gather
-        if (rows16) {
-            k_compact_inplace_rows<2><<<U, kInplaceThreads, 0, st>>>(p);
-            k_gather_rows<true><<<grid, kGatherThreads, 0, st>>>(p);
-        } else if (src->k_kind == 3 && p.v_vec != 0) {
-            dim3 grid8(U, (budget + 2 * kFastRowsPerBlock - 1) / (2 * kFastRowsPerBlock));
-            k_compact_inplace_rows<1><<<U, kInplaceThreads, 0, st>>>(p);
-            k_gather_rows<true, 1><<<grid8, kGatherThreads, 0, st>>>(p);
-        } else {
-            k_compact_inplace_any<<<U, kInplaceThreads, 0, st>>>(p);
-        }
-    } else if (rows16) {
-        k_gather_rows<false><<<grid, kGatherThreads, 0, st>>>(p);
+    // in place: the prefix whose sources lie inside the destination range goes tile by tile in one block
+    // per unit; everything behind it is a hazard-free gather
+    const bool in_place = aliases(src, dst);
+    if (rows16) {
+        launch_compact<16>(in_place, U, budget, st, p);
     } else if (src->k_kind == 3 && p.v_vec != 0) {
-        dim3 grid8(U, (budget + 2 * kFastRowsPerBlock - 1) / (2 * kFastRowsPerBlock));      // 128-byte rows: two slots per warp step
-        k_gather_rows<false, 1><<<grid8, kGatherThreads, 0, st>>>(p);
+        launch_compact<8>(in_place, U, budget, st, p);
+    } else if (src->k_kind == 5 && p.v_vec != 0) {
+        // units enough for two blocks on each multiprocessor: the first pass in place goes on to the end (512 units, 2,048 of up to
+        // 2,176 rows: @@ us against @@)
+        p.whole = in_place && U >= 2 * c->n_sm;
+        launch_compact<5>(in_place, U, budget, st, p);
+    } else if (in_place) {
+        k_compact_inplace_any<<<U, kInplaceThreads, 0, st>>>(p);
     } else {
         dim3 grid_any(U, (budget + kGatherRowsPerBlock - 1) / kGatherRowsPerBlock);
         k_gather_any<<<grid_any, kGatherThreads, 0, st>>>(p);

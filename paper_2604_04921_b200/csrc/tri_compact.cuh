@@ -17,8 +17,9 @@ struct CompactParams {
     int32_t *new_seq_lens;     // [S] or NULL
     int32_t S, H, budget;
     int32_t u0;                // first unit of this launch
-    int32_t k_vec;             // 16-byte vectors per K row (16 for bf16, 32 for fp32, 8 for fp8)
-    int32_t v_vec;             // 16-byte vectors per V row (16, 8 for fp8, or 0 without a value cache)
+    int32_t k_vec;             // 16-byte vectors per K row (16 for bf16, 32 for fp32, 8 for fp8, 5 for 4 bits)
+    int32_t v_vec;             // 16-byte vectors per V row (16, 8 for fp8, 5 for 4 bits, or 0 without a value cache)
+    int32_t whole;             // in place: the first pass moves all rows, there is no second
     int32_t k_esize;           // bytes per K element
     int32_t v_esize;           // bytes per V element
     int32_t *device_status;
@@ -66,21 +67,29 @@ constexpr int kFastIters = 2;
 constexpr int kFastRowsPerBlock = kGatherWarps * kFastRows * kFastIters;
 constexpr int kInplaceRows = 128;       // rows per tile of the in-place schedule
 
-// ESZ = bytes per element: 2 = bf16 rows as described; 1 = e4m3 rows of 128 bytes, 8 lanes per row, so a half-warp
-// carries the K and V row of one slot and a warp two slots at a time (16 rows in flight per warp).
-template <bool AFTER_PREFIX, int ESZ = 2>
+// PIECES = 16-byte pieces per row: 16 = bf16 rows as described; 8 = e4m3 rows of 128 bytes, 8 lanes per row, so a half-warp
+// carries the K and V row of one slot and a warp two slots at a time (16 rows in flight per warp); 5 = 4-bit rows of 80
+// bytes, 10 lanes per slot, three slots at a time (lanes 30 and 31 move nothing).
+template <int PIECES> struct RowShape {
+    static constexpr int kElement = PIECES == 16 ? 2 : 1;                 // bytes per element of the view's strides
+    static constexpr int kSlots = 16 / PIECES;                            // slots a warp moves per step: 1, 2 or 3
+    static constexpr bool kIdle = 32 % (2 * PIECES) != 0;                 // lanes that move nothing
+    static constexpr int kGroup = kFastRows * kSlots;                     // rows in flight per warp
+    static constexpr int kRowsPerBlock = kFastRowsPerBlock * kSlots;      // of the gather
+    static constexpr int kTile = kInplaceRows * kSlots;                   // rows per tile of the in-place schedule
+};
+
+template <bool AFTER_PREFIX, int PIECES = 16>
 __global__ void __launch_bounds__(kGatherThreads, 4) k_gather_rows(const CompactParams p)
 {
-    constexpr int kPieces = 8 * ESZ;                 // 16-byte pieces per row
-    constexpr int kSlots = 16 / kPieces;             // slots a warp moves per step: 1 or 2
-    constexpr int kGroup = kFastRows * kSlots;       // rows in flight per warp
+    constexpr int kPieces = PIECES, ESZ = RowShape<PIECES>::kElement, kSlots = RowShape<PIECES>::kSlots, kGroup = RowShape<PIECES>::kGroup;
     const int u = p.u0 + blockIdx.x;
     const int h = u % p.H, s = (u / p.H) % p.S, l = u / (p.H * p.S);
     const int cnt = min(__ldg(p.kept_cnt + u), p.budget);
     if (!AFTER_PREFIX && blockIdx.y == 0 && threadIdx.x == 0 && p.new_seq_lens && h == 0 && l == 0)
         p.new_seq_lens[s] = cnt;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int jw = blockIdx.y * (kFastRowsPerBlock * kSlots) + warp * (kGroup * kFastIters);
+    const int jw = blockIdx.y * RowShape<PIECES>::kRowsPerBlock + warp * (kGroup * kFastIters);
     if (jw >= cnt) return;
     const int32_t *idx = p.kept_idx + (int64_t)u * p.budget;
     const bool is_v = (lane / kPieces) & 1;
@@ -93,7 +102,7 @@ __global__ void __launch_bounds__(kGatherThreads, 4) k_gather_rows(const Compact
     for (int it = 0; it < kFastIters; ++it) {
         const int j0 = jw + it * kGroup;
         if (j0 >= cnt) break;
-        if (AFTER_PREFIX && __ldg(idx + (j0 & ~(kInplaceRows * kSlots - 1))) < cnt) continue;   // the first phase moved this tile
+        if (AFTER_PREFIX && __ldg(idx + j0 / RowShape<PIECES>::kTile * RowShape<PIECES>::kTile) < cnt) continue;   // the first phase moved this tile
         // lane r resolves row j0 + r; rows past the count, indices outside the unit and bad page ids are skipped
         int mine = -1;
         int64_t so = -1, dof = -1;
@@ -111,12 +120,14 @@ __global__ void __launch_bounds__(kGatherThreads, 4) k_gather_rows(const Compact
         uint4 val[kFastRows];
 #pragma unroll
         for (int r = 0; r < kFastRows; ++r) {
-            const int64_t o = __shfl_sync(0xffffffffu, so, r * kSlots + sub);
+            int64_t o = __shfl_sync(0xffffffffu, so, r * kSlots + sub);
+            if constexpr (RowShape<PIECES>::kIdle) if (sub >= kSlots) o = -1;
             if (o >= 0) val[r] = AFTER_PREFIX ? ld_stream(sb + o * ESZ) : ld_once(sb + o * ESZ);   // in place: no read-only path
         }
 #pragma unroll
         for (int r = 0; r < kFastRows; ++r) {
-            const int64_t o = __shfl_sync(0xffffffffu, dof, r * kSlots + sub);
+            int64_t o = __shfl_sync(0xffffffffu, dof, r * kSlots + sub);
+            if constexpr (RowShape<PIECES>::kIdle) if (sub >= kSlots) o = -1;
             if (o >= 0) st_once(db + o * ESZ, val[r]);
         }
         if (p.dst.positions && mine >= 0)
@@ -200,11 +211,11 @@ __global__ void __launch_bounds__(kGatherThreads) k_gather_any(const CompactPara
 constexpr int kInplaceThreads = 512;
 static_assert(kInplaceRows == (kInplaceThreads / 32) * kFastRows, "a tile is 8 rows per warp");
 
-// ESZ as in k_gather_rows: with 128-byte rows a warp holds 16 rows and a tile is 256 rows.
-template <int ESZ = 2>
+// PIECES as in k_gather_rows: with 128-byte rows a warp holds 16 rows and a tile is 256 rows, with 80-byte rows 24 and 384.
+template <int PIECES = 16>
 __global__ void __launch_bounds__(kInplaceThreads, 2) k_compact_inplace_rows(const CompactParams p)
 {
-    constexpr int kPieces = 8 * ESZ, kSlots = 16 / kPieces, kGroup = kFastRows * kSlots;
+    constexpr int kPieces = PIECES, ESZ = RowShape<PIECES>::kElement, kSlots = RowShape<PIECES>::kSlots, kGroup = RowShape<PIECES>::kGroup;
     const int u = p.u0 + blockIdx.x;
     const int h = u % p.H, s = (u / p.H) % p.S, l = u / (p.H * p.S);
     const int cnt = min(__ldg(p.kept_cnt + u), p.budget);
@@ -217,8 +228,8 @@ __global__ void __launch_bounds__(kInplaceThreads, 2) k_compact_inplace_rows(con
     char *db = (is_v ? p.dst.v : p.dst.k) + (lane % kPieces) * 16;
     const int n_src = p.src.n_max;
 
-    for (int t0 = 0; t0 < cnt; t0 += kInplaceRows * kSlots) {
-        if (__ldg(idx + t0) >= cnt) break;                   // the parallel pass takes over from here
+    for (int t0 = 0; t0 < cnt; t0 += RowShape<PIECES>::kTile) {
+        if (!p.whole && __ldg(idx + t0) >= cnt) break;       // the parallel pass takes over from here
         const int j0 = t0 + warp * kGroup;
         int mine = -1, pos = 0;
         int64_t so = -1, dof = -1;
@@ -242,13 +253,15 @@ __global__ void __launch_bounds__(kInplaceThreads, 2) k_compact_inplace_rows(con
         uint4 val[kFastRows];
 #pragma unroll
         for (int r = 0; r < kFastRows; ++r) {
-            const int64_t o = __shfl_sync(0xffffffffu, so, r * kSlots + sub);
+            int64_t o = __shfl_sync(0xffffffffu, so, r * kSlots + sub);
+            if constexpr (RowShape<PIECES>::kIdle) if (sub >= kSlots) o = -1;
             if (o >= 0) val[r] = ld_stream(sb + o * ESZ);
         }
         __syncthreads();                                     // every source of the tile has been read
 #pragma unroll
         for (int r = 0; r < kFastRows; ++r) {
-            const int64_t o = __shfl_sync(0xffffffffu, dof, r * kSlots + sub);
+            int64_t o = __shfl_sync(0xffffffffu, dof, r * kSlots + sub);
+            if constexpr (RowShape<PIECES>::kIdle) if (sub >= kSlots) o = -1;
             if (o >= 0) *reinterpret_cast<uint4 *>(db + o * ESZ) = val[r];
         }
         if (p.dst.positions && mine >= 0) p.dst.positions[(int64_t)u * p.dst.n_max + j0 + lane] = pos;
