@@ -11,6 +11,7 @@
 #include <nvtx3/nvToolsExt.h>
 
 #include "tri_append.cuh"
+#include "tri_append4.cuh"
 #include "tri_attend.cuh"
 #include "tri_attend4.cuh"
 #include "tri_attend_umma.cuh"
@@ -481,7 +482,9 @@ cudaError_t prepare_device()
     if ((e = allow_attend_smem<true, 8>()) != cudaSuccess) return e;
     if ((e = allow_attend_smem<true, 16>()) != cudaSuccess) return e;
     if ((e = allow_attend4_smem<4>()) != cudaSuccess || (e = allow_attend4_smem<8>()) != cudaSuccess || (e = allow_attend4_smem<16>()) != cudaSuccess) return e;
-    if ((e = load_append<0, 5>()) != cudaSuccess || (e = load_append<1, 5>()) != cudaSuccess) return e;
+    if ((e = load_kernels(k_append4<0, false, 1>, k_append4<0, false, kAppendTokens>, k_append4<0, true, 1>, k_append4<0, true, kAppendTokens>,
+                          k_append4<1, false, 1>, k_append4<1, false, kAppendTokens>, k_append4<1, true, 1>, k_append4<1, true, kAppendTokens>)) !=
+        cudaSuccess) return e;
     if ((e = load_kernels(k_read<0, 2>, k_read<1, 2>, k_read<2, 2>, k_read<3, 2>, k_read<5, 2>, k_read<0, 4>, k_read<1, 4>, k_read<2, 4>,
                           k_read<3, 4>, k_read<5, 4>)) != cudaSuccess) return e;
     if ((e = load_append<0, 0>()) != cudaSuccess || (e = load_append<0, 1>()) != cudaSuccess) return e;
@@ -1244,13 +1247,20 @@ cudaError_t launch_append(bool split, unsigned blocks, int tt, cudaStream_t st, 
     return split ? launch_append<KIND, KK, true>(blocks, tt, st, p) : launch_append<KIND, KK, false>(blocks, tt, st, p);
 }
 
+template <int KIND, bool SPLIT>
+cudaError_t launch_append4(unsigned blocks, int tt, cudaStream_t st, const AppendParams &p)
+{
+    return tt == 1 ? launch_under(k_append4<KIND, SPLIT, 1>, blocks, kAppendThreads, 0, st, p)
+                   : launch_under(k_append4<KIND, SPLIT, kAppendTokens>, blocks, kAppendThreads, 0, st, p);
+}
+
 template <int KIND>
 cudaError_t launch_append(int kk, bool split, unsigned blocks, int tt, cudaStream_t st, const AppendParams &p)
 {
     if (kk == 0) return launch_append<KIND, 0>(split, blocks, tt, st, p);
     if (kk == 1) return launch_append<KIND, 1>(split, blocks, tt, st, p);
     if (kk == 2) return launch_append<KIND, 2>(split, blocks, tt, st, p);
-    if (kk == 5) return launch_append<KIND, 5>(split, blocks, tt, st, p);
+    if (kk == 5) return split ? launch_append4<KIND, true>(blocks, tt, st, p) : launch_append4<KIND, false>(blocks, tt, st, p);
     return launch_append<KIND, 3>(split, blocks, tt, st, p);
 }
 

@@ -12,7 +12,6 @@
 // its rows (H keys, H values, H * G queries), so that the sines and cosines of a token are formed once, by one thread per
 // band, and used from registers for every head.
 #pragma once
-#include "tri_row4.cuh"
 #include "tri_score_tma.cuh"
 #include "tri_step.cuh"
 
@@ -110,36 +109,6 @@ __device__ __forceinline__ void store16(char *row, int c, const float (&x)[16])
     }
 }
 
-// The same to a 4-bit row (tri_row4.cuh).  The lane has half of group c / 2 (SPLIT: quarters of groups c / 4 and c / 4 + 2), and the
-// lanes of a group, all of them in `lanes`, find its range together.
-template <bool SPLIT>
-__device__ __forceinline__ void store_row4(char *row, int c, const float (&x)[16], uint32_t lanes)
-{
-    constexpr int NG = SPLIT ? 2 : 1, EL = 16 / NG;
-    float s[NG], m[NG];
-#pragma unroll
-    for (int j = 0; j < NG; ++j) {
-        float lo = x[EL * j], hi = lo;
-#pragma unroll
-        for (int i = 1; i < EL; ++i) { lo = min_nan(lo, x[EL * j + i]); hi = max_nan(hi, x[EL * j + i]); }
-#pragma unroll
-        for (int d = 1; d < 32 / EL; d *= 2) {
-            lo = min_nan(lo, __shfl_xor_sync(lanes, lo, d));
-            hi = max_nan(hi, __shfl_xor_sync(lanes, hi, d));
-        }
-        row4_group(lo, hi, s[j], m[j]);
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {                            // a word each: group g, unit t
-        const int g = SPLIT ? (c >> 2) + 2 * i : c >> 1, t = SPLIT ? c & 3 : 2 * (c & 1) + i;
-        *reinterpret_cast<uint32_t *>(row + 16 * t + 4 * g) = row4_word(x + 8 * i, s[SPLIT ? i : 0], m[SPLIT ? i : 0]);
-        if (t == 0) {
-            *reinterpret_cast<uint16_t *>(row + kRow4Scales + 2 * g) = (uint16_t)(__float_as_uint(s[SPLIT ? i : 0]) >> 16);
-            *reinterpret_cast<uint16_t *>(row + kRow4Centres + 2 * g) = (uint16_t)(__float_as_uint(m[SPLIT ? i : 0]) >> 16);
-        }
-    }
-}
-
 // Bands 8c .. 8c+7 of the 16 components: pair j is (x[2j], x[2j+1]) interleaved, (x[j], x[j+8]) half-split.
 template <bool SPLIT>
 __device__ __forceinline__ void rotate16(float (&x)[16], const float2 (&cs)[8])
@@ -157,8 +126,8 @@ __device__ __forceinline__ void rotate16(float (&x)[16], const float2 (&cs)[8])
 template <int KIND, int KK, bool SPLIT, int TT>
 __global__ void __launch_bounds__(kAppendThreads) k_append(const AppendParams p)
 {
-    constexpr int kES = KK == 1 ? 4 : (KK == 3 || KK == 5 ? 1 : 2), vES = KK == 3 || KK == 5 ? 1 : 2;
-    constexpr bool kRotateKeys = KK == 0 || KK == 3 || KK == 5;
+    constexpr int kES = KK == 1 ? 4 : (KK == 3 ? 1 : 2), vES = KK == 3 ? 1 : 2;
+    constexpr bool kRotateKeys = KK == 0 || KK == 3;
     constexpr int kGroups = kAppendThreads / 8 / TT;          // row groups (of 8 lanes) per token
     __shared__ float2 cs_s[TT][kBands];
 
@@ -246,8 +215,7 @@ __global__ void __launch_bounds__(kAppendThreads) k_append(const AppendParams p)
                             for (int i = 0; i < 16; ++i) x[i] = __fdiv_rn(x[i], scale);
                         }
                     }
-                    if (KK == 5) store_row4<SPLIT>((is_k ? p.dst.k : p.dst.v) + off, c, x, 0xffu << (tid & 24));
-                    else if (is_k) store16<kES, SPLIT>(p.dst.k + off * kES, c, x);
+                    if (is_k) store16<kES, SPLIT>(p.dst.k + off * kES, c, x);
                     else store16<vES, SPLIT>(p.dst.v + off * vES, c, x);
                     if (is_k && c == 0 && p.dst.positions)
                         p.dst.positions[(((int64_t)p.layer * p.S + s) * p.H + h) * p.dst.n_max + slot] = (int32_t)at;

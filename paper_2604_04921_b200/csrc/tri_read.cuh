@@ -11,7 +11,7 @@
 
 namespace tri {
 
-constexpr int kReadThreads = 256, kReadRows = 4, kReadTile = kReadThreads / 8 * kReadRows;
+constexpr int kReadThreads = 256, kReadRows = 2, kReadTile = kReadThreads / 8 * kReadRows;
 
 struct ReadParams {
     View src;
@@ -81,6 +81,21 @@ __device__ __forceinline__ void read_store(char *row, int c, const float (&x)[16
     }
 }
 
+// A loaded row to elements of OS bytes.
+template <int F, int OS>
+__device__ __forceinline__ void read_put(char *row, int c, const ReadRaw<F> &raw, float scale)
+{
+    if constexpr (F == 5 && OS == 2) {
+        char *to = row + (64 * (c & 1) + 8 * (c >> 1)) * 2;
+        *reinterpret_cast<uint4 *>(to) = row4_bf16(raw.codes.x, __byte_perm(raw.s, 0, 0x1010), __byte_perm(raw.c, 0, 0x1010));
+        *reinterpret_cast<uint4 *>(to + 64) = row4_bf16(raw.codes.y, __byte_perm(raw.s, 0, 0x3232), __byte_perm(raw.c, 0, 0x3232));
+    } else {
+        float x[16];
+        read_widen<F>(raw, scale, x);
+        read_store<F, OS>(row, c, x);
+    }
+}
+
 // KK: the cache's k_kind.  OS: bytes per element of the outputs.
 template <int KK, int OS>
 __global__ void __launch_bounds__(kReadThreads) k_read(const ReadParams p)
@@ -116,15 +131,8 @@ __global__ void __launch_bounds__(kReadThreads) k_read(const ReadParams p)
     for (int u = 0; u < U; ++u) {
         if (off[u] == -1) continue;
         const int i = grp + u * (kReadThreads / 8), t = t_block + (i & ((1 << p.tok_shift) - 1)), h = h_block + (i >> p.tok_shift);
-        float x[16];
-        if (p.k) {
-            read_widen<KK>(rk[u], p.k_scale ? p.k_scale[h] : 1.f, x);
-            read_store<KK, OS>(p.k + (s * p.ks_seq + t * p.ks_tok + h * p.ks_head) * OS, c, x);
-        }
-        if (p.v) {
-            read_widen<VK>(rv[u], p.v_scale ? p.v_scale[h] : 1.f, x);
-            read_store<VK, OS>(p.v + (s * p.vs_seq + t * p.vs_tok + h * p.vs_head) * OS, c, x);
-        }
+        if (p.k) read_put<KK, OS>(p.k + (s * p.ks_seq + t * p.ks_tok + h * p.ks_head) * OS, c, rk[u], p.k_scale ? p.k_scale[h] : 1.f);
+        if (p.v) read_put<VK, OS>(p.v + (s * p.vs_seq + t * p.vs_tok + h * p.vs_head) * OS, c, rv[u], p.v_scale ? p.v_scale[h] : 1.f);
     }
 }
 

@@ -18,6 +18,18 @@ __device__ __forceinline__ float min_nan(float a, float b)
     asm("min.NaN.f32 %0, %1, %2;\n" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
+__device__ __forceinline__ float min_nan(float a, float b, float c)
+{
+    float r;
+    asm("min.NaN.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b, float c)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 __device__ __forceinline__ float max_nan(float a, float b)
 {
     float r;
@@ -27,26 +39,58 @@ __device__ __forceinline__ float max_nan(float a, float b)
 
 // Scale and centre of a group from its smallest and largest value.  (8 hi + 7 lo) / 15 as (hi / 2 + 7 lo / 16) / (15 / 16), which
 // cannot overflow; with bf16 inputs every step up to the division is exact or rounded once, so that c is the correctly rounded
-// one.  A NaN or an infinity among the values makes c not finite.
-__device__ __forceinline__ void row4_group(float lo, float hi, float &s, float &c)
+// one.  A NaN or an infinity among the values makes c not finite.  Returns whether c or s lies so near the border of two bf16 numbers
+// that lo and hi, if they are off by a few steps of fp32, may have put it on the wrong side.
+__device__ __forceinline__ bool row4_group(float lo, float hi, float &s, float &c)
 {
-    c = bf16_lo(cvt_bf16x2(0.f, __fdiv_rn(fmaf(hi, 0.5f, lo * 0.4375f), 0.9375f)));
+    const float c32 = __fdiv_rn(fmaf(hi, 0.5f, lo * 0.4375f), 0.9375f);
+    c = bf16_lo(cvt_bf16x2(0.f, c32));
     const float need = fmaxf(__fdiv_rn(hi - c, 7.f), (c - lo) * 0.125f);
     // rounded up to bf16; the smallest normal number, where that is more
     const uint32_t up = max((__float_as_uint(need) + 0xffffu) & 0xffff0000u, 0x00800000u);
     s = need > 0.f ? __uint_as_float(up) : 0.f;
     if (!(fabsf(c) < INFINITY)) { c = __uint_as_float(0x7fc00000u); s = 0.f; }
+    return ((__float_as_uint(c32) + 0x8010u) & 0xffffu) <= 0x20u || (need > 0.f && ((__float_as_uint(need) + 0x10u) & 0xffffu) <= 0x20u);
 }
 
-// The codes of 8 neighbouring components as a word.  Adding 1.5 * 2^23 + 8 rounds to the nearest integer (ties to even) and leaves
-// the code in the low bits of the sum; the sum of the shifted words carries a constant that is taken off at the end.
-__device__ __forceinline__ uint32_t row4_word(const float *x, float s, float c)
+// The codes of 8 neighbouring components as a word, inv = 1 / s.  Adding 1.5 * 2^23 + 8 rounds a quotient to the nearest integer (ties
+// to even) and leaves the code in the low bits of the sum; the sum of the shifted words carries a constant that is taken off at the
+// end.  TIES: the quotient is an approximate one, corrected by its exact remainder (Markstein's division): where (x - c) / s lies
+// halfway between two codes, which is common with bf16 values, it is exact.  Otherwise it may be off by 2^-20, and `off` receives the
+// largest distance of a quotient from its code.
+template <bool TIES>
+__device__ __forceinline__ uint32_t row4_word(const float *x, float s, float inv, float c, float &off)
 {
-    const float by = s > 0.f ? s : 1.f;
+    constexpr float kMagic = 12582912.f + 8.f;
     uint32_t w = 0;
 #pragma unroll
-    for (int d = 0; d < 8; ++d) w += __float_as_uint(__fdiv_rn(x[d] - c, by) + (12582912.f + 8.f)) << 4 * ((d >> 1) + 4 * (d & 1));
+    for (int d = 0; d < 8; ++d) {
+        const float v = x[d] - c;
+        float t;
+        if (TIES) {
+            const float q = v * inv;
+            t = fmaf(fmaf(-q, s, v), inv, q) + kMagic;
+        } else {
+            t = fmaf(v, inv, kMagic);
+            off = fmaxf(off, fabsf(fmaf(v, inv, -(t - kMagic))));
+        }
+        w += __float_as_uint(t) << 4 * ((d >> 1) + 4 * (d & 1));
+    }
     return w - 0x4b400000u * 0x11111111u;                    // (1.5 * 2^23 has the bits 0x4b400000)
+}
+
+// The 8 components a word stands for in bf16, rounded once: a nibble or-ed under 0x4300 is the bf16 value 128 + code, which less 136
+// is exact, and the multiply-add rounds (code - 8) s + c.  s and c are pairs of the same value.
+__device__ __forceinline__ uint4 row4_bf16(uint32_t w, uint32_t s, uint32_t c)
+{
+    uint32_t r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t n = ((w >> 4 * i) & 0x000f000fu) | 0x43004300u;
+        asm("sub.rn.bf16x2 %0, %0, %1;\n" : "+r"(n) : "r"(0x43084308u));
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;\n" : "=r"(r[i]) : "r"(n), "r"(s), "r"(c));
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
 // The 8 components a word stands for.

@@ -83,7 +83,7 @@ def test_rows_hold_what_was_put_there():
 
 def test_kernels_read_nothing_through_the_read_only_path():
     """They begin while their predecessor still runs; a read-only load may be moved before the wait for it."""
-    for name in ("tri_row4.cuh", "tri_read.cuh", "tri_attend4.cuh"):
+    for name in ("tri_row4.cuh", "tri_append4.cuh", "tri_read.cuh", "tri_attend4.cuh"):
         with open(os.path.join(ROOT, "paper_2604_04921_b200", "csrc", name)) as f:
             code = [line.split("//")[0] for line in f]
         assert not [line for line in code if "__ldg" in line or ".nc." in line or " row_offset(" in line], name
