@@ -482,8 +482,8 @@ cudaError_t prepare_device()
     if ((e = allow_attend_smem<true, 8>()) != cudaSuccess) return e;
     if ((e = allow_attend_smem<true, 16>()) != cudaSuccess) return e;
     if ((e = allow_attend4_smem<4>()) != cudaSuccess || (e = allow_attend4_smem<8>()) != cudaSuccess || (e = allow_attend4_smem<16>()) != cudaSuccess) return e;
-    if ((e = load_kernels(k_append4<0, false, 1>, k_append4<0, false, kAppendTokens>, k_append4<0, true, 1>, k_append4<0, true, kAppendTokens>,
-                          k_append4<1, false, 1>, k_append4<1, false, kAppendTokens>, k_append4<1, true, 1>, k_append4<1, true, kAppendTokens>)) !=
+    if ((e = load_kernels(k_append4_one<0, false>, k_append4<0, false, kAppendTokens>, k_append4_one<0, true>, k_append4<0, true, kAppendTokens>,
+                          k_append4_one<1, false>, k_append4<1, false, kAppendTokens>, k_append4_one<1, true>, k_append4<1, true, kAppendTokens>)) !=
         cudaSuccess) return e;
     if ((e = load_kernels(k_read<0, 2>, k_read<1, 2>, k_read<2, 2>, k_read<3, 2>, k_read<5, 2>, k_read<0, 4>, k_read<1, 4>, k_read<2, 4>,
                           k_read<3, 4>, k_read<5, 4>)) != cudaSuccess) return e;
@@ -1250,8 +1250,11 @@ cudaError_t launch_append(bool split, unsigned blocks, int tt, cudaStream_t st, 
 template <int KIND, bool SPLIT>
 cudaError_t launch_append4(unsigned blocks, int tt, cudaStream_t st, const AppendParams &p)
 {
-    return tt == 1 ? launch_under(k_append4<KIND, SPLIT, 1>, blocks, kAppendThreads, 0, st, p)
-                   : launch_under(k_append4<KIND, SPLIT, kAppendTokens>, blocks, kAppendThreads, 0, st, p);
+    // the blocks of the queries read the lengths only where these are the positions; lengths in place are then stored too early
+    const int32_t *lens_in = p.unit_lens ? p.unit_lens : p.dst.seq_lens;
+    const int roles = p.q && (p.pos || p.new_lens != lens_in) && blocks < 0x40000000u ? 2 : 1;
+    return tt == 1 ? launch_under(k_append4_one<KIND, SPLIT>, blocks * roles, kAppendThreads, 0, st, p, roles)
+                   : launch_under(k_append4<KIND, SPLIT, kAppendTokens>, blocks * roles, kAppendThreads, 0, st, p, roles);
 }
 
 template <int KIND>

@@ -53,31 +53,58 @@ __device__ __forceinline__ bool row4_group(float lo, float hi, float &s, float &
     return ((__float_as_uint(c32) + 0x8010u) & 0xffffu) <= 0x20u || (need > 0.f && ((__float_as_uint(need) + 0x10u) & 0xffffu) <= 0x20u);
 }
 
-// The codes of 8 neighbouring components as a word, inv = 1 / s.  Adding 1.5 * 2^23 + 8 rounds a quotient to the nearest integer (ties
-// to even) and leaves the code in the low bits of the sum; the sum of the shifted words carries a constant that is taken off at the
-// end.  TIES: the quotient is an approximate one, corrected by its exact remainder (Markstein's division): where (x - c) / s lies
-// halfway between two codes, which is common with bf16 values, it is exact.  Otherwise it may be off by 2^-20, and `off` receives the
-// largest distance of a quotient from its code.
+// Pairs of fp32 values in one register pair: sm_100a adds and multiplies both in one instruction.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair_of(float a, float b)
+{
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};\n" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void parts_of(f32x2 x, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;\n" : "=f"(a), "=f"(b) : "l"(x)); }
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b)
+{
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
+{
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
+{
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+// Codes of pairs of components, inv = 1 / s.  Adding 1.5 * 2^23 + 8 rounds a quotient to the nearest integer (ties to even) and leaves
+// the code in the low bits of the sum.  TIES: the quotient is an approximate one, corrected by its exact remainder (Markstein's
+// division): where (x - c) / s lies halfway between two codes, which is common with bf16 values, it is exact.  Otherwise it may be
+// off by 2^-20, and `off` receives the largest distance of a quotient from its code.
 template <bool TIES>
-__device__ __forceinline__ uint32_t row4_word(const float *x, float s, float inv, float c, float &off)
+__device__ __forceinline__ void row4_codes(f32x2 x, float s, float inv, float c, float &off, uint32_t &a, uint32_t &b)
 {
     constexpr float kMagic = 12582912.f + 8.f;
-    uint32_t w = 0;
-#pragma unroll
-    for (int d = 0; d < 8; ++d) {
-        const float v = x[d] - c;
-        float t;
-        if (TIES) {
-            const float q = v * inv;
-            t = fmaf(fmaf(-q, s, v), inv, q) + kMagic;
-        } else {
-            t = fmaf(v, inv, kMagic);
-            off = fmaxf(off, fabsf(fmaf(v, inv, -(t - kMagic))));
-        }
-        w += __float_as_uint(t) << 4 * ((d >> 1) + 4 * (d & 1));
+    const f32x2 magic = pair_of(kMagic, kMagic), inv2 = pair_of(inv, inv), v = add2(x, pair_of(-c, -c));
+    f32x2 t;
+    if (TIES) {
+        const f32x2 q = mul2(v, inv2);
+        t = add2(fma2(fma2(q, pair_of(-s, -s), v), inv2, q), magic);
+    } else {
+        t = fma2(v, inv2, magic);
+        float e0, e1;
+        parts_of(fma2(v, inv2, fma2(t, pair_of(-1.f, -1.f), magic)), e0, e1);
+        off = fmaxf(off, fmaxf(fabsf(e0), fabsf(e1)));
     }
-    return w - 0x4b400000u * 0x11111111u;                    // (1.5 * 2^23 has the bits 0x4b400000)
+    float t0, t1;
+    parts_of(t, t0, t1);
+    a = __float_as_uint(t0); b = __float_as_uint(t1);
 }
+constexpr uint32_t kRow4Bias = 0x4b400000u * 0x11111111u;    // what the bits of 1.5 * 2^23 add to a word of eight shifted codes
 
 // The 8 components a word stands for in bf16, rounded once: a nibble or-ed under 0x4300 is the bf16 value 128 + code, which less 136
 // is exact, and the multiply-add rounds (code - 8) s + c.  s and c are pairs of the same value.
