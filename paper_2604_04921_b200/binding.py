@@ -143,7 +143,7 @@ def lib():
     L.tri_score_static_bytes.restype = sz
     L.tri_select.argtypes = [P, P, P, i32, i32, i32, P, P, P, sz, P]
     L.tri_select.restype = ctypes.c_int
-    L.tri_compact.argtypes = [P, VP, P, P, i32, i32, VP, P, P]
+    L.tri_compact.argtypes = [P, P, P, P, i32, i32, P, P, P]      # views as addresses or packed bytes
     L.tri_compact.restype = ctypes.c_int
     L.tri_compress.argtypes = [P, VP, i32, P, i32, VP, P, P, P, P, P, sz, P]
     L.tri_compress.restype = ctypes.c_int
@@ -245,6 +245,10 @@ class CacheView:
     pre_rope: bool = False                        # bf16 keys are pre-RoPE vectors (k_kind 2); fp32 keys always are
 
     def c_view(self) -> _CacheView:
+        return _CacheView.from_buffer_copy(self.packed())
+
+    def packed(self) -> bytes:
+        """The view as the bytes of a tri_cache_view."""
         k, v, dt = self.k, self.v, self.k.dtype
         row4, fp8 = dt is torch.uint8, dt is torch.float8_e4m3fn     # 4-bit rows of bytes (k_kind 5); e4m3 (k_kind 3): keys and values alike
         shape, strides = k.shape, k.stride()
@@ -274,8 +278,8 @@ class CacheView:
             assert self.positions.dtype == torch.int32 and self.positions.is_contiguous()
             assert self.positions.shape[-1] == n_max
             pos_addr = self.positions.data_ptr()
-        return _CacheView.from_buffer_copy(_pack_view(k.data_ptr(), _addr(v) or 0, kind, int(self.page_table is not None), sl, ss, sh, st, pages, per,
-                                                      size, n_pages, sp, sslot, sl_addr, pos_addr, n_max))
+        return _pack_view(k.data_ptr(), _addr(v) or 0, kind, int(self.page_table is not None), sl, ss, sh, st, pages, per, size, n_pages,
+                          sp, sslot, sl_addr, pos_addr, n_max)
 
 
 class LayerCache:
@@ -411,11 +415,15 @@ class TriContext:
 
     def compact(self, src: CacheView, kept_idx: torch.Tensor, kept_cnt: torch.Tensor, S: int, budget: int,
                 dst: CacheView, new_seq_lens: Optional[torch.Tensor] = None):
-        cs, cd = src.c_view(), dst.c_view()
-        assert kept_idx.dtype == torch.int32 and kept_idx.numel() == self.units(S) * budget
-        assert kept_cnt.dtype == torch.int32 and kept_cnt.numel() == self.units(S)
-        _check(lib().tri_compact(self._h, ctypes.byref(cs), kept_idx.data_ptr(), kept_cnt.data_ptr(), S, budget,
-                                 ctypes.byref(cd), _addr(new_seq_lens), _stream_on(torch.cuda.current_device())), "tri_compact")
+        cs = src.packed()
+        cd = cs if dst is src else dst.packed()
+        units = self.units(S)
+        assert kept_idx.dtype is torch.int32 and kept_idx.numel() == units * budget
+        assert kept_cnt.dtype is torch.int32 and kept_cnt.numel() == units
+        code = lib().tri_compact(self._h, cs, kept_idx.data_ptr(), kept_cnt.data_ptr(), S, budget, cd, _addr(new_seq_lens),
+                                 _stream_on(torch.cuda.current_device()))
+        if code:
+            _check(code, "tri_compact")
 
     def compress(self, src: CacheView, cur_pos: torch.Tensor, budget: int, dst: CacheView, ws: torch.Tensor,
                  kept_idx: Optional[torch.Tensor] = None, kept_cnt: Optional[torch.Tensor] = None,

@@ -720,7 +720,7 @@ tri_status run_compact(tri_ctx *c, const tri_cache_view *src, const int32_t *kep
         launch_compact<8>(in_place, U, budget, st, p);
     } else if (src->k_kind == 5 && p.v_vec != 0) {
         // units enough for two blocks on each multiprocessor: the first pass in place goes on to the end (512 units, 2,048 of up to
-        // 2,176 rows: @@ us against @@)
+        // 2,176 rows: 76 us against 86)
         p.whole = in_place && U >= 2 * c->n_sm;
         launch_compact<5>(in_place, U, budget, st, p);
     } else if (in_place) {
@@ -1438,7 +1438,7 @@ cudaError_t launch_attend_clusters(int rows, unsigned units, cudaStream_t st, co
                      : launch_clusters(k_attend_cluster<KEY8, 16>, kAttCluster, units * kAttCluster, kAttThreads, kAttRingBytes, st, p, pre);
 }
 
-// (G: query rows of a unit.  Up to 4, with the columns used twice, 131,072 rows of 8 heads take @@ us against @@.)
+// (G: query rows of a unit.  Up to 4, with the columns used twice, 131,072 rows of 8 heads take 41.3 us against 43.6.)
 cudaError_t launch_attend4(int G, unsigned blocks, cudaStream_t st, const AttendParams &p)
 {
     if (G <= 4) return launch_under(k_attend4<4>, blocks, kA4Threads, kA4RingBytes, st, p);
@@ -1527,7 +1527,7 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
 
     // few short units, prefixes included: one launch (the rows of a prefix are then read for each of its sequences, from L2)
     if ((int64_t)S * H * kAttCluster <= pl.blocks &&
-        (int64_t)src->view->n_max + (P > 0 ? prefix->view->n_max : 0) <= kAttClusterRows &&
+        (int64_t)src->view->n_max + (P > 0 ? prefix->view->n_max : 0) <= (!rows4 ? kAttClusterRows : (G <= 8 ? kA4ClusterRows : kA4ClusterRowsWide)) &&
         (P == 0 || prefix->view->k_kind == src->view->k_kind)) {
         AttendParams p = attend_params(c, src, S, S, io, device_status), pre = p;
         p.finish = 1;

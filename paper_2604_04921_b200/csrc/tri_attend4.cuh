@@ -10,7 +10,7 @@
 //            brought to [2^14, 2^15) by a power of two and goes in as f16, a sixteenth of it where the codes are 16 times as large: a
 //            bf16 value is exact unless it is 2^28 times smaller than the row's largest.  Centres, and the 8 that each code is too
 //            large by, go through one matrix instruction more: c_ng against Q_g and s_ng against -8 Q_g, both in two bf16 parts, that
-//            is to 2^-17.
+//            is to 2^-16.
 //   sums     the 16 rows of A are components, its 16 columns cached rows, operands likewise: A's upper 8 rows carry 16 times the lower
 //            ones.  8 times the weights' sum is taken off in the same accumulators, by a matrix of constants.  The weights p_n s_ng are rounded
 //            once to f16: the bound on the logits that p is taken against goes by the largest scale of the rows so far, too, so that
@@ -31,6 +31,10 @@ constexpr int kA4ScaleBytes = kA4Rows * 48;                      // scales of K,
 constexpr int kA4WarpBytes = kA4Stages * kA4StageBytes + kA4ScaleBytes, kA4RingBytes = kA4Warps * kA4WarpBytes;
 constexpr int kA4Tile = kA4Warps * kA4Rows;
 constexpr int kA4UnitCost = 2;                                   // a unit's own cost, in tiles
+// Units that go to a cluster each, as in tri_attend.cuh, have up to so many rows, by query rows (one sequence of 8 heads, cluster against
+// the whole GPU: G = 4, 600 rows 4.6 / 8.1 us, 4,352 8.4 / 10.4, 8,192 11.3 / 11.8, 16,384 18.5 / 14.0; G = 16, 600 rows 7.4 / 10.5, 2,176
+// 10.2 / 11.8, 4,352 12.8 / 12.1).
+constexpr int kA4ClusterRows = 8192, kA4ClusterRowsWide = 3584;  // up to 8 query rows, more
 template <int RT> constexpr int kA4BlocksPerSM = RT <= 8 ? 3 : 2;
 constexpr float kA4NoBound = -3e38f;                             // below every logit; finite, so that 2^(-infinity - m) is 0
 constexpr uint32_t kLow = 0x000f000fu, kHigh = 0x00f000f0u;     // nibbles that are pairs of f16 values u 2^-24, u 2^-20

@@ -2,15 +2,18 @@
 them on.
 
 Error bounds used by the tests (half a step relative to the value: bf16 2^-8, f16 2^-11, fp32 2^-24):
-  append   keys are rotated in fp32 before they are quantised: a component x is off by e = (2^-21 + p 2^-51) |z|, |z| the pair's
-           magnitude (see step_reference.py); values are quantised as they come (e = 0).  From the stored s and c: c is off by one
-           rounding to bf16 of its formula, whose inputs are off by e, and fp32 roundings (2^-22); s is not below the formula's
-           bound, taken with the stored c, by more than those, and the bf16 number below s is not above it by more; a component is
-           off by s / 2, e, and what the fp32 division moves over a border (8 s 2^-23)
+  append   keys are rotated before they are quantised, in fp32 (fp64 for rows that fp32 leaves in doubt): a component x is off by e =
+           (2^-21 + p 2^-51) |z|, |z| the pair's magnitude (see step_reference.py); values are quantised as they come (e = 0).  From
+           the stored s and c: c is off by one rounding to bf16 of its formula, whose inputs are off by e, and fp32 roundings
+           (2^-22); s is not below the formula's bound, taken with the stored c, by more than those, and the bf16 number below s
+           is not above it by more; a component is off by s / 2, e, and what the fp32 quotient, off by 2^-20 at most (8 in
+           magnitude, two roundings), moves over a border
   read     fp32: one rounding of the sum (2^-24 of the value, the product is exact); bf16: one more, 2^-8
-  attend   d, what a logit is off by: per group of 32 the sum over q (128 + u) from -136 Q passes through at most 8 truncations of
-           2^-23 of at most 279 sum |q| (two matrix instructions, u <= 15) and 6 roundings of 136 Q, together below 2^-11 sum |q|,
-           times s; the centres c Q below 2^-19 |c| sum |q|; the sum of both below 2^-19 sum |q k|; all times the scale.
+  attend   d, what a logit is off by: per group of 32, with |q| the sum of the queries' magnitudes: two matrix instructions over u q, u <=
+           15, some 8 truncations of 2^-23 of at most 15 |q|: 2^-16 |q|; Q and -8 Q, |Q| <= |q|, in two bf16 parts: 2^-16 of 8 |q|;
+           together below 2^-12 |q|, times s; the centres likewise 2^-16 |c| |q|, and 2^-19 for the instruction's truncations, below
+           2^-15 |c| |q|; a query in f16 beside one 2^28 times as large, 2^-24 of that one, is far below; the sum of all below 2^-19
+           sum |q k|; all times the scale.
            A weight: the factor e^d, 2^-20 of it (exponential, products), and over the coded part of a value one rounding to f16:
            2^-11 of it, or, where f16 ends, 2^-25 steps of weights of which the largest is at least 2^11 and of scales that are below
            2 s_max: 2^-35 s_max 8 for each row.  Sums: 2^-15 of sum p |v| as in step_reference.py.  One rounding to bf16.
@@ -146,7 +149,7 @@ def attention(q, krows, vrows, scale):
     _, ks, kc = parts(krows)
     aq = q.abs()
     qg = aq.unflatten(-1, (4, 32)).sum(-1)
-    d = abs(scale) * float((2.0 ** -11 * (ks @ qg) + 2.0 ** -19 * (kc.abs() @ qg) + 2.0 ** -19 * (k.abs() @ aq)).max())
+    d = abs(scale) * float((2.0 ** -12 * (ks @ qg) + 2.0 ** -15 * (kc.abs() @ qg) + 2.0 ** -19 * (k.abs() @ aq)).max())
     m = x.max()
     p = torch.exp(x - m)
     l = p.sum()

@@ -44,7 +44,7 @@ def check_row(row, x, e):
     assert bool((s >= need - slack).all())
     assert bool((s <= R.bf16_not_below((need + slack).clamp(min=0)) + 0 * s).all())
     off = ((code - 8) * s.repeat_interleave(32) + c.repeat_interleave(32) - x).abs()
-    assert bool((off <= s.repeat_interleave(32) * (0.5 + 8 * 2.0 ** -23) + e + 2.0 ** -22 * span.repeat_interleave(32)).all())
+    assert bool((off <= s.repeat_interleave(32) * (0.5 + 2.0 ** -20) + e + 2.0 ** -22 * span.repeat_interleave(32)).all())
 
 
 def check_append(kind, half_split, page, order, H, G, lens, n_new, T, pos, per_head=False, positions=True, in_place_lens=False, seed=0,
@@ -350,6 +350,7 @@ def test_attend_lengths():
     check_attend(4, 2, [5, -3, 900, 64], rows=80, page=16)                   # below 0: 0; above the capacity: the capacity
     check_attend(4, 3, [[5, 0, 300], [0, 0, 0], [129, 1, 64]] * 5, per_head=True, page=16)
     check_attend(5, 1, [4352]), check_attend(4, 1, [4353]), check_attend(16, 1, [9000], page=48)
+    check_attend(4, 2, [8192, 8100]), check_attend(8, 1, [8193], page=16), check_attend(12, 1, [3584, 100]), check_attend(9, 1, [3585])
     check_attend(4, 8, [20000], page=16, seed=3), check_attend(8, 1, [20000, 3])
     check_attend(2, 1, [1]), check_attend(8, 1, [1], page=16)
 
@@ -507,6 +508,31 @@ def test_compact(page, order, in_place, keep):
     assert new.tolist() == [min(B, n) for n in lens]
 
 
+def test_compact_many_units_in_place():
+    """Units enough to fill the GPU: one launch moves all of their rows, whatever part lies behind the kept count."""
+    S, H, N, B = 40, 8, 400, 200
+    g = gen(0)
+    c = Cache4(1, S, H, N, page=16)
+    c.k.copy_(torch.randint(0, 256, c.k.shape, dtype=torch.uint8, device=DEV, generator=g))
+    c.v.copy_(torch.randint(0, 256, c.v.shape, dtype=torch.uint8, device=DEV, generator=g))
+    lens = [N if s % 3 else 10 * (s % 7) for s in range(S)]
+    cnt = int32([[min(B, n)] * H for n in lens])
+    score = torch.rand(S, H, N, generator=g, device=DEV) - 2.0 * (torch.arange(N, device=DEV) >= int32(lens)[:, None, None])
+    idx = score.topk(B, -1).indices
+    idx = (idx + N * (torch.arange(B, device=DEV) >= cnt[..., None])).sort(-1).values % N
+    want_k, want_v = c.k.clone(), c.v.clone()
+    for s in range(S):
+        n = min(B, lens[s])
+        for h in range(H):
+            for t, w in ((c.k, want_k), (c.v, want_v)):
+                c.put(w, 0, s, h, c.unit(t, 0, s, h, N)[idx[s, h, :n]])
+    new = int32([0] * S)
+    view = c.view(tb, seq_lens=int32(lens))
+    context(1, H, 1).compact(view, idx.to(torch.int32).contiguous(), cnt.contiguous(), S, B, view, new)
+    torch.cuda.synchronize()
+    assert torch.equal(c.k, want_k) and torch.equal(c.v, want_v) and new.tolist() == [min(B, n) for n in lens]
+
+
 def test_compact_keys_alone_and_indices_outside():
     """Without values the keys move alone; indices outside the unit move nothing."""
     for in_place in (False, True):
@@ -578,6 +604,55 @@ def test_prompt_round_and_decode_steps_together():
             for i in range(G):
                 want, _, tol, _ = R.attention(q_rot[s, 0, h * G + i].double(), c.unit(c.k, 0, s, h, n), c.unit(c.v, 0, s, h, n), D ** -0.5)
                 assert bool(((out[s, h * G + i].double() - want).abs() <= tol + U_BF16 * want.abs()).all())
+
+
+def test_rows_beyond_32_bits_of_offset():
+    """A unit whose last rows lie 2^31 bytes behind its first: append, read back, attention and a move, in the second of two layers that
+    lie 2^32 bytes apart.  The rows between are zeros (logit 0, value 0)."""
+    N, G, L = 28_000_000, 2, 2                                        # 2.24e9 bytes of keys and of values per layer
+    k, v = (torch.zeros(L, 1, 1, N, ROW, dtype=torch.uint8, device=DEV) for _ in range(2))
+    for t in (k, v):
+        t[1, ..., :64] = 0x88
+    ctx = context(L, 1, G)
+    lens, after = int32([N - 3]), int32([0])
+    g = gen(3)
+    x = torch.randn(1, 3, 1, D, generator=g, device=DEV).to(torch.bfloat16)
+    view = tb.CacheView(k, v, seq_lens=lens)
+    ctx.append(tb.LayerCache(view, 1), x, x, torch.tensor([5], device=DEV), new_lens=after)
+    then = tb.LayerCache(tb.CacheView(k, v, seq_lens=after), 1)
+    kb, vb = (torch.zeros(1, 3, 1, D, device=DEV) for _ in range(2))
+    ctx.read(then, kb, vb, first=lens)
+    torch.cuda.synchronize()
+    assert int(after) == N
+    for t in range(3):
+        row = k[1, 0, 0, N - 3 + t]
+        want = rope(x[0, t, 0].double(), 5 + t, 1e6, False)
+        check_row(row, want, (2.0 ** -21 + 2.0 ** -48) * pair_magnitude(want, False))
+        assert torch.allclose(kb[0, t, 0].double(), values(row), rtol=2.0 ** -23, atol=0)
+        assert torch.allclose(vb[0, t, 0].double(), values(v[1, 0, 0, N - 3 + t]), rtol=2.0 ** -23, atol=0)
+    assert not k[0].any() and not v[0].any() and bool((k[1, 0, 0, :N - 3, 64:] == 0).all())
+    q = (6 * kb[0, 1:2, 0].expand(1, G, D)).to(torch.bfloat16).contiguous()       # a logit that outweighs 28 million zeros
+    out, lse = torch.zeros(1, G, D, dtype=torch.bfloat16, device=DEV), torch.zeros(1, G, device=DEV)
+    ctx.attend(then, q, out, ctx.attend_workspace(1), lse=lse)
+    torch.cuda.synchronize()
+    rows_k, rows_v = k[1, 0, 0, N - 3:], v[1, 0, 0, N - 3:]
+    for i in range(G):
+        qi = q[0, i].double()
+        logit = values(rows_k) @ qi * D ** -0.5
+        top = max(float(logit.max()), 0.0)
+        p = torch.exp(logit - top)
+        total = float(p.sum()) + (N - 3) * math.exp(-top)
+        want = p @ values(rows_v) / total
+        _, _, tol, tl = R.attention(qi, rows_k, rows_v, D ** -0.5)
+        # (zero rows: their logits are off by d, too, and N weights, each rounded, are summed: 2^-15 of the sum as for all)
+        assert bool(((out[0, i].double() - want).abs() <= 2 * tol + U_BF16 * want.abs() + 2.0 ** -14 * values(rows_v).abs().amax(0)).all())
+        assert abs(float(lse[0, i]) - (top + math.log(total))) <= 2 * tl + 2.0 ** -14
+    # the three rows to the front of the unit
+    idx, cnt, new = int32([[0, 0, 0], [N - 3, N - 2, N - 1]]), int32([0, 3]), int32([0])
+    want_k, want_v = rows_k.clone(), rows_v.clone()
+    ctx.compact(view, idx, cnt, 1, 3, view, new)
+    torch.cuda.synchronize()
+    assert torch.equal(k[1, 0, 0, :3], want_k) and torch.equal(v[1, 0, 0, :3], want_v)
 
 
 def step_inputs(S, H, G, N, seed):
