@@ -443,9 +443,9 @@ cudaError_t allow_attend_smem()
 template <int RT>
 cudaError_t allow_attend4_smem()
 {
-    cudaError_t e = cudaFuncSetAttribute(k_attend4_cluster<RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kA4RingBytes);
+    cudaError_t e = cudaFuncSetAttribute(k_attend4_cluster<RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kA4RingBytes<RT>);
     if (e != cudaSuccess) return e;
-    return cudaFuncSetAttribute(k_attend4<RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kA4RingBytes);
+    return cudaFuncSetAttribute(k_attend4<RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kA4RingBytes<RT>);
 }
 
 // Loads kernels that need no attribute, so that a program's first call may already be captured into a graph.
@@ -1441,16 +1441,16 @@ cudaError_t launch_attend_clusters(int rows, unsigned units, cudaStream_t st, co
 // (G: query rows of a unit.  Up to 4, with the columns used twice, 131,072 rows of 8 heads take 41.3 us against 43.6.)
 cudaError_t launch_attend4(int G, unsigned blocks, cudaStream_t st, const AttendParams &p)
 {
-    if (G <= 4) return launch_under(k_attend4<4>, blocks, kA4Threads, kA4RingBytes, st, p);
-    return G <= 8 ? launch_under(k_attend4<8>, blocks, kA4Threads, kA4RingBytes, st, p)
-                  : launch_under(k_attend4<16>, blocks, kA4Threads, kA4RingBytes, st, p);
+    if (G <= 4) return launch_under(k_attend4<4>, blocks, kA4Threads, kA4RingBytes<4>, st, p);
+    return G <= 8 ? launch_under(k_attend4<8>, blocks, kA4Threads, kA4RingBytes<8>, st, p)
+                  : launch_under(k_attend4<16>, blocks, kA4Threads, kA4RingBytes<16>, st, p);
 }
 
 cudaError_t launch_attend4_clusters(int G, unsigned units, cudaStream_t st, const AttendParams &p)
 {
-    if (G <= 4) return launch_clusters(k_attend4_cluster<4>, kAttCluster, units * kAttCluster, kA4Threads, kA4RingBytes, st, p);
-    return G <= 8 ? launch_clusters(k_attend4_cluster<8>, kAttCluster, units * kAttCluster, kA4Threads, kA4RingBytes, st, p)
-                  : launch_clusters(k_attend4_cluster<16>, kAttCluster, units * kAttCluster, kA4Threads, kA4RingBytes, st, p);
+    if (G <= 4) return launch_clusters(k_attend4_cluster<4>, kAttCluster, units * kAttCluster, kA4Threads, kA4RingBytes<4>, st, p);
+    return G <= 8 ? launch_clusters(k_attend4_cluster<8>, kAttCluster, units * kAttCluster, kA4Threads, kA4RingBytes<8>, st, p)
+                  : launch_clusters(k_attend4_cluster<16>, kAttCluster, units * kAttCluster, kA4Threads, kA4RingBytes<16>, st, p);
 }
 
 // rows4: whether the call takes 4-bit rows.

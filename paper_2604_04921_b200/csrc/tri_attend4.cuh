@@ -2,7 +2,7 @@
 //
 // Mathematics.  As in tri_attend.cuh, with k_n = s_ng (u - 8) + c_ng for the codes u of group g (32 components), and v_n likewise:
 //       q . k_n  = sum_g s_ng (sum_d q_d u_nd - 8 Q_g) + sum_g c_ng Q_g,      Q_g = sum of q over group g
-//       sum_n p_n v_n = sum_n (p_n s_ng) (u - 8) + sum_n p_n c_ng
+//       sum_n p_n v_n = sum_n (p_n s_ng) u + sum_n p_n (c_ng - 8 s_ng)
 // so that the matrix instructions work on codes, and scales and centres are applied per row and group:
 //   logits   keys are the 16 rows of A, 8 query rows the columns of B.  A nibble in 16 bits of its own is the f16 value u 2^-24, or
 //            u 2^-20 where it lies four bits further up: 5 integer instructions make operands of 8 codes (as bf16, with 128 or-ed in,
@@ -12,7 +12,10 @@
 //            large by, go through one matrix instruction more: c_ng against Q_g and s_ng against -8 Q_g, both in two bf16 parts, that
 //            is to 2^-16.
 //   sums     the 16 rows of A are components, its 16 columns cached rows, operands likewise: A's upper 8 rows carry 16 times the lower
-//            ones.  8 times the weights' sum is taken off in the same accumulators, by a matrix of constants.  The weights p_n s_ng are rounded
+//            ones.  They sum p_n s_ng u; the 8 goes with the centres, sum_n p_n (c_ng - 8 s_ng).  The matrix instructions truncate, so
+//            that sums of positive terms drift by some 2^-25 per instruction, against which a difference of the two would not last:
+//            every 16 steps the accumulators go to sums in shared memory.  (8 taken off in the accumulators, by a matrix of constants,
+//            made the kernel 8 % slower.)  The weights p_n s_ng are rounded
 //            once to f16: the bound on the logits that p is taken against goes by the largest scale of the rows so far, too, so that
 //            they use f16's range from 2^15 down.  The centres are summed in fp32.
 //
@@ -28,7 +31,10 @@ namespace tri {
 constexpr int kA4Warps = kAttWarps, kA4Threads = 32 * kA4Warps, kA4Rows = 32, kA4Stages = 2;      // (one step ahead)
 constexpr int kA4Half = kA4Rows * kRow4Bytes, kA4StageBytes = 2 * kA4Half;                  // K | V
 constexpr int kA4ScaleBytes = kA4Rows * 48;                      // scales of K, scales and centres of V in fp32
-constexpr int kA4WarpBytes = kA4Stages * kA4StageBytes + kA4ScaleBytes, kA4RingBytes = kA4Warps * kA4WarpBytes;
+constexpr int kA4SumSteps = 16;                                  // steps between two additions to the sums in shared memory
+template <int RT> constexpr int kA4SumBytes = (RT == 16 ? 2 : 1) * 8 * 512;
+template <int RT> constexpr int kA4WarpBytes = kA4Stages * kA4StageBytes + kA4ScaleBytes + kA4SumBytes<RT>;
+template <int RT> constexpr int kA4RingBytes = kA4Warps * kA4WarpBytes<RT>;
 constexpr int kA4Tile = kA4Warps * kA4Rows;
 constexpr int kA4UnitCost = 2;                                   // a unit's own cost, in tiles
 // Units that go to a cluster each, as in tri_attend.cuh, have up to so many rows, by query rows (one sequence of 8 heads, cluster against
@@ -114,7 +120,8 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
     __shared__ __align__(16) float part[CL ? COLS : 1][kAttRowPitch];      // this block's sums, and (m, l)
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
-    const uint32_t ring = smem_u32(dyn) + warp * kA4WarpBytes, scales = ring + ST * kA4StageBytes;
+    const uint32_t ring = smem_u32(dyn) + warp * kA4WarpBytes<RT>, scales = ring + ST * kA4StageBytes;
+    float4 *sums = reinterpret_cast<float4 *>(dyn + warp * kA4WarpBytes<RT> + ST * kA4StageBytes + kA4ScaleBytes) + lane;      // 32 apart
     // Cached row of row i of a matrix tile of keys: i / 2 + 4 (i % 2) of 8 (the second 8 rows 8 further on).  Rows 4 apart are 64 bytes
     // apart in the banks: two rows' 64 bytes of codes, one load's phase, take all of them.  The sums over cached rows then take
     // columns 2 t4, 2 t4 + 1 of A from rows t4, t4 + 4.
@@ -249,8 +256,23 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
     uint32_t qsum[CT][2];                                 // Q and -8 Q in two bf16 parts, B operand of centres and scales
     float o[CT][4][2][4], oc[CT][GP][2], m[CT][2], l[CT][2];
     float top = 0.f, above = 0.f;                         // largest size of values so far, a power of two; 15 less its exponent
-    uint32_t less[2];                                     // -8 2^-24, -8 2^-20 as f16 pairs (kept in registers)
-    asm volatile("mov.u32 %0, 0x80088008;\nmov.u32 %1, 0x80808080;\n" : "=r"(less[0]), "=r"(less[1]));
+    bool summed = false;                                  // whether there are sums in shared memory
+    auto to_sums = [&]() {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                float (&a)[4] = o[ct][x >> 1][x & 1];
+                float4 y = make_float4(a[0], a[1], a[2], a[3]);
+                if (summed) {
+                    const float4 z = sums[32 * (8 * ct + x)];
+                    y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
+                }
+                sums[32 * (8 * ct + x)] = y;
+                a[0] = a[1] = a[2] = a[3] = 0.f;
+            }
+        summed = true;
+    };
     for (;;) {
         if (j.it == j.kb) {
             // ---------------- the next unit: the one whose first step has been copied ----------------
@@ -306,6 +328,7 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
                 m[ct][0] = m[ct][1] = kA4NoBound;
                 l[ct][0] = l[ct][1] = 0.f;
             }
+            summed = false;
             top = 0x1p-81f; above = kAttAbove<true> + 81.f;
         }
         // the other stage has been read, or used and released in joining a unit
@@ -324,12 +347,13 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
         const uint32_t miss = (bad >> (2 * stage)) & 3u;
         const bool cut = have < ROWS || miss;
         const uint32_t kb_s = ring + stage * kA4StageBytes, vb_s = kb_s + kA4Half;
-        // a lane widens the scales (of groups 0, 2, 1, 3) and centres of one row for all
+        // a lane widens the scales (of groups 0, 2, 1, 3) and centres (of V: c - 8 s) of one row for all
         const uint4 k_par = lds128(kb_s + lane * kRow4Bytes + kRow4Scales), v_par = lds128(vb_s + lane * kRow4Bytes + kRow4Scales);
         const uint32_t row48 = scales + lane * 48;
         sts128(row48, bf16_lo(k_par.x), bf16_lo(k_par.y), bf16_hi(k_par.x), bf16_hi(k_par.y));
         sts128(row48 + 16, bf16_lo(v_par.x), bf16_lo(v_par.y), bf16_hi(v_par.x), bf16_hi(v_par.y));
-        sts128(row48 + 32, bf16_lo(v_par.z), bf16_lo(v_par.w), bf16_hi(v_par.z), bf16_hi(v_par.w));
+        sts128(row48 + 32, fmaf(-8.f, bf16_lo(v_par.x), bf16_lo(v_par.z)), fmaf(-8.f, bf16_lo(v_par.y), bf16_lo(v_par.w)),
+               fmaf(-8.f, bf16_hi(v_par.x), bf16_hi(v_par.z)), fmaf(-8.f, bf16_hi(v_par.y), bf16_hi(v_par.w)));
         const uint32_t s_max = max_bf16x2(v_par.x, v_par.y), c_max = max_bf16x2(v_par.z & 0x7fff7fffu, v_par.w & 0x7fff7fffu);
         __syncwarp();
         // logits: 16 cached rows x 8 query rows; the thread holds rows g8, g8 + 8 of the tile for query rows 2 t4, 2 t4 + 1
@@ -385,6 +409,17 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
                 raise = raise || mx[ct][i] > m[ct][i] + above;
             }
         if (__any_sync(0xffffffffu, raise)) {
+            if (summed) {                                 // (the sums are scaled below as what they were: accumulators)
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) {
+                        const float4 z = sums[32 * (8 * ct + x)];
+                        float (&a)[4] = o[ct][x >> 1][x & 1];
+                        a[0] += z.x; a[1] += z.y; a[2] += z.z; a[3] += z.w;
+                    }
+                summed = false;
+            }
 #pragma unroll
             for (int d = 1; d < 32; d *= 2) sm = fmaxf(sm, __shfl_xor_sync(0xffffffffu, sm, d));
             if (sm > top) {                               // (all lanes alike)
@@ -454,17 +489,19 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
                 const uint32_t xa8 = xa >> 8, xb8 = xb >> 8;
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
-                    mma_f16_16816(o[ct][g][0], less[0], less[1], less[0], less[1], pw[ct][g * GP / 4][0], pw[ct][g * GP / 4][1]);
-                    mma_f16_16816(o[ct][g][1], less[0], less[1], less[0], less[1], pw[ct][g * GP / 4][0], pw[ct][g * GP / 4][1]);
                     mma_f16_16816(o[ct][g][0], xa & kLow, xa & kHigh, xb & kLow, xb & kHigh, pw[ct][g * GP / 4][0], pw[ct][g * GP / 4][1]);
                     mma_f16_16816(o[ct][g][1], xa8 & kLow, xa8 & kHigh, xb8 & kLow, xb8 & kHigh, pw[ct][g * GP / 4][0], pw[ct][g * GP / 4][1]);
                 }
             }
         }
         __syncwarp();
-        uint8_t *used = dyn + warp * kA4WarpBytes + stage * kA4StageBytes;
+        uint8_t *used = dyn + warp * kA4WarpBytes<RT> + stage * kA4StageBytes;
         stage ^= 1;
-        if (++j.it < j.kb) continue;
+        if (++j.it < j.kb) {
+            if (j.it % kA4SumSteps == 0) to_sums();
+            continue;
+        }
+        if (summed) to_sums();
 
         // ---------------- the unit's rows of this share are through: join the warps ----------------
         // per 8 query rows: each leaves its sums in the stage it has just read, fragment by fragment, and takes a group of all
@@ -485,9 +522,15 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
             for (int g = 0; g < 4; ++g)
 #pragma unroll
                 for (int y = 0; y < 2; ++y)
+                {
+                    if (summed) {
+                        const float4 z = sums[32 * (8 * ct + 2 * g + y)];
+                        o[ct][g][y][0] = z.x; o[ct][g][y][1] = z.y; o[ct][g][y][2] = z.z; o[ct][g][y][3] = z.w;
+                    }
                     *reinterpret_cast<float4 *>(used + (2 * g + y) * 512 + lane * 16) =
                         make_float4(fmaf(o[ct][g][y][0], 0x1p24f, oc[ct][g * GP / 4][0]), fmaf(o[ct][g][y][1], 0x1p24f, oc[ct][g * GP / 4][1]),
                                     fmaf(o[ct][g][y][2], 0x1p20f, oc[ct][g * GP / 4][0]), fmaf(o[ct][g][y][3], 0x1p20f, oc[ct][g * GP / 4][1]));
+                }
             __syncthreads();
             const int from = RT == 4 ? 4 * g8 + (t4 & 1) + 2 * (warp & 1) : lane;          // (RT = 4: where the group's columns are)
             // components 32 warp + 8 (g8 / 2) + g8 % 2 + 0, 2, 4, 6 of query rows 2 t4, 2 t4 + 1 (+ 8 ct)
@@ -509,7 +552,7 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
             for (int y = 0; y < 2; ++y)
 #pragma unroll
                 for (int w2 = 0; w2 < kA4Warps; ++w2) {
-                    const float4 x = *reinterpret_cast<const float4 *>(used + (w2 - warp) * kA4WarpBytes + (2 * warp + y) * 512 + from * 16);
+                    const float4 x = *reinterpret_cast<const float4 *>(used + (w2 - warp) * kA4WarpBytes<RT> + (2 * warp + y) * 512 + from * 16);
                     z[0][2 * y] += x.x * by[w2][0]; z[1][2 * y] += x.y * by[w2][1];
                     z[0][2 * y + 1] += x.z * by[w2][0]; z[1][2 * y + 1] += x.w * by[w2][1];
                 }

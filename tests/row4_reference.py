@@ -14,9 +14,10 @@ Error bounds used by the tests (half a step relative to the value: bf16 2^-8, f1
            together below 2^-12 |q|, times s; the centres likewise 2^-16 |c| |q|, and 2^-19 for the instruction's truncations, below
            2^-15 |c| |q|; a query in f16 beside one 2^28 times as large, 2^-24 of that one, is far below; the sum of all below 2^-19
            sum |q k|; all times the scale.
-           A weight: the factor e^d, 2^-20 of it (exponential, products), and over the coded part of a value one rounding to f16:
-           2^-11 of it, or, where f16 ends, 2^-25 steps of weights of which the largest is at least 2^11 and of scales that are below
-           2 s_max: 2^-35 s_max 8 for each row.  Sums: 2^-15 of sum p |v| as in step_reference.py.  One rounding to bf16.
+           A weight: the factor e^d, 2^-20 of it (exponential, products).  Values are summed as p s u and p (c - 8 s), the weights p s
+           of the former with one rounding to f16: 2^-11 of p s u, or, where f16 ends, 2^-25 steps of weights of which the largest is at least 2^11 and of scales that are below
+           2 s_max: 2^-35 s_max 8 for each row.  Sums: 2^-15 of all that is summed, as in step_reference.py: sum
+           p (s u + |c| + 8 s).  One rounding to bf16.
 """
 from __future__ import annotations
 
@@ -155,6 +156,6 @@ def attention(q, krows, vrows, scale):
     l = p.sum()
     p = p / l
     _, vs, vc = parts(vrows)
-    coded = p @ (v - vc.repeat_interleave(32, -1)).abs()
-    tol = (2 * d + 2.0 ** -15) * (p @ v.abs()) + 2.0 ** -15 * (p @ vc.abs().repeat_interleave(32, -1)) + (2.0 ** -11 + 2.0 ** -15) * coded
+    coded = p @ (v - (vc - 8 * vs).repeat_interleave(32, -1))         # s u >= 0
+    tol = 2 * d * (p @ v.abs()) + 2.0 ** -15 * (p @ (vc.abs() + 8 * vs).repeat_interleave(32, -1)) + (2.0 ** -11 + 2.0 ** -15) * coded
     return p @ v, float(m + torch.log(l)), tol + n * 2.0 ** -32 * float(vs.max()), d + 2.0 ** -18
