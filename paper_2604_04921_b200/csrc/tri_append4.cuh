@@ -173,7 +173,7 @@ __device__ __forceinline__ void row4_fp64(const char *from, char *to, int c, dou
         const float need = __double2float_ru(fmax((hi - (double)m) / 7.0, ((double)m - lo) * 0.125));
         const uint32_t up = max((__float_as_uint(need) + 0xffffu) & 0xffff0000u, 0x00800000u);
         float s = need > 0.f ? __uint_as_float(up) : 0.f;
-        if (nan || !(fabsf(m) < INFINITY)) { m = __uint_as_float(0x7fc00000u); s = 0.f; }
+        if (nan || !(fabsf((float)((double)m - lo)) < INFINITY)) { m = __uint_as_float(0x7fc00000u); s = 0.f; }
         r.m[j] = m; r.s[j] = s;
         const double by = s > 0.f ? (double)s : 1.0;
 #pragma unroll

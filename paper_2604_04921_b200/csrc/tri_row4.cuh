@@ -39,7 +39,7 @@ __device__ __forceinline__ float max_nan(float a, float b)
 
 // Scale and centre of a group from its smallest and largest value.  (8 hi + 7 lo) / 15 as (hi / 2 + 7 lo / 16) / (15 / 16), which
 // cannot overflow; with bf16 inputs every step up to the division is exact or rounded once, so that c is the correctly rounded
-// one.  A NaN or an infinity among the values makes c not finite.  Returns whether c or s lies so near the border of two bf16 numbers
+// one.  With a NaN or an infinity among the values, or a range that fp32 does not hold, c - lo is not finite.  Returns whether c or s lies so near the border of two bf16 numbers
 // that lo and hi, if they are off by a few steps of fp32, may have put it on the wrong side.
 __device__ __forceinline__ bool row4_group(float lo, float hi, float &s, float &c)
 {
@@ -49,7 +49,7 @@ __device__ __forceinline__ bool row4_group(float lo, float hi, float &s, float &
     // rounded up to bf16; the smallest normal number, where that is more
     const uint32_t up = max((__float_as_uint(need) + 0xffffu) & 0xffff0000u, 0x00800000u);
     s = need > 0.f ? __uint_as_float(up) : 0.f;
-    if (!(fabsf(c) < INFINITY)) { c = __uint_as_float(0x7fc00000u); s = 0.f; }
+    if (!(fabsf(c - lo) < INFINITY)) { c = __uint_as_float(0x7fc00000u); s = 0.f; }
     return ((__float_as_uint(c32) + 0x8010u) & 0xffffu) <= 0x20u || (need > 0.f && ((__float_as_uint(need) + 0x10u) & 0xffffu) <= 0x20u);
 }
 

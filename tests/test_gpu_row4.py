@@ -182,6 +182,69 @@ def test_append_unusual_groups():
     assert torch.equal(bad.any(-1), want)
 
 
+def test_append_groups_as_wide_as_fp32():
+    """A group from -m to n has c - lo = 8 (m + n) / 15: up to fp32's range it is quantised, beyond that it becomes NaN, on every
+    path that keys and values take."""
+    x = torch.randn(D, generator=gen(3), device=DEV)
+    x[0:32:2], x[1:32:2] = 3.1e38, -3.1e38
+    x[32:64:2], x[33:64:2] = 3.38e38, -3.38e38
+    x[64:80], x[80:96] = -3.38e38, 2.9e38
+    x = x.to(torch.bfloat16)
+    ctx = context(1, 1, 1)
+    code, s, c = R.quantised(x.double())
+    for T in (1, 3):
+        for dtype in (torch.bfloat16, torch.float32):
+            cache = Cache4(1, 1, 1, 16)
+            rows = x.to(dtype).expand(1, T, 1, D).contiguous()
+            ctx.append(tb.LayerCache(cache.view(tb, seq_lens=int32([0])), 0), rows, rows.clone(), torch.zeros(1, dtype=torch.int64, device=DEV),
+                       n_new=int32([1]))
+            torch.cuda.synchronize()
+            for got in (cache.at(cache.k, 0, 0, 0, 0), cache.at(cache.v, 0, 0, 0, 0)):
+                got_code, got_s, got_c = parts(got)
+                assert torch.equal(got_c.isnan(), torch.tensor([False, True, False, False], device=DEV)) and float(got_s[1]) == 0
+                for g in (0, 2, 3):
+                    assert torch.equal(got_code[32 * g:32 * g + 32], code[32 * g:32 * g + 32]), (T, dtype, g)
+                    assert float(got_s[g]) == float(s[g]) and float(got_c[g]) == float(c[g])
+
+
+@pytest.mark.parametrize("H", [1, 8, 40])
+def test_append_keys_that_are_all_in_doubt(H):
+    """Keys at position 0 stay as they are, and sixteenths put many (x - c) / s halfway between two codes: each row is done again, and
+    is what the definition says byte for byte; so are more rows than a block lists, and the rows of the other tokens stay right."""
+    T = 9
+    x = (torch.randint(-40, 41, (1, T, H, D), generator=gen(6), device=DEV) / 16).to(torch.bfloat16)
+    ctx = context(1, H, 1)
+    cache = Cache4(1, 1, H, 16)
+    status = int32([0])
+    ctx.append(tb.LayerCache(cache.view(tb, seq_lens=int32([0])), 0), x, x.clone(), torch.zeros(1, dtype=torch.int64, device=DEV), device_status=status)
+    torch.cuda.synchronize()
+    assert int(status) == 0
+    want = as_rows(x[0].double())
+    for t in range(T):
+        for h in range(H):
+            assert torch.equal(cache.at(cache.v, 0, 0, h, t), want[t, h])
+            wk = rope(x[0, t, h].double(), t, 1e6, False)
+            check_row(cache.at(cache.k, 0, 0, h, t), wk, 2.0 ** -21 * pair_magnitude(wk, False))
+            if t == 0:
+                assert torch.equal(cache.at(cache.k, 0, 0, h, t), want[t, h])
+
+
+@pytest.mark.parametrize("T", [1, 9])
+@pytest.mark.parametrize("half_split", [False, True])
+def test_append_queries_in_place(T, half_split):
+    S, H, G = 3, 2, 5
+    ctx = context(1, H, G, half_split=half_split)
+    g = gen(T)
+    q, k = (torch.randn(S, T, n, D, generator=g, device=DEV).to(torch.bfloat16) for n in (G * H, H))
+    pos = torch.tensor([0, 7, 1000], device=DEV)
+    want = torch.empty_like(q)
+    for to in (want, q):
+        cache = Cache4(1, S, H, 16)
+        ctx.append(tb.LayerCache(cache.view(tb, seq_lens=int32([0, 3, 5])), 0), k, k.clone(), pos, q=q, q_out=to)
+    torch.cuda.synchronize()
+    assert torch.equal(q, want)
+
+
 def test_append_without_values_and_rows_without_a_place():
     ctx, S = context(1, 1, 1), 1
     k = torch.randn(1, 4, 1, D, generator=gen(0), device=DEV)
