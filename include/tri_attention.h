@@ -375,14 +375,17 @@ typedef struct {
  *   keys     k_kind 0, 3: band f of the key is rotated by the angle p * omega_f (Section 2.1; the band layout is the
  *            context's pair_layout), in fp32 with the angle reduced in fp64, and rounded once to bf16 or e4m3;
  *            k_kind 1, 2: stored as they are (fp32, bf16), these caches hold pre-RoPE vectors
- *            k_kind 5: rotated likewise, in fp32, and quantised as below
+ *            k_kind 5: rotated likewise and quantised as below; formed in fp32, and where that lies so near the border of
+ *            two codes, scales or centres that its rounding could decide (and for single tokens) in fp64.  Where a group
+ *            is tiny beside the pairs it was rotated from, a few steps of fp32 of those remain
  *   values   rounded to the cache's format (k_kind 5: quantised as below)
  *   e4m3     round(x / scale) to nearest even, beyond +-448 to +-448, NaN to NaN
  *   4 bits   (k_kind 5) each group of 32 components has a scale s and a centre c in bf16, and a component stands for
  *            (code - 8) s + c.  With the group's smallest and largest value lo and hi: c = bf16((8 hi + 7 lo) / 15), s = the
  *            smallest bf16 that is not below (hi - c) / 7 and (c - lo) / 8 (at least 2^-126, or 0 if both are 0), code =
  *            8 + (x - c) / s, rounded to nearest even and kept within 0..15: no component is off by more than s / 2 and the
- *            rounding of (x - c) / s.  A group with a NaN or an infinity becomes NaN throughout (c NaN, s 0).
+ *            rounding of (x - c) / s.  A group with a NaN or an infinity, or whose c - lo or c exceeds its type, becomes NaN
+ *            throughout (c NaN, s 0).
  *            A row is TRI_ROW4_BYTES bytes: component 32 g + 8 t + 2 i + h (g, t, i < 4, h < 2) in bits 4 (i + 4 h) .. + 3 of
  *            the 32-bit word 4 t + g (little endian), the scales of the four groups from byte 64 on, the centres from byte 72 on.
  *   positions of the view, if any, receive p
@@ -444,8 +447,10 @@ size_t tri_attend_workspace_bytes(const tri_ctx *ctx, int32_t S, int32_t P);
  * used, whatever they hold.  Logits, softmax statistics and sums are fp32; the weights of the sum over values enter
  * the tensor cores as a 16-bit value plus the 16-bit rest of it (shared prefixes with S * G > 16 * P: rounded once, to
  * bf16, which raises the error of bf16 outputs by up to 1.45 times, over 8-bit values to f16, which does not).  Over 4-bit
- * values a weight is multiplied by the scale of its row and group and rounded once, to f16 (2^-12 of the weight, or 2^-36 of
- * the largest weight times the largest scale of the unit so far where that is more); the centres are summed in fp32.  Sums
+ * values a weight times the scale of its row and group is rounded once, to f16 (by 2^-11 of it at most, or 2^-36 of the
+ * largest weight times the largest scale of the unit so far where that is more), and centres enter the logits to 2^-16;
+ * query components 2^28 times smaller than the largest of their row lose bits; scales must not be negative, and scales and
+ * centres should stay below 2^100.  Sums
  * are formed in a fixed order: equal inputs give equal bits.  Ragged batches are cut into equal shares over the GPU; S * n_kv_heads * (n_max / 64 + 3) must stay below
  * 2^31 (for prefixes, with P + S in place of S at most), else TRI_ERR_UNSUPPORTED.  An infinity among the values of a
  * unit's rows makes the outputs of its component infinite or NaN.

@@ -687,7 +687,8 @@ void launch_compact(bool in_place, int U, int32_t budget, cudaStream_t st, const
 {
     const dim3 grid(U, (budget + RowShape<PIECES>::kRowsPerBlock - 1) / RowShape<PIECES>::kRowsPerBlock);
     if (in_place) {
-        k_compact_inplace_rows<PIECES><<<U, kInplaceThreads, 0, st>>>(p);
+        if constexpr (PIECES == 5) k_compact_inplace_rows4<<<U, kInplaceThreads, 0, st>>>(p);
+        else k_compact_inplace_rows<PIECES><<<U, kInplaceThreads, 0, st>>>(p);
         if (!p.whole) k_gather_rows<true, PIECES><<<grid, kGatherThreads, 0, st>>>(p);
     } else {
         k_gather_rows<false, PIECES><<<grid, kGatherThreads, 0, st>>>(p);
@@ -719,9 +720,11 @@ tri_status run_compact(tri_ctx *c, const tri_cache_view *src, const int32_t *kep
     } else if (src->k_kind == 3 && p.v_vec != 0) {
         launch_compact<8>(in_place, U, budget, st, p);
     } else if (src->k_kind == 5 && p.v_vec != 0) {
-        // units enough for two blocks on each multiprocessor: the first pass in place goes on to the end (512 units, 2,048 of up to
-        // 2,176 rows: 76 us against 86)
-        p.whole = in_place && U >= 2 * c->n_sm;
+        // In place the first pass goes on to the end where it moves most of the rows anyway, or where there are units enough to keep the
+        // GPU busy (one launch against two, 2,048 rows kept; 8 units of 2,176 rows 14.7 against 17.9 us, of 4,096 15.5 / 16.4, of
+        // 8,192 15.4 / 13.8, of 32,768 15.8 / 11.0; 64 units of 8,192 18.6 / 18.9; 256 of 2,176 28.7 / 34.5, of 8,192 43.4 / 51.1; 512
+        // of 2,176 63.5 / 83, of 32,768 112 / 127)
+        p.whole = in_place && (src->n_max <= 2 * (int64_t)budget || 2 * U >= c->n_sm);
         launch_compact<5>(in_place, U, budget, st, p);
     } else if (in_place) {
         k_compact_inplace_any<<<U, kInplaceThreads, 0, st>>>(p);
@@ -1438,7 +1441,7 @@ cudaError_t launch_attend_clusters(int rows, unsigned units, cudaStream_t st, co
                      : launch_clusters(k_attend_cluster<KEY8, 16>, kAttCluster, units * kAttCluster, kAttThreads, kAttRingBytes, st, p, pre);
 }
 
-// (G: query rows of a unit.  Up to 4, with the columns used twice, 131,072 rows of 8 heads take 41.3 us against 43.6.)
+// (G: query rows of a unit.  Up to 4, with the columns used twice, 131,072 rows of 8 heads take 39.0 us against 41.2.)
 cudaError_t launch_attend4(int G, unsigned blocks, cudaStream_t st, const AttendParams &p)
 {
     if (G <= 4) return launch_under(k_attend4<4>, blocks, kA4Threads, kA4RingBytes<4>, st, p);

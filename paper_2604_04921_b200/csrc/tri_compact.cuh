@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(kGatherThreads) k_gather_any(const CompactPara
 constexpr int kInplaceThreads = 512;
 static_assert(kInplaceRows == (kInplaceThreads / 32) * kFastRows, "a tile is 8 rows per warp");
 
-// PIECES as in k_gather_rows: with 128-byte rows a warp holds 16 rows and a tile is 256 rows, with 80-byte rows 24 and 384.
+// PIECES as in k_gather_rows, 16 or 8: with 128-byte rows a warp holds 16 rows and a tile is 256 rows.
 template <int PIECES = 16>
 __global__ void __launch_bounds__(kInplaceThreads, 2) k_compact_inplace_rows(const CompactParams p)
 {
@@ -229,7 +229,7 @@ __global__ void __launch_bounds__(kInplaceThreads, 2) k_compact_inplace_rows(con
     const int n_src = p.src.n_max;
 
     for (int t0 = 0; t0 < cnt; t0 += RowShape<PIECES>::kTile) {
-        if (!p.whole && __ldg(idx + t0) >= cnt) break;       // the parallel pass takes over from here
+        if (__ldg(idx + t0) >= cnt) break;                   // the parallel pass takes over from here
         const int j0 = t0 + warp * kGroup;
         int mine = -1, pos = 0;
         int64_t so = -1, dof = -1;
@@ -253,18 +253,84 @@ __global__ void __launch_bounds__(kInplaceThreads, 2) k_compact_inplace_rows(con
         uint4 val[kFastRows];
 #pragma unroll
         for (int r = 0; r < kFastRows; ++r) {
-            int64_t o = __shfl_sync(0xffffffffu, so, r * kSlots + sub);
-            if constexpr (RowShape<PIECES>::kIdle) if (sub >= kSlots) o = -1;
+            const int64_t o = __shfl_sync(0xffffffffu, so, r * kSlots + sub);
             if (o >= 0) val[r] = ld_stream(sb + o * ESZ);
         }
         __syncthreads();                                     // every source of the tile has been read
 #pragma unroll
         for (int r = 0; r < kFastRows; ++r) {
-            int64_t o = __shfl_sync(0xffffffffu, dof, r * kSlots + sub);
-            if constexpr (RowShape<PIECES>::kIdle) if (sub >= kSlots) o = -1;
+            const int64_t o = __shfl_sync(0xffffffffu, dof, r * kSlots + sub);
             if (o >= 0) *reinterpret_cast<uint4 *>(db + o * ESZ) = val[r];
         }
         if (p.dst.positions && mine >= 0) p.dst.positions[(int64_t)u * p.dst.n_max + j0 + lane] = pos;
+    }
+}
+
+// 80-byte rows, 384 of them a tile.  Where a lane's row comes from and goes to is looked up one tile ahead, while the rows of the tile
+// before are on their way (512 units, 2,048 of up to 2,176 rows: 66 us against 76; the registers of longer rows do not reach for that).
+// `whole`: it goes on to the end, and there is no second pass.
+__global__ void __launch_bounds__(kInplaceThreads, 2) k_compact_inplace_rows4(const CompactParams p)
+{
+    constexpr int PIECES = 5, kPieces = PIECES, ESZ = RowShape<PIECES>::kElement, kSlots = RowShape<PIECES>::kSlots, kGroup = RowShape<PIECES>::kGroup;
+    const int u = p.u0 + blockIdx.x;
+    const int h = u % p.H, s = (u / p.H) % p.S, l = u / (p.H * p.S);
+    const int cnt = min(__ldg(p.kept_cnt + u), p.budget);
+    if (threadIdx.x == 0 && p.new_seq_lens && h == 0 && l == 0) p.new_seq_lens[s] = cnt;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int32_t *idx = p.kept_idx + (int64_t)u * p.budget;
+    const bool is_v = (lane / kPieces) & 1;
+    const int sub = lane / (2 * kPieces);
+    const char *sb = (is_v ? p.src.v : p.src.k) + (lane % kPieces) * 16;
+    char *db = (is_v ? p.dst.v : p.dst.k) + (lane % kPieces) * 16;
+    const int n_src = p.src.n_max;
+
+    // where this lane's row of a tile comes from and goes to
+    int mine = -1, pos = 0;
+    int64_t so = -1, dof = -1;
+    bool after = false;                                      // the parallel pass takes over from this tile on
+    auto look_up = [&](int t0) {
+        mine = -1; pos = 0; so = -1; dof = -1;
+        after = !p.whole && __ldg(idx + t0) >= cnt;
+        const int j = t0 + warp * kGroup + lane;
+        if (lane >= kGroup || j >= cnt) return;
+        mine = __ldg(idx + j);
+        if (mine == j) {
+            mine = -1;                                       // already in its slot
+            return;
+        }
+        if (mine >= 0 && mine < n_src) {
+            so = row_offset(p.src, l, s, h, mine);
+            dof = row_offset(p.dst, l, s, h, j);
+        }
+        if (so < 0 || dof < 0) {
+            if (p.device_status) atomicExch(p.device_status, (int)TRI_ERR_DEVICE_CHECK);
+            mine = -1; so = -1; dof = -1;
+        } else if (p.dst.positions) {
+            pos = p.src.positions ? p.src.positions[(int64_t)u * p.src.n_max + mine] : mine;
+        }
+    };
+    if (cnt > 0) look_up(0);
+    for (int t0 = 0; t0 < cnt; t0 += RowShape<PIECES>::kTile) {
+        if (after) break;
+        uint4 val[kFastRows];
+#pragma unroll
+        for (int r = 0; r < kFastRows; ++r) {
+            int64_t o = __shfl_sync(0xffffffffu, so, r * kSlots + sub);
+            if (sub >= kSlots) o = -1;
+            if (o >= 0) val[r] = ld_stream(sb + o * ESZ);
+        }
+        const int pos_now = pos;
+        const bool moves = mine >= 0;
+        const int64_t dof_now = dof;
+        if (t0 + RowShape<PIECES>::kTile < cnt) look_up(t0 + RowShape<PIECES>::kTile);
+        __syncthreads();                                     // every source of the tile has been read
+#pragma unroll
+        for (int r = 0; r < kFastRows; ++r) {
+            int64_t o = __shfl_sync(0xffffffffu, dof_now, r * kSlots + sub);
+            if (sub >= kSlots) o = -1;
+            if (o >= 0) *reinterpret_cast<uint4 *>(db + o * ESZ) = val[r];
+        }
+        if (p.dst.positions && moves) p.dst.positions[(int64_t)u * p.dst.n_max + t0 + warp * kGroup + lane] = pos_now;
     }
 }
 
