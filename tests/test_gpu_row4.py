@@ -353,7 +353,7 @@ def test_read_keys_or_values_alone_and_bad_pages():
 # attention
 # ------------------------------------------------------------------------------------------------
 def check_attend(G, H, lens, page=0, order="heads", per_head=False, scale=None, rows=None, seed=0, q_spread=2.0, k_spread=0.5, v_spread=1.0, layer=1,
-                 fill=None, status=0):
+                 fill=None, status=0, spot=1):
     S, L = len(lens), 2
     unit = lens if per_head else [[n] * H for n in lens]
     N = rows or max(max(max(r) for r in unit), 1)
@@ -382,8 +382,8 @@ def check_attend(G, H, lens, page=0, order="heads", per_head=False, scale=None, 
     ctx.attend(src, q, again[..., :D], ws, scale=scale, lse=lse)
     assert torch.equal(out[..., :D].contiguous().view(torch.int16), again[..., :D].contiguous().view(torch.int16))
     sc = D ** -0.5 if scale is None else scale
-    for s in range(S):
-        for h in range(H):
+    for s in range(0, S, spot):                                      # (each spot-th sequence, and the head that goes with it)
+        for h in range(H) if spot == 1 else (s % H,):
             n = have[s][h]
             k, v = c.unit(c.k, layer, s, h, n), c.unit(c.v, layer, s, h, n)
             for i in range(G):
@@ -443,6 +443,24 @@ def test_attend_logits_far_apart():
         x = torch.randn(1, D, generator=gen(3), device=DEV) * torch.linspace(0, 3, n, device=DEV)[:, None]
         c.put(c.k, l, s, h, as_rows(x))
     check_attend(8, 2, [900, 60], fill=rising, q_spread=3.0)
+
+
+@pytest.mark.parametrize("G", [4, 8, 16])
+def test_attend_bounds_raised_before_and_behind_the_sums_of_16_steps(G):
+    """Logits, or the sizes of values, that go on growing or falling along rows that one block walks past multiples of 16 steps of 128
+    rows: in a cluster, and (many units of other lengths) in shares of the line."""
+    def grows(keys, first, last):
+        def fill(c, l, s, h, n):
+            by = torch.linspace(first, last, max(n, 1), device=DEV)[:n, None]
+            if keys and n:
+                c.put(c.k, l, s, h, as_rows(by * torch.randn(1, D, generator=gen(3), device=DEV)))
+            elif n:
+                c.put(c.v, l, s, h, as_rows(torch.exp2(by) * torch.randn(n, D, generator=gen(n), device=DEV)))
+        return fill
+    for i, fill in enumerate((grows(True, 0, 3), grows(True, -3, 0), grows(False, -12, 12), grows(False, 12, -12))):
+        check_attend(G, 1, [4480 if G <= 8 else 3500, 2100], fill=fill, q_spread=3.0 if i < 2 else 0.5, seed=i)
+        if i in (0, 2):
+            check_attend(G, 16, [2300] * 30 + [2100, 1], fill=fill, q_spread=3.0 if i < 2 else 0.5, seed=i, page=16, spot=3)
 
 
 def test_attend_scales_of_values_far_apart():
