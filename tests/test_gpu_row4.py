@@ -614,6 +614,31 @@ def test_compact_many_units_in_place():
     assert torch.equal(c.k, want_k) and torch.equal(c.v, want_v) and new.tolist() == [min(B, n) for n in lens]
 
 
+@pytest.mark.parametrize("page", [0, 16])
+def test_compact_few_units_of_many_rows_in_place(page):
+    """Few units that keep less than half of their rows: a first launch for the rows from within the kept count, a second for the rest."""
+    H, N, B = 6, 3000, 1200
+    g = torch.Generator().manual_seed(page)
+    c = Cache4(1, 1, H, N, page)
+    c.k.copy_(torch.randint(0, 256, c.k.shape, dtype=torch.uint8, generator=g))
+    c.v.copy_(torch.randint(0, 256, c.v.shape, dtype=torch.uint8, generator=g))
+    pos = torch.randint(0, 10 ** 6, (1, 1, H, c.rows), dtype=torch.int32, generator=g).to(DEV)
+    keep = [torch.randperm(N, generator=g)[:B].sort().values, torch.arange(N - B, N), torch.arange(B),
+            torch.cat((torch.arange(1, 401), torch.arange(N - 800, N))), torch.cat((torch.arange(0, 2 * 500, 2), torch.arange(2000, 2100))), torch.arange(0)]
+    idx = torch.full((1, 1, H, B), 1 << 29, dtype=torch.int32)
+    cnt = int32([[[len(x) for x in keep]]])
+    want_k, want_v, want_p = c.k.clone(), c.v.clone(), pos.clone()
+    for h, sel in enumerate(keep):
+        idx[0, 0, h, :len(sel)] = sel.to(torch.int32)
+        for t, w in ((c.k, want_k), (c.v, want_v)):
+            c.put(w, 0, 0, h, c.unit(t, 0, 0, h, N)[sel.to(DEV)])
+        want_p[0, 0, h, :len(sel)] = pos[0, 0, h, sel.to(DEV)]
+    view = c.view(tb, seq_lens=int32([N]), positions=pos)
+    context(1, H, 1).compact(view, idx.to(DEV), cnt, 1, B, view)
+    torch.cuda.synchronize()
+    assert torch.equal(c.k, want_k) and torch.equal(c.v, want_v) and torch.equal(pos, want_p)
+
+
 def test_compact_keys_alone_and_indices_outside():
     """Without values the keys move alone; indices outside the unit move nothing."""
     for in_place in (False, True):
