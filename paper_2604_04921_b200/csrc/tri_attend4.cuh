@@ -403,7 +403,7 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
         }
         // The bound m on the logits, and `top` on the sizes of values: scales, and centres by 2^-30 (weights times centres stay below
         // 2^45).  m keeps weights times top in [2^11, 2^15] where they are largest.  Both are looked at by a vote and searched for only
-        // when one has to be raised.
+        // when one has to be raised.  m is a whole number, so that top's exponent goes into it and out of it (at the join) exactly.
         float mx[CT][2], sm = fmaxf(fmaxf(bf16_lo(s_max), bf16_hi(s_max)), fmaxf(bf16_lo(c_max), bf16_hi(c_max)) * 0x1p-30f);
         bool raise = sm > top;
 #pragma unroll
@@ -440,15 +440,20 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
                     for (int d = 4; d < 32; d *= 2) mx[ct][i] = fmaxf(mx[ct][i], __shfl_xor_sync(0xffffffffu, mx[ct][i], d));
                     // the largest logit so far is at most m + above as it was, that is as far above m as the weights may reach
                     float to = m[ct][i];
-                    if (mx[ct][i] > m[ct][i] + above) to = mx[ct][i] - above + (kAttAbove<true> - kAttBelow<true>);
-                    const float by = to == m[ct][i] ? 1.f : ex2(m[ct][i] - to);       // 0 where there was no bound yet
+                    if (mx[ct][i] > m[ct][i] + above) to = floorf(mx[ct][i] - above + (kAttAbove<true> - kAttBelow<true>));
+                    // Two factors: where top rises from next to nothing to 2^100, rows that weigh as much as the new one are brought
+                    // down by more than 2^126, which one factor would flush to 0.  (0 where there was no bound yet.)
+                    const float down = m[ct][i] - to, part = fmaxf(down, -100.f), by = ex2(part), rest = ex2(down - part);
                     m[ct][i] = to;
-                    l[ct][i] *= by;
+                    l[ct][i] = l[ct][i] * by * rest;
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
-                        if (g < GP) oc[ct][g][i] *= by;
+                        if (g < GP) oc[ct][g][i] = oc[ct][g][i] * by * rest;
 #pragma unroll
-                        for (int y = 0; y < 2; ++y) { o[ct][g][y][i] *= by; o[ct][g][y][i + 2] *= by; }
+                        for (int y = 0; y < 2; ++y) {
+                            o[ct][g][y][i] = o[ct][g][y][i] * by * rest;
+                            o[ct][g][y][i + 2] = o[ct][g][y][i + 2] * by * rest;
+                        }
                     }
                 }
         }
@@ -509,8 +514,11 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
         if (summed) to_sums();
 
         // ---------------- the unit's rows of this share are through: join the warps ----------------
-        // per 8 query rows: each leaves its sums in the stage it has just read, fragment by fragment, and takes a group of all
+        // per 8 query rows: each leaves its sums in the stage it has just read, fragment by fragment, and takes a group of all.
+        // Whoever joins parts multiplies them by 2^(difference of their bounds), which has to be one of logits alone: top, of which
+        // every warp has its own, leaves the bound here.  (2^-20: 2^31 weights of 2^15 times values of 2^100 stay in fp32's range.)
         const bool final = j.complete && p.finish;
+        const float unit = top * 0x1p-20f, shift = above - kAttAbove<true> + 20.f;      // 2^(shift) = 1 / unit
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
 #pragma unroll
@@ -521,7 +529,7 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
 #pragma unroll
                     for (int g = 0; g < GP; ++g) oc[ct][g][i] += __shfl_xor_sync(0xffffffffu, oc[ct][g][i], d);
                 }
-                if (g8 == 0) stat[warp][8 * ct + 2 * t4 + i] = make_float2(m[ct][i], l[ct][i]);
+                if (g8 == 0) stat[warp][8 * ct + 2 * t4 + i] = make_float2(m[ct][i] + shift, l[ct][i] * unit);
             }
 #pragma unroll
             for (int g = 0; g < 4; ++g)
@@ -532,8 +540,8 @@ __device__ __forceinline__ void attend4_block(const AttendParams &p)
                         o[ct][g][y][0] = z.x; o[ct][g][y][1] = z.y; o[ct][g][y][2] = z.z; o[ct][g][y][3] = z.w;
                     }
                     *reinterpret_cast<float4 *>(used + (2 * g + y) * 512 + lane * 16) =
-                        make_float4(fmaf(o[ct][g][y][0], 0x1p24f, oc[ct][g * GP / 4][0]), fmaf(o[ct][g][y][1], 0x1p24f, oc[ct][g * GP / 4][1]),
-                                    fmaf(o[ct][g][y][2], 0x1p20f, oc[ct][g * GP / 4][0]), fmaf(o[ct][g][y][3], 0x1p20f, oc[ct][g * GP / 4][1]));
+                        make_float4(fmaf(o[ct][g][y][0], 0x1p24f, oc[ct][g * GP / 4][0]) * unit, fmaf(o[ct][g][y][1], 0x1p24f, oc[ct][g * GP / 4][1]) * unit,
+                                    fmaf(o[ct][g][y][2], 0x1p20f, oc[ct][g * GP / 4][0]) * unit, fmaf(o[ct][g][y][3], 0x1p20f, oc[ct][g * GP / 4][1]) * unit);
                 }
             __syncthreads();
             const int from = RT == 4 ? 4 * g8 + (t4 & 1) + 2 * (warp & 1) : lane;          // (RT = 4: where the group's columns are)

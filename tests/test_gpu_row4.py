@@ -484,6 +484,36 @@ def test_attend_scales_of_values_far_apart():
     check_attend(4, 2, [300, 41], fill=lambda c, l, s, h, m: c.put(c.v, l, s, h, as_rows(1e20 * torch.randn(m, D, generator=gen(m), device=DEV))))
 
 
+@pytest.mark.parametrize("sizes", [(None, 50), (None, 99), (-100, 90)])
+@pytest.mark.parametrize("constant", [False, True])
+def test_attend_rows_of_no_size_beside_huge_ones(sizes, constant):
+    """All rows weigh about the same, and some hold values of size 2^50 to 2^99, others zeros or values down to 2^-100: before and
+    behind one another in one warp, row by row, in warps, in blocks of a cluster and in shares of the line.  None drops out of the
+    softmax.  `constant`: the huge groups have scale 0 and a huge centre."""
+    small, big = sizes
+
+    def rows_of(n, e, g):
+        x = torch.zeros(n, D, dtype=torch.float64, device=DEV)
+        if e is not None:
+            x = 2.0 ** e * (1 + (0.0 if constant and e == big else 0.25) * torch.randn(n, D, generator=g, device=DEV).double())
+        return as_rows(x)
+
+    def fill(is_big):
+        def put(c, l, s, h, n):
+            g = gen(n)
+            big_rows = is_big(torch.arange(n, device=DEV), n)
+            c.put(c.v, l, s, h, torch.where(big_rows[:, None], rows_of(n, big, g), rows_of(n, small, g)))
+        return put
+    where = [lambda i, n: i >= n // 2, lambda i, n: i < (n + 1) // 2, lambda i, n: i % 2 == 1, lambda i, n: i % 64 >= 32,
+             lambda i, n: i % 64 < 32, lambda i, n: i % 256 >= 128, lambda i, n: i == n - 1, lambda i, n: i == 0]
+    for j, is_big in enumerate(where):
+        G = (4, 8, 4, 16, 4, 1, 4, 8)[j]
+        check_attend(G, 1, [2, 300, 2600], fill=fill(is_big), q_spread=0.25, seed=j)                          # clusters
+        check_attend(G, 1, [9000, 33], fill=fill(is_big), q_spread=0.25, seed=j, page=16)                     # the whole GPU
+        if j == 3:
+            check_attend(G, 3, [130 + i for i in range(20)], fill=fill(is_big), q_spread=0.25, seed=j, spot=7)   # units cut between blocks
+
+
 def test_attend_centres_far_from_zero():
     def fill(c, l, s, h, m):
         c.put(c.k, l, s, h, as_rows(20 + 0.1 * torch.randn(m, D, generator=gen(m), device=DEV)))
