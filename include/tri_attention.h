@@ -384,7 +384,8 @@ typedef struct {
  *            (code - 8) s + c.  With the group's smallest and largest value lo and hi: c = bf16((8 hi + 7 lo) / 15), s = the
  *            smallest bf16 that is not below (hi - c) / 7 and (c - lo) / 8 (at least 2^-126, or 0 if both are 0), code =
  *            8 + (x - c) / s, rounded to nearest even and kept within 0..15: no component is off by more than s / 2 and the
- *            rounding of (x - c) / s.  A group with a NaN or an infinity, or whose c - lo or c exceeds its type, becomes NaN
+ *            rounding of (x - c) / s.  Values are quantised in fp32: s is exact for the c stored beside it, c for values that
+ *            are bf16 numbers (others may put it on the wrong side of the border of two), and x - c is rounded to fp32.  A group with a NaN or an infinity, or whose c - lo or c exceeds its type, becomes NaN
  *            throughout (c NaN, s 0).
  *            A row is TRI_ROW4_BYTES bytes: component 32 g + 8 t + 2 i + h (g, t, i < 4, h < 2) in bits 4 (i + 4 h) .. + 3 of
  *            the 32-bit word 4 t + g (little endian), the scales of the four groups from byte 64 on, the centres from byte 72 on.

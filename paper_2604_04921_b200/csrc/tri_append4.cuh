@@ -171,10 +171,11 @@ __device__ __forceinline__ void row4_fp64(const char *from, char *to, int c, dou
             nan = __shfl_xor_sync(lanes, (int)nan, d) || nan;
         }
         float m = bf16_lo(cvt_bf16x2(0.f, (float)((8.0 * hi + 7.0 * lo) / 15.0)));
-        const float need = __double2float_ru(fmax((hi - (double)m) / 7.0, ((double)m - lo) * 0.125));
+        const double below = __dsub_ru((double)m, lo);
+        const float need = __double2float_ru(fmax(__ddiv_ru(__dsub_ru(hi, (double)m), 7.0), below * 0.125));      // (upwards, as in row4_group)
         const uint32_t up = max((__float_as_uint(need) + 0xffffu) & 0xffff0000u, 0x00800000u);
         float s = need > 0.f ? __uint_as_float(up) : 0.f;
-        if (nan || !(fabsf((float)((double)m - lo)) < INFINITY)) { m = __uint_as_float(0x7fc00000u); s = 0.f; }
+        if (nan || !(fabsf((float)below) < INFINITY)) { m = __uint_as_float(0x7fc00000u); s = 0.f; }
         r.m[j] = m; r.s[j] = s;
         const double by = s > 0.f ? (double)s : 1.0;
 #pragma unroll

@@ -39,17 +39,22 @@ __device__ __forceinline__ float max_nan(float a, float b)
 
 // Scale and centre of a group from its smallest and largest value.  (8 hi + 7 lo) / 15 as (hi / 2 + 7 lo / 16) / (15 / 16), which
 // cannot overflow; with bf16 inputs every step up to the division is exact or rounded once, so that c is the correctly rounded
-// one.  With a NaN or an infinity among the values, or a range that fp32 does not hold, c - lo is not finite.  Returns whether c or s lies so near the border of two bf16 numbers
-// that lo and hi, if they are off by a few steps of fp32, may have put it on the wrong side.
+// one.  s is exact for that c: the differences are rounded upwards (7 s or 8 s for the s sought is an fp32 number, which they do
+// not pass; to nearest, c - lo becomes c for a tiny lo < 0, and s ends a step below), the quotient by 7 is taken with a factor
+// below 1 / 7, which leaves s right or a step below, and 7 s, exact, is compared with the difference.  (Divisions rounded upwards cost
+// 7 % of a whole prompt's append.)  With a NaN or an infinity among the values, or a range that fp32 does not hold, c - lo is not
+// finite.  Returns whether c or s lies so near the border of two bf16 numbers that lo and hi, if they are off by a few steps of fp32,
+// may have put it on the wrong side.
 __device__ __forceinline__ bool row4_group(float lo, float hi, float &s, float &c)
 {
     const float c32 = __fdiv_rn(fmaf(hi, 0.5f, lo * 0.4375f), 0.9375f);
     c = bf16_lo(cvt_bf16x2(0.f, c32));
-    const float need = fmaxf(__fdiv_rn(hi - c, 7.f), (c - lo) * 0.125f);
+    const float over = __fsub_ru(hi, c), below = __fsub_ru(c, lo), need = fmaxf(over * 0x1.249248p-3f, below * 0.125f);
     // rounded up to bf16; the smallest normal number, where that is more
-    const uint32_t up = max((__float_as_uint(need) + 0xffffu) & 0xffff0000u, 0x00800000u);
+    uint32_t up = max((__float_as_uint(need) + 0xffffu) & 0xffff0000u, 0x00800000u);
+    if (__uint_as_float(up) * 7.f < over) up += 0x10000u;
     s = need > 0.f ? __uint_as_float(up) : 0.f;
-    if (!(fabsf(c - lo) < INFINITY)) { c = __uint_as_float(0x7fc00000u); s = 0.f; }
+    if (!(fabsf(below) < INFINITY)) { c = __uint_as_float(0x7fc00000u); s = 0.f; }
     return ((__float_as_uint(c32) + 0x8010u) & 0xffffu) <= 0x20u || (need > 0.f && ((__float_as_uint(need) + 0x10u) & 0xffffu) <= 0x20u);
 }
 

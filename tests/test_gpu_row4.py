@@ -153,6 +153,48 @@ def test_append_bf16_values_as_the_definition_has_them():
     assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T", [1, 520])
+def test_append_groups_whose_scale_lies_behind_a_border(T, dtype):
+    """A group from -t to hi with t tiny: (c - lo) / 8 is just above c / 8, itself a bf16 number, so that the smallest bf16 not below it
+    is the next one; likewise (hi - c) / 7 with hi tiny.  Values and the keys of position 0 are the reference's byte for byte."""
+    hi = torch.cat((1 + torch.arange(128, device=DEV) / 128, 0.7 * torch.exp2(torch.arange(-1, 1, device=DEV))))
+    rows = []
+    for t in (1e-9, 1e-8, 1e-7, 3e-11):
+        x = hi[:, None] * torch.rand(len(hi), D, generator=gen(7), device=DEV)
+        x[:, 5], x[:, 6] = hi, -t                                                # group 0
+        x[:, 40], x[:, 41] = 256 * hi, -t                                        # group 1: not above 256
+        x[:, 64:96] *= -1
+        x[:, 70], x[:, 71] = -hi * 15 / 8, t                                     # group 2: hi - c = -c, for hi = 1: 7 / 8
+        rows.append(x)
+    x = torch.cat(rows).to(torch.bfloat16)
+    want = as_rows(x.double())
+    assert float((parts(want)[1][:, 0] * 8 > parts(want)[2][:, 0]).double().mean()) > 0.2                # what the case is about
+    n = x.shape[0]
+    assert n == 520
+    ctx = context(1, 1, 1)
+    S = n // T
+    cache = Cache4(1, S, 1, T)
+    v = x.to(dtype).view(S, T, 1, D)
+    if T == 1:
+        ctx.append(tb.LayerCache(cache.view(tb, seq_lens=int32([0] * S)), 0), v, v.clone(), torch.zeros(S, dtype=torch.int64, device=DEV))
+        torch.cuda.synchronize()
+        assert torch.equal(cache.k[0, :, 0, 0], want)
+        got = cache.v[0, :, 0, 0]
+    else:
+        ctx.append(tb.LayerCache(cache.view(tb, seq_lens=int32([0])), 0), torch.zeros_like(v), v, torch.zeros(1, dtype=torch.int64, device=DEV))
+        torch.cuda.synchronize()
+        got = cache.v[0, 0, 0]
+        for i in range(0, n, 40):                                                # tokens at position 0
+            one = Cache4(1, 1, 1, 16)
+            k = v[:, i:i + 1].expand(1, 2, 1, D).contiguous()
+            ctx.append(tb.LayerCache(one.view(tb, seq_lens=int32([0])), 0), k, k.clone(), torch.zeros(1, dtype=torch.int64, device=DEV),
+                       n_new=int32([1]))
+            torch.cuda.synchronize()
+            assert torch.equal(one.k[0, 0, 0, 0], want[i]) and torch.equal(one.v[0, 0, 0, 0], want[i])
+    assert torch.equal(got, want)
+
+
 def test_append_unusual_groups():
     """Constants, zeros, one outlier, values far from zero, tiny and huge ones, NaN and infinities."""
     x = torch.zeros(13, D, device=DEV)
