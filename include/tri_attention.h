@@ -398,8 +398,8 @@ typedef struct {
  *   device_status  device int32[1] or NULL; set to TRI_ERR_DEVICE_CHECK if a row had no slot below n_max, a page id
  *             outside [0, n_pages) or a position outside [0, 2^31) -- such rows are skipped -- or if n_new[s] was
  *             outside [0, T] (the nearest bound counts)
- * The rows must not overlap the cache, and two sequences must not append into one page.  Destinations that meet in one place (a
- * cache whose heads or sequences are broadcast, strides of q_out below 128) are refused.
+ * The rows must not overlap the cache, and two sequences must not append into one page.  Strides under which two rows of the
+ * cache's layer or of q_out meet (broadcast heads or sequences, strides below a row, two dimensions of one stride) are refused.
  */
 tri_status tri_append(tri_ctx *ctx, const tri_layer_cache *dst, int32_t S, const tri_append_rows *rows,
                       int32_t *new_lens, int32_t *device_status, void *stream);
@@ -422,7 +422,8 @@ typedef struct {
  * or not.  With T at least the longest length the result is a contiguous cache of the same slots ([S][H][N][128] by its
  * strides), which tri_score and the round take; with first = the lengths before an append it is what the append has stored.
  *   device_status  device int32[1] or NULL; TRI_ERR_DEVICE_CHECK if a page id was outside [0, n_pages): such rows are skipped
- * The outputs must not overlap the cache or each other; destinations that meet in one place are refused.
+ * The outputs must not overlap the cache or each other (k == v is refused, other overlaps are not looked for).  Strides under
+ * which two rows of an output meet are refused.
  */
 tri_status tri_read(tri_ctx *ctx, const tri_layer_cache *src, int32_t S, const tri_read_rows *rows,
                     int32_t *device_status, void *stream);

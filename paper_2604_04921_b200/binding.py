@@ -24,7 +24,7 @@ HEADERS = [_ROOT / "include" / "tri_attention.h", _PKG / "csrc" / "tri_common.cu
            _PKG / "csrc" / "tri_score_pre.cuh", _PKG / "csrc" / "tri_score_tma.cuh", _PKG / "csrc" / "tri_score_umma.cuh", _PKG / "csrc" / "tri_calib.cuh", _PKG / "csrc" / "tri_calib_tma.cuh",
            _PKG / "csrc" / "tri_select.cuh", _PKG / "csrc" / "tri_compact.cuh",
            _PKG / "csrc" / "tri_step.cuh", _PKG / "csrc" / "tri_append.cuh", _PKG / "csrc" / "tri_attend.cuh", _PKG / "csrc" / "tri_attend_umma.cuh",
-           _PKG / "csrc" / "tri_row4.cuh", _PKG / "csrc" / "tri_append4.cuh", _PKG / "csrc" / "tri_attend4.cuh", _PKG / "csrc" / "tri_read.cuh"]
+           _PKG / "csrc" / "tri_row4.cuh", _PKG / "csrc" / "tri_append4.cuh", _PKG / "csrc" / "tri_attend4.cuh", _PKG / "csrc" / "tri_read.cuh", _PKG / "csrc" / "tri_rows.h"]
 
 EXPORTS = ["tri_create", "tri_destroy", "tri_workspace_bytes", "tri_score", "tri_select", "tri_compact",
            "tri_compress", "tri_select_budgets", "tri_compress_budgets", "tri_compress_windowed", "tri_compress_host", "tri_score_static", "tri_score_static_bytes", "tri_compress_launches", "tri_set_pipeline", "tri_set_score_kernel", "tri_last_cuda_error",

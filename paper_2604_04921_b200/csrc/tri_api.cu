@@ -19,6 +19,7 @@
 #include "tri_calib_tma.cuh"
 #include "tri_compact.cuh"
 #include "tri_read.cuh"
+#include "tri_rows.h"
 #include "tri_score.cuh"
 #include "tri_score_pre.cuh"
 #include "tri_score_tma.cuh"
@@ -1233,10 +1234,6 @@ bool rows16_ok(const void *p, int64_t a, int64_t b, int64_t c, int es)
     return p && !((uintptr_t)p & 15) && (a * es) % 16 == 0 && (b * es) % 16 == 0 && (c * es) % 16 == 0;
 }
 
-// Rows that are written, `n` of them `stride` elements apart, lie side by side: a broadcast dimension, whose rows meet in one
-// place, would be written by several blocks at a time.
-bool rows_apart(int64_t n, int64_t stride, int row = kHeadDim) { return n <= 1 || stride >= row || stride <= -row; }
-
 template <int KIND, int KK, bool SPLIT>
 cudaError_t launch_append(unsigned blocks, int tt, cudaStream_t st, const AppendParams &p)
 {
@@ -1291,7 +1288,7 @@ extern "C" tri_status tri_append(tri_ctx *c, const tri_layer_cache *dst, int32_t
     if (rows->q) {
         if (!rows_ok(rows->q, rows->q_stride_seq, rows->q_stride_tok, rows->q_stride_head, H * G, es)) return TRI_ERR_INVALID_ARG;
         if (!rows_ok(rows->q_out, rows->qo_stride_seq, rows->qo_stride_tok, rows->qo_stride_head, H * G, 2)) return TRI_ERR_INVALID_ARG;
-        if (!rows_apart(S, rows->qo_stride_seq) || !rows_apart(rows->T, rows->qo_stride_tok) || !rows_apart(H * G, rows->qo_stride_head))
+        if (!rows_apart({S, rows->qo_stride_seq}, {rows->T, rows->qo_stride_tok}, {H * G, rows->qo_stride_head}, kHeadDim))
             return TRI_ERR_INVALID_ARG;
         if (rows->q == rows->q_out && (rows->kind != 0 || (S > 1 && rows->q_stride_seq != rows->qo_stride_seq) ||
                                        (rows->T > 1 && rows->q_stride_tok != rows->qo_stride_tok) ||
@@ -1300,10 +1297,9 @@ extern "C" tri_status tri_append(tri_ctx *c, const tri_layer_cache *dst, int32_t
     }
     if (!rows->pos && dst->unit_lens) return TRI_ERR_INVALID_ARG;
     const tri_cache_view *dv = dst->view;
-    const int row = row_elements(dv->k_kind);
-    if (!rows_apart(H, dv->stride_head, row) ||
-        !(dv->paged ? rows_apart(dv->n_pages == 1 ? 1 : 2, dv->stride_page, row) : rows_apart(S, dv->stride_seq, row)))
-        return TRI_ERR_INVALID_ARG;
+    const RowDim seqs = dv->paged ? RowDim{dv->n_pages > 0 ? dv->n_pages : 2, dv->stride_page} : RowDim{S, dv->stride_seq};
+    const RowDim slots = dv->paged ? RowDim{dv->page_size, dv->stride_slot} : RowDim{dv->n_max, dv->stride_tok};
+    if (!rows_apart(seqs, {H, dv->stride_head}, slots, row_elements(dv->k_kind))) return TRI_ERR_INVALID_ARG;
     if ((r = check_device(c)) != TRI_OK) return r;
 
     AppendParams p;
@@ -1368,7 +1364,7 @@ extern "C" tri_status tri_read(tri_ctx *c, const tri_layer_cache *src, int32_t S
     const int32_t H = c->desc.n_kv_heads, T = rows->T;
     const int es = rows->kind == 0 ? 2 : 4;
     auto rows_ok = [&](const void *x, int64_t seq, int64_t tok, int64_t head) {      // (the stride of a dimension of size 1 is never used)
-        return rows16_ok(x, S > 1 ? seq : 0, T > 1 ? tok : 0, H > 1 ? head : 0, es) && rows_apart(S, seq) && rows_apart(T, tok) && rows_apart(H, head);
+        return rows16_ok(x, S > 1 ? seq : 0, T > 1 ? tok : 0, H > 1 ? head : 0, es) && rows_apart({S, seq}, {T, tok}, {H, head}, kHeadDim);
     };
     if (rows->k && !rows_ok(rows->k, rows->k_stride_seq, rows->k_stride_tok, rows->k_stride_head)) return TRI_ERR_INVALID_ARG;
     if (rows->v && !rows_ok(rows->v, rows->v_stride_seq, rows->v_stride_tok, rows->v_stride_head)) return TRI_ERR_INVALID_ARG;
@@ -1516,7 +1512,7 @@ tri_status run_attend(tri_ctx *c, const tri_layer_cache *prefix, int32_t P, cons
     const int32_t H = c->desc.n_kv_heads, G = c->desc.group_size;
     if (!rows16_ok(io->q, S > 1 ? io->q_stride_seq : 0, H * G > 1 ? io->q_stride_head : 0, 0, 2) ||
         !rows16_ok(io->out, S > 1 ? io->out_stride_seq : 0, H * G > 1 ? io->out_stride_head : 0, 0, 2) || io->q == io->out ||
-        !rows_apart(S, io->out_stride_seq) || !rows_apart((int64_t)H * G, io->out_stride_head) ||
+        !rows_apart({S, io->out_stride_seq}, {(int64_t)H * G, io->out_stride_head}, {1, 0}, kHeadDim) ||
         !std::isfinite(io->scale * 1.44269504f))
         return TRI_ERR_INVALID_ARG;
     if ((r = check_device(c)) != TRI_OK) return r;

@@ -980,3 +980,48 @@ def test_another_current_device_and_host_pointers_are_refused_by_the_binding():
                 lambda: ctx.read(lc, x.to(DEV), device_status=torch.zeros(1, dtype=torch.int32))):
         with pytest.raises(AssertionError):
             bad()
+
+
+def test_rows_that_meet_under_their_strides_together_are_refused():
+    """Strides that are each as long as a row, but bring two rows to one place; layouts that are unusual and sound are taken."""
+    S, H, G, T = 2, 2, 3, 2
+    ctx = context(1, H, G)
+    c = Cache4(1, S, H, 32)
+    lens = int32([3, 5])
+    for s in range(S):
+        for h in range(H):
+            c.fill(0, s, h, 5, gen(2 * s + h))
+    lc = tb.LayerCache(c.view(tb, seq_lens=lens), 0)
+    room = torch.zeros(1 << 14, dtype=torch.bfloat16, device=DEV)
+
+    def refused(call):
+        with pytest.raises(tb.TriError) as e:
+            call()
+        assert e.value.code == 1
+
+    def rows(*strides, n=(S, T, H)):
+        return room.as_strided((*n, D), (*strides, 1))
+    sound = torch.zeros(S, T, H, D, dtype=torch.bfloat16, device=DEV)
+    for strides in ((512, 128, 128), (128, 256, 128), (128, 128, 512), (256, 384, 128), (1024, 200, 256)):
+        refused(lambda: ctx.read(lc, rows(*strides)))
+        refused(lambda: ctx.read(lc, None, rows(*strides)))
+        refused(lambda: ctx.read(lc, sound, rows(*strides)))
+    ctx.read(lc, sound)
+    ctx.read(lc, rows(1024, 384, 256))                                   # not nested, and apart
+    torch.cuda.synchronize()
+    assert torch.equal(rows(1024, 384, 256), sound) and bool((sound != 0).any())
+    # outputs of attention, rotated queries, a cache's heads among its slots
+    q = torch.zeros(S, H * G, D, dtype=torch.bfloat16, device=DEV)
+    refused(lambda: ctx.attend(lc, q, rows(256, 128, n=(S, H * G)), ctx.attend_workspace(S)))
+    k, pos = torch.zeros(S, 1, H, D, dtype=torch.bfloat16, device=DEV), torch.zeros(S, dtype=torch.int64, device=DEV)
+    q1, k2, q2 = q[:, None], k.expand(S, T, H, D).contiguous(), q[:, None].expand(S, T, H * G, D).contiguous()
+    refused(lambda: ctx.append(lc, k, k.clone(), pos, q=q1, q_out=rows(256, 4096, 128, n=(S, 1, H * G))))
+    refused(lambda: ctx.append(lc, k2, k2.clone(), pos, q=q2, q_out=rows(4096, 256, 128, n=(S, T, H * G))))
+    pool = torch.zeros(1 << 16, dtype=torch.uint8, device=DEV)
+    for strides in ((1 << 13, 80, 80), (80, 80 * 32, 80), (80 * 32, 80 * 32, 80), (80 * 32, 80 * 16, 80)):
+        heads = tb.LayerCache(tb.CacheView(pool.as_strided((1, S, H, 32, ROW), (1 << 15, *strides, 1)), None, seq_lens=lens), 0)
+        refused(lambda: ctx.append(heads, k, None, pos))
+    for strides in ((80 * 64, 80, 160), (80, 80 * 64, 160)):
+        heads = tb.LayerCache(tb.CacheView(pool.as_strided((1, S, H, 32, ROW), (1 << 15, *strides, 1)), None, seq_lens=lens), 0)
+        ctx.append(heads, k, None, pos)
+    torch.cuda.synchronize()

@@ -118,3 +118,54 @@ def test_caches_and_rows_of_another_device_never_reach_the_library(monkeypatch):
     assert not reached
     ctx.read(lc, x, x.clone(), first=lens)
     assert reached == ["tri_read"]
+
+
+def test_strides_under_which_rows_meet(tmp_path):
+    """tri_rows.h against all pairs of rows, for random strides, nested ones and ones that only interleave."""
+    src = r"""
+#include <cstdio>
+#include <cstdlib>
+#include <vector>
+#include "tri_rows.h"
+using tri::RowDim;
+static bool brute(const RowDim *d, int64_t row)
+{
+    std::vector<int64_t> at;
+    for (int64_t i = 0; i < d[0].n; ++i) for (int64_t j = 0; j < d[1].n; ++j) for (int64_t k = 0; k < d[2].n; ++k)
+        at.push_back(i * d[0].stride + j * d[1].stride + k * d[2].stride);
+    std::sort(at.begin(), at.end());
+    for (size_t i = 1; i < at.size(); ++i) if (at[i] - at[i - 1] < row) return false;
+    return true;
+}
+int main()
+{
+    srand(1);
+    int apart = 0, meet = 0, woven = 0, wrong = 0;
+    for (int t = 0; t < 300000; ++t) {
+        RowDim d[3];
+        const int64_t row = t % 2 ? 128 : 80;
+        for (RowDim &x : d) x = {1 + rand() % 5, (rand() % 2 ? 8 * (rand() % 130) : row * (rand() % 9)) * (rand() % 4 ? 1 : -1)};
+        const bool want = brute(d, row), got = tri::rows_apart(d[0], d[1], d[2], row);
+        wrong += want != got;
+        (want ? apart : meet)++;
+        if (want) {                                          // apart although no order of the strides nests
+            std::sort(d, d + 3, [](RowDim a, RowDim b) { return llabs(a.n > 1 ? a.stride : 0) < llabs(b.n > 1 ? b.stride : 0); });
+            int64_t extent = row;
+            bool nested = true;
+            for (RowDim &x : d) if (x.n > 1) { nested = nested && llabs(x.stride) >= extent; extent += (x.n - 1) * llabs(x.stride); }
+            woven += !nested;
+        }
+    }
+    const int64_t far = INT64_MAX / 4, h = 128;
+    const bool edges = tri::rows_apart({4, far}, {2, h}, {1, 0}, h) && !tri::rows_apart({2, INT64_MIN}, {2, INT64_MIN}, {1, 7}, h) &&
+        tri::rows_apart({2, INT64_MIN}, {1, 0}, {1, 0}, h) && tri::rows_apart({1, 0}, {1, 0}, {1, 0}, h) &&
+        tri::rows_apart({1 << 20, 1 << 20}, {64, 128}, {128, 64 * 128}, h) && !tri::rows_apart({2, h}, {2, h}, {1, 0}, h) &&
+        !tri::rows_apart({1000000, 256}, {8, 384}, {4, 768}, h);
+    printf("%d %d %d %d %d\n", wrong, apart, meet, woven, edges);
+}
+"""
+    (tmp_path / "r.cpp").write_text(src)
+    subprocess.run(["g++", "-O2", "-std=c++17", "-Wall", "-Werror", "-I", os.path.join(ROOT, "paper_2604_04921_b200", "csrc"), "-o", str(tmp_path / "r"),
+                    str(tmp_path / "r.cpp")], check=True)
+    wrong, apart, meet, woven, edges = map(int, subprocess.run([str(tmp_path / "r")], check=True, capture_output=True, text=True).stdout.split())
+    assert wrong == 0 and edges and min(apart, meet, woven) > 500
