@@ -453,7 +453,7 @@ size_t tri_attend_workspace_bytes(const tri_ctx *ctx, int32_t S, int32_t P);
  * largest weight times the largest scale of the unit so far where that is more), and centres enter the logits to 2^-16;
  * query components 2^28 times smaller than the largest of their row lose bits; scales must not be negative, and scales,
  * centres and query components should stay below 2^100, and centres above 2^-120 of the unit's largest scale where they
- * count.  Sums
+ * count; rows lie less than 2^31 bytes apart (TRI_ERR_UNSUPPORTED).  Sums
  * are formed in a fixed order: equal inputs give equal bits.  Ragged batches are cut into equal shares over the GPU; S * n_kv_heads * (n_max / 64 + 3) must stay below
  * 2^31 (for prefixes, with P + S in place of S at most), else TRI_ERR_UNSUPPORTED.  An infinity among the values of a
  * unit's rows makes the outputs of its component infinite or NaN.

@@ -290,6 +290,8 @@ __global__ void __launch_bounds__(kAppendThreads) k_append4_one(const AppendPara
 
 // KIND: input 0 bf16, 1 fp32.  TT: tokens per block.  roles = 2: of two blocks of the same tokens the first takes keys and values, the
 // second the queries, so that a multiprocessor has both kinds of work, one bound by instructions and the other by memory, at any time.
+// (bf16: 64 registers spill 84 to 144 bytes; three blocks of 80, without spills, take as long: 88.8 against 88.3 us for 16,384 tokens
+// with the read back, 43.5 against 43.3 for ragged pieces.)
 template <int KIND, bool SPLIT, int TT>
 __global__ void __launch_bounds__(kAppendThreads, KIND == 0 ? 4 : 2) k_append4(const AppendParams p, int roles)
 {

@@ -19,10 +19,11 @@
 //            taken against goes by the largest scale of the rows so far, too, so that they use f16's range from 2^15 down.  The
 //            centres are summed in fp32.
 //
-// What bounds it.  160 bytes per row and head: at HBM speed a multiprocessor gets 16 rows every 60 ns, and the instructions that turn
-// 16 x 256 codes into operands have to fit in there.  131,072 rows of 8 heads, G = 4: 39.4 us, 4.3 TB/s (0.66 of the copy rate); 312
-// warp instructions per 16 rows, issued in 0.53 of the cycles by the 3 warps that a scheduler has; half of the ALU's cycles, 0.23 of
-// the tensor pipe's.  (Shifts as multiplications on the other pipe: 41.5 us; four blocks per multiprocessor spill; widening to tensor
+// What bounds it.  160 bytes per row and head: at HBM speed a multiprocessor gets 16 rows every 60 ns, in which 316 warp instructions
+// have to be issued.  131,072 rows of 8 heads, G = 4: 40.0 us, 4.2 TB/s (0.65 of the copy rate).  No unit is full: issue slots 0.54,
+// ALU 0.51, tensor pipe 0.23, HBM 0.5.  What is waited for is the chain within a step (scales to shared memory and back, matrix
+// instructions, the vote, exponentials, transposes, matrix instructions), which the 3 warps that a scheduler has do not cover; fixed
+// latency is the first of the stalls.  (Shifts as multiplications on the other pipe: 41.5 us; four blocks per multiprocessor spill; widening to tensor
 // memory for tcgen05.mma, whose instructions then cost nothing: 55 us, the widening of a row per thread takes longer.)
 // Copies are 16-byte asynchronous ones into a ring of stages that each warp keeps for itself; a stage is 32 rows of K and of V (bulk
 // copies per warp: 44 us).  Work split, records and parts are those of tri_attend.cuh.
